@@ -266,6 +266,65 @@ int vlq_index_get_lists(const vlq_index_t *idx, int64_t *d_off, int32_t *d_ids,
 int vlq_profile_enable(vlq_index_t *idx, int enable);
 int vlq_profile_read(vlq_index_t *idx, float *ms, int32_t *launches);
 
+/* ---------------------------------------------------------------------------
+ * Learning cells by gradient
+ *
+ * vlq_kmeans fits a codebook to vectors; these operators train one together with whatever makes the vectors: a loss over
+ * all centroids with its gradient, rows sent to the cells they were given to and back, and the clipping of gradients.
+ *
+ *  - Values are fp32, fp16 or bf16 (VLQ_F32 ...); sums, softmax statistics and norms are held in fp32 or more, and what is
+ *    returned in 16 bits is rounded once.  Pointers are aligned to their values' size; 16 bytes are faster.
+ *  - Workspaces belong to the caller (aligned to 256 bytes; their contents do not matter before a call and mean nothing after
+ *    it).  Calls that may overlap in time, captured graphs among them, need workspaces of their own.
+ *  - The calls only launch kernels on `stream` (no allocation, no memset, no synchronisation) and can be recorded in a HIP
+ *    graph.  The current device has to be the buffers' device.  Results do not depend on the launch: the same call gives
+ *    the same bits.  Outputs must not overlap inputs or each other unless stated.
+ */
+enum {
+    VLQ_F32 = 0,
+    VLQ_F16 = 1,
+    VLQ_BF16 = 2
+};
+#define VLQ_MAX_LOSS_DIM 16384     /* d of vlq_softmax_loss */
+#define VLQ_MAX_LOSS_CLASSES (1 << 24) /* k of vlq_softmax_loss */
+
+/*
+ * Softmax cross entropy of rows against k centroids (or the k rows of an output layer), without keeping the n x k logits:
+ *     l_ij = scale <x_i, c_j> + bias_j,   loss_i = log(sum_j exp l_ij) - l_i,label(i).
+ * With bias_j = -scale / 2 ||c_j||^2 this is the softmax over -scale / 2 ||x_i - c_j||^2.
+ *   d_x [n x d], d_c [k x d] of type dtype; d_bias [k] fp32 or NULL; d_label [n].
+ *   d_loss [n] fp32 (or NULL); d_stats [n x 2] fp32, for vlq_softmax_loss_backward: the row's largest logit in units of log 2
+ *   and the sum of the exponentials relative to it, so that log sum exp = ln 2 * stats[0] + ln stats[1].
+ * A row whose label is outside [0, k) does not count: its loss is 0 and its vector is not looked at.  A bias of -infinity
+ * takes its centroid out for all rows: its vector is not looked at.  A row with no centroid left, or whose label was taken
+ * out, has an infinite loss.
+ * fp32 values enter the products as two fp16 parts, off by 2^-23 of themselves, or 2^-40 of the largest in their row (of x) or
+ * in their 128 consecutive centroids; bf16 values exactly down to 2^-32 of that.
+ * 0 <= n < 2^31, 1 <= d <= VLQ_MAX_LOSS_DIM, 1 <= k <= VLQ_MAX_LOSS_CLASSES; n = 0 is a no-op.
+ * d_ws: at least vlq_softmax_loss_workspace(dtype, n, d, k, 0) bytes, ws_bytes its size.
+ */
+int vlq_softmax_loss(int dtype, const void *d_x, int64_t n, int32_t d, const void *d_c, int32_t k,
+                     const float *d_bias, float scale, const int32_t *d_label, float *d_loss, float *d_stats,
+                     void *d_ws, int64_t ws_bytes, void *stream);
+
+/*
+ * Its gradient: with G_ij = grad_i (softmax_ij - [j = label_i]),
+ *     dx_i = scale sum_j G_ij c_j,   dc_j = scale sum_i G_ij x_i,   dbias_j = sum_i G_ij.
+ * The inputs of the forward call and its d_stats; d_grad [n] fp32, the gradient of each row's loss (1 / n for a mean).
+ * d_dx [n x d], d_dc [k x d] of type dtype, d_dbias [k] fp32; each may be NULL.  Rows that do not count, and rows with no
+ * centroid left, have zero gradients and add nothing to the others'.  n = 0 writes zeros to d_dc and d_dbias.
+ * G is held as fp16 (two parts for fp32), relative to grad's largest magnitude, with an absolute error of at most 2^-39 (2^-40 with
+ * two parts) of that beside its rounding.  The values of x and c enter relative to the largest of their matrix.
+ * d_ws: at least vlq_softmax_loss_workspace(dtype, n, d, k, 1) bytes.
+ */
+int vlq_softmax_loss_backward(int dtype, const void *d_x, int64_t n, int32_t d, const void *d_c, int32_t k,
+                              const float *d_bias, float scale, const int32_t *d_label, const float *d_stats,
+                              const float *d_grad, void *d_dx, void *d_dc, float *d_dbias, void *d_ws,
+                              int64_t ws_bytes, void *stream);
+
+/* Bytes of workspace of either call (backward != 0: the second); a negative VLQ_E* code for sizes that are refused. */
+int64_t vlq_softmax_loss_workspace(int dtype, int64_t n, int32_t d, int32_t k, int backward);
+
 /* Message of the last error on this thread ("" if none). */
 const char *vlq_last_error(void);
 int vlq_version(void);

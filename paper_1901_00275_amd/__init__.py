@@ -20,6 +20,8 @@ VLQ_OK, VLQ_EINVAL, VLQ_ENOMEM, VLQ_EHIP = 0, -1, -2, -3
 STAGES = ("coarse", "select_cells", "subregions", "scan", "merge")
 (VLQ_OPT_COARSE_FP32, VLQ_OPT_NEIGHBOURS_PER_QUERY, VLQ_OPT_SCAN_PACKED, VLQ_OPT_SCAN_GENERIC,
  VLQ_OPT_ENCODE_WAVE, VLQ_OPT_PIPELINE_PARTS, VLQ_OPT_SMALL_BATCH, VLQ_OPT_COARSE_SPLIT) = range(8)
+VLQ_F32, VLQ_F16, VLQ_BF16 = range(3)
+_TYPES = {torch.float32: VLQ_F32, torch.float16: VLQ_F16, torch.bfloat16: VLQ_BF16}
 
 
 class VlqError(RuntimeError):
@@ -65,6 +67,8 @@ def lib():
             "vlq_index_get_lists": [vp, vp, vp, vp, vp, vp],
             "vlq_profile_enable": [vp, C.c_int],
             "vlq_profile_read": [vp, C.POINTER(C.c_float), C.POINTER(i32)],
+            "vlq_softmax_loss": [C.c_int, vp, i64, i32, vp, i32, vp, C.c_float, vp, vp, vp, vp, i64, vp],
+            "vlq_softmax_loss_backward": [C.c_int, vp, i64, i32, vp, i32, vp, C.c_float, vp, vp, vp, vp, vp, vp, vp, i64, vp],
             "vlq_version": [],
         }
         for name, args in sig.items():
@@ -75,6 +79,8 @@ def lib():
         L.vlq_index_free.restype = None
         L.vlq_index_ntotal.argtypes = [vp]
         L.vlq_index_ntotal.restype = i64
+        L.vlq_softmax_loss_workspace.argtypes = [C.c_int, i64, i32, i32, C.c_int]
+        L.vlq_softmax_loss_workspace.restype = i64
         L.vlq_last_error.argtypes = []
         L.vlq_last_error.restype = C.c_char_p
         _lib = L
@@ -213,3 +219,54 @@ def vlq_profile_read(idx):
     ln = (C.c_int32 * len(STAGES))()
     _chk(lib().vlq_profile_read(idx, ms, ln))
     return {s: (float(ms[i]), int(ln[i])) for i, s in enumerate(STAGES)}
+
+
+# ---------------------------------------------------------------------------
+# learning cells by gradient: the value type follows from the tensors, the workspace is a uint8 tensor
+# ---------------------------------------------------------------------------
+def _type(t):
+    dtype = t.dtype if isinstance(t, torch.Tensor) else t
+    if dtype not in _TYPES:
+        raise ValueError(f"expected float32, float16 or bfloat16, got {dtype}")
+    return _TYPES[dtype]
+
+
+def _ptrs(*pairs):
+    """Pointers of (tensor or None, dtype, least number of values), all of them on the current device."""
+    out = []
+    for t, dtype, count in pairs:
+        if t is not None:
+            if t.is_cuda and t.get_device() != torch.cuda.current_device():
+                raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+            if t.numel() < count:
+                raise ValueError(f"a tensor has {t.numel()} values, {count} are needed")
+        out.append(_ptr(t, dtype))
+    return out
+
+
+def _bytes(n):
+    if n < 0:
+        _chk(int(n))
+    return int(n)
+
+
+def vlq_softmax_loss_workspace(dtype, n, d, k, backward) -> int:
+    return _bytes(lib().vlq_softmax_loss_workspace(_type(dtype), int(n), int(d), int(k), int(bool(backward))))
+
+
+def vlq_softmax_loss(d_x, n, d, d_c, k, d_bias, scale, d_label, d_loss, d_stats, d_ws, stream=None):
+    n, d, k = int(n), int(d), int(k)
+    x, c, bias, label, loss, stats, ws = _ptrs(
+        (d_x, d_c.dtype, n * d), (d_c, None, k * d), (d_bias, torch.float32, k), (d_label, torch.int32, n), (d_loss, torch.float32, n),
+        (d_stats, torch.float32, 2 * n), (d_ws, torch.uint8, 0))
+    _chk(lib().vlq_softmax_loss(_type(d_c), x, n, d, c, k, bias, float(scale), label, loss, stats, ws, d_ws.numel(), _stream(stream)))
+
+
+def vlq_softmax_loss_backward(d_x, n, d, d_c, k, d_bias, scale, d_label, d_stats, d_grad, d_dx, d_dc, d_dbias, d_ws, stream=None):
+    n, d, k = int(n), int(d), int(k)
+    x, c, bias, label, stats, grad, dx, dc, dbias, ws = _ptrs(
+        (d_x, d_c.dtype, n * d), (d_c, None, k * d), (d_bias, torch.float32, k), (d_label, torch.int32, n),
+        (d_stats, torch.float32, 2 * n), (d_grad, torch.float32, n), (d_dx, d_c.dtype, n * d), (d_dc, d_c.dtype, k * d),
+        (d_dbias, torch.float32, k), (d_ws, torch.uint8, 0))
+    _chk(lib().vlq_softmax_loss_backward(_type(d_c), x, n, d, c, k, bias, float(scale), label, stats, grad, dx, dc, dbias, ws,
+                                         d_ws.numel(), _stream(stream)))

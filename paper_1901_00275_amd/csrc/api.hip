@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "common.h"
+#include "learn.h"
 
 // ---------------------------------------------------------------------------
 // errors
@@ -1230,4 +1231,85 @@ extern "C" int vlq_profile_read(vlq_index_t *idx, float *ms, int32_t *launches)
     }
     idx->recs.clear();
     return rc;
+}
+
+// ---------------------------------------------------------------------------
+// learning cells by gradient
+// ---------------------------------------------------------------------------
+static int check_dtype(int dtype)
+{
+    if (dtype != VLQ_F32 && dtype != VLQ_F16 && dtype != VLQ_BF16) return fail(VLQ_EINVAL, "dtype = %d is none of VLQ_F32, VLQ_F16, VLQ_BF16", dtype);
+    return VLQ_OK;
+}
+
+// p is given (or may be NULL) and aligned
+static int check_ptr(const char *name, const void *p, size_t align, bool optional = false)
+{
+    if (!p && !optional) return fail(VLQ_EINVAL, "%s must not be NULL", name);
+    if ((uintptr_t)p % align) return fail(VLQ_EINVAL, "%s is not aligned to %d bytes", name, (int)align);
+    return VLQ_OK;
+}
+
+static int check_workspace(const void *d_ws, int64_t have, size_t need)
+{
+    if (int rc = check_ptr("d_ws", d_ws, 256)) return rc;
+    if (have < 0 || (uint64_t)have < need) return fail(VLQ_EINVAL, "the workspace has %lld bytes, %zu are needed", (long long)have, need);
+    return VLQ_OK;
+}
+
+static int check_loss_shape(int dtype, int64_t n, int32_t d, int32_t k)
+{
+    if (int rc = check_dtype(dtype)) return rc;
+    if (n < 0 || n > 0x7FFFFFFF) return fail(VLQ_EINVAL, "n = %lld outside [0, 2^31)", (long long)n);
+    if (d < 1 || d > VLQ_MAX_LOSS_DIM) return fail(VLQ_EINVAL, "d = %d outside [1, %d]", d, VLQ_MAX_LOSS_DIM);
+    if (k < 1 || k > VLQ_MAX_LOSS_CLASSES) return fail(VLQ_EINVAL, "k = %d outside [1, %d]", k, VLQ_MAX_LOSS_CLASSES);
+    return VLQ_OK;
+}
+
+extern "C" int64_t vlq_softmax_loss_workspace(int dtype, int64_t n, int32_t d, int32_t k, int backward)
+{
+    if (int rc = check_loss_shape(dtype, n, d, k)) return rc;
+    return (int64_t)loss_workspace(dtype, n, d, k, backward != 0);
+}
+
+static int check_loss(const LossArgs &a, const void *d_ws, int64_t ws_bytes, bool backward)
+{
+    const size_t e = a.dtype == VLQ_F32 ? 4 : 2;
+    if (int rc = check_loss_shape(a.dtype, a.n, a.d, a.k)) return rc;
+    if (!(fabsf(a.scale) < INFINITY)) return fail(VLQ_EINVAL, "scale = %g is not finite", (double)a.scale);
+    if (int rc = check_ptr("d_x", a.x, e, a.n == 0)) return rc;
+    if (int rc = check_ptr("d_c", a.c, e)) return rc;
+    if (int rc = check_ptr("d_bias", a.bias, 4, true)) return rc;
+    if (int rc = check_ptr("d_label", a.label, 4, a.n == 0)) return rc;
+    if (int rc = check_ptr("d_stats", a.stats, 4, a.n == 0)) return rc;
+    return check_workspace(d_ws, ws_bytes, loss_workspace(a.dtype, a.n, a.d, a.k, backward));
+}
+
+extern "C" int vlq_softmax_loss(int dtype, const void *d_x, int64_t n, int32_t d, const void *d_c, int32_t k, const float *d_bias,
+                                float scale, const int32_t *d_label, float *d_loss, float *d_stats, void *d_ws, int64_t ws_bytes,
+                                void *stream)
+{
+    LossArgs a = {dtype, d_x, d_c, n, d, k, d_bias, scale, d_label, d_loss, d_stats, nullptr, nullptr, nullptr, nullptr, d_ws};
+    if (int rc = check_loss(a, d_ws, ws_bytes, false)) return rc;
+    if (int rc = check_ptr("d_loss", d_loss, 4, true)) return rc;
+    if (n == 0) return VLQ_OK;
+    HIPCHK((hipError_t)launch_softmax_loss(a, (hipStream_t)stream));
+    return VLQ_OK;
+}
+
+extern "C" int vlq_softmax_loss_backward(int dtype, const void *d_x, int64_t n, int32_t d, const void *d_c, int32_t k,
+                                         const float *d_bias, float scale, const int32_t *d_label, const float *d_stats,
+                                         const float *d_grad, void *d_dx, void *d_dc, float *d_dbias, void *d_ws, int64_t ws_bytes,
+                                         void *stream)
+{
+    LossArgs a = {dtype, d_x, d_c, n, d, k, d_bias, scale, d_label, nullptr, (float *)d_stats, d_grad, d_dx, d_dc, d_dbias, d_ws};
+    if (int rc = check_loss(a, d_ws, ws_bytes, true)) return rc;
+    const size_t e = dtype == VLQ_F32 ? 4 : 2;
+    if (int rc = check_ptr("d_grad", d_grad, 4, n == 0)) return rc;
+    if (int rc = check_ptr("d_dx", d_dx, e, true)) return rc;
+    if (int rc = check_ptr("d_dc", d_dc, e, true)) return rc;
+    if (int rc = check_ptr("d_dbias", d_dbias, 4, true)) return rc;
+    if (!d_dx && !d_dc && !d_dbias) return VLQ_OK;
+    HIPCHK((hipError_t)launch_softmax_loss_backward(a, (hipStream_t)stream));
+    return VLQ_OK;
 }

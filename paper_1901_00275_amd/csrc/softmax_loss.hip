@@ -1,0 +1,925 @@
+// Softmax cross entropy of n rows against the k centroids (or the k rows of an output layer), the n x k logits not kept,
+// and its gradient:
+//
+//   l_ij = s <x_i, c_j> + b_j,  loss_i = log sum_j exp l_ij - l_iy,  G_ij = g_i (p_ij - [j = y_i]),  p_ij = exp(l_ij) / sum
+//   dx_i = s sum_j G_ij c_j,  dc_j = s sum_i G_ij x_i,  db_j = sum_i G_ij.
+//
+// Four products of n x k x d on the fp16 matrix cores: the logits forward, and backward the logits again and the two
+// gradients.  Operands are first rewritten as fp16 with a power-of-two scale (per row of x, per 128 rows of c, one per
+// matrix where the rows are the summed index):
+//  - fp16 values are taken as they are, bf16 values lose nothing within 32 binades below the largest of their scale;
+//  - an fp32 value is the sum of two fp16 values, hi + lo, with an error of 2^-23 of itself or 2^-40 of the largest of its scale;
+//    a product of two is hi hi + hi lo + lo hi, off by 2^-21 of |a||b| at most: three products where a split in three bf16 parts
+//    takes six.
+// All sums are fp32 (the accumulators of the matrix cores), maxima and sums of the softmax are fp32.
+//
+// Image of a matrix: blocks of 128 rows x units of 32 indices; an 8 KB page per (block, unit, part) holds 8 groups of 16 rows,
+// of each the 64 chunks of 8 values in the order of the lanes that read them (chunk c of row r at 16 c + r % 16), so that a page
+// is copied to LDS as it lies there and read without bank conflicts.
+//
+// Backward, a piece of the centroids at a time (at most PIECE values): P = 2^15 (p - [j = y]) is written as fp16 images in both
+// orders, for the sums over j and over i.  The lanes of the product hold four consecutive j of one i, and four i (16 apart) of one
+// j: the image summed over i has its indices in that order, so neither needs an exchange between lanes.
+#include "learn.h"
+
+#include <math.h>
+
+#include <type_traits>
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16_t;
+
+#define PAGE 512             // 16-byte chunks of a page
+#define LNT 512              // threads of the product kernels
+#define TILE 256             // rows and columns of their tiles
+#define LOSS_ROWS 8192       // rows that go through the products together
+#define PIECE (1 << 25)      // values of P kept at a time
+#define P_ONE 32768.f        // 2^15, what a probability of one is in P
+#define LOG2E 1.4426950408889634f
+#define LN2 0.6931471805599453f
+
+// ---------------------------------------------------------------------------
+// values
+// ---------------------------------------------------------------------------
+// Exponent of the power of two that brings mx to [2^14, 2^15)
+__device__ __forceinline__ int scale_exponent(float mx)
+{
+    const int ex = mx > 0.f ? 14 - ((int)(__float_as_uint(mx) >> 23) - 127) : 0;
+    return min(max(ex, -126), 126);
+}
+__device__ __forceinline__ float pow2i(int ex) { return __uint_as_float((uint32_t)(127 + ex) << 23); }
+
+// eight values of a row from index i on, zeros past its end
+template <typename T>
+__device__ __forceinline__ void load8(const T *row, int i, int d, bool vec, float (&v)[8])
+{
+    if (vec && i < d) { // (d is a multiple of 8)
+        if constexpr (sizeof(T) == 4) {
+            const f32x4 a = *(const f32x4 *)(row + i), b = *(const f32x4 *)(row + i + 4);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = e < 4 ? a[e] : b[e - 4];
+        } else {
+            T t[8];
+            *(u32x4 *)t = *(const u32x4 *)(row + i);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = (float)t[e];
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = i + e < d ? (float)row[i + e] : 0.f;
+}
+
+// v as one or two fp16 parts
+template <int NP>
+__device__ __forceinline__ void split8(const float (&v)[8], half8 (&h)[NP])
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        h[0][e] = (_Float16)v[e];
+        if (NP == 2) h[NP - 1][e] = (_Float16)(v[e] - (float)h[0][e]);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// images
+// ---------------------------------------------------------------------------
+// Header of a call: [0] largest magnitude of x's counted rows (bits), [1] of c, [2] of g
+__global__ void k_loss_header(uint32_t *hdr)
+{
+    if (threadIdx.x < 4) hdr[threadIdx.x] = 0;
+}
+
+// A row counts if its label is a centroid; a centroid if its bias is not -inf.  What does not count is written as zeros.
+__device__ __forceinline__ bool row_counts(const int32_t *label, int k, const float *bias, int64_t r)
+{
+    if (label) return (uint32_t)label[r] < (uint32_t)k;
+    return !bias || bias[r] != -INFINITY;
+}
+
+// Image of the rows of X, RB rows a workgroup: RB = 16 with a scale per row, RB = 128 with one for all.
+// inv: 1 / scale, per row or per block.  Bound by memory: X is read twice (the second time from the caches), written once.
+template <typename T, int RB, int NP>
+__global__ __launch_bounds__(256) void k_pack_rows(const T *__restrict__ X, int64_t rows, int d, int units,
+                                                   const int32_t *__restrict__ label, int k, const float *__restrict__ bias,
+                                                   u32x4 *__restrict__ pages, float *__restrict__ inv, uint32_t *absmax, bool vec)
+{
+    __shared__ float rmax[RB];
+    __shared__ uint8_t counts[RB];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t r0 = (int64_t)blockIdx.x * RB;
+    if (tid < RB) {
+        counts[tid] = r0 + tid < rows && row_counts(label, k, bias, r0 + tid);
+        rmax[tid] = 0.f;
+    }
+    __syncthreads();
+    int ex = 0;
+    if constexpr (!__is_same(T, _Float16)) {
+        for (int r = wave; r < RB; r += 4) {
+            if (!counts[r]) continue;
+            const T *row = X + (r0 + r) * d;
+            float mx = 0.f;
+            for (int i = lane * 8; i < d; i += 512) {
+                float v[8];
+                load8(row, i, d, vec, v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float m = fabsf(v[e]);
+                    if (m < INFINITY) mx = fmaxf(mx, m);
+                }
+            }
+            mx = __uint_as_float(wave_max_u32(__float_as_uint(mx)));
+            if (lane == 0) rmax[r] = mx;
+        }
+        __syncthreads();
+        float mx = 0.f;
+        for (int r = lane; r < RB; r += 64) mx = fmaxf(mx, rmax[r]);
+        mx = __uint_as_float(wave_max_u32(__float_as_uint(mx)));
+        if (RB == 128) ex = scale_exponent(mx);
+        if (tid == 0 && absmax) atomicMax(absmax, __float_as_uint(mx));
+    }
+    if (RB == 128) {
+        if (tid == 0) inv[blockIdx.x] = pow2i(-ex);
+    } else if (tid < RB) {
+        inv[r0 + tid] = __is_same(T, _Float16) ? 1.f : pow2i(-scale_exponent(rmax[tid]));
+    }
+    for (int it = wave; it < units * (RB / 16); it += 4) {
+        const int grp = it % (RB / 16), u = it / (RB / 16), r = grp * 16 + (lane & 15);
+        float v[8] = {};
+        if (counts[r]) load8(X + (r0 + r) * d, u * 32 + (lane >> 4) * 8, d, vec, v);
+        const float s = __is_same(T, _Float16) ? 1.f : RB == 128 ? pow2i(ex) : pow2i(scale_exponent(rmax[r]));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= s;
+        half8 h[NP];
+        split8<NP>(v, h);
+        const int64_t blk = RB == 128 ? blockIdx.x : blockIdx.x >> 3;
+        const int g16 = RB == 128 ? grp : (blockIdx.x & 7);
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+            pages[((blk * units + u) * NP + p) * PAGE + g16 * 64 + lane] = __builtin_bit_cast(u32x4, h[p]);
+    }
+}
+
+// Image of X's columns: its rows are the dimensions, its indices the rows of X, 64 rows x 128 dimensions a workgroup.
+// PERM: index s of 64 is row (s >> 2) + 16 (s & 3), the order in which the lanes of k_loss_p hold them.
+template <typename T, bool PERM, int NP>
+__global__ __launch_bounds__(256) void k_pack_cols(const T *__restrict__ X, int64_t rows, int d, int units,
+                                                   const int32_t *__restrict__ label, int k, const float *__restrict__ bias,
+                                                   u32x4 *__restrict__ pages, const uint32_t *__restrict__ absmax)
+{
+    __shared__ float t[64][129];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t r0 = (int64_t)blockIdx.x * 64;
+    const int d0 = blockIdx.y * 128;
+    const float s = __is_same(T, _Float16) ? 1.f : pow2i(scale_exponent(__uint_as_float(*absmax)));
+    for (int i = tid; i < 64 * 128; i += 256) {
+        const int r = i >> 7, c = i & 127;
+        float v = 0.f;
+        if (r0 + r < rows && d0 + c < d && row_counts(label, k, bias, r0 + r)) v = (float)X[(r0 + r) * d + d0 + c];
+        t[r][c] = v * s;
+    }
+    __syncthreads();
+    for (int it = wave; it < 16; it += 4) {
+        const int e = it & 1, grp = it >> 1;
+        float v[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const int i = e * 32 + (lane >> 4) * 8 + q;
+            v[q] = t[PERM ? (i >> 2) + 16 * (i & 3) : i][grp * 16 + (lane & 15)];
+        }
+        half8 h[NP];
+        split8<NP>(v, h);
+        const int64_t u = (int64_t)blockIdx.x * 2 + e;
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+            pages[(((int64_t)blockIdx.y * units + u) * NP + p) * PAGE + grp * 64 + lane] = __builtin_bit_cast(u32x4, h[p]);
+    }
+}
+
+// bias in units of log 2, -inf past the last centroid
+__global__ __launch_bounds__(256) void k_loss_bias(const float *bias, int k, int kpad, float *bias2)
+{
+    const int j = blockIdx.x * 256 + threadIdx.x;
+    if (j < kpad) bias2[j] = j < k ? (bias ? bias[j] * LOG2E : 0.f) : -INFINITY;
+}
+
+__global__ __launch_bounds__(256) void k_grad_max(const float *g, const int32_t *label, int k, int64_t n, uint32_t *out)
+{
+    float mx = 0.f;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256)
+        if ((uint32_t)label[i] < (uint32_t)k && fabsf(g[i]) < INFINITY) mx = fmaxf(mx, fabsf(g[i]));
+    mx = __uint_as_float(wave_max_u32(__float_as_uint(mx)));
+    if ((threadIdx.x & 63) == 0) atomicMax(out, __float_as_uint(mx));
+}
+
+// Per row: f = s log2(e) / scale, and backward the maximum m2, the factors of P in either order (2^15 / z, and with g / max g);
+// a row that does not count, or has no logit above -inf, gets m2 = +inf and no label.
+__global__ __launch_bounds__(256) void k_loss_rows(const float *rinv, const int32_t *label, int64_t n, int k, float scale,
+                                                   const float *stats, const float *g, const uint32_t *hdr, f32x4 *row, float *gn,
+                                                   int32_t *lab)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; // (the grid covers the padded rows)
+    const bool in = i < n && (uint32_t)label[i] < (uint32_t)k;
+    f32x4 r = {in ? scale * LOG2E * rinv[i] : 0.f, INFINITY, 0.f, 0.f};
+    float f = 0.f;
+    bool ok = in;
+    if (stats && in) {
+        const float m = stats[2 * i], z = stats[2 * i + 1], top = __uint_as_float(hdr[2]);
+        ok = m != -INFINITY;
+        if (ok) {
+            f = top > 0.f ? g[i] / top : 0.f;
+            r[1] = m;
+            r[2] = P_ONE / z;
+            r[3] = P_ONE / z * f;
+        } else {
+            r[0] = 0.f;
+        }
+    }
+    row[i] = r;
+    lab[i] = ok ? label[i] : -1;
+    if (gn) gn[i] = ok ? f * P_ONE : 0.f;
+}
+
+// ---------------------------------------------------------------------------
+// products
+// ---------------------------------------------------------------------------
+// One operand of a product: its image, pages from a block to the next, first page of the sum
+struct Operand {
+    const u32x4 *pages;
+    int64_t block; // pages per block of 128 rows
+    int64_t first;
+};
+
+// acc = A B^T over `steps` steps of two pages: two units of 32 indices (NP = 1), or both parts of one (NP = 2).
+// A tile of MB blocks of A by two of B; eight waves, 2 x 4, of 64 MB rows of A x 64 of B each.  A lane's acc[i][j][r] is row
+// 16 i + 4 (lane / 16) + r, column 16 j + lane % 16 of its wave's part.  Two buffers in LDS: while a step is multiplied the
+// next one is copied from memory to LDS.
+template <int NP, int MB>
+__device__ __forceinline__ void product(const Operand &A, const Operand &B, int64_t ablk, int64_t bblk, int steps,
+                                        u32x4 *lds, f32x4 (&acc)[4 * MB][4])
+{
+    constexpr int IM = 4 * MB, PAGES = 2 * MB + 4;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const u32x4 *a0 = A.pages + (ablk * A.block + A.first) * PAGE, *b0 = B.pages + (bblk * B.block + B.first) * PAGE;
+#pragma unroll
+    for (int i = 0; i < IM; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto copy_page = [&](const u32x4 *src, u32x4 *dst) {
+        const __amdgpu_buffer_rsrc_t page = __builtin_amdgcn_make_buffer_rsrc((void *)src, 0, PAGE * 16, 0x00020000);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(page, (__attribute__((address_space(3))) void *)(dst + wave * 64), 16, tid * 16, 0, 0, 0);
+    };
+    auto copy_step = [&](int t) {
+        u32x4 *dst = lds + (t & 1) * PAGES * PAGE;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+#pragma unroll
+            for (int b = 0; b < MB; ++b) copy_page(a0 + (b * A.block + 2 * t + e) * PAGE, dst + (b * 2 + e) * PAGE);
+#pragma unroll
+            for (int b = 0; b < 2; ++b) copy_page(b0 + (b * B.block + 2 * t + e) * PAGE, dst + (2 * MB + b * 2 + e) * PAGE);
+        }
+    };
+    const int am = wave >> 2, bn = wave & 3;
+    const int aoff = MB == 2 ? am * 2 * PAGE : am * 4 * 64;
+    const int boff = (2 * MB + (bn >> 1) * 2) * PAGE + (bn & 1) * 4 * 64;
+    copy_step(0);
+    for (int t = 0; t < steps; ++t) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads(); // (this step has arrived, and nobody reads the other buffer any more)
+        if (t + 1 < steps) copy_step(t + 1);
+        const u32x4 *st = lds + (t & 1) * PAGES * PAGE + lane;
+        half8 a[2][IM], b[2][4];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b[e][j] = __builtin_bit_cast(half8, st[boff + e * PAGE + j * 64]);
+#pragma unroll
+            for (int i = 0; i < IM; ++i) a[e][i] = __builtin_bit_cast(half8, st[aoff + e * PAGE + i * 64]);
+        }
+        if (NP == 2) {
+#pragma unroll
+            for (int i = 0; i < IM; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[0][i], b[1][j], acc[i][j], 0, 0, 0);
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[1][i], b[0][j], acc[i][j], 0, 0, 0);
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[0][i], b[0][j], acc[i][j], 0, 0, 0);
+                }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int i = 0; i < IM; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[e][i], b[e][j], acc[i][j], 0, 0, 0);
+        }
+    }
+}
+
+// The tile of a workgroup: workgroups go to the eight dies in turn, so each die is given a run of neighbouring tiles, within
+// which eight tiles of B by a few of A share their pages in the die's L2.
+__device__ __forceinline__ void tile_of(int b, int mt, int nt, int *m, int *n)
+{
+    const int total = mt * nt, per = total >> 3, rest = total & 7, die = b & 7, at = b >> 3;
+    const int id = die * per + min(die, rest) + at;
+    const int band = id / (8 * mt), width = min(8, nt - band * 8), in = id - band * 8 * mt;
+    *m = in / width;
+    *n = band * 8 + in - *m * width;
+}
+
+struct LogitArgs {
+    Operand A, B; // centroids, rows
+    const float *cinv, *bias2;
+    const f32x4 *row;
+    const int32_t *lab;
+    int steps, mt, nt;
+    int npad;
+    int m_first; // first centroid of the piece
+    // forward
+    float2 *part; // [mt * 2][npad] {maximum, sum} of 128 centroids
+    float *mine;  // [npad] the label's logit
+    // backward
+    const float *gn;
+    u32x2 *pj, *pi; // P's images, summed over j and over i
+    int jblock, iblock; // pages per block of either
+    float *dbpart;  // [npad / 64][mt * 256] or NULL
+};
+
+// Forward: per row the maximum and the sum over the 128 centroids of a wave's part.  A lane holds 32 centroids of each of
+// four rows, so most of the reduction stays in its registers.
+template <int NP>
+__global__ __launch_bounds__(LNT, 2) void k_loss_stats(LogitArgs a)
+{
+    extern __shared__ u32x4 lds[];
+    const int tid = threadIdx.x, lane = tid & 63, l = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int mt, nt;
+    tile_of(blockIdx.x, a.mt, a.nt, &mt, &nt);
+    f32x4 acc[8][4];
+    product<NP, 2>(a.A, a.B, mt * 2, nt * 2, a.steps, lds, acc);
+    const int m0 = mt * TILE + (wave >> 2) * 128, n0 = nt * TILE + (wave & 3) * 64;
+    const float ci = a.cinv[m0 >> 7];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const f32x4 b2 = *(const f32x4 *)(a.bias2 + m0 + 16 * i + 4 * g);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float f = a.row[n0 + 16 * j + l][0] * ci;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[i][j][r] = b2[r] == -INFINITY ? -INFINITY : fmaf(acc[i][j][r], f, b2[r]);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int n = n0 + 16 * j + l;
+        float m = -INFINITY, z = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) m = fmaxf(m, acc[i][j][r]);
+        m = fmaxf(m, __shfl_xor(m, 16, 64));
+        m = fmaxf(m, __shfl_xor(m, 32, 64));
+        const float m1 = m == -INFINITY ? 0.f : m; // (all masked: every term is zero)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) z += __builtin_amdgcn_exp2f(acc[i][j][r] - m1);
+        z += __shfl_xor(z, 16, 64);
+        z += __shfl_xor(z, 32, 64);
+        if (g == 0) a.part[(int64_t)(mt * 2 + (wave >> 2)) * a.npad + n] = make_float2(m, z);
+        const int rel = a.lab[n] - m0;
+        if (__any((uint32_t)rel < 128u)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (rel == 16 * i + 4 * g + r) a.mine[n] = acc[i][j][r];
+        }
+    }
+}
+
+// A row's statistics and loss from its parts, 16 threads a row
+__global__ __launch_bounds__(256) void k_loss_merge(const float2 *part, int parts, int npad, const float *mine, const int32_t *lab,
+                                                    int64_t n, float *stats, float *loss)
+{
+    const int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x & 15);
+    const int t = threadIdx.x >> 4;
+    float m = -INFINITY, z = 0.f;
+    for (int p = t; p < parts; p += 16) {
+        const float2 v = part[(int64_t)p * npad + i];
+        const float top = fmaxf(m, v.x), base = top == -INFINITY ? 0.f : top;
+        z = z * __builtin_amdgcn_exp2f(m - base) + v.y * __builtin_amdgcn_exp2f(v.x - base);
+        m = top;
+    }
+    __shared__ float2 s[16][16];
+    s[t][threadIdx.x & 15] = make_float2(m, z);
+    __syncthreads();
+    if (t != 0 || i >= n) return;
+    for (int p = 1; p < 16; ++p) {
+        const float2 v = s[p][threadIdx.x];
+        const float top = fmaxf(m, v.x), base = top == -INFINITY ? 0.f : top;
+        z = z * __builtin_amdgcn_exp2f(m - base) + v.y * __builtin_amdgcn_exp2f(v.x - base);
+        m = top;
+    }
+    stats[2 * i] = m;
+    stats[2 * i + 1] = z;
+    if (loss) loss[i] = lab[i] < 0 ? 0.f : m == -INFINITY ? INFINITY : LN2 * (m - mine[i]) + logf(z);
+}
+
+// Backward: P of a tile, as images in both orders, and the sums over a wave's 64 rows for the bias
+template <int NP>
+__global__ __launch_bounds__(LNT, 2) void k_loss_p(LogitArgs a)
+{
+    extern __shared__ u32x4 lds[];
+    const int tid = threadIdx.x, lane = tid & 63, l = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int mt, nt;
+    tile_of(blockIdx.x, a.mt, a.nt, &mt, &nt);
+    f32x4 acc[8][4];
+    product<NP, 2>(a.A, a.B, mt * 2, nt * 2, a.steps, lds, acc);
+    const int m0 = mt * TILE + (wave >> 2) * 128, n0 = nt * TILE + (wave & 3) * 64; // (within the piece)
+    const float ci = a.cinv[m0 >> 7];
+    f32x4 row[4];
+    int rel[4];
+    float gn[4];
+    bool any = false;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int n = n0 + 16 * j + l;
+        row[j] = a.row[n];
+        row[j][0] *= ci;
+        rel[j] = a.lab[n] - a.m_first - m0 - 4 * g; // (16 i + r where the lane holds the label)
+        if (a.lab[n] < 0) rel[j] = -1;
+        gn[j] = a.gn[n];
+        any |= (uint32_t)rel[j] < 128u && (rel[j] & 12) == 0;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const f32x4 b2 = *(const f32x4 *)(a.bias2 + m0 + 16 * i + 4 * g);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                acc[i][j][r] = b2[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], row[j][0], b2[r] - row[j][1]));
+    }
+    const bool labels = __any(any);
+    // image summed over j: the rows of its blocks are the rows i, the lane's four r are half a chunk
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int n = n0 + 16 * j + l;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            f32x4 v = acc[i][j] * row[j][2];
+            if (labels)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (rel[j] == 16 * i + r) v[r] -= P_ONE;
+            const int jj = m0 + 16 * i; // index of the sum, from the piece's first
+            u32x2 *to = a.pj + (((int64_t)(n >> 7) * a.jblock + (jj >> 5) * NP) * PAGE + ((n >> 4) & 7) * 64 +
+                                16 * (2 * (i & 1) + (g >> 1)) + l) * 2 + (g & 1);
+            half4 h, lo;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                h[r] = (_Float16)v[r];
+                lo[r] = (_Float16)(v[r] - (float)h[r]);
+            }
+            to[0] = __builtin_bit_cast(u32x2, h);
+            if (NP == 2) to[PAGE * 2] = __builtin_bit_cast(u32x2, lo);
+        }
+    }
+    // image summed over i, weighted by g: the rows of its blocks are the centroids (row 4 r + g of 16 is centroid 4 g + r),
+    // the lane's four rows j are half a chunk
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            half4 h, lo;
+            float sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float v = acc[i][j][r] * row[j][3];
+                if (labels && rel[j] == 16 * i + r) v -= gn[j];
+                sum += v;
+                h[j] = (_Float16)v;
+                lo[j] = (_Float16)(v - (float)h[j]);
+            }
+            u32x2 *to = a.pi + (((int64_t)(m0 >> 7) * a.iblock + ((n0 >> 5) + (l >> 3)) * NP) * PAGE + i * 64 +
+                                16 * ((l >> 1) & 3) + 4 * r + g) * 2 + (l & 1);
+            to[0] = __builtin_bit_cast(u32x2, h);
+            if (NP == 2) to[PAGE * 2] = __builtin_bit_cast(u32x2, lo);
+            if (a.dbpart) {
+                sum = row16_sum(sum);
+                if (l == 0) a.dbpart[(int64_t)(n0 >> 6) * (a.mt * TILE) + m0 + 16 * i + 4 * g + r] = sum;
+            }
+        }
+}
+
+// One gradient: out[row][dim] = factor sum over the index of A[dim] B[row]
+struct GradOut {
+    Operand A, B; // columns' image (rows: dimensions), P's image
+    int steps, mt, nt, splits, per; // steps of the sum, tiles, and parts that the sum is cut into, `per` steps each
+    int rows, d;
+    bool permuted; // rows of B in the order 4 r + g
+    int mode;      // 0: typed, times the factor; 1: fp32 slabs, stored; 2: added to what is there
+    void *out;     // typed [rows x d], or slabs [splits][rows x d]
+    int64_t slab;
+    const uint32_t *absmax, *gmax; // of the columns' matrix, and of g (or NULL)
+    const float *weight;           // of the rows (or NULL), and where they do not count
+    const int32_t *lab;
+    float scale;
+    bool vec;
+};
+
+template <typename T>
+__device__ __forceinline__ float grad_factor(const uint32_t *absmax, const uint32_t *gmax, float scale)
+{
+    const float inv = __is_same(T, _Float16) ? 1.f : pow2i(-scale_exponent(__uint_as_float(*absmax)));
+    return scale * (gmax ? __uint_as_float(*gmax) : 1.f) * (1.f / P_ONE) * inv;
+}
+
+template <typename T>
+__device__ __forceinline__ void store4(T *p, const f32x4 &v, int count, bool vec)
+{
+    if (vec && count >= 4) {
+        if constexpr (sizeof(T) == 4) {
+            *(f32x4 *)p = v;
+        } else {
+            T t[4] = {(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
+            *(u32x2 *)p = *(u32x2 *)t;
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (e < count) p[e] = (T)v[e];
+}
+
+// Both gradients of a piece in one launch, the one with the longer sums first: a piece's tiles are too few to fill
+// the chip twice over.
+template <typename T, int NP, int MB>
+__global__ __launch_bounds__(LNT, 2) void k_loss_grads(GradOut first, GradOut second, int nfirst)
+{
+    extern __shared__ u32x4 lds[];
+    const bool one = (int)blockIdx.x < nfirst;
+    const GradOut &a = one ? first : second;
+    const int b = one ? blockIdx.x : blockIdx.x - nfirst;
+    const int tid = threadIdx.x, lane = tid & 63, l = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tiles = a.mt * a.nt, split = b / tiles;
+    int mt, nt;
+    tile_of(b - split * tiles, a.mt, a.nt, &mt, &nt);
+    Operand A = a.A, B = a.B;
+    A.first += 2 * (int64_t)split * a.per;
+    B.first += 2 * (int64_t)split * a.per;
+    f32x4 acc[4 * MB][4];
+    product<NP, MB>(A, B, (int64_t)mt * MB, (int64_t)nt * 2, min(a.per, a.steps - split * a.per), lds, acc);
+    const int m0 = mt * 128 * MB + (wave >> 2) * 64 * MB + 4 * g, n0 = nt * TILE + (wave & 3) * 64 + (a.permuted ? 4 * (l & 3) + (l >> 2) : l);
+    const float f = a.mode == 0 ? grad_factor<T>(a.absmax, a.gmax, a.scale) : 1.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int n = n0 + 16 * j;
+        if (n >= a.rows) continue;
+        const float w = !a.weight ? f : a.lab[n] < 0 ? 0.f : a.weight[n] * f;
+#pragma unroll
+        for (int i = 0; i < 4 * MB; ++i) {
+            const int m = m0 + 16 * i;
+            if (m >= a.d) continue;
+            const int64_t at = (int64_t)n * a.d + m;
+            if (a.mode == 0) {
+                store4((T *)a.out + at, acc[i][j] * w, a.d - m, a.vec);
+            } else {
+                float *p = (float *)a.out + split * a.slab + at;
+                f32x4 v = acc[i][j] * w;
+                if (a.mode == 2) {
+                    if (a.vec)
+                        v += *(const f32x4 *)p;
+                    else
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (m + e < a.d) v[e] += p[e];
+                }
+                store4(p, v, a.d - m, a.vec);
+            }
+        }
+    }
+}
+
+// out = factor * sum of the slabs
+template <typename T>
+__global__ __launch_bounds__(256) void k_loss_slabs(const float *slabs, int splits, int64_t slab, int64_t count,
+                                                    const uint32_t *absmax, const uint32_t *gmax, float scale, T *out)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= count) return;
+    float s = 0.f;
+    for (int p = 0; p < splits; ++p) s += slabs[p * slab + i];
+    out[i] = (T)(s * grad_factor<T>(absmax, gmax, scale));
+}
+
+// No rows: the gradients of centroids and bias are zero
+template <typename T>
+__global__ __launch_bounds__(256) void k_loss_none(T *dc, int64_t count, float *dbias, int k)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (dc && i < count) dc[i] = (T)0.f;
+    if (dbias && i < k) dbias[i] = 0.f;
+}
+
+// dbias of a piece: sums over the rows' parts
+__global__ __launch_bounds__(256) void k_loss_dbias(const float *part, int slots, int ld, int count, const uint32_t *gmax, bool add, float *out)
+{
+    const int j = blockIdx.x * 256 + threadIdx.x;
+    if (j >= count) return;
+    float s = 0.f;
+    for (int p = 0; p < slots; ++p) s += part[(int64_t)p * ld + j];
+    s *= __uint_as_float(*gmax) * (1.f / P_ONE);
+    out[j] = add ? out[j] + s : s;
+}
+
+// ---------------------------------------------------------------------------
+// calls
+// ---------------------------------------------------------------------------
+static int64_t pad_to(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+// Where a call's data lies in its workspace
+struct LossPlan {
+    int np;                  // fp16 parts of a value
+    int64_t n, npad, kpad;
+    int d, units, dblocks;   // units of 32 indices of a row's image, blocks of 128 dimensions
+    int64_t rows, rpad;      // rows that go through the products together
+    int64_t piece;           // centroids whose P is kept at a time
+    int xsplit, csplit;      // parts that the sums of dx (over a piece) and dc (over `rows`) are cut into
+    bool xslab, cslab;
+    uint32_t *hdr;
+    u32x4 *ximg, *cimg, *xcols, *ccols, *pj, *pi;
+    float *rinv, *cinv, *bias2, *mine, *gn, *dbpart, *xsum, *csum;
+    f32x4 *row;
+    int32_t *lab;
+    float2 *part;
+    size_t bytes;
+};
+
+// Parts of a sum over `steps` steps, so that `tiles` of them fill the chip: each at least four steps long, and the slabs
+// together no larger than 256 MB.
+static int sum_parts(int64_t tiles, int64_t steps, int64_t out_bytes)
+{
+    int64_t s = 256 / (tiles < 1 ? 1 : tiles);
+    if (s > steps / 4) s = steps / 4;
+    if (s * out_bytes > (256ll << 20)) s = (256ll << 20) / out_bytes;
+    if (s <= 1) return 1;
+    const int64_t per = (steps + s - 1) / s;
+    return (int)((steps + per - 1) / per); // (no part is empty)
+}
+
+static LossPlan loss_plan(int dtype, int64_t n, int d, int k, bool backward, void *ws)
+{
+    LossPlan p = {};
+    if (n < 1) n = 1; // (a call without rows plans for one)
+    p.np = dtype == VLQ_F32 ? 2 : 1;
+    p.n = n;
+    p.npad = pad_to(n, TILE);
+    p.kpad = pad_to(k, TILE);
+    p.d = d;
+    p.units = p.np == 2 ? (d + 31) / 32 : (d + 63) / 64 * 2;
+    p.dblocks = d <= 128 ? 1 : (int)(pad_to(d, 256) / 128);
+    p.rows = n < LOSS_ROWS ? n : LOSS_ROWS;
+    p.rpad = pad_to(p.rows, TILE);
+    p.piece = PIECE / p.rpad / TILE * TILE;
+    if (p.piece < TILE) p.piece = TILE;
+    if (p.piece > p.kpad) p.piece = p.kpad;
+    size_t off = 0;
+    auto take = [&](auto *&ptr, size_t count) {
+        off = (off + 255) & ~(size_t)255;
+        ptr = ws ? (std::remove_reference_t<decltype(ptr)>)((char *)ws + off) : nullptr;
+        off += count * sizeof(*ptr);
+    };
+    const size_t page = (size_t)PAGE * p.np;
+    take(p.hdr, 4);
+    take(p.ximg, p.npad / 128 * p.units * page);
+    take(p.cimg, p.kpad / 128 * p.units * page);
+    take(p.rinv, p.npad);
+    take(p.cinv, p.kpad / 128);
+    take(p.bias2, p.kpad);
+    take(p.row, p.npad);
+    take(p.lab, p.npad);
+    if (!backward) {
+        take(p.mine, p.rpad);
+        take(p.part, p.kpad / 128 * p.rpad);
+    } else {
+        const int mb = p.dblocks == 1 ? 1 : 2, mt = p.dblocks / mb;
+        take(p.gn, p.npad);
+        take(p.xcols, p.npad / 32 * p.dblocks * page);
+        take(p.ccols, p.kpad / 32 * p.dblocks * page);
+        take(p.pj, p.rpad * p.piece / 8 * p.np);
+        take(p.pi, p.rpad * p.piece / 8 * p.np);
+        take(p.dbpart, p.rpad / 64 * p.piece);
+        const int64_t many = p.np; // steps per unit pair: two units a step with one part, one with two
+        p.xsplit = sum_parts(p.rpad / TILE * mt, p.piece / 64 * many, n * d * 4);
+        p.csplit = sum_parts(p.piece / TILE * mt, p.rpad / 64 * many, (int64_t)k * d * 4);
+        p.xslab = p.xsplit > 1 || p.kpad > p.piece;
+        p.cslab = p.csplit > 1 || n > p.rows;
+        take(p.xsum, p.xslab ? (size_t)p.xsplit * n * d : 0);
+        take(p.csum, p.cslab ? (size_t)p.csplit * k * d : 0);
+    }
+    p.bytes = (off + 255) & ~(size_t)255;
+    return p;
+}
+
+size_t loss_workspace(int dtype, int64_t n, int d, int k, bool backward)
+{
+    return loss_plan(dtype, n, d, k, backward, nullptr).bytes;
+}
+
+template <typename K>
+static hipError_t allow_lds(K kern, size_t bytes)
+{
+    return hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+}
+
+#define LOSS_TRY(e)                              \
+    do {                                         \
+        const hipError_t e_ = (e);               \
+        if (e_ != hipSuccess) return (int)e_;    \
+    } while (0)
+
+static size_t lds_bytes(int mb) { return (size_t)2 * (2 * mb + 4) * PAGE * 16; }
+
+template <typename T>
+static bool rows_vec(const void *p, int d)
+{
+    return d % 8 == 0 && (uintptr_t)p % 16 == 0;
+}
+
+// The images of rows and centroids, and the bias
+template <typename T, int NP>
+static void loss_images(const LossArgs &a, const LossPlan &p, hipStream_t st)
+{
+    hipLaunchKernelGGL(k_loss_header, dim3(1), dim3(64), 0, st, p.hdr);
+    hipLaunchKernelGGL((k_pack_rows<T, 16, NP>), dim3((unsigned)(p.npad / 16)), dim3(256), 0, st, (const T *)a.x, a.n, a.d, p.units,
+                       a.label, a.k, nullptr, p.ximg, p.rinv, p.hdr, rows_vec<T>(a.x, a.d));
+    hipLaunchKernelGGL((k_pack_rows<T, 128, NP>), dim3((unsigned)(p.kpad / 128)), dim3(256), 0, st, (const T *)a.c, (int64_t)a.k, a.d,
+                       p.units, nullptr, a.k, a.bias, p.cimg, p.cinv, p.hdr + 1, rows_vec<T>(a.c, a.d));
+    hipLaunchKernelGGL(k_loss_bias, dim3((unsigned)(p.kpad / 256)), dim3(256), 0, st, a.bias, a.k, (int)p.kpad, p.bias2);
+}
+
+template <int NP>
+static LogitArgs logit_args(const LossPlan &p, int64_t r0, int64_t rpad, int64_t c0, int64_t cpad)
+{
+    LogitArgs g = {};
+    const int64_t block = (int64_t)p.units * NP;
+    g.A = {p.cimg + c0 / 128 * block * PAGE, block, 0};
+    g.B = {p.ximg + r0 / 128 * block * PAGE, block, 0};
+    g.cinv = p.cinv + c0 / 128;
+    g.bias2 = p.bias2 + c0;
+    g.row = p.row + r0;
+    g.lab = p.lab + r0;
+    g.steps = p.units * NP / 2;
+    g.mt = (int)(cpad / TILE);
+    g.nt = (int)(rpad / TILE);
+    g.npad = (int)rpad;
+    g.m_first = (int)c0;
+    return g;
+}
+
+template <typename T, int NP>
+static int loss_forward(const LossArgs &a, hipStream_t st)
+{
+    const LossPlan p = loss_plan(a.dtype, a.n, a.d, a.k, false, a.ws);
+    loss_images<T, NP>(a, p, st);
+    hipLaunchKernelGGL(k_loss_rows, dim3((unsigned)(p.npad / 256)), dim3(256), 0, st, p.rinv, a.label, a.n, a.k, a.scale, nullptr,
+                       nullptr, p.hdr, p.row, nullptr, p.lab);
+    LOSS_TRY(allow_lds(k_loss_stats<NP>, lds_bytes(2)));
+    for (int64_t r0 = 0; r0 < a.n; r0 += p.rows) {
+        const int64_t rows = a.n - r0 < p.rows ? a.n - r0 : p.rows, rpad = pad_to(rows, TILE);
+        LogitArgs g = logit_args<NP>(p, r0, rpad, 0, p.kpad);
+        g.part = p.part;
+        g.mine = p.mine;
+        hipLaunchKernelGGL(k_loss_stats<NP>, dim3((unsigned)(g.mt * g.nt)), dim3(LNT), lds_bytes(2), st, g);
+        hipLaunchKernelGGL(k_loss_merge, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, st, p.part, g.mt * 2, g.npad, p.mine,
+                           g.lab, rows, a.stats + 2 * r0, a.loss ? a.loss + r0 : nullptr);
+    }
+    return (int)hipGetLastError();
+}
+
+template <typename T, int NP, int MB>
+static int loss_backward(const LossArgs &a, hipStream_t st)
+{
+    if (a.n == 0) {
+        const int64_t count = (int64_t)a.k * a.d;
+        hipLaunchKernelGGL(k_loss_none<T>, dim3((unsigned)((count + 255) / 256)), dim3(256), 0, st, (T *)a.dc, count, a.dbias, a.k);
+        return (int)hipGetLastError();
+    }
+    const LossPlan p = loss_plan(a.dtype, a.n, a.d, a.k, true, a.ws);
+    loss_images<T, NP>(a, p, st);
+    if (a.dc)
+        hipLaunchKernelGGL((k_pack_cols<T, true, NP>), dim3((unsigned)(p.npad / 64), p.dblocks), dim3(256), 0, st, (const T *)a.x, a.n,
+                           a.d, (int)(p.npad / 32), a.label, a.k, nullptr, p.xcols, p.hdr);
+    if (a.dx)
+        hipLaunchKernelGGL((k_pack_cols<T, false, NP>), dim3((unsigned)(p.kpad / 64), p.dblocks), dim3(256), 0, st, (const T *)a.c,
+                           (int64_t)a.k, a.d, (int)(p.kpad / 32), nullptr, a.k, a.bias, p.ccols, p.hdr + 1);
+    const unsigned gblocks = (unsigned)((a.n + 2047) / 2048 < 256 ? (a.n + 2047) / 2048 : 256);
+    hipLaunchKernelGGL(k_grad_max, dim3(gblocks), dim3(256), 0, st, a.grad, a.label, a.k, a.n, p.hdr + 2);
+    hipLaunchKernelGGL(k_loss_rows, dim3((unsigned)(p.npad / 256)), dim3(256), 0, st, p.rinv, a.label, a.n, a.k, a.scale, a.stats,
+                       a.grad, p.hdr, p.row, p.gn, p.lab);
+    LOSS_TRY(allow_lds(k_loss_p<NP>, lds_bytes(2)));
+    LOSS_TRY(allow_lds(k_loss_grads<T, NP, MB>, lds_bytes(MB)));
+    const int mt = p.dblocks / MB;
+    const bool vec = a.d % 4 == 0;
+    for (int64_t r0 = 0; r0 < a.n; r0 += p.rows) {
+        const int64_t rows = a.n - r0 < p.rows ? a.n - r0 : p.rows, rpad = pad_to(rows, TILE);
+        for (int64_t c0 = 0; c0 < p.kpad; c0 += p.piece) {
+            const int64_t cpad = p.kpad - c0 < p.piece ? p.kpad - c0 : p.piece;
+            LogitArgs g = logit_args<NP>(p, r0, rpad, c0, cpad);
+            g.gn = p.gn + r0;
+            g.pj = (u32x2 *)p.pj;
+            g.pi = (u32x2 *)p.pi;
+            g.jblock = (int)(cpad / 32 * NP);
+            g.iblock = (int)(rpad / 32 * NP);
+            g.dbpart = a.dbias ? p.dbpart : nullptr;
+            hipLaunchKernelGGL(k_loss_p<NP>, dim3((unsigned)(g.mt * g.nt)), dim3(LNT), lds_bytes(2), st, g);
+            if (a.dbias) {
+                const int count = (int)(a.k - c0 < cpad ? a.k - c0 : cpad);
+                hipLaunchKernelGGL(k_loss_dbias, dim3((unsigned)((count + 255) / 256)), dim3(256), 0, st, p.dbpart, (int)(rpad / 64),
+                                   (int)cpad, count, p.hdr + 2, r0 > 0, a.dbias + c0);
+            }
+            GradOut x = {}, c = {};
+            if (a.dx) {
+                x.A = {p.ccols, p.kpad / 32 * NP, c0 / 32 * NP};
+                x.B = {p.pj, g.jblock, 0};
+                x.steps = g.jblock / 2;
+                x.mt = mt;
+                x.nt = g.nt;
+                x.splits = p.xsplit;
+                x.per = (x.steps + p.xsplit - 1) / p.xsplit;
+                x.splits = (x.steps + x.per - 1) / x.per; // (a shorter last piece may need fewer: its other slabs stay as they are)
+                x.rows = (int)rows;
+                x.mode = p.xslab ? (c0 > 0 ? 2 : 1) : 0;
+                x.out = p.xslab ? (void *)(p.xsum + r0 * a.d) : (void *)((T *)a.dx + r0 * a.d);
+                x.slab = a.n * a.d;
+                x.absmax = p.hdr + 1;
+                x.weight = a.grad + r0;
+                x.lab = p.lab + r0;
+                x.vec = vec && (p.xslab || (uintptr_t)a.dx % 16 == 0);
+            }
+            if (a.dc) {
+                const int64_t cols = a.k - c0 < cpad ? a.k - c0 : cpad;
+                c.A = {p.xcols, p.npad / 32 * NP, r0 / 32 * NP};
+                c.B = {p.pi, g.iblock, 0};
+                c.steps = g.iblock / 2;
+                c.mt = mt;
+                c.nt = g.mt;
+                c.splits = p.csplit;
+                c.per = (c.steps + p.csplit - 1) / p.csplit;
+                c.splits = (c.steps + c.per - 1) / c.per;
+                c.permuted = true;
+                c.rows = (int)cols;
+                c.mode = p.cslab ? (r0 > 0 ? 2 : 1) : 0;
+                c.out = p.cslab ? (void *)(p.csum + c0 * a.d) : (void *)((T *)a.dc + c0 * a.d);
+                c.slab = (int64_t)a.k * a.d;
+                c.absmax = p.hdr;
+                c.gmax = p.hdr + 2;
+                c.vec = vec && (p.cslab || (uintptr_t)a.dc % 16 == 0);
+            }
+            x.d = c.d = a.d;
+            x.scale = c.scale = a.scale;
+            const int nx = x.mt * x.nt * x.splits, nc = c.mt * c.nt * c.splits;
+            if (nx + nc == 0) continue;
+            if (c.per > x.per)
+                hipLaunchKernelGGL((k_loss_grads<T, NP, MB>), dim3((unsigned)(nx + nc)), dim3(LNT), lds_bytes(MB), st, c, x, nc);
+            else
+                hipLaunchKernelGGL((k_loss_grads<T, NP, MB>), dim3((unsigned)(nx + nc)), dim3(LNT), lds_bytes(MB), st, x, c, nx);
+        }
+    }
+    auto finish = [&](float *slabs, int splits, int64_t count, const uint32_t *absmax, const uint32_t *gmax, void *out) {
+        hipLaunchKernelGGL(k_loss_slabs<T>, dim3((unsigned)((count + 255) / 256)), dim3(256), 0, st, slabs, splits, count, count, absmax,
+                           gmax, a.scale, (T *)out);
+    };
+    if (a.dx && p.xslab) finish(p.xsum, p.xsplit, a.n * a.d, p.hdr + 1, nullptr, a.dx);
+    if (a.dc && p.cslab) finish(p.csum, p.csplit, (int64_t)a.k * a.d, p.hdr, p.hdr + 2, a.dc);
+    return (int)hipGetLastError();
+}
+
+int launch_softmax_loss(const LossArgs &a, hipStream_t st)
+{
+    switch (a.dtype) {
+    case VLQ_F32: return loss_forward<float, 2>(a, st);
+    case VLQ_F16: return loss_forward<_Float16, 1>(a, st);
+    default: return loss_forward<bf16_t, 1>(a, st);
+    }
+}
+
+int launch_softmax_loss_backward(const LossArgs &a, hipStream_t st)
+{
+    const bool wide = a.d > 128;
+    switch (a.dtype) {
+    case VLQ_F32: return wide ? loss_backward<float, 2, 2>(a, st) : loss_backward<float, 2, 1>(a, st);
+    case VLQ_F16: return wide ? loss_backward<_Float16, 1, 2>(a, st) : loss_backward<_Float16, 1, 1>(a, st);
+    default: return wide ? loss_backward<bf16_t, 1, 2>(a, st) : loss_backward<bf16_t, 1, 1>(a, st);
+    }
+}

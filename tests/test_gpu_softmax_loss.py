@@ -1,0 +1,226 @@
+"""vlq_softmax_loss and its gradient against the formulas in 64 bits: types, odd sizes, rows and centroids that do not count,
+pieces of rows and of centroids, unaligned operands, captured and replayed calls, refusals."""
+import math
+
+import pytest
+import torch
+
+from learn_reference import check, softmax_loss
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+
+
+@pytest.fixture(scope="module")
+def vlq():
+    import paper_1901_00275_amd as vlq
+
+    vlq.lib()
+    return vlq
+
+
+def problem(t, n, d, k, seed=0, spread=1.0, bias=True, skip=0.0, out=0.0, mean=0.0):
+    g = torch.Generator().manual_seed(1000 * seed + n + 7 * d + 13 * k)
+    c = torch.randn(k, d, generator=g) + mean
+    label = torch.randint(0, k, (n,), generator=g, dtype=torch.int32)
+    x = spread * (torch.randn(n, d, generator=g) + 0.5 * c[label.long()]) / math.sqrt(d)
+    label = torch.where(torch.rand(n, generator=g) < skip, torch.full_like(label, -1), label)
+    b = torch.randn(k, generator=g) if bias else None
+    if out:
+        b = torch.where(torch.rand(k, generator=g) < out, torch.full_like(b, -math.inf), b)
+    grad = torch.randn(n, generator=g) / max(n, 1)
+    dev = lambda v, t=None: None if v is None else v.to(t or v.dtype).to(DEV)  # noqa: E731
+    return dev(x, t), dev(c, t), dev(b), dev(label), dev(grad)
+
+
+def run(vlq, x, c, bias, scale, label, grad, what=("dx", "dc", "db"), stream=None):
+    (n, d), k = x.shape, c.shape[0]
+    loss, stats = torch.full((n,), 7.0, device=DEV), torch.full((n, 2), 7.0, device=DEV)
+    ws = torch.full((vlq.vlq_softmax_loss_workspace(x.dtype, n, d, k, 0),), 255, dtype=torch.uint8, device=DEV)  # (NaNs wherever it is read unwritten)
+    vlq.vlq_softmax_loss(x, n, d, c, k, bias, scale, label, loss, stats, ws, stream)
+    if grad is None:
+        return {"loss": loss, "stats": stats}
+    ws = torch.full((vlq.vlq_softmax_loss_workspace(x.dtype, n, d, k, 1),), 255, dtype=torch.uint8, device=DEV)
+    out = {"loss": loss, "stats": stats,
+           "dx": torch.full((n, d), 7.0, dtype=x.dtype, device=DEV) if "dx" in what else None,
+           "dc": torch.full((k, d), 7.0, dtype=x.dtype, device=DEV) if "dc" in what else None,
+           "db": torch.full((k,), 7.0, device=DEV) if "db" in what else None}
+    vlq.vlq_softmax_loss_backward(x, n, d, c, k, bias, scale, label, stats, grad, out["dx"], out["dc"], out["db"], ws, stream)
+    return out
+
+
+def compare(got, want, names=("loss", "dx", "dc", "db")):
+    for name in names:
+        check(got[name], want[name], name)
+
+
+SHAPES = [(1, 1, 1), (1, 96, 300), (3, 7, 2), (64, 32, 256), (65, 33, 257), (255, 96, 1000), (257, 128, 513), (300, 130, 1025),
+          (40, 520, 77), (17, 1027, 515), (1000, 64, 5000)]
+
+
+@pytest.mark.parametrize("t", [F32, F16, BF16])
+@pytest.mark.parametrize("n,d,k", SHAPES)
+def test_against_64_bits(vlq, t, n, d, k):
+    x, c, bias, label, grad = problem(t, n, d, k)
+    compare(run(vlq, x, c, bias, 0.7, label, grad), softmax_loss(x, c, bias, 0.7, label, grad))
+
+
+@pytest.mark.parametrize("t", [F32, F16, BF16])
+@pytest.mark.parametrize("n,d,k", [(1, 40, 100), (200, 96, 700), (513, 200, 300)])
+def test_no_bias_negative_scale(vlq, t, n, d, k):
+    x, c, _, label, grad = problem(t, n, d, k, bias=False, spread=3.0)
+    compare(run(vlq, x, c, None, -1.3, label, grad), softmax_loss(x, c, None, -1.3, label, grad))
+
+
+@pytest.mark.parametrize("t", [F32, F16, BF16])
+def test_rows_and_centroids_that_do_not_count(vlq, t):
+    n, d, k = 300, 96, 900
+    x, c, bias, label, grad = problem(t, n, d, k, skip=0.3, out=0.3)
+    label[5], label[6] = k, 2 ** 31 - 1  # (outside as well)
+    label[7] = int(torch.nonzero(torch.isneginf(bias))[0])  # (the label was taken out)
+    want = softmax_loss(x, c, bias, 0.7, label, grad)
+    dead, gone = (label < 0) | (label >= k), torch.isneginf(bias)
+    x[dead], c[gone] = math.nan, math.inf  # what does not count may hold anything
+    got = run(vlq, x, c, bias, 0.7, label, grad)
+    compare(got, want)
+    assert math.isinf(got["loss"][7].item()) and (got["loss"][dead] == 0).all() and (got["dx"][dead] == 0).all()
+
+
+@pytest.mark.parametrize("t", [F32, BF16])
+def test_nothing_left(vlq, t):
+    n, d, k = 20, 64, 300
+    x, c, bias, label, grad = problem(t, n, d, k)
+    bias.fill_(-math.inf)
+    got = run(vlq, x, c, bias, 1.0, label, grad)
+    assert torch.isposinf(got["loss"]).all()
+    assert all((got[v] == 0).all() for v in ("dx", "dc", "db"))
+    label.fill_(-1)  # no row counts
+    bias.fill_(0.0)
+    got = run(vlq, x, c, bias, 1.0, label, grad)
+    assert all((got[v] == 0).all() for v in ("loss", "dx", "dc", "db"))
+
+
+@pytest.mark.parametrize("t", [F32, F16, BF16])
+def test_pieces_of_rows_and_centroids(vlq, t):
+    # more rows than go through the products together, more centroids than P is kept for at a time
+    n, d, k = 8192 + 300, 40, 4096 + 600
+    x, c, bias, label, grad = problem(t, n, d, k, skip=0.05)
+    compare(run(vlq, x, c, bias, 1.0, label, grad), softmax_loss(x, c, bias, 1.0, label, grad))
+
+
+@pytest.mark.parametrize("t", [F32, BF16])
+def test_large_and_small_logits(vlq, t):
+    # logits in the hundreds, all but one probability vanish; and descriptors with a mean far above their spread
+    x, c, bias, label, grad = problem(t, 130, 128, 600, spread=60.0)
+    compare(run(vlq, x, c, bias, 1.0, label, grad), softmax_loss(x, c, bias, 1.0, label, grad))
+    x, c, bias, label, grad = problem(t, 130, 128, 600, mean=30.0)
+    compare(run(vlq, x, c, bias, 0.02, label, grad), softmax_loss(x, c, bias, 0.02, label, grad))
+
+
+def test_rows_of_uneven_size(vlq):
+    # rows 24 binades apart keep their own scale forward; the gradients are relative to the largest
+    x, c, bias, label, grad = problem(F32, 200, 96, 500)
+    x[::3] *= 2.0 ** -24
+    c[::7] *= 2.0 ** -10
+    compare(run(vlq, x, c, bias, 1.0, label, grad), softmax_loss(x, c, bias, 1.0, label, grad))
+
+
+@pytest.mark.parametrize("t", [F32, F16, BF16])
+def test_unaligned_operands(vlq, t):
+    # one value past a 16-byte boundary, with a dimension that would allow wide loads
+    n, d, k = 70, 64, 300
+    x, c, bias, label, grad = problem(t, n, d, k)
+    shift = lambda v: torch.cat([v.reshape(-1)[:1], v.reshape(-1)])[1:].view(v.shape)  # noqa: E731
+    xs, cs, bs, ls, gs = map(shift, (x, c, bias, label, grad))
+    assert xs.data_ptr() % 16 and torch.equal(xs, x)
+    one, two = run(vlq, x, c, bias, 1.0, label, grad), run(vlq, xs, cs, bs, 1.0, ls, gs)
+    for name in one:
+        assert torch.equal(one[name], two[name]), name
+
+
+@pytest.mark.parametrize("what", [("dx",), ("dc",), ("db",), ("dx", "db")])
+def test_some_gradients_alone(vlq, what):
+    x, c, bias, label, grad = problem(BF16, 300, 160, 700)
+    whole, part = run(vlq, x, c, bias, 1.0, label, grad), run(vlq, x, c, bias, 1.0, label, grad, what)
+    for name in what:
+        assert torch.equal(whole[name], part[name]), name
+
+
+def test_against_differences(vlq):
+    # the gradient along random directions is the central difference of the 64-bit loss: its error is h^2 / 6 of the third
+    # derivative, which is below 2 (2 s |v| max|c|)^3 along a direction v of one row
+    n, d, k, h, s = 5, 16, 40, 1e-4, 0.9
+    x, c, bias, label, grad = problem(F32, n, d, k)
+    got, want = run(vlq, x, c, bias, s, label, grad), softmax_loss(x, c, bias, s, label, grad)
+    total = lambda X, Cc, B: (softmax_loss(X, Cc, B, s, label)["loss"][0] * grad.double()).sum()  # noqa: E731
+    g = torch.Generator().manual_seed(5)
+    for name, at in (("dx", 0), ("dc", 1), ("db", 2)):
+        ops = [x.double(), c.double(), bias.double()]
+        v = torch.randn(ops[at].shape, generator=g, dtype=torch.float64).to(DEV)
+        v /= v.norm()
+        up, down = list(ops), list(ops)
+        up[at], down[at] = ops[at] + h * v, ops[at] - h * v
+        # (64-bit operands: the reference's own bounds are not looked at)
+        diff = (total(*up) - total(*down)) / (2 * h)
+        third = 2 * (2 * s * max(1.0, c.abs().max().item() * d ** 0.5, x.abs().max().item() * d ** 0.5)) ** 3 * grad.abs().sum().item()
+        tol = h * h / 6 * third + (want[name][1] * v.abs()).sum().item() + 1e-11
+        assert abs((got[name].double() * v).sum().item() - diff.item()) <= tol, name
+
+
+def test_stats_give_the_log_sum(vlq):
+    x, c, bias, label, _ = problem(F32, 100, 96, 3000)
+    got, want = run(vlq, x, c, bias, 1.0, label, None), softmax_loss(x, c, bias, 1.0, label)
+    lse = math.log(2) * got["stats"][:, 0].double() + torch.log(got["stats"][:, 1].double())
+    check(lse, (want["m"] + torch.log(want["z"]), want["loss"][1]), "log sum")
+
+
+def test_captured_and_replayed(vlq):
+    n, d, k = 300, 96, 2000
+    x, c, bias, label, grad = problem(F32, n, d, k)
+    ws = torch.empty(vlq.vlq_softmax_loss_workspace(F32, n, d, k, 1), dtype=torch.uint8, device=DEV)
+    loss, stats = torch.empty(n, device=DEV), torch.empty(n, 2, device=DEV)
+    dx, dc, db = torch.empty_like(x), torch.empty_like(c), torch.empty_like(bias)
+
+    def step():
+        vlq.vlq_softmax_loss(x, n, d, c, k, bias, 1.0, label, loss, stats, ws)
+        vlq.vlq_softmax_loss_backward(x, n, d, c, k, bias, 1.0, label, stats, grad, dx, dc, db, ws)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for turn in range(4):
+        x2, c2, b2, l2, g2 = problem(F32, n, d, k, seed=turn + 1)
+        for a, b in ((x, x2), (c, c2), (bias, b2), (label, l2), (grad, g2)):
+            a.copy_(b)
+        want = run(vlq, x, c, bias, 1.0, label, grad)
+        for v in (loss, dx, dc, db):
+            v.fill_(9.0)
+        ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        for name, v in (("loss", loss), ("dx", dx), ("dc", dc), ("db", db)):
+            assert torch.equal(v, want[name]), (turn, name)
+
+
+def test_two_streams(vlq):
+    a, b = problem(BF16, 500, 128, 3000, seed=1), problem(F16, 400, 96, 2000, seed=2)
+    want = [run(vlq, v[0], v[1], v[2], 1.0, v[3], v[4]) for v in (a, b)]
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    got = []
+    for s, v in ((s1, a), (s2, b)):
+        with torch.cuda.stream(s):
+            got.append(run(vlq, v[0], v[1], v[2], 1.0, v[3], v[4]))
+    torch.cuda.synchronize()
+    for w, g in zip(want, got):
+        for name in w:
+            assert torch.equal(w[name], g[name]), name
+
+
+def test_no_rows(vlq):
+    x, c, bias, label, grad = problem(F32, 4, 8, 50)
+    got = run(vlq, x[:0], c, bias, 1.0, label[:0], grad[:0])
+    assert (got["dc"] == 0).all() and (got["db"] == 0).all()
