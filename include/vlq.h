@@ -287,6 +287,9 @@ enum {
 };
 #define VLQ_MAX_LOSS_DIM 16384     /* d of vlq_softmax_loss */
 #define VLQ_MAX_LOSS_CLASSES (1 << 24) /* k of vlq_softmax_loss */
+#define VLQ_MAX_GROUP_CELLS (1 << 24)  /* cells of vlq_group_rows */
+#define VLQ_MAX_ROW (1 << 20)          /* d of the calls on grouped rows */
+#define VLQ_MAX_TENSORS (1 << 20)      /* tensors of vlq_clip_grads */
 
 /*
  * Softmax cross entropy of rows against k centroids (or the k rows of an output layer), without keeping the n x k logits:
@@ -324,6 +327,56 @@ int vlq_softmax_loss_backward(int dtype, const void *d_x, int64_t n, int32_t d, 
 
 /* Bytes of workspace of either call (backward != 0: the second); a negative VLQ_E* code for sizes that are refused. */
 int64_t vlq_softmax_loss_workspace(int dtype, int64_t n, int32_t d, int32_t k, int backward);
+
+/*
+ * Rows grouped by cell: the n x w (row, choice) pairs of d_cell [n x w] (the w nearest cells of a row, or the experts it goes
+ * to) in the order of their cells, pairs of one cell in the order row * w + choice.  A pair whose cell is outside [0, cells) is
+ * dropped; the same cell may come twice in a row.
+ *   d_off [cells + 1] int64: places d_off[c] .. d_off[c + 1] - 1 belong to cell c, d_off[cells] pairs are kept;
+ *   d_place [n x w]: the place of a pair, -1 if it is dropped;
+ *   d_source [n * w]: the pair row * w + choice at a place, -1 behind the last kept pair.
+ * 0 <= n, 1 <= w, n * w < 2^31, 1 <= cells <= VLQ_MAX_GROUP_CELLS; n = 0 writes zeros to d_off.
+ * d_ws: at least vlq_group_rows_workspace(n, w, cells) bytes.
+ */
+int vlq_group_rows(const int32_t *d_cell, int64_t n, int32_t w, int32_t cells, int64_t *d_off, int32_t *d_place,
+                   int32_t *d_source, void *d_ws, int64_t ws_bytes, void *stream);
+int64_t vlq_group_rows_workspace(int64_t n, int32_t w, int32_t cells);
+
+/*
+ * The rows of d_x [n x d] in grouped order: d_y [n * w x d], row p is the row of the pair at place p (d_source of
+ * vlq_group_rows); rows behind the last kept pair are left as they were.  Its gradient is vlq_combine_rows of the gradient of
+ * d_y without weights.  1 <= d <= VLQ_MAX_ROW; n = 0 is a no-op.
+ */
+int vlq_gather_rows(int dtype, const void *d_x, int64_t n, int32_t w, int32_t d, const int32_t *d_source, void *d_y,
+                    void *stream);
+
+/*
+ * Grouped rows back to theirs: d_out[i] = sum over c of d_weight[i][c] d_y[d_place[i][c]], in the order of c, in fp32,
+ * rounded once.  d_weight [n x w] fp32, NULL for ones.  Dropped pairs add nothing, whatever their weight; a row all of whose
+ * pairs are dropped is zero.  n = 0 is a no-op.
+ */
+int vlq_combine_rows(int dtype, const void *d_y, int64_t n, int32_t w, int32_t d, const int32_t *d_place,
+                     const float *d_weight, void *d_out, void *stream);
+
+/*
+ * Its gradient: d_dy[d_place[i][c]] = d_weight[i][c] d_dout[i], d_dweight[i][c] = <d_dout[i], d_y[d_place[i][c]]> (fp32; zero for
+ * dropped pairs).  d_dy and d_dweight may each be NULL, d_y with d_dweight.  Rows of d_dy that no pair has are left as they were.
+ */
+int vlq_combine_rows_backward(int dtype, const void *d_dout, const void *d_y, int64_t n, int32_t w, int32_t d,
+                              const int32_t *d_place, const float *d_weight, void *d_dy, float *d_dweight, void *stream);
+
+/*
+ * The norm of `tensors` gradient tensors together, and the gradients brought to at most max_norm:
+ *     norm = sqrt(sum of all squares),   d_out[t] = d_grads[t] * min(1, max_norm / norm).
+ * dtypes, counts, d_grads and d_out are HOST arrays, read before the call returns: tensor t has counts[t] >= 0 values of type
+ * dtypes[t] at d_grads[t]; d_out[t] is d_grads[t] itself (in place) or a buffer apart from all others.  d_out NULL: the norm
+ * alone.  d_norm: one fp32, or NULL.  Squares are summed in fp64.  A norm that is not finite leaves the values as they are
+ * (d_norm tells).  max_norm > 0 (infinity: copies).  Buffers that overlap are refused.
+ * d_ws: at least vlq_clip_grads_workspace(tensors, counts) bytes.
+ */
+int vlq_clip_grads(int32_t tensors, const int32_t *dtypes, const int64_t *counts, const void *const *d_grads,
+                   float max_norm, void *const *d_out, float *d_norm, void *d_ws, int64_t ws_bytes, void *stream);
+int64_t vlq_clip_grads_workspace(int32_t tensors, const int64_t *counts);
 
 /* Message of the last error on this thread ("" if none). */
 const char *vlq_last_error(void);

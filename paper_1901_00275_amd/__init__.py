@@ -69,6 +69,11 @@ def lib():
             "vlq_profile_read": [vp, C.POINTER(C.c_float), C.POINTER(i32)],
             "vlq_softmax_loss": [C.c_int, vp, i64, i32, vp, i32, vp, C.c_float, vp, vp, vp, vp, i64, vp],
             "vlq_softmax_loss_backward": [C.c_int, vp, i64, i32, vp, i32, vp, C.c_float, vp, vp, vp, vp, vp, vp, vp, i64, vp],
+            "vlq_group_rows": [vp, i64, i32, i32, vp, vp, vp, vp, i64, vp],
+            "vlq_gather_rows": [C.c_int, vp, i64, i32, i32, vp, vp, vp],
+            "vlq_combine_rows": [C.c_int, vp, i64, i32, i32, vp, vp, vp, vp],
+            "vlq_combine_rows_backward": [C.c_int, vp, vp, i64, i32, i32, vp, vp, vp, vp, vp],
+            "vlq_clip_grads": [i32, vp, vp, vp, C.c_float, vp, vp, vp, i64, vp],
             "vlq_version": [],
         }
         for name, args in sig.items():
@@ -81,6 +86,10 @@ def lib():
         L.vlq_index_ntotal.restype = i64
         L.vlq_softmax_loss_workspace.argtypes = [C.c_int, i64, i32, i32, C.c_int]
         L.vlq_softmax_loss_workspace.restype = i64
+        L.vlq_group_rows_workspace.argtypes = [i64, i32, i32]
+        L.vlq_group_rows_workspace.restype = i64
+        L.vlq_clip_grads_workspace.argtypes = [i32, vp]
+        L.vlq_clip_grads_workspace.restype = i64
         L.vlq_last_error.argtypes = []
         L.vlq_last_error.restype = C.c_char_p
         _lib = L
@@ -270,3 +279,55 @@ def vlq_softmax_loss_backward(d_x, n, d, d_c, k, d_bias, scale, d_label, d_stats
         (d_dbias, torch.float32, k), (d_ws, torch.uint8, 0))
     _chk(lib().vlq_softmax_loss_backward(_type(d_c), x, n, d, c, k, bias, float(scale), label, stats, grad, dx, dc, dbias, ws,
                                          d_ws.numel(), _stream(stream)))
+
+
+def vlq_group_rows_workspace(n, w, cells) -> int:
+    return _bytes(lib().vlq_group_rows_workspace(int(n), int(w), int(cells)))
+
+
+def vlq_group_rows(d_cell, n, w, cells, d_off, d_place, d_source, d_ws, stream=None):
+    n, w, cells = int(n), int(w), int(cells)
+    cell, off, place, source, ws = _ptrs((d_cell, torch.int32, n * w), (d_off, torch.int64, cells + 1), (d_place, torch.int32, n * w),
+                                         (d_source, torch.int32, n * w), (d_ws, torch.uint8, 0))
+    _chk(lib().vlq_group_rows(cell, n, w, cells, off, place, source, ws, d_ws.numel(), _stream(stream)))
+
+
+def vlq_gather_rows(d_x, n, w, d, d_source, d_y, stream=None):
+    n, w, d = int(n), int(w), int(d)
+    x, source, y = _ptrs((d_x, None, n * d), (d_source, torch.int32, n * w), (d_y, d_x.dtype, n * w * d))
+    _chk(lib().vlq_gather_rows(_type(d_x), x, n, w, d, source, y, _stream(stream)))
+
+
+def vlq_combine_rows(d_y, n, w, d, d_place, d_weight, d_out, stream=None):
+    n, w, d = int(n), int(w), int(d)
+    y, place, weight, out = _ptrs((d_y, None, n * w * d), (d_place, torch.int32, n * w), (d_weight, torch.float32, n * w),
+                                  (d_out, d_y.dtype, n * d))
+    _chk(lib().vlq_combine_rows(_type(d_y), y, n, w, d, place, weight, out, _stream(stream)))
+
+
+def vlq_combine_rows_backward(d_dout, d_y, n, w, d, d_place, d_weight, d_dy, d_dweight, stream=None):
+    n, w, d = int(n), int(w), int(d)
+    dout, y, place, weight, dy, dweight = _ptrs(
+        (d_dout, None, n * d), (d_y, d_dout.dtype, n * w * d), (d_place, torch.int32, n * w), (d_weight, torch.float32, n * w),
+        (d_dy, d_dout.dtype, n * w * d), (d_dweight, torch.float32, n * w))
+    _chk(lib().vlq_combine_rows_backward(_type(d_dout), dout, y, n, w, d, place, weight, dy, dweight, _stream(stream)))
+
+
+def vlq_clip_grads_workspace(grads) -> int:
+    counts = (C.c_int64 * max(1, len(grads)))(*[g.numel() for g in grads])
+    return _bytes(lib().vlq_clip_grads_workspace(len(grads), counts))
+
+
+def vlq_clip_grads(d_grads, max_norm, d_out, d_norm, d_ws, stream=None):
+    """d_grads: a list of tensors; d_out: a list as long (its tensors may be those of d_grads), or None for the norm alone."""
+    n = len(d_grads)
+    if d_out is not None and (len(d_out) != n or any(o.numel() != g.numel() for o, g in zip(d_out, d_grads))):
+        raise ValueError("d_out must have a tensor of the same size for every tensor of d_grads")
+    ptrs = _ptrs(*[(g, None, 0) for g in d_grads])
+    outs = None if d_out is None else _ptrs(*[(o, g.dtype, 0) for o, g in zip(d_out, d_grads)])
+    norm, ws = _ptrs((d_norm, torch.float32, 1), (d_ws, torch.uint8, 0))
+    many = max(1, n)
+    counts = (C.c_int64 * many)(*[g.numel() for g in d_grads])
+    dtypes = (C.c_int32 * many)(*[_type(g) for g in d_grads])
+    _chk(lib().vlq_clip_grads(n, dtypes, counts, (C.c_void_p * many)(*ptrs), float(max_norm),
+                              None if outs is None else (C.c_void_p * many)(*outs), norm, ws, d_ws.numel(), _stream(stream)))

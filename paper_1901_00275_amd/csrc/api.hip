@@ -1274,7 +1274,7 @@ extern "C" int64_t vlq_softmax_loss_workspace(int dtype, int64_t n, int32_t d, i
 
 static int check_loss(const LossArgs &a, const void *d_ws, int64_t ws_bytes, bool backward)
 {
-    const size_t e = a.dtype == VLQ_F32 ? 4 : 2;
+    const size_t e = type_bytes(a.dtype);
     if (int rc = check_loss_shape(a.dtype, a.n, a.d, a.k)) return rc;
     if (!(fabsf(a.scale) < INFINITY)) return fail(VLQ_EINVAL, "scale = %g is not finite", (double)a.scale);
     if (int rc = check_ptr("d_x", a.x, e, a.n == 0)) return rc;
@@ -1304,12 +1304,146 @@ extern "C" int vlq_softmax_loss_backward(int dtype, const void *d_x, int64_t n, 
 {
     LossArgs a = {dtype, d_x, d_c, n, d, k, d_bias, scale, d_label, nullptr, (float *)d_stats, d_grad, d_dx, d_dc, d_dbias, d_ws};
     if (int rc = check_loss(a, d_ws, ws_bytes, true)) return rc;
-    const size_t e = dtype == VLQ_F32 ? 4 : 2;
+    const size_t e = type_bytes(dtype);
     if (int rc = check_ptr("d_grad", d_grad, 4, n == 0)) return rc;
     if (int rc = check_ptr("d_dx", d_dx, e, true)) return rc;
     if (int rc = check_ptr("d_dc", d_dc, e, true)) return rc;
     if (int rc = check_ptr("d_dbias", d_dbias, 4, true)) return rc;
     if (!d_dx && !d_dc && !d_dbias) return VLQ_OK;
     HIPCHK((hipError_t)launch_softmax_loss_backward(a, (hipStream_t)stream));
+    return VLQ_OK;
+}
+
+static int check_rows(int64_t n, int32_t w, int32_t d)
+{
+    if (n < 0) return fail(VLQ_EINVAL, "n = %lld is negative", (long long)n);
+    if (w < 1 || n > 0x7FFFFFFF / w) return fail(VLQ_EINVAL, "n = %lld rows of w = %d choices: w must be positive, n * w below 2^31", (long long)n, w);
+    if (d < 1 || d > VLQ_MAX_ROW) return fail(VLQ_EINVAL, "d = %d outside [1, %d]", d, VLQ_MAX_ROW);
+    return VLQ_OK;
+}
+
+static int check_group(int64_t n, int32_t w, int32_t cells)
+{
+    if (int rc = check_rows(n, w, 1)) return rc;
+    if (cells < 1 || cells > VLQ_MAX_GROUP_CELLS) return fail(VLQ_EINVAL, "cells = %d outside [1, %d]", cells, VLQ_MAX_GROUP_CELLS);
+    return VLQ_OK;
+}
+
+extern "C" int64_t vlq_group_rows_workspace(int64_t n, int32_t w, int32_t cells)
+{
+    if (int rc = check_group(n, w, cells)) return rc;
+    return (int64_t)group_workspace(n * w, cells);
+}
+
+extern "C" int vlq_group_rows(const int32_t *d_cell, int64_t n, int32_t w, int32_t cells, int64_t *d_off, int32_t *d_place,
+                              int32_t *d_source, void *d_ws, int64_t ws_bytes, void *stream)
+{
+    if (int rc = check_group(n, w, cells)) return rc;
+    if (int rc = check_ptr("d_cell", d_cell, 4, n == 0)) return rc;
+    if (int rc = check_ptr("d_off", d_off, 8)) return rc;
+    if (int rc = check_ptr("d_place", d_place, 4, n == 0)) return rc;
+    if (int rc = check_ptr("d_source", d_source, 4, n == 0)) return rc;
+    if (int rc = check_workspace(d_ws, ws_bytes, group_workspace(n * w, cells))) return rc;
+    HIPCHK((hipError_t)launch_group_rows(d_cell, n * w, cells, d_off, d_place, d_source, d_ws, (hipStream_t)stream));
+    return VLQ_OK;
+}
+
+extern "C" int vlq_gather_rows(int dtype, const void *d_x, int64_t n, int32_t w, int32_t d, const int32_t *d_source, void *d_y,
+                               void *stream)
+{
+    if (int rc = check_dtype(dtype)) return rc;
+    if (int rc = check_rows(n, w, d)) return rc;
+    if (n == 0) return VLQ_OK;
+    if (int rc = check_ptr("d_x", d_x, type_bytes(dtype))) return rc;
+    if (int rc = check_ptr("d_source", d_source, 4)) return rc;
+    if (int rc = check_ptr("d_y", d_y, type_bytes(dtype))) return rc;
+    HIPCHK((hipError_t)launch_gather_rows(dtype, d_x, n, w, d, d_source, d_y, (hipStream_t)stream));
+    return VLQ_OK;
+}
+
+extern "C" int vlq_combine_rows(int dtype, const void *d_y, int64_t n, int32_t w, int32_t d, const int32_t *d_place,
+                                const float *d_weight, void *d_out, void *stream)
+{
+    if (int rc = check_dtype(dtype)) return rc;
+    if (int rc = check_rows(n, w, d)) return rc;
+    if (n == 0) return VLQ_OK;
+    if (int rc = check_ptr("d_y", d_y, type_bytes(dtype))) return rc;
+    if (int rc = check_ptr("d_place", d_place, 4)) return rc;
+    if (int rc = check_ptr("d_weight", d_weight, 4, true)) return rc;
+    if (int rc = check_ptr("d_out", d_out, type_bytes(dtype))) return rc;
+    HIPCHK((hipError_t)launch_combine_rows(dtype, d_y, n, w, d, d_place, d_weight, d_out, (hipStream_t)stream));
+    return VLQ_OK;
+}
+
+extern "C" int vlq_combine_rows_backward(int dtype, const void *d_dout, const void *d_y, int64_t n, int32_t w, int32_t d,
+                                         const int32_t *d_place, const float *d_weight, void *d_dy, float *d_dweight, void *stream)
+{
+    if (int rc = check_dtype(dtype)) return rc;
+    if (int rc = check_rows(n, w, d)) return rc;
+    if (n == 0 || (!d_dy && !d_dweight)) return VLQ_OK;
+    if (int rc = check_ptr("d_dout", d_dout, type_bytes(dtype))) return rc;
+    if (int rc = check_ptr("d_y", d_y, type_bytes(dtype), !d_dweight)) return rc;
+    if (int rc = check_ptr("d_place", d_place, 4)) return rc;
+    if (int rc = check_ptr("d_weight", d_weight, 4, true)) return rc;
+    if (int rc = check_ptr("d_dy", d_dy, type_bytes(dtype), true)) return rc;
+    if (int rc = check_ptr("d_dweight", d_dweight, 4, true)) return rc;
+    HIPCHK((hipError_t)launch_combine_rows_backward(dtype, d_dout, d_y, n, w, d, d_place, d_weight, d_dy, d_dweight, (hipStream_t)stream));
+    return VLQ_OK;
+}
+
+static int check_counts(int32_t tensors, const int64_t *counts)
+{
+    if (tensors < 0 || tensors > VLQ_MAX_TENSORS) return fail(VLQ_EINVAL, "tensors = %d outside [0, %d]", tensors, VLQ_MAX_TENSORS);
+    if (tensors > 0 && !counts) return fail(VLQ_EINVAL, "counts must not be NULL");
+    int64_t total = 0;
+    for (int32_t t = 0; t < tensors; ++t) {
+        if (counts[t] < 0 || counts[t] > ((int64_t)1 << 48) - total) return fail(VLQ_EINVAL, "counts[%d] = %lld is negative, or all of them reach 2^48", t, (long long)counts[t]);
+        total += counts[t];
+    }
+    return VLQ_OK;
+}
+
+extern "C" int64_t vlq_clip_grads_workspace(int32_t tensors, const int64_t *counts)
+{
+    if (int rc = check_counts(tensors, counts)) return rc;
+    return (int64_t)clip_workspace(tensors, counts);
+}
+
+extern "C" int vlq_clip_grads(int32_t tensors, const int32_t *dtypes, const int64_t *counts, const void *const *d_grads,
+                              float max_norm, void *const *d_out, float *d_norm, void *d_ws, int64_t ws_bytes, void *stream)
+{
+    if (int rc = check_counts(tensors, counts)) return rc;
+    if (tensors > 0 && (!dtypes || !d_grads)) return fail(VLQ_EINVAL, "dtypes and d_grads must not be NULL");
+    if (!(max_norm > 0.f)) return fail(VLQ_EINVAL, "max_norm = %g must be positive", (double)max_norm);
+    if (int rc = check_ptr("d_norm", d_norm, 4, true)) return rc;
+    if (int rc = check_workspace(d_ws, ws_bytes, clip_workspace(tensors, counts))) return rc;
+    // every buffer given and aligned, and none over another (but an output on its own input)
+    struct Span {
+        uintptr_t from, to;
+    };
+    Span few[128], *span = few;
+    if (tensors > 64) {
+        span = (Span *)malloc((size_t)tensors * 2 * sizeof(Span));
+        if (!span) return fail(VLQ_ENOMEM, "out of host memory");
+    }
+    int32_t spans = 0, rc = VLQ_OK;
+    for (int32_t t = 0; t < tensors && rc == VLQ_OK; ++t) {
+        rc = check_dtype(dtypes[t]);
+        if (rc != VLQ_OK || counts[t] == 0) continue;
+        const size_t e = type_bytes(dtypes[t]), bytes = (size_t)counts[t] * e;
+        rc = check_ptr("a tensor of d_grads", d_grads[t], e);
+        if (rc == VLQ_OK) span[spans++] = {(uintptr_t)d_grads[t], (uintptr_t)d_grads[t] + bytes};
+        if (rc != VLQ_OK || !d_out || d_out[t] == d_grads[t]) continue;
+        rc = check_ptr("a tensor of d_out", d_out[t], e);
+        if (rc == VLQ_OK) span[spans++] = {(uintptr_t)d_out[t], (uintptr_t)d_out[t] + bytes};
+    }
+    if (rc == VLQ_OK && d_out) { // (without outputs tensors may share memory)
+        std::sort(span, span + spans, [](const Span &a, const Span &b) { return a.from < b.from; });
+        for (int32_t i = 1; i < spans && rc == VLQ_OK; ++i)
+            if (span[i].from < span[i - 1].to) rc = fail(VLQ_EINVAL, "two tensors overlap");
+    }
+    if (span != few) free(span);
+    if (rc != VLQ_OK) return rc;
+    HIPCHK((hipError_t)launch_clip_grads(tensors, dtypes, counts, d_grads, max_norm, d_out, d_norm, d_ws, (hipStream_t)stream));
     return VLQ_OK;
 }

@@ -1,0 +1,561 @@
+// Rows sent to the cells (experts) they were given to, and back: a stable counting sort of the n w (row, choice) pairs by
+// cell, the rows gathered in that order, and their weighted sums row by row, with the gradients of both.
+//
+// The sort goes by digits of at most DIGIT bits, the lowest first, and keeps the order of equal ones: every workgroup counts
+// the digits of a tile, the counts of a digit are summed over the tiles, and the workgroup ranks its pairs: a wave's
+// pairs in turn, 64 at a time, those of one digit told apart by ballots.  No atomics on memory, so the order is the pairs' own.
+// The rest moves memory: whole 16 bytes where rows lie on them, several rows' loads under way at a time.
+#include "learn.h"
+
+#include <type_traits>
+
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16_t;
+
+#define DIGIT 11
+#define BINS (1 << DIGIT)
+#define GNT 256          // threads of a workgroup of the sort
+#define GWAVES (GNT / 64)
+#define SMALL_NT 1024    // threads where one workgroup sorts everything
+#define SMALL_PAIRS 16384
+
+// lanes whose digit is this lane's
+__device__ __forceinline__ uint64_t same_digit(uint32_t digit, int bits, bool there)
+{
+    uint64_t m = __ballot(there);
+    for (int b = 0; b < bits; ++b) {
+        const bool one = (digit >> b) & 1;
+        const uint64_t v = __ballot(one);
+        m &= one ? v : ~v;
+    }
+    return m;
+}
+
+struct SortPass {
+    const int32_t *cell;         // the first pass reads the cells, the later ones keys and pairs
+    const uint32_t *key, *pair;
+    uint32_t *key_out, *pair_out;
+    int32_t *place, *source;     // the last pass
+    int64_t *off;                // the only pass
+    uint32_t *count;             // [bins][tiles]
+    uint32_t *total;             // [bins]
+    int64_t pairs;
+    int cells, shift, bits, tile, tiles;
+    bool last, only;
+};
+
+__device__ __forceinline__ uint32_t key_at(const SortPass &a, int64_t i)
+{
+    if (!a.cell) return a.key[i];
+    const uint32_t c = (uint32_t)a.cell[i];
+    return c < (uint32_t)a.cells ? c : (uint32_t)a.cells; // (dropped pairs stand behind all cells)
+}
+
+__global__ __launch_bounds__(GNT) void k_group_count(SortPass a)
+{
+    __shared__ uint32_t h[BINS];
+    const int bins = 1 << a.bits;
+    for (int b = threadIdx.x; b < bins; b += GNT) h[b] = 0;
+    __syncthreads();
+    const int64_t i0 = (int64_t)blockIdx.x * a.tile;
+    const int count = (int)(a.pairs - i0 < a.tile ? a.pairs - i0 : a.tile);
+    for (int i = threadIdx.x; i < count; i += GNT) atomicAdd(&h[(key_at(a, i0 + i) >> a.shift) & (bins - 1)], 1u);
+    __syncthreads();
+    for (int b = threadIdx.x; b < bins; b += GNT) a.count[(int64_t)b * a.tiles + blockIdx.x] = h[b];
+}
+
+// wave-wide inclusive sum
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v, int lane)
+{
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t u = __shfl_up(v, o, 64);
+        if (lane >= o) v += u;
+    }
+    return v;
+}
+
+// exclusive sums of a digit's counts over the tiles, a wave per digit
+__global__ __launch_bounds__(GNT) void k_group_tiles(uint32_t *count, uint32_t *total, int tiles, int bins)
+{
+    const int lane = threadIdx.x & 63, b = blockIdx.x * GWAVES + (threadIdx.x >> 6);
+    if (b >= bins) return;
+    uint32_t *c = count + (int64_t)b * tiles, sum = 0;
+    for (int t = 0; t < tiles; t += 64) {
+        const uint32_t v = t + lane < tiles ? c[t + lane] : 0, s = wave_scan(v, lane);
+        if (t + lane < tiles) c[t + lane] = sum + s - v;
+        sum += __shfl(s, 63, 64);
+    }
+    if (lane == 0) total[b] = sum;
+}
+
+// in place: exclusive sums of v[0 .. bins) by NT threads, v in LDS; the values behind are not touched
+template <int NT>
+__device__ __forceinline__ void block_scan(uint32_t *v, int bins, uint32_t *wsum)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int per = (bins + NT - 1) / NT;
+    uint32_t sum = 0;
+    for (int i = tid * per; i < min(tid * per + per, bins); ++i) sum += v[i];
+    const uint32_t s = wave_scan(sum, lane);
+    if (lane == 63) wsum[wave] = s;
+    __syncthreads();
+    uint32_t base = s - sum;
+    for (int w = 0; w < wave; ++w) base += wsum[w];
+    for (int i = tid * per; i < min(tid * per + per, bins); ++i) {
+        const uint32_t t = v[i];
+        v[i] = base;
+        base += t;
+    }
+    __syncthreads();
+}
+
+// The pairs of a wave (i0 .. i0 + count) to their places: at[digit] is the next place of a digit, kept up by the wave alone
+__device__ __forceinline__ void place_pairs(const SortPass &a, uint32_t *at, int64_t i0, int count, int lane)
+{
+    const uint64_t below = ((uint64_t)1 << lane) - 1;
+    for (int i = 0; i < count; i += 64) {
+        const bool there = i + lane < count;
+        const int64_t id = i0 + i + lane;
+        const uint32_t key = there ? key_at(a, id) : 0, digit = (key >> a.shift) & ((1u << a.bits) - 1);
+        const uint64_t same = same_digit(digit, a.bits, there);
+        uint32_t p = 0;
+        if (there) p = at[digit] + __popcll(same & below);
+        wave_lds_order();
+        if (there && !(same & below)) at[digit] += __popcll(same);
+        wave_lds_order();
+        if (!there) continue;
+        const uint32_t pair = a.cell ? (uint32_t)id : a.pair[id];
+        if (!a.last) {
+            a.key_out[p] = key;
+            a.pair_out[p] = pair;
+        } else {
+            const bool in = key < (uint32_t)a.cells;
+            a.source[p] = in ? (int32_t)pair : -1;
+            a.place[pair] = in ? (int32_t)p : -1;
+            if (!a.only) a.key_out[p] = key;
+        }
+    }
+}
+
+__global__ __launch_bounds__(GNT) void k_group_place(SortPass a)
+{
+    __shared__ uint32_t first[BINS], at[GWAVES][BINS], wsum[GWAVES];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, bins = 1 << a.bits;
+    for (int b = tid; b < bins; b += GNT) {
+        first[b] = a.total[b];
+        for (int w = 0; w < GWAVES; ++w) at[w][b] = 0;
+    }
+    __syncthreads();
+    block_scan<GNT>(first, bins, wsum);
+    if (a.only && blockIdx.x == 0) // (cells + 1 <= bins)
+        for (int b = tid; b <= a.cells; b += GNT) a.off[b] = first[b];
+    const int64_t i0 = (int64_t)blockIdx.x * a.tile;
+    const int per = a.tile / GWAVES, count = (int)max((int64_t)0, min((int64_t)per, a.pairs - i0 - wave * per));
+    for (int i = lane; i < count; i += 64) atomicAdd(&at[wave][(key_at(a, i0 + wave * per + i) >> a.shift) & (bins - 1)], 1u);
+    __syncthreads();
+    for (int b = tid; b < bins; b += GNT) {
+        uint32_t next = first[b] + a.count[(int64_t)b * a.tiles + blockIdx.x];
+        for (int w = 0; w < GWAVES; ++w) {
+            const uint32_t c = at[w][b];
+            at[w][b] = next;
+            next += c;
+        }
+    }
+    __syncthreads();
+    place_pairs(a, at[wave], i0 + wave * per, count, lane);
+}
+
+// Few pairs, few cells: one workgroup, one launch
+__global__ __launch_bounds__(SMALL_NT) void k_group_small(SortPass a)
+{
+    extern __shared__ uint32_t lds[]; // [16][bins] a wave's next places, [bins] a digit's first
+    constexpr int W = SMALL_NT / 64;
+    __shared__ uint32_t wsum[W];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, bins = 1 << a.bits;
+    uint32_t *first = lds + W * bins;
+    for (int b = tid; b < W * bins; b += SMALL_NT) lds[b] = 0;
+    __syncthreads();
+    const int per = ((int)a.pairs + W * 64 - 1) / (W * 64) * 64, i0 = wave * per, count = max(0, min(per, (int)a.pairs - i0));
+    for (int i = lane; i < count; i += 64) atomicAdd(&lds[wave * bins + key_at(a, i0 + i)], 1u);
+    __syncthreads();
+    for (int b = tid; b < bins; b += SMALL_NT) {
+        uint32_t sum = 0;
+        for (int w = 0; w < W; ++w) sum += lds[w * bins + b];
+        first[b] = sum;
+    }
+    __syncthreads();
+    block_scan<SMALL_NT>(first, bins, wsum);
+    for (int b = tid; b < bins; b += SMALL_NT) {
+        uint32_t next = first[b];
+        if (b <= a.cells) a.off[b] = next;
+        for (int w = 0; w < W; ++w) {
+            const uint32_t c = lds[w * bins + b];
+            lds[w * bins + b] = next;
+            next += c;
+        }
+    }
+    __syncthreads();
+    place_pairs(a, lds + wave * bins, i0, count, lane);
+}
+
+// off[c]: the first place whose cell is c or more
+__global__ __launch_bounds__(256) void k_group_offsets(const uint32_t *key, int64_t pairs, int cells, int64_t *off)
+{
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c > cells) return;
+    int64_t lo = 0, hi = pairs;
+    while (lo < hi) {
+        const int64_t mid = (lo + hi) >> 1;
+        if (key[mid] < (uint32_t)c)
+            lo = mid + 1;
+        else
+            hi = mid;
+    }
+    off[c] = lo;
+}
+
+__global__ __launch_bounds__(256) void k_group_none(int cells, int64_t *off)
+{
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c <= cells) off[c] = 0;
+}
+
+struct GroupPlan {
+    int passes, bits[3], tile, tiles;
+    size_t count_off, total_off, key_off[2], pair_off[2], bytes;
+    bool small;
+};
+
+static GroupPlan group_plan(int64_t pairs, int cells)
+{
+    GroupPlan p = {};
+    int bits = 1;
+    while (((int64_t)1 << bits) < (int64_t)cells + 1) ++bits;
+    p.passes = (bits + DIGIT - 1) / DIGIT;
+    for (int i = 0, left = bits; i < p.passes; ++i) {
+        p.bits[i] = (left + p.passes - i - 1) / (p.passes - i);
+        left -= p.bits[i];
+    }
+    p.small = p.passes == 1 && pairs <= SMALL_PAIRS;
+    // tiles: enough of them for every compute unit, large enough that the counts are fewer than the pairs
+    p.tile = 1024;
+    while (p.tile < 8192 && pairs / p.tile > 512) p.tile *= 2;
+    p.tiles = (int)((pairs + p.tile - 1) / p.tile);
+    size_t off = 0;
+    auto take = [&](size_t bytes) {
+        const size_t at = off;
+        off = (off + bytes + 255) & ~(size_t)255;
+        return at;
+    };
+    if (!p.small) {
+        p.count_off = take((size_t)BINS * p.tiles * 4);
+        p.total_off = take((size_t)BINS * 4);
+        if (p.passes > 1)
+            for (int i = 0; i < 2; ++i) {
+                p.key_off[i] = take((size_t)pairs * 4);
+                p.pair_off[i] = take((size_t)pairs * 4);
+            }
+    }
+    p.bytes = off + 256;
+    return p;
+}
+
+size_t group_workspace(int64_t pairs, int cells) { return group_plan(pairs, cells).bytes; }
+
+int launch_group_rows(const int32_t *cell, int64_t pairs, int cells, int64_t *off, int32_t *place, int32_t *source, void *ws,
+                      hipStream_t st)
+{
+    const dim3 cgrid((unsigned)(cells / 256 + 1));
+    if (pairs == 0) {
+        hipLaunchKernelGGL(k_group_none, cgrid, dim3(256), 0, st, cells, off);
+        return (int)hipGetLastError();
+    }
+    const GroupPlan p = group_plan(pairs, cells);
+    char *base = (char *)ws;
+    SortPass a = {};
+    a.cell = cell;
+    a.place = place;
+    a.source = source;
+    a.off = off;
+    a.count = (uint32_t *)(base + p.count_off);
+    a.total = (uint32_t *)(base + p.total_off);
+    a.pairs = pairs;
+    a.cells = cells;
+    a.tile = p.tile;
+    a.tiles = p.tiles;
+    a.only = p.passes == 1;
+    if (p.small) {
+        a.bits = p.bits[0];
+        a.last = true;
+        const size_t bytes = (size_t)(SMALL_NT / 64 + 1) * (4u << a.bits);
+        const hipError_t e = hipFuncSetAttribute((const void *)k_group_small, hipFuncAttributeMaxDynamicSharedMemorySize, (SMALL_NT / 64 + 1) * BINS * 4);
+        if (e != hipSuccess) return (int)e;
+        hipLaunchKernelGGL(k_group_small, dim3(1), dim3(SMALL_NT), bytes, st, a);
+        return (int)hipGetLastError();
+    }
+    for (int i = 0; i < p.passes; ++i) {
+        a.bits = p.bits[i];
+        a.last = i == p.passes - 1;
+        a.key_out = (uint32_t *)(base + p.key_off[i & 1]);
+        a.pair_out = (uint32_t *)(base + p.pair_off[i & 1]);
+        hipLaunchKernelGGL(k_group_count, dim3((unsigned)p.tiles), dim3(GNT), 0, st, a);
+        hipLaunchKernelGGL(k_group_tiles, dim3((unsigned)(((1 << a.bits) + GWAVES - 1) / GWAVES)), dim3(GNT), 0, st, a.count, a.total,
+                           p.tiles, 1 << a.bits);
+        hipLaunchKernelGGL(k_group_place, dim3((unsigned)p.tiles), dim3(GNT), 0, st, a);
+        a.cell = nullptr;
+        a.key = a.key_out;
+        a.pair = a.pair_out;
+        a.shift += a.bits;
+    }
+    if (p.passes > 1) hipLaunchKernelGGL(k_group_offsets, cgrid, dim3(256), 0, st, a.key, pairs, cells, off);
+    return (int)hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------
+// rows
+// ---------------------------------------------------------------------------
+// A piece of a row: 16 bytes, or one value where rows do not lie on 16 bytes
+template <typename T, bool VEC>
+struct Piece {
+    static constexpr int N = VEC ? 16 / (int)sizeof(T) : 1;
+    T v[N];
+};
+template <typename T, bool VEC>
+__device__ __forceinline__ Piece<T, VEC> load_piece(const T *p)
+{
+    Piece<T, VEC> r;
+    if constexpr (VEC)
+        *(u32x4 *)r.v = *(const u32x4 *)p;
+    else
+        r.v[0] = *p;
+    return r;
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void store_piece(T *p, const Piece<T, VEC> &r)
+{
+    if constexpr (VEC)
+        *(u32x4 *)p = *(const u32x4 *)r.v;
+    else
+        *p = r.v[0];
+}
+
+#define ROW_NT 256
+#define ROW_ITEMS 4 // pieces a thread has under way
+
+struct RowsArgs {
+    int64_t n;
+    int w, d;
+    uint32_t per;  // pieces of a row
+    uint32_t rows; // rows of a workgroup
+    const int32_t *index; // source or place
+    const float *weight;
+};
+
+// y[p] = x[source[p] / w]: the pieces of a workgroup's rows, ROW_ITEMS a thread at a time
+template <typename T, bool VEC>
+__global__ __launch_bounds__(ROW_NT) void k_gather_rows(RowsArgs a, const T *__restrict__ x, T *__restrict__ y)
+{
+    using P = Piece<T, VEC>;
+    const int64_t places = a.n * a.w, p0 = (int64_t)blockIdx.x * a.rows;
+    const uint32_t pieces = (uint32_t)min((int64_t)a.rows, places - p0) * a.per;
+    for (uint32_t i0 = threadIdx.x; i0 < pieces; i0 += ROW_NT * ROW_ITEMS) {
+        P v[ROW_ITEMS];
+        int64_t to[ROW_ITEMS];
+#pragma unroll
+        for (int u = 0; u < ROW_ITEMS; ++u) {
+            const uint32_t i = i0 + u * ROW_NT, r = i / a.per, c = i - r * a.per;
+            to[u] = -1;
+            if (i >= pieces) continue;
+            const int32_t s = a.index[p0 + r];
+            if ((int64_t)s >= places || s < 0) continue; // (a place behind the last pair)
+            v[u] = load_piece<T, VEC>(x + (int64_t)((uint32_t)s / (uint32_t)a.w) * a.d + c * P::N);
+            to[u] = (p0 + r) * a.d + c * P::N;
+        }
+#pragma unroll
+        for (int u = 0; u < ROW_ITEMS; ++u)
+            if (to[u] >= 0) store_piece<T, VEC>(y + to[u], v[u]);
+    }
+}
+
+// out[i] = sum over the row's choices of weight y[place], in their order, in fp32
+template <typename T, bool VEC>
+__global__ __launch_bounds__(ROW_NT) void k_combine_rows(RowsArgs a, const T *__restrict__ y, T *__restrict__ out)
+{
+    using P = Piece<T, VEC>;
+    const int64_t places = a.n * a.w, r0 = (int64_t)blockIdx.x * a.rows;
+    const uint32_t pieces = (uint32_t)min((int64_t)a.rows, a.n - r0) * a.per;
+    for (uint32_t i = threadIdx.x; i < pieces; i += ROW_NT) {
+        const uint32_t r = i / a.per, c = i - r * a.per;
+        const int32_t *pl = a.index + (r0 + r) * a.w;
+        const float *wt = a.weight ? a.weight + (r0 + r) * a.w : nullptr;
+        float s[P::N] = {};
+        for (int q0 = 0; q0 < a.w; q0 += 8) { // (eight rows' loads under way)
+            P v[8];
+            float f[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                f[q] = 0.f;
+                const int32_t p = q0 + q < a.w ? pl[q0 + q] : -1;
+                const bool in = p >= 0 && p < places;
+                v[q] = load_piece<T, VEC>(y + (in ? (int64_t)p * a.d : 0) + c * P::N);
+                if (in) f[q] = wt ? wt[q0 + q] : 1.f;
+                if (!in)
+#pragma unroll
+                    for (int e = 0; e < P::N; ++e) v[q].v[e] = (T)0.f;
+            }
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+#pragma unroll
+                for (int e = 0; e < P::N; ++e) s[e] = fmaf(f[q], (float)v[q].v[e], s[e]);
+        }
+        P o;
+#pragma unroll
+        for (int e = 0; e < P::N; ++e) o.v[e] = (T)s[e];
+        store_piece<T, VEC>(out + (r0 + r) * a.d + c * P::N, o);
+    }
+}
+
+// dy[place] = weight dout[i], dweight[i][c] = <dout[i], y[place]>: L lanes a row, eight choices at a time
+template <typename T, bool VEC, int L>
+__global__ __launch_bounds__(ROW_NT) void k_combine_back(RowsArgs a, const T *__restrict__ dout, const T *__restrict__ y,
+                                                         T *__restrict__ dy, float *__restrict__ dweight)
+{
+    using P = Piece<T, VEC>;
+    const int lane = threadIdx.x & (L - 1);
+    const int64_t places = a.n * a.w, r = (int64_t)blockIdx.x * (ROW_NT / L) + threadIdx.x / L;
+    if (r >= a.n) return;
+    for (int q0 = 0; q0 < a.w; q0 += 8) {
+        int64_t p[8];
+        float f[8], dot[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const int32_t at = q0 + q < a.w ? a.index[r * a.w + q0 + q] : -1;
+            p[q] = at >= 0 && at < places ? at : -1;
+            f[q] = p[q] < 0 ? 0.f : a.weight ? a.weight[r * a.w + q0 + q] : 1.f;
+            dot[q] = 0.f;
+        }
+        for (uint32_t c = lane; c < a.per; c += L) {
+            const P g = load_piece<T, VEC>(dout + r * a.d + c * P::N);
+            P v[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                if (dweight && p[q] >= 0) v[q] = load_piece<T, VEC>(y + p[q] * a.d + c * P::N);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                if (p[q] < 0) continue;
+                P o;
+#pragma unroll
+                for (int e = 0; e < P::N; ++e) {
+                    o.v[e] = (T)(f[q] * (float)g.v[e]);
+                    if (dweight) dot[q] = fmaf((float)g.v[e], (float)v[q].v[e], dot[q]);
+                }
+                if (dy) store_piece<T, VEC>(dy + p[q] * a.d + c * P::N, o);
+            }
+        }
+        if (!dweight) continue;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+#pragma unroll
+            for (int o = L / 2; o > 0; o >>= 1) dot[q] += __shfl_xor(dot[q], o, 64);
+            if (lane == 0 && q0 + q < a.w) dweight[r * a.w + q0 + q] = p[q] < 0 ? 0.f : dot[q];
+        }
+    }
+}
+
+template <typename T>
+static bool whole_pieces(int d, const void *p, const void *q, const void *r)
+{
+    return (size_t)d * sizeof(T) % 16 == 0 && ((uintptr_t)p | (uintptr_t)q | (uintptr_t)r) % 16 == 0;
+}
+
+// rows of a workgroup: about `pieces` pieces
+static uint32_t rows_of(uint32_t per, uint32_t pieces) { return per >= pieces ? 1 : pieces / per; }
+
+template <typename T>
+static int gather(const RowsArgs &args, const T *x, T *y, hipStream_t st)
+{
+    RowsArgs a = args;
+    auto go = [&](auto VEC) {
+        constexpr bool V = decltype(VEC)::value;
+        a.per = a.d / Piece<T, V>::N;
+        a.rows = rows_of(a.per, ROW_NT * ROW_ITEMS);
+        hipLaunchKernelGGL((k_gather_rows<T, V>), dim3((unsigned)((a.n * a.w + a.rows - 1) / a.rows)), dim3(ROW_NT), 0, st, a, x, y);
+    };
+    if (whole_pieces<T>(a.d, x, y, nullptr))
+        go(std::true_type{});
+    else
+        go(std::false_type{});
+    return (int)hipGetLastError();
+}
+
+template <typename T>
+static int combine(const RowsArgs &args, const T *y, T *out, hipStream_t st)
+{
+    RowsArgs a = args;
+    auto go = [&](auto VEC) {
+        constexpr bool V = decltype(VEC)::value;
+        a.per = a.d / Piece<T, V>::N;
+        a.rows = rows_of(a.per, ROW_NT);
+        hipLaunchKernelGGL((k_combine_rows<T, V>), dim3((unsigned)((a.n + a.rows - 1) / a.rows)), dim3(ROW_NT), 0, st, a, y, out);
+    };
+    if (whole_pieces<T>(a.d, y, out, nullptr))
+        go(std::true_type{});
+    else
+        go(std::false_type{});
+    return (int)hipGetLastError();
+}
+
+template <typename T>
+static int combine_back(const RowsArgs &args, const T *dout, const T *y, T *dy, float *dweight, hipStream_t st)
+{
+    RowsArgs a = args;
+    auto go = [&](auto VEC) {
+        constexpr bool V = decltype(VEC)::value;
+        a.per = a.d / Piece<T, V>::N;
+        auto lanes = [&](auto L) {
+            constexpr int N = decltype(L)::value, R = ROW_NT / N;
+            hipLaunchKernelGGL((k_combine_back<T, V, N>), dim3((unsigned)((a.n + R - 1) / R)), dim3(ROW_NT), 0, st, a, dout, y, dy, dweight);
+        };
+        if (a.per > 32)
+            lanes(std::integral_constant<int, 64>{});
+        else if (a.per > 16)
+            lanes(std::integral_constant<int, 32>{});
+        else
+            lanes(std::integral_constant<int, 16>{});
+    };
+    if (whole_pieces<T>(a.d, dout, y, dy))
+        go(std::true_type{});
+    else
+        go(std::false_type{});
+    return (int)hipGetLastError();
+}
+
+int launch_gather_rows(int dtype, const void *x, int64_t n, int w, int d, const int32_t *source, void *y, hipStream_t st)
+{
+    const RowsArgs a = {n, w, d, 0, 0, source, nullptr};
+    if (dtype == VLQ_F32) return gather(a, (const float *)x, (float *)y, st);
+    return gather(a, (const uint16_t *)x, (uint16_t *)y, st); // (values are moved, not looked at)
+}
+
+int launch_combine_rows(int dtype, const void *y, int64_t n, int w, int d, const int32_t *place, const float *weight, void *out,
+                        hipStream_t st)
+{
+    const RowsArgs a = {n, w, d, 0, 0, place, weight};
+    switch (dtype) {
+    case VLQ_F32: return combine(a, (const float *)y, (float *)out, st);
+    case VLQ_F16: return combine(a, (const _Float16 *)y, (_Float16 *)out, st);
+    default: return combine(a, (const bf16_t *)y, (bf16_t *)out, st);
+    }
+}
+
+int launch_combine_rows_backward(int dtype, const void *dout, const void *y, int64_t n, int w, int d, const int32_t *place,
+                                 const float *weight, void *dy, float *dweight, hipStream_t st)
+{
+    const RowsArgs a = {n, w, d, 0, 0, place, weight};
+    switch (dtype) {
+    case VLQ_F32: return combine_back(a, (const float *)dout, (const float *)y, (float *)dy, dweight, st);
+    case VLQ_F16: return combine_back(a, (const _Float16 *)dout, (const _Float16 *)y, (_Float16 *)dy, dweight, st);
+    default: return combine_back(a, (const bf16_t *)dout, (const bf16_t *)y, (bf16_t *)dy, dweight, st);
+    }
+}

@@ -72,3 +72,69 @@ def test_binding_wants_device_tensors(vlq):
     x = torch.zeros(4, 8)
     with pytest.raises(ValueError):
         vlq.vlq_softmax_loss(x, 4, 8, x, 4, None, 1.0, torch.zeros(4, dtype=torch.int32), None, torch.zeros(4, 2), torch.zeros(64, dtype=torch.uint8))
+
+
+@pytest.mark.parametrize("change", [
+    dict(n=-1), dict(w=0), dict(n=1 << 30, w=2), dict(cells=0), dict(cells=(1 << 24) + 1), dict(cell=None), dict(off=None), dict(place=None),
+    dict(source=None), dict(ws=None), dict(cell=C.c_void_p(4098)), dict(off=C.c_void_p(4100)), dict(ws=C.c_void_p(4104)), dict(size=0)])
+def test_group(vlq, change):
+    a = dict(dict(cell=P, n=10, w=2, cells=5, off=P, place=P, source=P, ws=P, size=BIG), **change)
+    assert vlq.lib().vlq_group_rows(a["cell"], a["n"], a["w"], a["cells"], a["off"], a["place"], a["source"], a["ws"], a["size"],
+                                    None) == vlq.VLQ_EINVAL
+    assert vlq.vlq_last_error() != ""
+
+
+def test_group_workspace(vlq):
+    L = vlq.lib()
+    assert L.vlq_group_rows_workspace(-1, 1, 1) == vlq.VLQ_EINVAL and L.vlq_group_rows_workspace(1, 0, 1) == vlq.VLQ_EINVAL
+    assert L.vlq_group_rows_workspace(0, 1, 1) > 0 and L.vlq_group_rows_workspace((1 << 31) - 1, 1, 1 << 24) > 0
+    need = L.vlq_group_rows_workspace(1 << 20, 8, 300)
+    assert L.vlq_group_rows(P, 1 << 20, 8, 300, P, P, P, P, need - 1, None) == vlq.VLQ_EINVAL
+
+
+@pytest.mark.parametrize("change", [
+    dict(dtype=7), dict(n=-1), dict(w=0), dict(n=1 << 30, w=4), dict(d=0), dict(d=(1 << 20) + 1), dict(x=None), dict(index=None), dict(y=None),
+    dict(x=C.c_void_p(4098)), dict(index=C.c_void_p(4097)), dict(y=C.c_void_p(4097))])
+def test_rows(vlq, change):
+    a = dict(dict(dtype=0, x=P, n=10, w=2, d=8, index=P, weight=None, y=P), **change)
+    L = vlq.lib()
+    assert L.vlq_gather_rows(a["dtype"], a["x"], a["n"], a["w"], a["d"], a["index"], a["y"], None) == vlq.VLQ_EINVAL
+    assert L.vlq_combine_rows(a["dtype"], a["x"], a["n"], a["w"], a["d"], a["index"], a["weight"], a["y"], None) == vlq.VLQ_EINVAL
+    back = lambda dout, y, dy, dw: L.vlq_combine_rows_backward(a["dtype"], dout, y, a["n"], a["w"], a["d"], a["index"], None, dy, dw, None)  # noqa: E731
+    assert back(a["x"], a["y"], P, P) == vlq.VLQ_EINVAL
+    assert L.vlq_combine_rows(0, P, 10, 2, 8, P, C.c_void_p(4098), P, None) == vlq.VLQ_EINVAL
+    assert L.vlq_combine_rows_backward(0, P, None, 10, 2, 8, P, None, P, P, None) == vlq.VLQ_EINVAL  # d_dweight needs d_y
+    assert L.vlq_combine_rows_backward(0, P, P, 10, 2, 8, P, None, C.c_void_p(4098), P, None) == vlq.VLQ_EINVAL
+
+
+def clip_call(vlq, counts, grads, outs, dtypes=None, limit=1.0, norm=P, ws=P, size=BIG, tensors=None):
+    n = len(counts)
+    many = max(1, n)
+    ptrs = lambda v: None if v is None else (C.c_void_p * many)(*v)  # noqa: E731
+    return vlq.lib().vlq_clip_grads(n if tensors is None else tensors, (C.c_int32 * many)(*(dtypes or [0] * n)), (C.c_int64 * many)(*counts),
+                                    ptrs(grads), limit, ptrs(outs), norm, ws, size, None)
+
+
+def test_clip(vlq):
+    bad = [
+        dict(counts=[5, -1], grads=[4096, 8192], outs=None), dict(counts=[5], grads=[None], outs=None), dict(counts=[5], grads=[4098], outs=None),
+        dict(counts=[5], grads=[4096], outs=[None]), dict(counts=[5], grads=[4096], outs=[8194]), dict(counts=[5], grads=None, outs=None),
+        dict(counts=[5], grads=[4096], outs=None, dtypes=[3]), dict(counts=[5], grads=[4096], outs=None, limit=0.0),
+        dict(counts=[5], grads=[4096], outs=None, limit=-1.0), dict(counts=[5], grads=[4096], outs=None, limit=float("nan")),
+        dict(counts=[5], grads=[4096], outs=None, ws=None), dict(counts=[5], grads=[4096], outs=None, size=8),
+        dict(counts=[5], grads=[4096], outs=None, norm=C.c_void_p(4098)), dict(counts=[5], grads=[4096], outs=None, tensors=-1),
+        dict(counts=[1 << 47, 1 << 48], grads=[4096, 8192], outs=None),
+        # overlaps: the same tensor twice, an output over its own input's middle, over another input, over another output
+        dict(counts=[5, 5], grads=[4096, 4096], outs=[4096, 4096]), dict(counts=[5], grads=[4096], outs=[4100]),
+        dict(counts=[5, 5], grads=[4096, 8192], outs=[4096, 4112]), dict(counts=[5, 5], grads=[4096, 8192], outs=[12288, 12300])]
+    for kw in bad:
+        assert clip_call(vlq, **kw) == vlq.VLQ_EINVAL, kw
+        assert vlq.vlq_last_error() != ""
+    many = 500
+    assert clip_call(vlq, [4] * many, [4096 + 16 * i for i in range(many)], [4096 + 16 * (many - i) for i in range(many)]) == vlq.VLQ_EINVAL
+
+
+def test_clip_workspace(vlq):
+    L = vlq.lib()
+    assert L.vlq_clip_grads_workspace(-1, None) == vlq.VLQ_EINVAL and L.vlq_clip_grads_workspace(1, None) == vlq.VLQ_EINVAL
+    assert L.vlq_clip_grads_workspace(0, None) > 0
