@@ -241,15 +241,23 @@ def _type(t):
 
 
 def _ptrs(*pairs):
-    """Pointers of (tensor or None, dtype, least number of values), all of them on the current device."""
-    out = []
+    """Addresses of (tensor or None, dtype, least number of values), all of them on the current device."""
+    out, dev = [], None
     for t, dtype, count in pairs:
-        if t is not None:
-            if t.is_cuda and t.get_device() != torch.cuda.current_device():
-                raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
-            if t.numel() < count:
-                raise ValueError(f"a tensor has {t.numel()} values, {count} are needed")
-        out.append(_ptr(t, dtype))
+        if t is None:
+            out.append(None)
+            continue
+        if not t.is_cuda or not t.is_contiguous():
+            raise ValueError("tensors passed to libvlq must be contiguous device tensors")
+        if dev is None:
+            dev = torch.cuda.current_device()
+        if t.get_device() != dev:
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
+        if dtype is not None and t.dtype != dtype:
+            raise ValueError(f"expected {dtype}, got {t.dtype}")
+        if t.numel() < count:
+            raise ValueError(f"a tensor has {t.numel()} values, {count} are needed")
+        out.append(t.data_ptr())
     return out
 
 

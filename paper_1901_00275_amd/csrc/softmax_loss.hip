@@ -5,7 +5,7 @@
 //   dx_i = s sum_j G_ij c_j,  dc_j = s sum_i G_ij x_i,  db_j = sum_i G_ij.
 //
 // Four products of n x k x d on the fp16 matrix cores: the logits forward, and backward the logits again and the two
-// gradients.  Operands are first rewritten as fp16 with a power-of-two scale (per row of x, per 128 rows of c, one per
+// gradients.  Operands are first rewritten as fp16 with a power-of-two scale (per row of x, per 16 rows of c, one per
 // matrix where the rows are the summed index):
 //  - fp16 values are taken as they are, bf16 values lose nothing within 32 binades below the largest of their scale;
 //  - an fp32 value is the sum of two fp16 values, hi + lo, with an error of 2^-23 of itself or 2^-40 of the largest of its scale;
@@ -38,6 +38,8 @@ typedef __bf16 bf16_t;
 #define TILE 256             // rows and columns of their tiles
 #define LOSS_ROWS 8192       // rows that go through the products together
 #define PIECE (1 << 25)      // values of P kept at a time
+#define FEW_ROWS 64          // up to so many rows the logits come from the centroids as they lie (k_loss_few)
+#define FEW_WIDE 65536       // from so many centroids on a wave takes 32 of them: then there are waves enough
 #define P_ONE 32768.f        // 2^15, what a probability of one is in P
 #define LOG2E 1.4426950408889634f
 #define LN2 0.6931471805599453f
@@ -101,29 +103,24 @@ __device__ __forceinline__ bool row_counts(const int32_t *label, int k, const fl
     return !bias || bias[r] != -INFINITY;
 }
 
-// Image of the rows of X, RB rows a workgroup: RB = 16 with a scale per row, RB = 128 with one for all.
-// inv: 1 / scale, per row or per block.  Bound by memory: X is read twice (the second time from the caches), written once.
-template <typename T, int RB, int NP>
+// Image of the rows of X, 16 rows a workgroup; a scale per row (OWN) or for all 16.  inv: 1 / scale, as many.
+// Bound by memory: X is read twice (the second time from the caches), written once.  (With 128 rows a workgroup and a scale for
+// all of them 128 MB took 99 us, for want of loads under way.)
+template <typename T, bool OWN, int NP>
 __global__ __launch_bounds__(256) void k_pack_rows(const T *__restrict__ X, int64_t rows, int d, int units,
                                                    const int32_t *__restrict__ label, int k, const float *__restrict__ bias,
                                                    u32x4 *__restrict__ pages, float *__restrict__ inv, uint32_t *absmax, bool vec)
 {
-    __shared__ float rmax[RB];
-    __shared__ uint8_t counts[RB];
+    __shared__ float rmax[16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t r0 = (int64_t)blockIdx.x * RB;
-    if (tid < RB) {
-        counts[tid] = r0 + tid < rows && row_counts(label, k, bias, r0 + tid);
-        rmax[tid] = 0.f;
-    }
-    __syncthreads();
-    int ex = 0;
+    const int64_t r0 = (int64_t)blockIdx.x * 16;
+    // pass 1: 16 lanes a row
     if constexpr (!__is_same(T, _Float16)) {
-        for (int r = wave; r < RB; r += 4) {
-            if (!counts[r]) continue;
+        const int r = tid >> 4;
+        float mx = 0.f;
+        if (r0 + r < rows && row_counts(label, k, bias, r0 + r)) {
             const T *row = X + (r0 + r) * d;
-            float mx = 0.f;
-            for (int i = lane * 8; i < d; i += 512) {
+            for (int i = (tid & 15) * 8; i < d; i += 128) {
                 float v[8];
                 load8(row, i, d, vec, v);
 #pragma unroll
@@ -132,35 +129,42 @@ __global__ __launch_bounds__(256) void k_pack_rows(const T *__restrict__ X, int6
                     if (m < INFINITY) mx = fmaxf(mx, m);
                 }
             }
-            mx = __uint_as_float(wave_max_u32(__float_as_uint(mx)));
-            if (lane == 0) rmax[r] = mx;
         }
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
+        if ((tid & 15) == 0) rmax[r] = mx;
         __syncthreads();
-        float mx = 0.f;
-        for (int r = lane; r < RB; r += 64) mx = fmaxf(mx, rmax[r]);
-        mx = __uint_as_float(wave_max_u32(__float_as_uint(mx)));
-        if (RB == 128) ex = scale_exponent(mx);
-        if (tid == 0 && absmax) atomicMax(absmax, __float_as_uint(mx));
     }
-    if (RB == 128) {
-        if (tid == 0) inv[blockIdx.x] = pow2i(-ex);
-    } else if (tid < RB) {
-        inv[r0 + tid] = __is_same(T, _Float16) ? 1.f : pow2i(-scale_exponent(rmax[tid]));
+    const int l = lane & 15;
+    float mine = 0.f, all = 0.f; // largest magnitudes of the lane's row, and of the 16
+    if constexpr (!__is_same(T, _Float16)) {
+        mine = rmax[l];
+        all = mine;
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor(all, o, 64));
+        if (tid == 0 && absmax) atomicMax(absmax, __float_as_uint(all));
     }
-    for (int it = wave; it < units * (RB / 16); it += 4) {
-        const int grp = it % (RB / 16), u = it / (RB / 16), r = grp * 16 + (lane & 15);
+    const int ex = __is_same(T, _Float16) ? 0 : scale_exponent(OWN ? mine : all);
+    if (tid < 16) {
+        if (OWN)
+            inv[r0 + tid] = pow2i(-ex);
+        else if (tid == 0)
+            inv[blockIdx.x] = pow2i(-ex);
+    }
+    const bool counts = r0 + l < rows && row_counts(label, k, bias, r0 + l);
+    const T *row = X + (counts ? r0 + l : 0) * d;
+    const float s = pow2i(ex);
+    u32x4 *to = pages + (int64_t)(blockIdx.x >> 3) * units * NP * PAGE + (blockIdx.x & 7) * 64 + lane;
+#pragma unroll 2
+    for (int u = wave; u < units; u += 4) {
         float v[8] = {};
-        if (counts[r]) load8(X + (r0 + r) * d, u * 32 + (lane >> 4) * 8, d, vec, v);
-        const float s = __is_same(T, _Float16) ? 1.f : RB == 128 ? pow2i(ex) : pow2i(scale_exponent(rmax[r]));
+        if (counts) load8(row, u * 32 + (lane >> 4) * 8, d, vec, v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] *= s;
         half8 h[NP];
         split8<NP>(v, h);
-        const int64_t blk = RB == 128 ? blockIdx.x : blockIdx.x >> 3;
-        const int g16 = RB == 128 ? grp : (blockIdx.x & 7);
 #pragma unroll
-        for (int p = 0; p < NP; ++p)
-            pages[((blk * units + u) * NP + p) * PAGE + g16 * 64 + lane] = __builtin_bit_cast(u32x4, h[p]);
+        for (int p = 0; p < NP; ++p) to[(int64_t)(u * NP + p) * PAGE] = __builtin_bit_cast(u32x4, h[p]);
     }
 }
 
@@ -169,18 +173,20 @@ __global__ __launch_bounds__(256) void k_pack_rows(const T *__restrict__ X, int6
 template <typename T, bool PERM, int NP>
 __global__ __launch_bounds__(256) void k_pack_cols(const T *__restrict__ X, int64_t rows, int d, int units,
                                                    const int32_t *__restrict__ label, int k, const float *__restrict__ bias,
-                                                   u32x4 *__restrict__ pages, const uint32_t *__restrict__ absmax)
+                                                   u32x4 *__restrict__ pages, const uint32_t *__restrict__ absmax, bool vec)
 {
     __shared__ float t[64][129];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t r0 = (int64_t)blockIdx.x * 64;
     const int d0 = blockIdx.y * 128;
     const float s = __is_same(T, _Float16) ? 1.f : pow2i(scale_exponent(__uint_as_float(*absmax)));
-    for (int i = tid; i < 64 * 128; i += 256) {
-        const int r = i >> 7, c = i & 127;
-        float v = 0.f;
-        if (r0 + r < rows && d0 + c < d && row_counts(label, k, bias, r0 + r)) v = (float)X[(r0 + r) * d + d0 + c];
-        t[r][c] = v * s;
+#pragma unroll
+    for (int i = tid; i < 64 * 16; i += 256) {
+        const int r = i >> 4, c = (i & 15) * 8;
+        float v[8] = {};
+        if (r0 + r < rows && row_counts(label, k, bias, r0 + r)) load8(X + (r0 + r) * d, d0 + c, d, vec, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t[r][c + e] = v[e] * s;
     }
     __syncthreads();
     for (int it = wave; it < 16; it += 4) {
@@ -364,9 +370,9 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_stats(LogitArgs a)
     f32x4 acc[8][4];
     product<NP, 2>(a.A, a.B, mt * 2, nt * 2, a.steps, lds, acc);
     const int m0 = mt * TILE + (wave >> 2) * 128, n0 = nt * TILE + (wave & 3) * 64;
-    const float ci = a.cinv[m0 >> 7];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
+        const float ci = a.cinv[(m0 >> 4) + i];
         const f32x4 b2 = *(const f32x4 *)(a.bias2 + m0 + 16 * i + 4 * g);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -404,32 +410,163 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_stats(LogitArgs a)
     }
 }
 
-// A row's statistics and loss from its parts, 16 threads a row
-__global__ __launch_bounds__(256) void k_loss_merge(const float2 *part, int parts, int npad, const float *mine, const int32_t *lab,
+// The statistics of two sets of logits together
+__device__ __forceinline__ float2 join(float2 a, float2 b)
+{
+    const float m = fmaxf(a.x, b.x), base = m == -INFINITY ? 0.f : m;
+    return make_float2(m, a.y * __builtin_amdgcn_exp2f(a.x - base) + b.y * __builtin_amdgcn_exp2f(b.x - base));
+}
+
+// A row's statistics and loss from its parts: R rows a workgroup of 256, 256 / R threads each.  Sixteen rows are read side by
+// side; where there are few rows and many parts one row has the whole workgroup.
+template <int R>
+__global__ __launch_bounds__(256) void k_loss_merge(const float2 *part, int parts, int npad, const float *mine, const int32_t *lab, int k,
                                                     int64_t n, float *stats, float *loss)
 {
-    const int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x & 15);
-    const int t = threadIdx.x >> 4;
-    float m = -INFINITY, z = 0.f;
-    for (int p = t; p < parts; p += 16) {
-        const float2 v = part[(int64_t)p * npad + i];
-        const float top = fmaxf(m, v.x), base = top == -INFINITY ? 0.f : top;
-        z = z * __builtin_amdgcn_exp2f(m - base) + v.y * __builtin_amdgcn_exp2f(v.x - base);
-        m = top;
+    constexpr int T = 256 / R;
+    const int64_t i = (int64_t)blockIdx.x * R + threadIdx.x % R;
+    const int t = threadIdx.x / R;
+    float2 v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = make_float2(-INFINITY, 0.f);
+    for (int p = t; p < parts; p += 4 * T)
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (p + u * T < parts && i < npad) v[u] = join(v[u], part[(int64_t)(p + u * T) * npad + i]);
+    v[0] = join(join(v[0], v[1]), join(v[2], v[3]));
+    if (R == 1) {
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) v[0] = join(v[0], make_float2(__shfl_xor(v[0].x, o, 64), __shfl_xor(v[0].y, o, 64)));
     }
-    __shared__ float2 s[16][16];
-    s[t][threadIdx.x & 15] = make_float2(m, z);
+    constexpr int S = R == 1 ? 4 : T;
+    __shared__ float2 s[S][R];
+    if (R > 1 || (t & 63) == 0) s[R == 1 ? t >> 6 : t][threadIdx.x % R] = v[0];
     __syncthreads();
     if (t != 0 || i >= n) return;
-    for (int p = 1; p < 16; ++p) {
-        const float2 v = s[p][threadIdx.x];
-        const float top = fmaxf(m, v.x), base = top == -INFINITY ? 0.f : top;
-        z = z * __builtin_amdgcn_exp2f(m - base) + v.y * __builtin_amdgcn_exp2f(v.x - base);
-        m = top;
-    }
+    for (int p = 1; p < S; ++p) v[0] = join(v[0], s[p][threadIdx.x % R]);
+    const float m = v[0].x, z = v[0].y;
     stats[2 * i] = m;
     stats[2 * i + 1] = z;
-    if (loss) loss[i] = lab[i] < 0 ? 0.f : m == -INFINITY ? INFINITY : LN2 * (m - mine[i]) + logf(z);
+    if (loss) loss[i] = (uint32_t)lab[i] >= (uint32_t)k ? 0.f : m == -INFINITY ? INFINITY : LN2 * (m - mine[i]) + logf(z);
+}
+
+// Few rows: every wave multiplies 16 G centroids, read once from where they lie, with all rows (NT tiles of 16), eight waves
+// a workgroup; 16-bit values on their own matrix instructions, fp32 on the fp32 ones (a read of 4 bytes needs 16 NT
+// multiplications, which these do in time up to NT = 4).  Nothing is rewritten first, so the centroids pass once; bound by that.
+struct FewArgs {
+    const void *x, *c;
+    const float *bias;
+    const int32_t *label;
+    float scale2; // in units of log 2
+    int n, d, k;
+    float2 *part; // [workgroups][n]
+    float *mine;
+};
+template <typename T>
+struct FewPiece { // what a lane reads of a row at a time: its share of STEP indices
+    static constexpr int N = 16 / sizeof(T), STEP = 4 * N;
+    T v[N];
+};
+template <typename T, bool VEC>
+__device__ __forceinline__ FewPiece<T> few_piece(const T *row, int i, int d, bool there)
+{
+    FewPiece<T> r;
+    if (VEC) {
+        u32x4 v = {0, 0, 0, 0};
+        if (there && i < d) v = *(const u32x4 *)(row + i);
+        *(u32x4 *)r.v = v;
+    } else {
+#pragma unroll
+        for (int e = 0; e < FewPiece<T>::N; ++e) r.v[e] = there && i + e < d ? row[i + e] : (T)0.f;
+    }
+    return r;
+}
+__device__ __forceinline__ void few_multiply(const FewPiece<float> &a, const FewPiece<float> &b, f32x4 &acc)
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[e], b.v[e], acc, 0, 0, 0);
+}
+__device__ __forceinline__ void few_multiply(const FewPiece<_Float16> &a, const FewPiece<_Float16> &b, f32x4 &acc)
+{
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(*(const half8 *)a.v, *(const half8 *)b.v, acc, 0, 0, 0);
+}
+__device__ __forceinline__ void few_multiply(const FewPiece<bf16_t> &a, const FewPiece<bf16_t> &b, f32x4 &acc)
+{
+    typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8 *)a.v, *(const bf16x8 *)b.v, acc, 0, 0, 0);
+}
+
+#define FEW_WAVES 8
+template <typename T, bool VEC, int G, int NT>
+__global__ __launch_bounds__(FEW_WAVES * 64) void k_loss_few(FewArgs a)
+{
+    constexpr int STEP = FewPiece<T>::STEP, N = FewPiece<T>::N, U = 16 / (G + NT) < 2 ? 2 : 16 / (G + NT);
+    const int tid = threadIdx.x, lane = tid & 63, l = lane & 15, g = lane >> 4, wave = tid >> 6;
+    const int m0 = (blockIdx.x * FEW_WAVES + wave) * 16 * G;
+    const T *crow[G], *xrow[NT];
+    bool cin[G], xin[NT];
+    f32x4 acc[G][NT];
+#pragma unroll
+    for (int i = 0; i < G; ++i) {
+        cin[i] = m0 + 16 * i + l < a.k;
+        crow[i] = (const T *)a.c + (int64_t)(cin[i] ? m0 + 16 * i + l : 0) * a.d;
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        xin[j] = 16 * j + l < a.n;
+        xrow[j] = (const T *)a.x + (int64_t)(xin[j] ? 16 * j + l : 0) * a.d;
+#pragma unroll
+        for (int i = 0; i < G; ++i) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    for (int k0 = g * N; k0 < a.d + g * N; k0 += U * STEP) { // (the same turns for all lanes)
+        FewPiece<T> cv[U][G], xv[U][NT];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+#pragma unroll
+            for (int i = 0; i < G; ++i) cv[u][i] = few_piece<T, VEC>(crow[i], k0 + u * STEP, a.d, cin[i]);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) xv[u][j] = few_piece<T, VEC>(xrow[j], k0 + u * STEP, a.d, xin[j]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < G; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) few_multiply(cv[u][i], xv[u][j], acc[i][j]);
+    }
+    __shared__ float2 s[FEW_WAVES][16 * NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        const int n = 16 * j + l, lab = n < a.n ? a.label[n] : -1;
+        float m = -INFINITY, z = 0.f;
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int c = m0 + 16 * i + 4 * g + r;
+                const float b = c >= a.k ? -INFINITY : a.bias ? a.bias[c] * LOG2E : 0.f;
+                const float v = b == -INFINITY ? -INFINITY : fmaf(acc[i][j][r], a.scale2, b);
+                if (c == lab && c < a.k) a.mine[n] = v;
+                m = fmaxf(m, v);
+                acc[i][j][r] = v;
+            }
+        m = fmaxf(m, __shfl_xor(m, 16, 64));
+        m = fmaxf(m, __shfl_xor(m, 32, 64));
+        const float m1 = m == -INFINITY ? 0.f : m;
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) z += __builtin_amdgcn_exp2f(acc[i][j][r] - m1);
+        z += __shfl_xor(z, 16, 64);
+        z += __shfl_xor(z, 32, 64);
+        if (g == 0) s[wave][n] = make_float2(m, z);
+    }
+    __syncthreads();
+    if (tid >= 16 * NT || tid >= a.n) return;
+    float2 v = s[0][tid];
+#pragma unroll
+    for (int w = 1; w < FEW_WAVES; ++w) v = join(v, s[w][tid]);
+    a.part[(int64_t)blockIdx.x * a.n + tid] = v;
 }
 
 // Backward: P of a tile, as images in both orders, and the sums over a wave's 64 rows for the bias
@@ -444,7 +581,6 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_p(LogitArgs a)
     f32x4 acc[8][4];
     product<NP, 2>(a.A, a.B, mt * 2, nt * 2, a.steps, lds, acc);
     const int m0 = mt * TILE + (wave >> 2) * 128, n0 = nt * TILE + (wave & 3) * 64; // (within the piece)
-    const float ci = a.cinv[m0 >> 7];
     f32x4 row[4];
     int rel[4];
     float gn[4];
@@ -453,7 +589,6 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_p(LogitArgs a)
     for (int j = 0; j < 4; ++j) {
         const int n = n0 + 16 * j + l;
         row[j] = a.row[n];
-        row[j][0] *= ci;
         rel[j] = a.lab[n] - a.m_first - m0 - 4 * g; // (16 i + r where the lane holds the label)
         if (a.lab[n] < 0) rel[j] = -1;
         gn[j] = a.gn[n];
@@ -461,12 +596,15 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_p(LogitArgs a)
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
+        const float ci = a.cinv[(m0 >> 4) + i];
         const f32x4 b2 = *(const f32x4 *)(a.bias2 + m0 + 16 * i + 4 * g);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < 4; ++j) {
+            const float f = row[j][0] * ci;
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                acc[i][j][r] = b2[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], row[j][0], b2[r] - row[j][1]));
+                acc[i][j][r] = b2[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], f, b2[r] - row[j][1]));
+        }
     }
     const bool labels = __any(any);
     // image summed over j: the rows of its blocks are the rows i, the lane's four r are half a chunk
@@ -704,7 +842,7 @@ static LossPlan loss_plan(int dtype, int64_t n, int d, int k, bool backward, voi
     take(p.ximg, p.npad / 128 * p.units * page);
     take(p.cimg, p.kpad / 128 * p.units * page);
     take(p.rinv, p.npad);
-    take(p.cinv, p.kpad / 128);
+    take(p.cinv, p.kpad / 16);
     take(p.bias2, p.kpad);
     take(p.row, p.npad);
     take(p.lab, p.npad);
@@ -733,6 +871,7 @@ static LossPlan loss_plan(int dtype, int64_t n, int d, int k, bool backward, voi
 
 size_t loss_workspace(int dtype, int64_t n, int d, int k, bool backward)
 {
+    if (!backward && n <= FEW_ROWS) return ((size_t)(k / (FEW_WAVES * 16) + 1) * 8 + 4) * (n < 1 ? 1 : n);
     return loss_plan(dtype, n, d, k, backward, nullptr).bytes;
 }
 
@@ -761,9 +900,9 @@ template <typename T, int NP>
 static void loss_images(const LossArgs &a, const LossPlan &p, hipStream_t st)
 {
     hipLaunchKernelGGL(k_loss_header, dim3(1), dim3(64), 0, st, p.hdr);
-    hipLaunchKernelGGL((k_pack_rows<T, 16, NP>), dim3((unsigned)(p.npad / 16)), dim3(256), 0, st, (const T *)a.x, a.n, a.d, p.units,
+    hipLaunchKernelGGL((k_pack_rows<T, true, NP>), dim3((unsigned)(p.npad / 16)), dim3(256), 0, st, (const T *)a.x, a.n, a.d, p.units,
                        a.label, a.k, nullptr, p.ximg, p.rinv, p.hdr, rows_vec<T>(a.x, a.d));
-    hipLaunchKernelGGL((k_pack_rows<T, 128, NP>), dim3((unsigned)(p.kpad / 128)), dim3(256), 0, st, (const T *)a.c, (int64_t)a.k, a.d,
+    hipLaunchKernelGGL((k_pack_rows<T, false, NP>), dim3((unsigned)(p.kpad / 16)), dim3(256), 0, st, (const T *)a.c, (int64_t)a.k, a.d,
                        p.units, nullptr, a.k, a.bias, p.cimg, p.cinv, p.hdr + 1, rows_vec<T>(a.c, a.d));
     hipLaunchKernelGGL(k_loss_bias, dim3((unsigned)(p.kpad / 256)), dim3(256), 0, st, a.bias, a.k, (int)p.kpad, p.bias2);
 }
@@ -775,7 +914,7 @@ static LogitArgs logit_args(const LossPlan &p, int64_t r0, int64_t rpad, int64_t
     const int64_t block = (int64_t)p.units * NP;
     g.A = {p.cimg + c0 / 128 * block * PAGE, block, 0};
     g.B = {p.ximg + r0 / 128 * block * PAGE, block, 0};
-    g.cinv = p.cinv + c0 / 128;
+    g.cinv = p.cinv + c0 / 16;
     g.bias2 = p.bias2 + c0;
     g.row = p.row + r0;
     g.lab = p.lab + r0;
@@ -787,9 +926,52 @@ static LogitArgs logit_args(const LossPlan &p, int64_t r0, int64_t rpad, int64_t
     return g;
 }
 
+static void launch_merge(const float2 *part, int parts, int npad, const float *mine, const int32_t *lab, int k, int64_t n, float *stats,
+                         float *loss, hipStream_t st)
+{
+    if (n <= FEW_ROWS)
+        hipLaunchKernelGGL(k_loss_merge<1>, dim3((unsigned)n), dim3(256), 0, st, part, parts, npad, mine, lab, k, n, stats, loss);
+    else
+        hipLaunchKernelGGL(k_loss_merge<16>, dim3((unsigned)((n + 15) / 16)), dim3(256), 0, st, part, parts, npad, mine, lab, k, n, stats, loss);
+}
+
+template <typename T>
+static int loss_few(const LossArgs &a, hipStream_t st)
+{
+    const bool wide = a.k >= FEW_WIDE;
+    const int groups = (a.k + FEW_WAVES * (wide ? 32 : 16) - 1) / (FEW_WAVES * (wide ? 32 : 16));
+    float2 *part = (float2 *)a.ws;
+    float *mine = (float *)(part + (int64_t)groups * a.n);
+    const FewArgs f = {a.x, a.c, a.bias, a.label, a.scale * LOG2E, (int)a.n, a.d, a.k, part, mine};
+    auto go = [&](auto VEC, auto G, auto NT) {
+        hipLaunchKernelGGL((k_loss_few<T, decltype(VEC)::value, decltype(G)::value, decltype(NT)::value>), dim3(groups), dim3(FEW_WAVES * 64), 0, st, f);
+    };
+    auto rows = [&](auto VEC, auto G) {
+        if (a.n <= 16)
+            go(VEC, G, std::integral_constant<int, 1>{});
+        else if (a.n <= 32)
+            go(VEC, G, std::integral_constant<int, 2>{});
+        else
+            go(VEC, G, std::integral_constant<int, 4>{});
+    };
+    auto cells = [&](auto VEC) {
+        if (wide)
+            rows(VEC, std::integral_constant<int, 2>{});
+        else
+            rows(VEC, std::integral_constant<int, 1>{});
+    };
+    if (a.d * sizeof(T) % 16 == 0 && ((uintptr_t)a.x | (uintptr_t)a.c) % 16 == 0)
+        cells(std::true_type{});
+    else
+        cells(std::false_type{});
+    launch_merge(part, groups, (int)a.n, mine, a.label, a.k, a.n, a.stats, a.loss, st);
+    return (int)hipGetLastError();
+}
+
 template <typename T, int NP>
 static int loss_forward(const LossArgs &a, hipStream_t st)
 {
+    if (a.n <= FEW_ROWS) return loss_few<T>(a, st);
     const LossPlan p = loss_plan(a.dtype, a.n, a.d, a.k, false, a.ws);
     loss_images<T, NP>(a, p, st);
     hipLaunchKernelGGL(k_loss_rows, dim3((unsigned)(p.npad / 256)), dim3(256), 0, st, p.rinv, a.label, a.n, a.k, a.scale, nullptr,
@@ -801,8 +983,7 @@ static int loss_forward(const LossArgs &a, hipStream_t st)
         g.part = p.part;
         g.mine = p.mine;
         hipLaunchKernelGGL(k_loss_stats<NP>, dim3((unsigned)(g.mt * g.nt)), dim3(LNT), lds_bytes(2), st, g);
-        hipLaunchKernelGGL(k_loss_merge, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, st, p.part, g.mt * 2, g.npad, p.mine,
-                           g.lab, rows, a.stats + 2 * r0, a.loss ? a.loss + r0 : nullptr);
+        launch_merge(p.part, g.mt * 2, g.npad, p.mine, g.lab, a.k, rows, a.stats + 2 * r0, a.loss ? a.loss + r0 : nullptr, st);
     }
     return (int)hipGetLastError();
 }
@@ -819,10 +1000,10 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
     loss_images<T, NP>(a, p, st);
     if (a.dc)
         hipLaunchKernelGGL((k_pack_cols<T, true, NP>), dim3((unsigned)(p.npad / 64), p.dblocks), dim3(256), 0, st, (const T *)a.x, a.n,
-                           a.d, (int)(p.npad / 32), a.label, a.k, nullptr, p.xcols, p.hdr);
+                           a.d, (int)(p.npad / 32), a.label, a.k, nullptr, p.xcols, p.hdr, rows_vec<T>(a.x, a.d));
     if (a.dx)
         hipLaunchKernelGGL((k_pack_cols<T, false, NP>), dim3((unsigned)(p.kpad / 64), p.dblocks), dim3(256), 0, st, (const T *)a.c,
-                           (int64_t)a.k, a.d, (int)(p.kpad / 32), nullptr, a.k, a.bias, p.ccols, p.hdr + 1);
+                           (int64_t)a.k, a.d, (int)(p.kpad / 32), nullptr, a.k, a.bias, p.ccols, p.hdr + 1, rows_vec<T>(a.c, a.d));
     const unsigned gblocks = (unsigned)((a.n + 2047) / 2048 < 256 ? (a.n + 2047) / 2048 : 256);
     hipLaunchKernelGGL(k_grad_max, dim3(gblocks), dim3(256), 0, st, a.grad, a.label, a.k, a.n, p.hdr + 2);
     hipLaunchKernelGGL(k_loss_rows, dim3((unsigned)(p.npad / 256)), dim3(256), 0, st, p.rinv, a.label, a.n, a.k, a.scale, a.stats,

@@ -56,7 +56,7 @@ def compare(got, want, names=("loss", "dx", "dc", "db")):
 
 
 SHAPES = [(1, 1, 1), (1, 96, 300), (3, 7, 2), (64, 32, 256), (65, 33, 257), (255, 96, 1000), (257, 128, 513), (300, 130, 1025),
-          (40, 520, 77), (17, 1027, 515), (1000, 64, 5000)]
+          (40, 520, 77), (17, 1027, 515), (1000, 64, 5000), (33, 48, 65537), (9, 200, 70001)]
 
 
 @pytest.mark.parametrize("t", [F32, F16, BF16])
@@ -126,10 +126,11 @@ def test_rows_of_uneven_size(vlq):
     compare(run(vlq, x, c, bias, 1.0, label, grad), softmax_loss(x, c, bias, 1.0, label, grad))
 
 
+@pytest.mark.parametrize("n", [20, 70])
 @pytest.mark.parametrize("t", [F32, F16, BF16])
-def test_unaligned_operands(vlq, t):
+def test_unaligned_operands(vlq, t, n):
     # one value past a 16-byte boundary, with a dimension that would allow wide loads
-    n, d, k = 70, 64, 300
+    d, k = 64, 300
     x, c, bias, label, grad = problem(t, n, d, k)
     shift = lambda v: torch.cat([v.reshape(-1)[:1], v.reshape(-1)])[1:].view(v.shape)  # noqa: E731
     xs, cs, bs, ls, gs = map(shift, (x, c, bias, label, grad))
