@@ -1,0 +1,111 @@
+// What the kernels of the softmax loss (softmax_loss.hip, softmax_loss_narrow.hip) share: values and their fp16 parts, the
+// images of matrices, the gradients' outputs.
+#pragma once
+#include "learn.h"
+
+#include <type_traits>
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16_t;
+
+#define PAGE 512      // 16-byte chunks of a page: 128 rows x 32 indices
+#define TILE 256      // rows of all images are padded to this
+#define P_ONE 32768.f // 2^15, what a probability of one is in P
+#define LOG2E 1.4426950408889634f
+#define LN2 0.6931471805599453f
+
+// Exponent of the power of two that brings mx to [2^14, 2^15)
+__device__ __forceinline__ int scale_exponent(float mx)
+{
+    const int ex = mx > 0.f ? 14 - ((int)(__float_as_uint(mx) >> 23) - 127) : 0;
+    return min(max(ex, -126), 126);
+}
+__device__ __forceinline__ float pow2i(int ex) { return __uint_as_float((uint32_t)(127 + ex) << 23); }
+
+// eight values of a row from index i on, zeros past its end
+template <typename T>
+__device__ __forceinline__ void load8(const T *row, int i, int d, bool vec, float (&v)[8])
+{
+    if (vec && i < d) { // (d is a multiple of 8)
+        if constexpr (sizeof(T) == 4) {
+            const f32x4 a = *(const f32x4 *)(row + i), b = *(const f32x4 *)(row + i + 4);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = e < 4 ? a[e] : b[e - 4];
+        } else {
+            T t[8];
+            *(u32x4 *)t = *(const u32x4 *)(row + i);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = (float)t[e];
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = i + e < d ? (float)row[i + e] : 0.f;
+}
+
+// v as one or two fp16 parts
+template <int NP>
+__device__ __forceinline__ void split8(const float (&v)[8], half8 (&h)[NP])
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        h[0][e] = (_Float16)v[e];
+        if (NP == 2) h[NP - 1][e] = (_Float16)(v[e] - (float)h[0][e]);
+    }
+}
+
+// Factor of a gradient: the scale of the columns' image, that of P, g's largest magnitude where P was taken relative to it
+template <typename T>
+__device__ __forceinline__ float grad_factor(const uint32_t *absmax, const uint32_t *gmax, float scale)
+{
+    const float inv = __is_same(T, _Float16) ? 1.f : pow2i(-scale_exponent(__uint_as_float(*absmax)));
+    return scale * (gmax ? __uint_as_float(*gmax) : 1.f) * (1.f / P_ONE) * inv;
+}
+
+template <typename T>
+__device__ __forceinline__ void store4(T *p, const f32x4 &v, int count, bool vec)
+{
+    if (vec && count >= 4) {
+        if constexpr (sizeof(T) == 4) {
+            *(f32x4 *)p = v;
+        } else {
+            T t[4] = {(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
+            *(u32x2 *)p = *(u32x2 *)t;
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (e < count) p[e] = (T)v[e];
+}
+
+
+// ---- softmax_loss_narrow.hip ----
+// rows that a workgroup keeps
+constexpr int narrow_rows(int parts) { return parts == 2 ? 128 : 256; }
+struct NarrowSide {
+    const u32x4 *q, *r, *rt; // images of the gradient's rows, of the other matrix's rows and columns
+    int qblocks, tiles, splits, per; // workgroups side by side; tiles of the other matrix, in so many parts of `per`
+    int rows;
+    int mode; // 0: typed; 1: slabs [splits][rows x d]
+    void *out;
+    const uint32_t *absmax, *gmax;
+    const float *weight; // of the rows (dx), and where they do not count
+    bool vec;
+};
+struct NarrowArgs {
+    NarrowSide x, c;
+    int units, d, nx; // workgroups of the first side
+    const f32x4 *row; // per row of x: factor, maximum, factors of P
+    const int32_t *lab;
+    const float *gn, *cinv, *bias2;
+    float *dbpart; // [splits of c][kpad] or NULL
+    int kpad;
+    float scale;
+};
+
+
+int launch_loss_narrow(int dtype, const NarrowArgs &a, hipStream_t st); // 0 or a hipError_t

@@ -20,80 +20,37 @@
 // Backward, a piece of the centroids at a time (at most PIECE values): P = 2^15 (p - [j = y]) is written as fp16 images in both
 // orders, for the sums over j and over i.  The lanes of the product hold four consecutive j of one i, and four i (16 apart) of one
 // j: the image summed over i has its indices in that order, so neither needs an exchange between lanes.
-#include "learn.h"
+#include "loss_image.h"
 
 #include <math.h>
 
-#include <type_traits>
-
-typedef _Float16 half8 __attribute__((ext_vector_type(8)));
-typedef _Float16 half4 __attribute__((ext_vector_type(4)));
-typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
-typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16_t;
-
-#define PAGE 512             // 16-byte chunks of a page
 #define LNT 512              // threads of the product kernels
-#define TILE 256             // rows and columns of their tiles
 #define LOSS_ROWS 8192       // rows that go through the products together
 #define PIECE (1 << 25)      // values of P kept at a time
+#define NARROW_DIM 128       // up to so many dimensions the gradients take the narrow form (softmax_loss_narrow.hip)
+#define NARROW_GROUPS 1024   // its workgroups, about: two rounds of two a compute unit
+#define NARROW_LEAST 8       // tiles of 32 rows that a workgroup of it takes at least
 #define FEW_ROWS 64          // up to so many rows the logits come from the centroids as they lie (k_loss_few)
 #define FEW_WIDE 65536       // from so many centroids on a wave takes 32 of them: then there are waves enough
-#define P_ONE 32768.f        // 2^15, what a probability of one is in P
-#define LOG2E 1.4426950408889634f
-#define LN2 0.6931471805599453f
-
-// ---------------------------------------------------------------------------
-// values
-// ---------------------------------------------------------------------------
-// Exponent of the power of two that brings mx to [2^14, 2^15)
-__device__ __forceinline__ int scale_exponent(float mx)
-{
-    const int ex = mx > 0.f ? 14 - ((int)(__float_as_uint(mx) >> 23) - 127) : 0;
-    return min(max(ex, -126), 126);
-}
-__device__ __forceinline__ float pow2i(int ex) { return __uint_as_float((uint32_t)(127 + ex) << 23); }
-
-// eight values of a row from index i on, zeros past its end
-template <typename T>
-__device__ __forceinline__ void load8(const T *row, int i, int d, bool vec, float (&v)[8])
-{
-    if (vec && i < d) { // (d is a multiple of 8)
-        if constexpr (sizeof(T) == 4) {
-            const f32x4 a = *(const f32x4 *)(row + i), b = *(const f32x4 *)(row + i + 4);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = e < 4 ? a[e] : b[e - 4];
-        } else {
-            T t[8];
-            *(u32x4 *)t = *(const u32x4 *)(row + i);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = (float)t[e];
-        }
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = i + e < d ? (float)row[i + e] : 0.f;
-}
-
-// v as one or two fp16 parts
-template <int NP>
-__device__ __forceinline__ void split8(const float (&v)[8], half8 (&h)[NP])
-{
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        h[0][e] = (_Float16)v[e];
-        if (NP == 2) h[NP - 1][e] = (_Float16)(v[e] - (float)h[0][e]);
-    }
-}
 
 // ---------------------------------------------------------------------------
 // images
 // ---------------------------------------------------------------------------
-// Header of a call: [0] largest magnitude of x's counted rows (bits), [1] of c, [2] of g
-__global__ void k_loss_header(uint32_t *hdr)
+// Header of a call: [0] largest magnitude of x's counted rows (bits), [1] of c, [2] of g; and the bias in units of log 2, -inf past
+// the last centroid
+__global__ __launch_bounds__(256) void k_loss_begin(const float *bias, int k, int kpad, float *bias2, uint32_t *hdr)
 {
-    if (threadIdx.x < 4) hdr[threadIdx.x] = 0;
+    const int j = blockIdx.x * 256 + threadIdx.x;
+    if (j < 4) hdr[j] = 0;
+    if (j < kpad) bias2[j] = j < k ? (bias ? bias[j] * LOG2E : 0.f) : -INFINITY;
+}
+
+// The largest of the callers' values into *to: an atomic only where it is larger than what is there (all of a launch's workgroups
+// on one address waited for each other: 3 126 of them 131 us, a third of that without)
+__device__ __forceinline__ void raise(uint32_t *to, float v)
+{
+    const uint32_t bits = __float_as_uint(v);
+    if (bits > __hip_atomic_load(to, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(to, bits);
 }
 
 // A row counts if its label is a centroid; a centroid if its bias is not -inf.  What does not count is written as zeros.
@@ -107,13 +64,13 @@ __device__ __forceinline__ bool row_counts(const int32_t *label, int k, const fl
 // Bound by memory: X is read twice (the second time from the caches), written once.  (With 128 rows a workgroup and a scale for
 // all of them 128 MB took 99 us, for want of loads under way.)
 template <typename T, bool OWN, int NP>
-__global__ __launch_bounds__(256) void k_pack_rows(const T *__restrict__ X, int64_t rows, int d, int units,
+__device__ __forceinline__ void pack_rows(int block, const T *__restrict__ X, int64_t rows, int d, int units,
                                                    const int32_t *__restrict__ label, int k, const float *__restrict__ bias,
                                                    u32x4 *__restrict__ pages, float *__restrict__ inv, uint32_t *absmax, bool vec)
 {
     __shared__ float rmax[16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t r0 = (int64_t)blockIdx.x * 16;
+    const int64_t r0 = (int64_t)block * 16;
     // pass 1: 16 lanes a row
     if constexpr (!__is_same(T, _Float16)) {
         const int r = tid >> 4;
@@ -142,19 +99,19 @@ __global__ __launch_bounds__(256) void k_pack_rows(const T *__restrict__ X, int6
         all = mine;
 #pragma unroll
         for (int o = 8; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor(all, o, 64));
-        if (tid == 0 && absmax) atomicMax(absmax, __float_as_uint(all));
+        if (tid == 0 && absmax) raise(absmax, all);
     }
     const int ex = __is_same(T, _Float16) ? 0 : scale_exponent(OWN ? mine : all);
     if (tid < 16) {
         if (OWN)
             inv[r0 + tid] = pow2i(-ex);
         else if (tid == 0)
-            inv[blockIdx.x] = pow2i(-ex);
+            inv[block] = pow2i(-ex);
     }
     const bool counts = r0 + l < rows && row_counts(label, k, bias, r0 + l);
     const T *row = X + (counts ? r0 + l : 0) * d;
     const float s = pow2i(ex);
-    u32x4 *to = pages + (int64_t)(blockIdx.x >> 3) * units * NP * PAGE + (blockIdx.x & 7) * 64 + lane;
+    u32x4 *to = pages + (int64_t)(block >> 3) * units * NP * PAGE + (block & 7) * 64 + lane;
 #pragma unroll 2
     for (int u = wave; u < units; u += 4) {
         float v[8] = {};
@@ -169,16 +126,17 @@ __global__ __launch_bounds__(256) void k_pack_rows(const T *__restrict__ X, int6
 }
 
 // Image of X's columns: its rows are the dimensions, its indices the rows of X, 64 rows x 128 dimensions a workgroup.
-// PERM: index s of 64 is row (s >> 2) + 16 (s & 3), the order in which the lanes of k_loss_p hold them.
-template <typename T, bool PERM, int NP>
-__global__ __launch_bounds__(256) void k_pack_cols(const T *__restrict__ X, int64_t rows, int d, int units,
+// ORDER 1: index s of 64 is row (s >> 2) + 16 (s & 3), the order in which the lanes of k_loss_p hold them; 2: index s of 32 is row
+// 16 (s / 4 % 2) + 4 (s / 8) + s % 4, as the lanes of k_loss_narrow hold them.
+template <typename T, int ORDER, int NP>
+__device__ __forceinline__ void pack_cols(int block, int dblock, const T *__restrict__ X, int64_t rows, int d, int units,
                                                    const int32_t *__restrict__ label, int k, const float *__restrict__ bias,
                                                    u32x4 *__restrict__ pages, const uint32_t *__restrict__ absmax, bool vec)
 {
     __shared__ float t[64][129];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t r0 = (int64_t)blockIdx.x * 64;
-    const int d0 = blockIdx.y * 128;
+    const int64_t r0 = (int64_t)block * 64;
+    const int d0 = dblock * 128;
     const float s = __is_same(T, _Float16) ? 1.f : pow2i(scale_exponent(__uint_as_float(*absmax)));
 #pragma unroll
     for (int i = tid; i < 64 * 16; i += 256) {
@@ -195,49 +153,55 @@ __global__ __launch_bounds__(256) void k_pack_cols(const T *__restrict__ X, int6
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
             const int i = e * 32 + (lane >> 4) * 8 + q;
-            v[q] = t[PERM ? (i >> 2) + 16 * (i & 3) : i][grp * 16 + (lane & 15)];
+            v[q] = t[ORDER == 1 ? (i >> 2) + 16 * (i & 3) : ORDER == 2 ? e * 32 + 16 * (q >> 2) + 4 * (lane >> 4) + (q & 3) : i][grp * 16 + (lane & 15)];
         }
         half8 h[NP];
         split8<NP>(v, h);
-        const int64_t u = (int64_t)blockIdx.x * 2 + e;
+        const int64_t u = (int64_t)block * 2 + e;
 #pragma unroll
         for (int p = 0; p < NP; ++p)
-            pages[(((int64_t)blockIdx.y * units + u) * NP + p) * PAGE + grp * 64 + lane] = __builtin_bit_cast(u32x4, h[p]);
+            pages[(((int64_t)dblock * units + u) * NP + p) * PAGE + grp * 64 + lane] = __builtin_bit_cast(u32x4, h[p]);
     }
 }
 
-// bias in units of log 2, -inf past the last centroid
-__global__ __launch_bounds__(256) void k_loss_bias(const float *bias, int k, int kpad, float *bias2)
-{
-    const int j = blockIdx.x * 256 + threadIdx.x;
-    if (j < kpad) bias2[j] = j < k ? (bias ? bias[j] * LOG2E : 0.f) : -INFINITY;
-}
-
-__global__ __launch_bounds__(256) void k_grad_max(const float *g, const int32_t *label, int k, int64_t n, uint32_t *out)
+__device__ __forceinline__ void grad_max(int block, int blocks, const float *g, const int32_t *label, int k, int64_t n, uint32_t *out)
 {
     float mx = 0.f;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256)
+    for (int64_t i = (int64_t)block * 256 + threadIdx.x; i < n; i += (int64_t)blocks * 256)
         if ((uint32_t)label[i] < (uint32_t)k && fabsf(g[i]) < INFINITY) mx = fmaxf(mx, fabsf(g[i]));
     mx = __uint_as_float(wave_max_u32(__float_as_uint(mx)));
-    if ((threadIdx.x & 63) == 0) atomicMax(out, __float_as_uint(mx));
+    if ((threadIdx.x & 63) == 0) raise(out, mx);
 }
 
-// Per row: f = s log2(e) / scale, and backward the maximum m2, the factors of P in either order (2^15 / z, and with g / max g);
-// a row that does not count, or has no logit above -inf, gets m2 = +inf and no label.
-__global__ __launch_bounds__(256) void k_loss_rows(const float *rinv, const int32_t *label, int64_t n, int k, float scale,
-                                                   const float *stats, const float *g, const uint32_t *hdr, f32x4 *row, float *gn,
-                                                   int32_t *lab)
+struct PackArgs {
+    const void *x, *c;
+    int64_t n;
+    int d, k, units;
+    const int32_t *label;
+    const float *bias, *g, *stats;
+    float scale;
+    u32x4 *ximg, *cimg, *xcols, *ccols;
+    float *rinv, *cinv, *gn;
+    f32x4 *row;
+    int32_t *lab;
+    uint32_t *hdr;
+    bool xvec, cvec;
+    int xblocks, cblocks, others, dblocks, xunits, cunits; // workgroups for x, for c, for the rest; units of the columns' images
+};
+
+// A row's numbers: factor s log2(e) / scale, and backward its maximum, the factors of P in either order (2^15 / z, and with
+// g / max g); a row that does not count, or has no logit above -inf, gets the maximum +inf and no label.
+__device__ __forceinline__ void row_numbers(const PackArgs &a, int64_t i, float inv)
 {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; // (the grid covers the padded rows)
-    const bool in = i < n && (uint32_t)label[i] < (uint32_t)k;
-    f32x4 r = {in ? scale * LOG2E * rinv[i] : 0.f, INFINITY, 0.f, 0.f};
+    const bool in = i < a.n && (uint32_t)a.label[i] < (uint32_t)a.k;
+    f32x4 r = {in ? a.scale * LOG2E * inv : 0.f, INFINITY, 0.f, 0.f};
     float f = 0.f;
     bool ok = in;
-    if (stats && in) {
-        const float m = stats[2 * i], z = stats[2 * i + 1], top = __uint_as_float(hdr[2]);
+    if (a.stats && in) {
+        const float m = a.stats[2 * i], z = a.stats[2 * i + 1], top = __uint_as_float(a.hdr[2]);
         ok = m != -INFINITY;
         if (ok) {
-            f = top > 0.f ? g[i] / top : 0.f;
+            f = top > 0.f ? a.g[i] / top : 0.f;
             r[1] = m;
             r[2] = P_ONE / z;
             r[3] = P_ONE / z * f;
@@ -245,9 +209,46 @@ __global__ __launch_bounds__(256) void k_loss_rows(const float *rinv, const int3
             r[0] = 0.f;
         }
     }
-    row[i] = r;
-    lab[i] = ok ? label[i] : -1;
-    if (gn) gn[i] = ok ? f * P_ONE : 0.f;
+    a.row[i] = r;
+    a.lab[i] = ok ? a.label[i] : -1;
+    if (a.gn) a.gn[i] = ok ? f * P_ONE : 0.f;
+}
+
+// Both matrices' images in one launch; forward the rows' numbers, backward the largest g
+template <typename T, int NP>
+__global__ __launch_bounds__(256) void k_pack_rows(PackArgs a)
+{
+    int b = blockIdx.x;
+    if (b < a.xblocks) {
+        pack_rows<T, true, NP>(b, (const T *)a.x, a.n, a.d, a.units, a.label, a.k, nullptr, a.ximg, a.rinv, a.hdr, a.xvec);
+        if (a.stats) return;
+        __syncthreads();
+        if (threadIdx.x < 16) row_numbers(a, (int64_t)b * 16 + threadIdx.x, a.rinv[(int64_t)b * 16 + threadIdx.x]);
+        return;
+    }
+    b -= a.xblocks;
+    if (b < a.cblocks)
+        pack_rows<T, false, NP>(b, (const T *)a.c, a.k, a.d, a.units, nullptr, a.k, a.bias, a.cimg, a.cinv, a.hdr + 1, a.cvec);
+    else
+        grad_max(b - a.cblocks, a.others, a.g, a.label, a.k, a.n, a.hdr + 2);
+}
+
+// Backward: both matrices' columns, and the rows' numbers
+template <typename T, int XORDER, int CORDER, int NP>
+__global__ __launch_bounds__(256) void k_pack_cols(PackArgs a)
+{
+    int b = blockIdx.x;
+    if (b < a.xblocks) {
+        pack_cols<T, XORDER, NP>(b / a.dblocks, b % a.dblocks, (const T *)a.x, a.n, a.d, a.xunits, a.label, a.k, nullptr, a.xcols, a.hdr, a.xvec);
+        return;
+    }
+    b -= a.xblocks;
+    if (b < a.cblocks) {
+        pack_cols<T, CORDER, NP>(b / a.dblocks, b % a.dblocks, (const T *)a.c, a.k, a.d, a.cunits, nullptr, a.k, a.bias, a.ccols, a.hdr + 1, a.cvec);
+        return;
+    }
+    const int64_t i = (int64_t)(b - a.cblocks) * 256 + threadIdx.x; // (the workgroups cover the padded rows)
+    row_numbers(a, i, a.rinv[i]);
 }
 
 // ---------------------------------------------------------------------------
@@ -378,7 +379,7 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_stats(LogitArgs a)
         for (int j = 0; j < 4; ++j) {
             const float f = a.row[n0 + 16 * j + l][0] * ci;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) acc[i][j][r] = b2[r] == -INFINITY ? -INFINITY : fmaf(acc[i][j][r], f, b2[r]);
+            for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(acc[i][j][r], f, b2[r]);
         }
     }
 #pragma unroll
@@ -603,7 +604,7 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_p(LogitArgs a)
             const float f = row[j][0] * ci;
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                acc[i][j][r] = b2[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], f, b2[r] - row[j][1]));
+                acc[i][j][r] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], f, b2[r] - row[j][1]));
         }
     }
     const bool labels = __any(any);
@@ -674,30 +675,6 @@ struct GradOut {
     bool vec;
 };
 
-template <typename T>
-__device__ __forceinline__ float grad_factor(const uint32_t *absmax, const uint32_t *gmax, float scale)
-{
-    const float inv = __is_same(T, _Float16) ? 1.f : pow2i(-scale_exponent(__uint_as_float(*absmax)));
-    return scale * (gmax ? __uint_as_float(*gmax) : 1.f) * (1.f / P_ONE) * inv;
-}
-
-template <typename T>
-__device__ __forceinline__ void store4(T *p, const f32x4 &v, int count, bool vec)
-{
-    if (vec && count >= 4) {
-        if constexpr (sizeof(T) == 4) {
-            *(f32x4 *)p = v;
-        } else {
-            T t[4] = {(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
-            *(u32x2 *)p = *(u32x2 *)t;
-        }
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (e < count) p[e] = (T)v[e];
-}
-
 // Both gradients of a piece in one launch, the one with the longer sums first: a piece's tiles are too few to fill
 // the chip twice over.
 template <typename T, int NP, int MB>
@@ -748,16 +725,35 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_grads(GradOut first, GradOut se
     }
 }
 
-// out = factor * sum of the slabs
+// out = factor * sum of the slabs, of both gradients in one launch, four values a thread
+struct SlabSum {
+    const float *slabs;
+    int splits, blocks;
+    int64_t count;
+    const uint32_t *absmax, *gmax;
+    void *out;
+};
 template <typename T>
-__global__ __launch_bounds__(256) void k_loss_slabs(const float *slabs, int splits, int64_t slab, int64_t count,
-                                                    const uint32_t *absmax, const uint32_t *gmax, float scale, T *out)
+__global__ __launch_bounds__(256) void k_loss_slabs(SlabSum x, SlabSum c, float scale)
 {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= count) return;
-    float s = 0.f;
-    for (int p = 0; p < splits; ++p) s += slabs[p * slab + i];
-    out[i] = (T)(s * grad_factor<T>(absmax, gmax, scale));
+    const bool first = (int)blockIdx.x < x.blocks;
+    const SlabSum &a = first ? x : c;
+    const int64_t i = ((int64_t)(first ? blockIdx.x : blockIdx.x - x.blocks) * 256 + threadIdx.x) * 4;
+    if (i >= a.count) return;
+    const float f = grad_factor<T>(a.absmax, a.gmax, scale);
+    const bool vec = a.count % 4 == 0 && (uintptr_t)a.out % (4 * sizeof(T)) == 0;
+    const int count = (int)min((int64_t)4, a.count - i);
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    if (vec) {
+#pragma unroll 4
+        for (int p = 0; p < a.splits; ++p) s += *(const f32x4 *)(a.slabs + p * a.count + i);
+    } else {
+        for (int p = 0; p < a.splits; ++p)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e < count) s[e] += a.slabs[p * a.count + i + e];
+    }
+    store4((T *)a.out + i, s * f, count, vec);
 }
 
 // No rows: the gradients of centroids and bias are zero
@@ -769,14 +765,19 @@ __global__ __launch_bounds__(256) void k_loss_none(T *dc, int64_t count, float *
     if (dbias && i < k) dbias[i] = 0.f;
 }
 
-// dbias of a piece: sums over the rows' parts
+// dbias of a piece: sums over the rows' parts, 64 centroids a workgroup, four waves taking the parts in turn
 __global__ __launch_bounds__(256) void k_loss_dbias(const float *part, int slots, int ld, int count, const uint32_t *gmax, bool add, float *out)
 {
-    const int j = blockIdx.x * 256 + threadIdx.x;
-    if (j >= count) return;
+    __shared__ float sum[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = blockIdx.x * 64 + lane;
     float s = 0.f;
-    for (int p = 0; p < slots; ++p) s += part[(int64_t)p * ld + j];
-    s *= __uint_as_float(*gmax) * (1.f / P_ONE);
+    if (j < count)
+#pragma unroll 4
+        for (int p = wave; p < slots; p += 4) s += part[(int64_t)p * ld + j];
+    sum[wave][lane] = s;
+    __syncthreads();
+    if (wave > 0 || j >= count) return;
+    s = ((sum[0][lane] + sum[1][lane]) + (sum[2][lane] + sum[3][lane])) * (__uint_as_float(*gmax) * (1.f / P_ONE));
     out[j] = add ? out[j] + s : s;
 }
 
@@ -794,6 +795,8 @@ struct LossPlan {
     int64_t piece;           // centroids whose P is kept at a time
     int xsplit, csplit;      // parts that the sums of dx (over a piece) and dc (over `rows`) are cut into
     bool xslab, cslab;
+    bool narrow;             // softmax_loss_narrow.hip
+    int xper, cper;          // its tiles of a part
     uint32_t *hdr;
     u32x4 *ximg, *cimg, *xcols, *ccols, *pj, *pi;
     float *rinv, *cinv, *bias2, *mine, *gn, *dbpart, *xsum, *csum;
@@ -813,6 +816,17 @@ static int sum_parts(int64_t tiles, int64_t steps, int64_t out_bytes)
     if (s <= 1) return 1;
     const int64_t per = (steps + s - 1) / s;
     return (int)((steps + per - 1) / per); // (no part is empty)
+}
+
+// The narrow form: parts of about `per` tiles of 32, fewer where their slabs would take more than 256 MB
+static int narrow_parts(int64_t tiles, int64_t per, int64_t out_bytes, int *tiles_each)
+{
+    int64_t s = (tiles + per - 1) / per;
+    if (s * out_bytes > (256ll << 20)) s = (256ll << 20) / out_bytes;
+    if (s < 1) s = 1;
+    const int64_t each = (tiles + s - 1) / s;
+    *tiles_each = (int)each;
+    return (int)((tiles + each - 1) / each);
 }
 
 static LossPlan loss_plan(int dtype, int64_t n, int d, int k, bool backward, void *ws)
@@ -854,6 +868,21 @@ static LossPlan loss_plan(int dtype, int64_t n, int d, int k, bool backward, voi
         take(p.gn, p.npad);
         take(p.xcols, p.npad / 32 * p.dblocks * page);
         take(p.ccols, p.kpad / 32 * p.dblocks * page);
+        p.narrow = d <= NARROW_DIM;
+        if (p.narrow) {
+            const int64_t rows = narrow_rows(p.np), xq = p.npad / rows, cq = p.kpad / rows, xt = p.kpad / 32, ct = p.npad / 32;
+            int64_t per = (xq * xt + cq * ct) / NARROW_GROUPS;
+            if (per < NARROW_LEAST) per = NARROW_LEAST;
+            p.xsplit = narrow_parts(xt, per, n * d * 4, &p.xper);
+            p.csplit = narrow_parts(ct, per, (int64_t)k * d * 4, &p.cper);
+            p.xslab = p.xsplit > 1;
+            p.cslab = p.csplit > 1;
+            take(p.dbpart, p.csplit * p.kpad);
+            take(p.xsum, p.xslab ? (size_t)p.xsplit * n * d : 0);
+            take(p.csum, p.cslab ? (size_t)p.csplit * k * d : 0);
+            p.bytes = (off + 255) & ~(size_t)255;
+            return p;
+        }
         take(p.pj, p.rpad * p.piece / 8 * p.np);
         take(p.pi, p.rpad * p.piece / 8 * p.np);
         take(p.dbpart, p.rpad / 64 * p.piece);
@@ -895,16 +924,28 @@ static bool rows_vec(const void *p, int d)
     return d % 8 == 0 && (uintptr_t)p % 16 == 0;
 }
 
-// The images of rows and centroids, and the bias
+// The images of rows and centroids, and the rest of what the products need: two launches, three backward
 template <typename T, int NP>
-static void loss_images(const LossArgs &a, const LossPlan &p, hipStream_t st)
+static void loss_images(const LossArgs &a, const LossPlan &p, bool backward, hipStream_t st)
 {
-    hipLaunchKernelGGL(k_loss_header, dim3(1), dim3(64), 0, st, p.hdr);
-    hipLaunchKernelGGL((k_pack_rows<T, true, NP>), dim3((unsigned)(p.npad / 16)), dim3(256), 0, st, (const T *)a.x, a.n, a.d, p.units,
-                       a.label, a.k, nullptr, p.ximg, p.rinv, p.hdr, rows_vec<T>(a.x, a.d));
-    hipLaunchKernelGGL((k_pack_rows<T, false, NP>), dim3((unsigned)(p.kpad / 16)), dim3(256), 0, st, (const T *)a.c, (int64_t)a.k, a.d,
-                       p.units, nullptr, a.k, a.bias, p.cimg, p.cinv, p.hdr + 1, rows_vec<T>(a.c, a.d));
-    hipLaunchKernelGGL(k_loss_bias, dim3((unsigned)(p.kpad / 256)), dim3(256), 0, st, a.bias, a.k, (int)p.kpad, p.bias2);
+    hipLaunchKernelGGL(k_loss_begin, dim3((unsigned)(p.kpad / 256)), dim3(256), 0, st, a.bias, a.k, (int)p.kpad, p.bias2, p.hdr);
+    PackArgs g = {a.x, a.c, a.n, a.d, a.k, p.units, a.label, a.bias, a.grad, backward ? a.stats : nullptr, a.scale, p.ximg, p.cimg,
+                  p.xcols, p.ccols, p.rinv, p.cinv, p.gn, p.row, p.lab, p.hdr, rows_vec<T>(a.x, a.d), rows_vec<T>(a.c, a.d)};
+    g.xblocks = (int)(p.npad / 16);
+    g.cblocks = (int)(p.kpad / 16);
+    g.others = !backward ? 0 : (int)((a.n + 2047) / 2048 < 64 ? (a.n + 2047) / 2048 : 64);
+    hipLaunchKernelGGL((k_pack_rows<T, NP>), dim3((unsigned)(g.xblocks + g.cblocks + g.others)), dim3(256), 0, st, g);
+    if (!backward) return;
+    g.dblocks = p.dblocks;
+    g.xunits = (int)(p.npad / 32);
+    g.cunits = (int)(p.kpad / 32);
+    g.xblocks = a.dc ? g.xunits / 2 * p.dblocks : 0;
+    g.cblocks = a.dx ? g.cunits / 2 * p.dblocks : 0;
+    const dim3 grid((unsigned)(g.xblocks + g.cblocks + p.npad / 256));
+    if (p.narrow)
+        hipLaunchKernelGGL((k_pack_cols<T, 2, 2, NP>), grid, dim3(256), 0, st, g);
+    else
+        hipLaunchKernelGGL((k_pack_cols<T, 1, 0, NP>), grid, dim3(256), 0, st, g);
 }
 
 template <int NP>
@@ -973,9 +1014,7 @@ static int loss_forward(const LossArgs &a, hipStream_t st)
 {
     if (a.n <= FEW_ROWS) return loss_few<T>(a, st);
     const LossPlan p = loss_plan(a.dtype, a.n, a.d, a.k, false, a.ws);
-    loss_images<T, NP>(a, p, st);
-    hipLaunchKernelGGL(k_loss_rows, dim3((unsigned)(p.npad / 256)), dim3(256), 0, st, p.rinv, a.label, a.n, a.k, a.scale, nullptr,
-                       nullptr, p.hdr, p.row, nullptr, p.lab);
+    loss_images<T, NP>(a, p, false, st);
     LOSS_TRY(allow_lds(k_loss_stats<NP>, lds_bytes(2)));
     for (int64_t r0 = 0; r0 < a.n; r0 += p.rows) {
         const int64_t rows = a.n - r0 < p.rows ? a.n - r0 : p.rows, rpad = pad_to(rows, TILE);
@@ -997,17 +1036,45 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
         return (int)hipGetLastError();
     }
     const LossPlan p = loss_plan(a.dtype, a.n, a.d, a.k, true, a.ws);
-    loss_images<T, NP>(a, p, st);
-    if (a.dc)
-        hipLaunchKernelGGL((k_pack_cols<T, true, NP>), dim3((unsigned)(p.npad / 64), p.dblocks), dim3(256), 0, st, (const T *)a.x, a.n,
-                           a.d, (int)(p.npad / 32), a.label, a.k, nullptr, p.xcols, p.hdr, rows_vec<T>(a.x, a.d));
-    if (a.dx)
-        hipLaunchKernelGGL((k_pack_cols<T, false, NP>), dim3((unsigned)(p.kpad / 64), p.dblocks), dim3(256), 0, st, (const T *)a.c,
-                           (int64_t)a.k, a.d, (int)(p.kpad / 32), nullptr, a.k, a.bias, p.ccols, p.hdr + 1, rows_vec<T>(a.c, a.d));
-    const unsigned gblocks = (unsigned)((a.n + 2047) / 2048 < 256 ? (a.n + 2047) / 2048 : 256);
-    hipLaunchKernelGGL(k_grad_max, dim3(gblocks), dim3(256), 0, st, a.grad, a.label, a.k, a.n, p.hdr + 2);
-    hipLaunchKernelGGL(k_loss_rows, dim3((unsigned)(p.npad / 256)), dim3(256), 0, st, p.rinv, a.label, a.n, a.k, a.scale, a.stats,
-                       a.grad, p.hdr, p.row, p.gn, p.lab);
+    loss_images<T, NP>(a, p, true, st);
+    auto finish = [&]() {
+        auto side = [&](float *slabs, int splits, int64_t count, const uint32_t *absmax, const uint32_t *gmax, void *out) {
+            return SlabSum{slabs, splits, (int)((count + 1023) / 1024), count, absmax, gmax, out};
+        };
+        SlabSum x = {}, c = {};
+        if (a.dx && p.xslab) x = side(p.xsum, p.xsplit, a.n * a.d, p.hdr + 1, nullptr, a.dx);
+        if (a.dc && p.cslab) c = side(p.csum, p.csplit, (int64_t)a.k * a.d, p.hdr, p.hdr + 2, a.dc);
+        if (x.blocks + c.blocks) hipLaunchKernelGGL(k_loss_slabs<T>, dim3((unsigned)(x.blocks + c.blocks)), dim3(256), 0, st, x, c, a.scale);
+    };
+    if (p.narrow) {
+        NarrowArgs g = {};
+        const int rows = narrow_rows(NP);
+        g.units = p.units;
+        g.d = a.d;
+        g.row = p.row;
+        g.lab = p.lab;
+        g.gn = p.gn;
+        g.cinv = p.cinv;
+        g.bias2 = p.bias2;
+        g.dbpart = a.dbias ? p.dbpart : nullptr;
+        g.kpad = (int)p.kpad;
+        g.scale = a.scale;
+        if (a.dx) {
+            g.x = {p.ximg, p.cimg, p.ccols, (int)(p.npad / rows), (int)(p.kpad / 32), p.xsplit, p.xper, (int)a.n, p.xslab,
+                   p.xslab ? (void *)p.xsum : a.dx, p.hdr + 1, nullptr, a.grad, a.d % 4 == 0 && (p.xslab || (uintptr_t)a.dx % 16 == 0)};
+            g.nx = g.x.qblocks * g.x.splits;
+        }
+        if (a.dc || a.dbias)
+            g.c = {p.cimg, p.ximg, p.xcols, (int)(p.kpad / rows), (int)(p.npad / 32), p.csplit, p.cper, a.k, p.cslab,
+                   !a.dc ? nullptr : p.cslab ? (void *)p.csum : a.dc, p.hdr, p.hdr + 2, nullptr,
+                   a.d % 4 == 0 && (p.cslab || (uintptr_t)a.dc % 16 == 0)};
+        LOSS_TRY((hipError_t)launch_loss_narrow(a.dtype, g, st));
+        finish();
+        if (a.dbias)
+            hipLaunchKernelGGL(k_loss_dbias, dim3((unsigned)((a.k + 63) / 64)), dim3(256), 0, st, p.dbpart, p.csplit, (int)p.kpad, a.k,
+                               p.hdr + 2, false, a.dbias);
+        return (int)hipGetLastError();
+    }
     LOSS_TRY(allow_lds(k_loss_p<NP>, lds_bytes(2)));
     LOSS_TRY(allow_lds(k_loss_grads<T, NP, MB>, lds_bytes(MB)));
     const int mt = p.dblocks / MB;
@@ -1026,7 +1093,7 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
             hipLaunchKernelGGL(k_loss_p<NP>, dim3((unsigned)(g.mt * g.nt)), dim3(LNT), lds_bytes(2), st, g);
             if (a.dbias) {
                 const int count = (int)(a.k - c0 < cpad ? a.k - c0 : cpad);
-                hipLaunchKernelGGL(k_loss_dbias, dim3((unsigned)((count + 255) / 256)), dim3(256), 0, st, p.dbpart, (int)(rpad / 64),
+                hipLaunchKernelGGL(k_loss_dbias, dim3((unsigned)((count + 63) / 64)), dim3(256), 0, st, p.dbpart, (int)(rpad / 64),
                                    (int)cpad, count, p.hdr + 2, r0 > 0, a.dbias + c0);
             }
             GradOut x = {}, c = {};
@@ -1077,12 +1144,7 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
                 hipLaunchKernelGGL((k_loss_grads<T, NP, MB>), dim3((unsigned)(nx + nc)), dim3(LNT), lds_bytes(MB), st, x, c, nx);
         }
     }
-    auto finish = [&](float *slabs, int splits, int64_t count, const uint32_t *absmax, const uint32_t *gmax, void *out) {
-        hipLaunchKernelGGL(k_loss_slabs<T>, dim3((unsigned)((count + 255) / 256)), dim3(256), 0, st, slabs, splits, count, count, absmax,
-                           gmax, a.scale, (T *)out);
-    };
-    if (a.dx && p.xslab) finish(p.xsum, p.xsplit, a.n * a.d, p.hdr + 1, nullptr, a.dx);
-    if (a.dc && p.cslab) finish(p.csum, p.csplit, (int64_t)a.k * a.d, p.hdr, p.hdr + 2, a.dc);
+    finish();
     return (int)hipGetLastError();
 }
 

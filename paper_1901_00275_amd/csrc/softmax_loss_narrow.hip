@@ -1,0 +1,265 @@
+// The gradients of the softmax loss for up to 128 dimensions: no piece of the n x k probabilities leaves the registers.
+//
+// A workgroup keeps 128 rows (256 with one fp16 part) of one matrix, of x for dx and of c for dc: their fragments and their gradient's
+// sums stay in registers while tiles of 32 rows of the other matrix pass through LDS, its image and the image of its
+// columns.  Per tile a wave multiplies 32 rows of the other matrix with its own (S = R Q^T), turns S into P with the row's
+// maximum and sum, and multiplies the other matrix's columns with P (dQ^T += R^T P).  S has four consecutive r of one q in a lane; P as the
+// second operand wants eight: those of both 16-row halves are taken together, which is an order of the 32 indices that the
+// columns' image is written in.
+//
+// Each side computes the logits, 8 n k d operations together where the wide form takes 6 n k d; but that one writes P twice
+// and reads it twice, 16 bytes a pair with two parts, which bounds it at so few dimensions.
+#include "loss_image.h"
+
+#define NARROW_NT 256
+// CENT: the gradient of the centroids
+template <typename T, int DU, bool CENT>
+__device__ __forceinline__ void narrow(const NarrowArgs &a, const NarrowSide &s, int b, u32x4 *lds)
+{
+    constexpr int NP = sizeof(T) == 4 ? 2 : 1, Q = narrow_rows(NP), QB = Q / 64, DB = 2 * DU;
+    constexpr int CHUNKS = 4 * DU * NP;             // KB of a tile: rows, then columns
+    constexpr int STAGE = (CHUNKS + 2) * 64;        // and two KB for the rows' numbers, in 16-byte pieces
+    const int tid = threadIdx.x, lane = tid & 63, l = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int split = b / s.qblocks, q0 = (b - split * s.qblocks) * Q + wave * 16 * QB;
+    const int t0 = split * s.per, t1 = min(s.tiles, t0 + s.per);
+
+    auto copy16 = [&](const void *src, int bytes, u32x4 *dst) { // 16 bytes a lane, zeros behind `bytes`
+        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void *)src, 0, bytes, 0x00020000);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void *)dst, 16, lane * 16, 0, 0, 0);
+    };
+    auto copy4 = [&](const void *src, int bytes, u32x4 *dst) {
+        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void *)src, 0, bytes, 0x00020000);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void *)dst, 4, lane * 4, 0, 0, 0);
+    };
+    auto copy_tile = [&](int t) {
+        u32x4 *dst = lds + (t & 1) * STAGE;
+        const u32x4 *rows = s.r + (int64_t)(t >> 2) * a.units * NP * PAGE + (t & 3) * 128;
+        const u32x4 *cols = s.rt + (int64_t)t * NP * PAGE;
+#pragma unroll
+        for (int e = 0; e < DU * NP; ++e) {
+            const int c = e * 4 + wave; // (rows: page c / 2, group c % 2; columns: part, then group of 16 dimensions)
+            const int cc = c - 2 * DU * NP;
+            const u32x4 *src = c < 2 * DU * NP ? rows + (c >> 1) * PAGE + (c & 1) * 64 : cols + (cc / DB) * PAGE + (cc % DB) * 64;
+            copy16(src, 1024, dst + c * 64);
+        }
+        u32x4 *num = dst + CHUNKS * 64;
+        if (CENT) { // {factor, maximum, -, factor of P} [32], labels [32], the label's share [32]: zeros fill a wave's copy up
+            if (wave == 0) copy16(a.row + t * 32, 512, num);
+            if (wave == 1) copy4(a.lab + t * 32, 128, num + 64);
+            if (wave == 2) copy4(a.gn + t * 32, 128, num + 80);
+        } else if (wave == 3) {
+            copy4(a.bias2 + t * 32, 128, num);
+        }
+    };
+
+    half8 qf[DU][NP][QB];
+#pragma unroll
+    for (int u = 0; u < DU; ++u)
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+#pragma unroll
+            for (int j = 0; j < QB; ++j)
+                qf[u][p][j] = __builtin_bit_cast(
+                    half8, s.q[(((int64_t)(q0 >> 7) * a.units + u) * NP + p) * PAGE + (((q0 >> 4) & 7) + j) * 64 + lane]);
+    float f[QB], m[QB], z[QB], db[QB]; // x: factor, maximum, factor of P; c: factor, bias
+    int lab[QB];
+#pragma unroll
+    for (int j = 0; j < QB; ++j) {
+        const int q = q0 + 16 * j + l;
+        db[j] = 0.f;
+        if (CENT) {
+            f[j] = a.cinv[q >> 4];
+            m[j] = a.bias2[q];
+        } else {
+            const f32x4 v = a.row[q];
+            f[j] = v[0];
+            m[j] = v[1];
+            z[j] = v[2];
+            lab[j] = a.lab[q];
+        }
+    }
+    f32x4 acc[DB][QB];
+#pragma unroll
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+        for (int j = 0; j < QB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    copy_tile(t0);
+    for (int t = t0; t < t1; ++t) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads(); // (this tile has arrived, and nobody reads the other buffer any more)
+        if (t + 1 < t1) copy_tile(t + 1);
+        const u32x4 *st = lds + (t & 1) * STAGE;
+        const float *num = (const float *)(st + CHUNKS * 64);
+        f32x4 S[2][QB];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < QB; ++j) S[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < DU; ++u) {
+            half8 r[NP][2];
+#pragma unroll
+            for (int p = 0; p < NP; ++p)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) r[p][i] = __builtin_bit_cast(half8, st[((u * NP + p) * 2 + i) * 64 + lane]);
+            if (NP == 2) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < QB; ++j) S[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(r[0][i], qf[u][NP - 1][j], S[i][j], 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < QB; ++j) S[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(r[NP - 1][i], qf[u][0][j], S[i][j], 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < QB; ++j) S[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(r[0][i], qf[u][0][j], S[i][j], 0, 0, 0);
+        }
+        // P, in units of 2^15
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if (CENT) {
+                f32x4 row[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) row[r] = *(const f32x4 *)(num + (16 * i + 4 * g + r) * 4);
+#pragma unroll
+                for (int j = 0; j < QB; ++j)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        S[i][j][r] = __builtin_amdgcn_exp2f(fmaf(S[i][j][r], row[r][0] * f[j], m[j] - row[r][1])) * row[r][3];
+            } else {
+                const f32x4 b2 = *(const f32x4 *)(num + 16 * i + 4 * g);
+                const float ci = a.cinv[t * 2 + i];
+#pragma unroll
+                for (int j = 0; j < QB; ++j) {
+                    const float fj = f[j] * ci;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) S[i][j][r] = __builtin_amdgcn_exp2f(fmaf(S[i][j][r], fj, b2[r] - m[j])) * z[j];
+                }
+            }
+        }
+        // the labels' own
+        if (CENT) {
+            const int *rl = (const int *)(num + 256);
+            if (__any((uint32_t)(rl[lane & 31] - q0) < 16u * QB)) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int at = 16 * i + 4 * g + r, of = rl[at] - q0 - l;
+                        const float gn = num[320 + at];
+#pragma unroll
+                        for (int j = 0; j < QB; ++j)
+                            if (of == 16 * j) S[i][j][r] -= gn;
+                    }
+            }
+        } else {
+            bool any = false;
+#pragma unroll
+            for (int j = 0; j < QB; ++j) any |= (uint32_t)(lab[j] - 32 * t) < 32u;
+            if (__any(any)) {
+#pragma unroll
+                for (int j = 0; j < QB; ++j)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (lab[j] - 32 * t == 16 * i + 4 * g + r) S[i][j][r] -= P_ONE;
+            }
+        }
+        half8 P[NP][QB];
+#pragma unroll
+        for (int j = 0; j < QB; ++j)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float v = S[i][j][r];
+                    P[0][j][4 * i + r] = (_Float16)v;
+                    if (NP == 2) P[NP - 1][j][4 * i + r] = (_Float16)(v - (float)P[0][j][4 * i + r]);
+                    if (CENT) db[j] += v;
+                }
+#pragma unroll
+        for (int i = 0; i < DB; ++i) {
+            half8 c[NP];
+#pragma unroll
+            for (int p = 0; p < NP; ++p) c[p] = __builtin_bit_cast(half8, st[(2 * DU * NP + p * DB + i) * 64 + lane]);
+            if (NP == 2) {
+#pragma unroll
+                for (int j = 0; j < QB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(c[0], P[NP - 1][j], acc[i][j], 0, 0, 0);
+#pragma unroll
+                for (int j = 0; j < QB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(c[NP - 1], P[0][j], acc[i][j], 0, 0, 0);
+            }
+#pragma unroll
+            for (int j = 0; j < QB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(c[0], P[0][j], acc[i][j], 0, 0, 0);
+        }
+    }
+
+    const float factor = s.mode == 0 ? grad_factor<T>(s.absmax, s.gmax, a.scale) : 1.f;
+    float *slab = (float *)s.out + (int64_t)split * s.rows * a.d;
+#pragma unroll
+    for (int j = 0; j < QB; ++j) {
+        const int q = q0 + 16 * j + l;
+        if (CENT && a.dbpart) {
+            float v = db[j];
+            v += __shfl_xor(v, 16, 64);
+            v += __shfl_xor(v, 32, 64);
+            if (g == 0) a.dbpart[(int64_t)split * a.kpad + q] = v;
+        }
+        if (q >= s.rows || !s.out) continue;
+        const float w = CENT ? factor : lab[j] < 0 ? 0.f : s.weight[q] * factor;
+#pragma unroll
+        for (int i = 0; i < DB; ++i) {
+            const int dim = 16 * i + 4 * g;
+            if (dim >= a.d) continue;
+            if (s.mode == 0)
+                store4((T *)s.out + (int64_t)q * a.d + dim, acc[i][j] * w, a.d - dim, s.vec);
+            else
+                store4(slab + (int64_t)q * a.d + dim, acc[i][j] * w, a.d - dim, s.vec);
+        }
+    }
+}
+
+template <typename T, int DU>
+__global__ __launch_bounds__(NARROW_NT, 2) void k_loss_narrow(NarrowArgs a)
+{
+    extern __shared__ u32x4 lds[];
+    if ((int)blockIdx.x < a.nx)
+        narrow<T, DU, false>(a, a.x, blockIdx.x, lds);
+    else
+        narrow<T, DU, true>(a, a.c, blockIdx.x - a.nx, lds);
+}
+
+template <typename T>
+static int narrow_units(const NarrowArgs &a, hipStream_t st)
+{
+    auto go = [&](auto units) -> int {
+        constexpr int DU = decltype(units)::value;
+        constexpr size_t bytes = 2 * (4 * DU * (sizeof(T) == 4 ? 2 : 1) + 2) * 1024;
+        if (bytes > 49152) { // (48 KB of dynamic LDS need no asking)
+            const hipError_t e = hipFuncSetAttribute((const void *)k_loss_narrow<T, DU>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+            if (e != hipSuccess) return (int)e;
+        }
+        hipLaunchKernelGGL((k_loss_narrow<T, DU>), dim3((unsigned)(a.nx + a.c.qblocks * a.c.splits)), dim3(NARROW_NT), bytes, st, a);
+        return 0;
+    };
+    switch ((a.d + 31) / 32) {
+    case 1: return go(std::integral_constant<int, 1>{});
+    case 2: return go(std::integral_constant<int, 2>{});
+    case 3: return go(std::integral_constant<int, 3>{});
+    default: return go(std::integral_constant<int, 4>{});
+    }
+}
+
+int launch_loss_narrow(int dtype, const NarrowArgs &a, hipStream_t st)
+{
+    switch (dtype) {
+    case VLQ_F32: return narrow_units<float>(a, st);
+    case VLQ_F16: return narrow_units<_Float16>(a, st);
+    default: return narrow_units<bf16_t>(a, st);
+    }
+}
