@@ -261,73 +261,144 @@ struct Operand {
     int64_t first;
 };
 
-// acc = A B^T over `steps` steps of two pages: two units of 32 indices (NP = 1), or both parts of one (NP = 2).
-// A tile of MB blocks of A by two of B; eight waves, 2 x 4, of 64 MB rows of A x 64 of B each.  A lane's acc[i][j][r] is row
-// 16 i + 4 (lane / 16) + r, column 16 j + lane % 16 of its wave's part.  Two buffers in LDS: while a step is multiplied the
-// next one is copied from memory to LDS.
-template <int NP, int MB>
-__device__ __forceinline__ void product(const Operand &A, const Operand &B, int64_t ablk, int64_t bblk, int steps,
-                                        u32x4 *lds, f32x4 (&acc)[4 * MB][4])
-{
-    constexpr int IM = 4 * MB, PAGES = 2 * MB + 4;
-    const int tid = threadIdx.x, lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const u32x4 *a0 = A.pages + (ablk * A.block + A.first) * PAGE, *b0 = B.pages + (bblk * B.block + B.first) * PAGE;
+// acc = A B^T over `steps` steps of two pages of every block: two units of 32 indices (NP = 1), or both parts of one (NP = 2).
+// A tile of two blocks of A by two of B; eight waves, 2 x 4, of 128 rows of A x 64 of B each.  A lane's acc[i][j][r] is row
+// 16 i + 4 (lane / 16) + r, column 16 j + lane % 16 of its wave's part.
+template <int NP>
+struct Product;
+
+// Two parts: two buffers of a step in LDS; while one is multiplied the next is copied from memory to the other.
+template <>
+struct Product<2> {
+    static constexpr int PAGES = 8, LDS = 2 * PAGES * PAGE * 16;
+    static __device__ __forceinline__ void run(const Operand &A, const Operand &B, int64_t ablk, int64_t bblk, int steps, u32x4 *lds,
+                                               f32x4 (&acc)[8][4])
+    {
+        const int tid = threadIdx.x, lane = tid & 63;
+        const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        const u32x4 *a0 = A.pages + (ablk * A.block + A.first) * PAGE, *b0 = B.pages + (bblk * B.block + B.first) * PAGE;
 #pragma unroll
-    for (int i = 0; i < IM; ++i)
+        for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    auto copy_page = [&](const u32x4 *src, u32x4 *dst) {
-        const __amdgpu_buffer_rsrc_t page = __builtin_amdgcn_make_buffer_rsrc((void *)src, 0, PAGE * 16, 0x00020000);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(page, (__attribute__((address_space(3))) void *)(dst + wave * 64), 16, tid * 16, 0, 0, 0);
-    };
-    auto copy_step = [&](int t) {
-        u32x4 *dst = lds + (t & 1) * PAGES * PAGE;
+            for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        auto copy_page = [&](const u32x4 *src, u32x4 *dst) {
+            const __amdgpu_buffer_rsrc_t page = __builtin_amdgcn_make_buffer_rsrc((void *)src, 0, PAGE * 16, 0x00020000);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(page, (__attribute__((address_space(3))) void *)(dst + wave * 64), 16, tid * 16, 0, 0, 0);
+        };
+        auto copy_step = [&](int t) {
+            u32x4 *dst = lds + (t & 1) * PAGES * PAGE;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
+            for (int e = 0; e < 2; ++e)
 #pragma unroll
-            for (int b = 0; b < MB; ++b) copy_page(a0 + (b * A.block + 2 * t + e) * PAGE, dst + (b * 2 + e) * PAGE);
+                for (int b = 0; b < 2; ++b) {
+                    copy_page(a0 + (b * A.block + 2 * t + e) * PAGE, dst + (b * 2 + e) * PAGE);
+                    copy_page(b0 + (b * B.block + 2 * t + e) * PAGE, dst + (4 + b * 2 + e) * PAGE);
+                }
+        };
+        const int aoff = (wave >> 2) * 2 * PAGE, boff = (4 + ((wave >> 1) & 1) * 2) * PAGE + (wave & 1) * 4 * 64;
+        copy_step(0);
+        for (int t = 0; t < steps; ++t) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads(); // (this step has arrived, and nobody reads the other buffer any more)
+            if (t + 1 < steps) copy_step(t + 1);
+            const u32x4 *st = lds + (t & 1) * PAGES * PAGE + lane;
+            half8 a[2][8], b[2][4];
 #pragma unroll
-            for (int b = 0; b < 2; ++b) copy_page(b0 + (b * B.block + 2 * t + e) * PAGE, dst + (2 * MB + b * 2 + e) * PAGE);
-        }
-    };
-    const int am = wave >> 2, bn = wave & 3;
-    const int aoff = MB == 2 ? am * 2 * PAGE : am * 4 * 64;
-    const int boff = (2 * MB + (bn >> 1) * 2) * PAGE + (bn & 1) * 4 * 64;
-    copy_step(0);
-    for (int t = 0; t < steps; ++t) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads(); // (this step has arrived, and nobody reads the other buffer any more)
-        if (t + 1 < steps) copy_step(t + 1);
-        const u32x4 *st = lds + (t & 1) * PAGES * PAGE + lane;
-        half8 a[2][IM], b[2][4];
+            for (int e = 0; e < 2; ++e) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
+                for (int j = 0; j < 4; ++j) b[e][j] = __builtin_bit_cast(half8, st[boff + e * PAGE + j * 64]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) b[e][j] = __builtin_bit_cast(half8, st[boff + e * PAGE + j * 64]);
+                for (int i = 0; i < 8; ++i) a[e][i] = __builtin_bit_cast(half8, st[aoff + e * PAGE + i * 64]);
+            }
 #pragma unroll
-            for (int i = 0; i < IM; ++i) a[e][i] = __builtin_bit_cast(half8, st[aoff + e * PAGE + i * 64]);
-        }
-        if (NP == 2) {
-#pragma unroll
-            for (int i = 0; i < IM; ++i)
+            for (int i = 0; i < 8; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[0][i], b[1][j], acc[i][j], 0, 0, 0);
                     acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[1][i], b[0][j], acc[i][j], 0, 0, 0);
                     acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[0][i], b[0][j], acc[i][j], 0, 0, 0);
                 }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-#pragma unroll
-                for (int i = 0; i < IM; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[e][i], b[e][j], acc[i][j], 0, 0, 0);
         }
     }
-}
+};
+
+// One part: a ring of four units in LDS.  A unit is asked for three before it is multiplied and has arrived one before, so that its
+// first fragments are read beside the last products of the unit before it: behind the barrier the products go on at once.
+template <>
+struct Product<1> {
+    static constexpr int PAGES = 4, RING = 4, LDS = RING * PAGES * PAGE * 16;
+    static __device__ __forceinline__ void run(const Operand &A, const Operand &B, int64_t ablk, int64_t bblk, int steps, u32x4 *lds,
+                                               f32x4 (&acc)[8][4])
+    {
+        const int tid = threadIdx.x, lane = tid & 63;
+        const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        const u32x4 *a0 = A.pages + (ablk * A.block + A.first) * PAGE, *b0 = B.pages + (bblk * B.block + B.first) * PAGE;
+        const int units = 2 * steps;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        auto copy_page = [&](const u32x4 *src, u32x4 *dst) {
+            const __amdgpu_buffer_rsrc_t page = __builtin_amdgcn_make_buffer_rsrc((void *)src, 0, PAGE * 16, 0x00020000);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(page, (__attribute__((address_space(3))) void *)(dst + wave * 64), 16, tid * 16, 0, 0, 0);
+        };
+        auto copy_unit = [&](int t) { // four copies a wave: the counts below rely on it
+            u32x4 *dst = lds + (t & (RING - 1)) * PAGES * PAGE;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                copy_page(a0 + (b * A.block + t) * PAGE, dst + b * PAGE);
+                copy_page(b0 + (b * B.block + t) * PAGE, dst + (2 + b) * PAGE);
+            }
+        };
+        const int aoff = (wave >> 2) * PAGE + lane, boff = (2 + ((wave >> 1) & 1)) * PAGE + (wave & 1) * 4 * 64 + lane;
+        half8 a[8], b[2][4];
+        auto read_a = [&](int t, int i) { a[i] = __builtin_bit_cast(half8, lds[(t & (RING - 1)) * PAGES * PAGE + aoff + i * 64]); };
+        auto first = [&](int t, int par) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b[par][j] = __builtin_bit_cast(half8, lds[(t & (RING - 1)) * PAGES * PAGE + boff + j * 64]);
+            read_a(t, 0);
+            read_a(t, 1);
+        };
+        copy_unit(0);
+        copy_unit(1);
+        if (units > 2) {
+            copy_unit(2);
+            asm volatile("s_waitcnt vmcnt(8)\n\ts_barrier" ::: "memory");
+        } else {
+            asm volatile("s_waitcnt vmcnt(4)\n\ts_barrier" ::: "memory");
+        }
+        first(0, 0);
+        auto unit = [&](int t, auto PAR) {
+            constexpr int par = decltype(PAR)::value;
+            // unit t + 1 has arrived (t + 2 may be under way); everyone is done with unit t - 1
+            if (t + 2 < units)
+                asm volatile("s_waitcnt vmcnt(4)\n\ts_barrier" ::: "memory");
+            else
+                asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+            if (t + 3 < units) copy_unit(t + 3);
+#pragma unroll
+            for (int i = 2; i < 8; ++i) read_a(t, i);
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[i], b[par][j], acc[i][j], 0, 0, 0);
+                if (i == 4) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    first(t + 1, par ^ 1); // (behind the last unit: what lies there, not used)
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            __builtin_amdgcn_s_setprio(0);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        for (int t = 0; t < units; t += 2) {
+            unit(t, std::integral_constant<int, 0>{});
+            unit(t + 1, std::integral_constant<int, 1>{});
+        }
+    }
+};
 
 // The tile of a workgroup: workgroups go to the eight dies in turn, so each die is given a run of neighbouring tiles, within
 // which eight tiles of B by a few of A share their pages in the die's L2.
@@ -369,7 +440,7 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_stats(LogitArgs a)
     int mt, nt;
     tile_of(blockIdx.x, a.mt, a.nt, &mt, &nt);
     f32x4 acc[8][4];
-    product<NP, 2>(a.A, a.B, mt * 2, nt * 2, a.steps, lds, acc);
+    Product<NP>::run(a.A, a.B, mt * 2, nt * 2, a.steps, lds, acc);
     const int m0 = mt * TILE + (wave >> 2) * 128, n0 = nt * TILE + (wave & 3) * 64;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -580,7 +651,7 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_p(LogitArgs a)
     int mt, nt;
     tile_of(blockIdx.x, a.mt, a.nt, &mt, &nt);
     f32x4 acc[8][4];
-    product<NP, 2>(a.A, a.B, mt * 2, nt * 2, a.steps, lds, acc);
+    Product<NP>::run(a.A, a.B, mt * 2, nt * 2, a.steps, lds, acc);
     const int m0 = mt * TILE + (wave >> 2) * 128, n0 = nt * TILE + (wave & 3) * 64; // (within the piece)
     f32x4 row[4];
     int rel[4];
@@ -677,7 +748,7 @@ struct GradOut {
 
 // Both gradients of a piece in one launch, the one with the longer sums first: a piece's tiles are too few to fill
 // the chip twice over.
-template <typename T, int NP, int MB>
+template <typename T, int NP>
 __global__ __launch_bounds__(LNT, 2) void k_loss_grads(GradOut first, GradOut second, int nfirst)
 {
     extern __shared__ u32x4 lds[];
@@ -692,9 +763,9 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_grads(GradOut first, GradOut se
     Operand A = a.A, B = a.B;
     A.first += 2 * (int64_t)split * a.per;
     B.first += 2 * (int64_t)split * a.per;
-    f32x4 acc[4 * MB][4];
-    product<NP, MB>(A, B, (int64_t)mt * MB, (int64_t)nt * 2, min(a.per, a.steps - split * a.per), lds, acc);
-    const int m0 = mt * 128 * MB + (wave >> 2) * 64 * MB + 4 * g, n0 = nt * TILE + (wave & 3) * 64 + (a.permuted ? 4 * (l & 3) + (l >> 2) : l);
+    f32x4 acc[8][4];
+    Product<NP>::run(A, B, (int64_t)mt * 2, (int64_t)nt * 2, min(a.per, a.steps - split * a.per), lds, acc);
+    const int m0 = mt * TILE + (wave >> 2) * 128 + 4 * g, n0 = nt * TILE + (wave & 3) * 64 + (a.permuted ? 4 * (l & 3) + (l >> 2) : l);
     const float f = a.mode == 0 ? grad_factor<T>(a.absmax, a.gmax, a.scale) : 1.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -702,7 +773,7 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_grads(GradOut first, GradOut se
         if (n >= a.rows) continue;
         const float w = !a.weight ? f : a.lab[n] < 0 ? 0.f : a.weight[n] * f;
 #pragma unroll
-        for (int i = 0; i < 4 * MB; ++i) {
+        for (int i = 0; i < 8; ++i) {
             const int m = m0 + 16 * i;
             if (m >= a.d) continue;
             const int64_t at = (int64_t)n * a.d + m;
@@ -864,7 +935,7 @@ static LossPlan loss_plan(int dtype, int64_t n, int d, int k, bool backward, voi
         take(p.mine, p.rpad);
         take(p.part, p.kpad / 128 * p.rpad);
     } else {
-        const int mb = p.dblocks == 1 ? 1 : 2, mt = p.dblocks / mb;
+        const int mt = p.dblocks / 2;
         take(p.gn, p.npad);
         take(p.xcols, p.npad / 32 * p.dblocks * page);
         take(p.ccols, p.kpad / 32 * p.dblocks * page);
@@ -915,8 +986,6 @@ static hipError_t allow_lds(K kern, size_t bytes)
         const hipError_t e_ = (e);               \
         if (e_ != hipSuccess) return (int)e_;    \
     } while (0)
-
-static size_t lds_bytes(int mb) { return (size_t)2 * (2 * mb + 4) * PAGE * 16; }
 
 template <typename T>
 static bool rows_vec(const void *p, int d)
@@ -1015,19 +1084,19 @@ static int loss_forward(const LossArgs &a, hipStream_t st)
     if (a.n <= FEW_ROWS) return loss_few<T>(a, st);
     const LossPlan p = loss_plan(a.dtype, a.n, a.d, a.k, false, a.ws);
     loss_images<T, NP>(a, p, false, st);
-    LOSS_TRY(allow_lds(k_loss_stats<NP>, lds_bytes(2)));
+    LOSS_TRY(allow_lds(k_loss_stats<NP>, Product<NP>::LDS));
     for (int64_t r0 = 0; r0 < a.n; r0 += p.rows) {
         const int64_t rows = a.n - r0 < p.rows ? a.n - r0 : p.rows, rpad = pad_to(rows, TILE);
         LogitArgs g = logit_args<NP>(p, r0, rpad, 0, p.kpad);
         g.part = p.part;
         g.mine = p.mine;
-        hipLaunchKernelGGL(k_loss_stats<NP>, dim3((unsigned)(g.mt * g.nt)), dim3(LNT), lds_bytes(2), st, g);
+        hipLaunchKernelGGL(k_loss_stats<NP>, dim3((unsigned)(g.mt * g.nt)), dim3(LNT), Product<NP>::LDS, st, g);
         launch_merge(p.part, g.mt * 2, g.npad, p.mine, g.lab, a.k, rows, a.stats + 2 * r0, a.loss ? a.loss + r0 : nullptr, st);
     }
     return (int)hipGetLastError();
 }
 
-template <typename T, int NP, int MB>
+template <typename T, int NP>
 static int loss_backward(const LossArgs &a, hipStream_t st)
 {
     if (a.n == 0) {
@@ -1075,9 +1144,9 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
                                p.hdr + 2, false, a.dbias);
         return (int)hipGetLastError();
     }
-    LOSS_TRY(allow_lds(k_loss_p<NP>, lds_bytes(2)));
-    LOSS_TRY(allow_lds(k_loss_grads<T, NP, MB>, lds_bytes(MB)));
-    const int mt = p.dblocks / MB;
+    LOSS_TRY(allow_lds(k_loss_p<NP>, Product<NP>::LDS));
+    LOSS_TRY(allow_lds(k_loss_grads<T, NP>, Product<NP>::LDS));
+    const int mt = p.dblocks / 2;
     const bool vec = a.d % 4 == 0;
     for (int64_t r0 = 0; r0 < a.n; r0 += p.rows) {
         const int64_t rows = a.n - r0 < p.rows ? a.n - r0 : p.rows, rpad = pad_to(rows, TILE);
@@ -1090,7 +1159,7 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
             g.jblock = (int)(cpad / 32 * NP);
             g.iblock = (int)(rpad / 32 * NP);
             g.dbpart = a.dbias ? p.dbpart : nullptr;
-            hipLaunchKernelGGL(k_loss_p<NP>, dim3((unsigned)(g.mt * g.nt)), dim3(LNT), lds_bytes(2), st, g);
+            hipLaunchKernelGGL(k_loss_p<NP>, dim3((unsigned)(g.mt * g.nt)), dim3(LNT), Product<NP>::LDS, st, g);
             if (a.dbias) {
                 const int count = (int)(a.k - c0 < cpad ? a.k - c0 : cpad);
                 hipLaunchKernelGGL(k_loss_dbias, dim3((unsigned)((count + 63) / 64)), dim3(256), 0, st, p.dbpart, (int)(rpad / 64),
@@ -1139,9 +1208,9 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
             const int nx = x.mt * x.nt * x.splits, nc = c.mt * c.nt * c.splits;
             if (nx + nc == 0) continue;
             if (c.per > x.per)
-                hipLaunchKernelGGL((k_loss_grads<T, NP, MB>), dim3((unsigned)(nx + nc)), dim3(LNT), lds_bytes(MB), st, c, x, nc);
+                hipLaunchKernelGGL((k_loss_grads<T, NP>), dim3((unsigned)(nx + nc)), dim3(LNT), Product<NP>::LDS, st, c, x, nc);
             else
-                hipLaunchKernelGGL((k_loss_grads<T, NP, MB>), dim3((unsigned)(nx + nc)), dim3(LNT), lds_bytes(MB), st, x, c, nx);
+                hipLaunchKernelGGL((k_loss_grads<T, NP>), dim3((unsigned)(nx + nc)), dim3(LNT), Product<NP>::LDS, st, x, c, nx);
         }
     }
     finish();
@@ -1159,10 +1228,9 @@ int launch_softmax_loss(const LossArgs &a, hipStream_t st)
 
 int launch_softmax_loss_backward(const LossArgs &a, hipStream_t st)
 {
-    const bool wide = a.d > 128;
     switch (a.dtype) {
-    case VLQ_F32: return wide ? loss_backward<float, 2, 2>(a, st) : loss_backward<float, 2, 1>(a, st);
-    case VLQ_F16: return wide ? loss_backward<_Float16, 1, 2>(a, st) : loss_backward<_Float16, 1, 1>(a, st);
-    default: return wide ? loss_backward<bf16_t, 1, 2>(a, st) : loss_backward<bf16_t, 1, 1>(a, st);
+    case VLQ_F32: return loss_backward<float, 2>(a, st);
+    case VLQ_F16: return loss_backward<_Float16, 1>(a, st);
+    default: return loss_backward<bf16_t, 1>(a, st);
     }
 }
