@@ -26,7 +26,7 @@
 
 #define LNT 512              // threads of the product kernels
 #define LOSS_ROWS 8192       // rows that go through the products together
-#define PIECE (1 << 25)      // values of P kept at a time
+#define PIECE (1 << 26)      // values of P kept at a time
 #define NARROW_DIM 128       // up to so many dimensions the gradients take the narrow form (softmax_loss_narrow.hip)
 #define NARROW_GROUPS 1024   // its workgroups, about: two rounds of two a compute unit
 #define NARROW_LEAST 8       // tiles of 32 rows that a workgroup of it takes at least
@@ -77,6 +77,7 @@ __device__ __forceinline__ void pack_rows(int block, const T *__restrict__ X, in
         float mx = 0.f;
         if (r0 + r < rows && row_counts(label, k, bias, r0 + r)) {
             const T *row = X + (r0 + r) * d;
+#pragma unroll 4
             for (int i = (tid & 15) * 8; i < d; i += 128) {
                 float v[8];
                 load8(row, i, d, vec, v);
@@ -112,7 +113,7 @@ __device__ __forceinline__ void pack_rows(int block, const T *__restrict__ X, in
     const T *row = X + (counts ? r0 + l : 0) * d;
     const float s = pow2i(ex);
     u32x4 *to = pages + (int64_t)(block >> 3) * units * NP * PAGE + (block & 7) * 64 + lane;
-#pragma unroll 2
+#pragma unroll 4
     for (int u = wave; u < units; u += 4) {
         float v[8] = {};
         if (counts) load8(row, u * 32 + (lane >> 4) * 8, d, vec, v);
@@ -220,7 +221,7 @@ __global__ __launch_bounds__(256) void k_pack_rows(PackArgs a)
 {
     int b = blockIdx.x;
     if (b < a.xblocks) {
-        pack_rows<T, true, NP>(b, (const T *)a.x, a.n, a.d, a.units, a.label, a.k, nullptr, a.ximg, a.rinv, a.hdr, a.xvec);
+        pack_rows<T, true, NP>(b, (const T *)a.x, a.n, a.d, a.units, a.label, a.k, nullptr, a.ximg, a.rinv, a.stats ? a.hdr : nullptr, a.xvec);
         if (a.stats) return;
         __syncthreads();
         if (threadIdx.x < 16) row_numbers(a, (int64_t)b * 16 + threadIdx.x, a.rinv[(int64_t)b * 16 + threadIdx.x]);
@@ -228,7 +229,7 @@ __global__ __launch_bounds__(256) void k_pack_rows(PackArgs a)
     }
     b -= a.xblocks;
     if (b < a.cblocks)
-        pack_rows<T, false, NP>(b, (const T *)a.c, a.k, a.d, a.units, nullptr, a.k, a.bias, a.cimg, a.cinv, a.hdr + 1, a.cvec);
+        pack_rows<T, false, NP>(b, (const T *)a.c, a.k, a.d, a.units, nullptr, a.k, a.bias, a.cimg, a.cinv, a.stats ? a.hdr + 1 : nullptr, a.cvec);
     else
         grad_max(b - a.cblocks, a.others, a.g, a.label, a.k, a.n, a.hdr + 2);
 }
@@ -261,142 +262,105 @@ struct Operand {
     int64_t first;
 };
 
-// acc = A B^T over `steps` steps of two pages of every block: two units of 32 indices (NP = 1), or both parts of one (NP = 2).
+// acc = A B^T over `units` units of 32 indices, NP pages of every block each.
 // A tile of two blocks of A by two of B; eight waves, 2 x 4, of 128 rows of A x 64 of B each.  A lane's acc[i][j][r] is row
 // 16 i + 4 (lane / 16) + r, column 16 j + lane % 16 of its wave's part.
+//
+// A goes through LDS (a ring of four units, asked for three ahead, there one ahead), the fragments of B straight to registers:
+// through LDS as well its 128 bytes a clock were the bound.  Between two barriers a wave has one unit; its memory
+// operations are spread between the products of its fragments, and the first fragments of A are read a unit ahead, so that the products go on
+// behind the barrier at once.  8 192 x 8 192 x 2 048, one part, on random operands: 1.46 PFLOP/s, x 8 192: 1.51 (both operands
+// through LDS, copies asked for together: 1.10 and 1.42; products from registers alone: 1.75 and 1.92).
 template <int NP>
-struct Product;
+struct Product {
+    static constexpr int RING = 4, AHEAD = 3, PAGES = 2 * NP; // pages of A of a unit
+    static constexpr int BAHEAD = NP == 1 ? 3 : 1, NB = BAHEAD + 1; // units that B's fragments are asked for ahead (a unit of two parts takes three times as long)
+    static constexpr int ROUND = 6 * NP;                      // memory operations of a wave and unit
+    static constexpr int LDS = RING * PAGES * PAGE * 16;
+    static_assert(RING > AHEAD, "a unit takes the place of the one before the present");
 
-// Two parts: two buffers of a step in LDS; while one is multiplied the next is copied from memory to the other.
-template <>
-struct Product<2> {
-    static constexpr int PAGES = 8, LDS = 2 * PAGES * PAGE * 16;
-    static __device__ __forceinline__ void run(const Operand &A, const Operand &B, int64_t ablk, int64_t bblk, int steps, u32x4 *lds,
+    static __device__ __forceinline__ void run(const Operand &A, const Operand &B, int64_t ablk, int64_t bblk, int units, u32x4 *lds,
                                                f32x4 (&acc)[8][4])
     {
         const int tid = threadIdx.x, lane = tid & 63;
         const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-        const u32x4 *a0 = A.pages + (ablk * A.block + A.first) * PAGE, *b0 = B.pages + (bblk * B.block + B.first) * PAGE;
+        const u32x4 *a0 = A.pages + (ablk * A.block + A.first) * PAGE;
+        const u32x4 *b0 = B.pages + ((bblk + ((wave >> 1) & 1)) * B.block + B.first) * PAGE + (wave & 1) * 4 * 64 + lane;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        auto copy_page = [&](const u32x4 *src, u32x4 *dst) {
+        // page q of unit t (behind the last: of the last, not used); the place in LDS is that of t all the same
+        auto copy_page = [&](int t, int q) {
+            u32x4 *dst = lds + ((t & (RING - 1)) * PAGES + q) * PAGE + wave * 64;
+            const u32x4 *src = a0 + ((q / NP) * A.block + (int64_t)min(t, units - 1) * NP + q % NP) * PAGE;
             const __amdgpu_buffer_rsrc_t page = __builtin_amdgcn_make_buffer_rsrc((void *)src, 0, PAGE * 16, 0x00020000);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(page, (__attribute__((address_space(3))) void *)(dst + wave * 64), 16, tid * 16, 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(page, (__attribute__((address_space(3))) void *)dst, 16, tid * 16, 0, 0, 0);
         };
-        auto copy_step = [&](int t) {
-            u32x4 *dst = lds + (t & 1) * PAGES * PAGE;
+        half8 a[8][NP];
+        u32x4 b[NB][NP][4];
+        auto read_a = [&](int t, int i) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
-#pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    copy_page(a0 + (b * A.block + 2 * t + e) * PAGE, dst + (b * 2 + e) * PAGE);
-                    copy_page(b0 + (b * B.block + 2 * t + e) * PAGE, dst + (4 + b * 2 + e) * PAGE);
-                }
+            for (int p = 0; p < NP; ++p)
+                a[i][p] = __builtin_bit_cast(half8, lds[((t & (RING - 1)) * PAGES + (wave >> 2) * NP + p) * PAGE + i * 64 + lane]);
         };
-        const int aoff = (wave >> 2) * 2 * PAGE, boff = (4 + ((wave >> 1) & 1) * 2) * PAGE + (wave & 1) * 4 * 64;
-        copy_step(0);
-        for (int t = 0; t < steps; ++t) {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __syncthreads(); // (this step has arrived, and nobody reads the other buffer any more)
-            if (t + 1 < steps) copy_step(t + 1);
-            const u32x4 *st = lds + (t & 1) * PAGES * PAGE + lane;
-            half8 a[2][8], b[2][4];
+        auto load_b = [&](int t, int slot, int q) { b[slot][q / 4][q % 4] = b0[((int64_t)min(t, units - 1) * NP + q / 4) * PAGE + q % 4 * 64]; };
+        // a wave's memory operations come in rounds, round t: B of unit t + BAHEAD, then A of unit t + AHEAD
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
+        for (int t = -AHEAD; t < 0; ++t) {
+            if (t + BAHEAD >= 0)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) b[e][j] = __builtin_bit_cast(half8, st[boff + e * PAGE + j * 64]);
+                for (int q = 0; q < 4 * NP; ++q) load_b(t + BAHEAD, t + BAHEAD, q);
+            asm volatile("" ::: "memory");
 #pragma unroll
-                for (int i = 0; i < 8; ++i) a[e][i] = __builtin_bit_cast(half8, st[aoff + e * PAGE + i * 64]);
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[0][i], b[1][j], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[1][i], b[0][j], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[0][i], b[0][j], acc[i][j], 0, 0, 0);
-                }
+            for (int q = 0; q < PAGES; ++q) copy_page(t + AHEAD, q);
+            asm volatile("" ::: "memory");
         }
-    }
-};
-
-// One part: a ring of four units in LDS.  A unit is asked for three before it is multiplied and has arrived one before, so that its
-// first fragments are read beside the last products of the unit before it: behind the barrier the products go on at once.
-template <>
-struct Product<1> {
-    static constexpr int PAGES = 4, RING = 4, LDS = RING * PAGES * PAGE * 16;
-    static __device__ __forceinline__ void run(const Operand &A, const Operand &B, int64_t ablk, int64_t bblk, int steps, u32x4 *lds,
-                                               f32x4 (&acc)[8][4])
-    {
-        const int tid = threadIdx.x, lane = tid & 63;
-        const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-        const u32x4 *a0 = A.pages + (ablk * A.block + A.first) * PAGE, *b0 = B.pages + (bblk * B.block + B.first) * PAGE;
-        const int units = 2 * steps;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        auto copy_page = [&](const u32x4 *src, u32x4 *dst) {
-            const __amdgpu_buffer_rsrc_t page = __builtin_amdgcn_make_buffer_rsrc((void *)src, 0, PAGE * 16, 0x00020000);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(page, (__attribute__((address_space(3))) void *)(dst + wave * 64), 16, tid * 16, 0, 0, 0);
-        };
-        auto copy_unit = [&](int t) { // four copies a wave: the counts below rely on it
-            u32x4 *dst = lds + (t & (RING - 1)) * PAGES * PAGE;
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                copy_page(a0 + (b * A.block + t) * PAGE, dst + b * PAGE);
-                copy_page(b0 + (b * B.block + t) * PAGE, dst + (2 + b) * PAGE);
-            }
-        };
-        const int aoff = (wave >> 2) * PAGE + lane, boff = (2 + ((wave >> 1) & 1)) * PAGE + (wave & 1) * 4 * 64 + lane;
-        half8 a[8], b[2][4];
-        auto read_a = [&](int t, int i) { a[i] = __builtin_bit_cast(half8, lds[(t & (RING - 1)) * PAGES * PAGE + aoff + i * 64]); };
-        auto first = [&](int t, int par) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) b[par][j] = __builtin_bit_cast(half8, lds[(t & (RING - 1)) * PAGES * PAGE + boff + j * 64]);
-            read_a(t, 0);
-            read_a(t, 1);
-        };
-        copy_unit(0);
-        copy_unit(1);
-        if (units > 2) {
-            copy_unit(2);
-            asm volatile("s_waitcnt vmcnt(8)\n\ts_barrier" ::: "memory");
-        } else {
-            asm volatile("s_waitcnt vmcnt(4)\n\ts_barrier" ::: "memory");
-        }
-        first(0, 0);
-        auto unit = [&](int t, auto PAR) {
-            constexpr int par = decltype(PAR)::value;
-            // unit t + 1 has arrived (t + 2 may be under way); everyone is done with unit t - 1
-            if (t + 2 < units)
-                asm volatile("s_waitcnt vmcnt(4)\n\ts_barrier" ::: "memory");
-            else
-                asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-            if (t + 3 < units) copy_unit(t + 3);
-#pragma unroll
-            for (int i = 2; i < 8; ++i) read_a(t, i);
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((BAHEAD == 3 ? 2 * ROUND : PAGES + ROUND)) : "memory");
+        read_a(0, 0);
+        read_a(0, 1);
+        auto unit = [&](int t, auto SLOT) {
+            constexpr int slot = decltype(SLOT)::value;
+            // A of unit t + 1 has arrived: it came with round t - 2; everyone is done with unit t - 1
+            asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(ROUND) : "memory");
+            read_a(t, 2);
+            read_a(t, 3);
             __builtin_amdgcn_sched_barrier(0);
-            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
+                if (NP == 2)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[i], b[par][j], acc[i][j], 0, 0, 0);
-                if (i == 4) {
-                    __builtin_amdgcn_sched_barrier(0);
-                    first(t + 1, par ^ 1); // (behind the last unit: what lies there, not used)
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+                    for (int j = 0; j < 4; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[i][0], __builtin_bit_cast(half8, b[slot][NP - 1][j]), acc[i][j], 0, 0, 0);
+                if (NP == 2)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[i][NP - 1], __builtin_bit_cast(half8, b[slot][0][j]), acc[i][j], 0, 0, 0);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[i][0], __builtin_bit_cast(half8, b[slot][0][j]), acc[i][j], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+                if (i < 4)
+#pragma unroll
+                    for (int q = 0; q < NP; ++q) load_b(t + BAHEAD, (slot + BAHEAD) % NB, i * NP + q);
+                else if (i - 4 < PAGES)
+                    copy_page(t + AHEAD, i - 4);
+                if (i < 4) read_a(t, i + 4);
+                if (i == 4) read_a(t + 1, 0);
+                if (i == 5) read_a(t + 1, 1);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            __builtin_amdgcn_s_setprio(0);
-            __builtin_amdgcn_sched_barrier(0);
         };
-        for (int t = 0; t < units; t += 2) {
-            unit(t, std::integral_constant<int, 0>{});
-            unit(t + 1, std::integral_constant<int, 1>{});
+        for (int t = 0; t < units; t += NB) {
+#define LOSS_UNIT(s) \
+    if (s < NB && (s == 0 || t + s < units)) unit(t + s, std::integral_constant<int, s % NB>{})
+            LOSS_UNIT(0);
+            LOSS_UNIT(1);
+            LOSS_UNIT(2);
+            LOSS_UNIT(3);
+#undef LOSS_UNIT
         }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); // (what was asked for behind the last unit)
     }
 };
 
@@ -416,7 +380,7 @@ struct LogitArgs {
     const float *cinv, *bias2;
     const f32x4 *row;
     const int32_t *lab;
-    int steps, mt, nt;
+    int units, mt, nt;
     int npad;
     int m_first; // first centroid of the piece
     // forward
@@ -440,7 +404,7 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_stats(LogitArgs a)
     int mt, nt;
     tile_of(blockIdx.x, a.mt, a.nt, &mt, &nt);
     f32x4 acc[8][4];
-    Product<NP>::run(a.A, a.B, mt * 2, nt * 2, a.steps, lds, acc);
+    Product<NP>::run(a.A, a.B, mt * 2, nt * 2, a.units, lds, acc);
     const int m0 = mt * TILE + (wave >> 2) * 128, n0 = nt * TILE + (wave & 3) * 64;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -651,7 +615,7 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_p(LogitArgs a)
     int mt, nt;
     tile_of(blockIdx.x, a.mt, a.nt, &mt, &nt);
     f32x4 acc[8][4];
-    Product<NP>::run(a.A, a.B, mt * 2, nt * 2, a.steps, lds, acc);
+    Product<NP>::run(a.A, a.B, mt * 2, nt * 2, a.units, lds, acc);
     const int m0 = mt * TILE + (wave >> 2) * 128, n0 = nt * TILE + (wave & 3) * 64; // (within the piece)
     f32x4 row[4];
     int rel[4];
@@ -733,7 +697,7 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_p(LogitArgs a)
 // One gradient: out[row][dim] = factor sum over the index of A[dim] B[row]
 struct GradOut {
     Operand A, B; // columns' image (rows: dimensions), P's image
-    int steps, mt, nt, splits, per; // steps of the sum, tiles, and parts that the sum is cut into, `per` steps each
+    int units, mt, nt, splits, per; // units of the sum, tiles, and parts that the sum is cut into, `per` units each
     int rows, d;
     bool permuted; // rows of B in the order 4 r + g
     int mode;      // 0: typed, times the factor; 1: fp32 slabs, stored; 2: added to what is there
@@ -761,10 +725,10 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_grads(GradOut first, GradOut se
     int mt, nt;
     tile_of(b - split * tiles, a.mt, a.nt, &mt, &nt);
     Operand A = a.A, B = a.B;
-    A.first += 2 * (int64_t)split * a.per;
-    B.first += 2 * (int64_t)split * a.per;
+    A.first += (int64_t)split * a.per * NP;
+    B.first += (int64_t)split * a.per * NP;
     f32x4 acc[8][4];
-    Product<NP>::run(A, B, (int64_t)mt * 2, (int64_t)nt * 2, min(a.per, a.steps - split * a.per), lds, acc);
+    Product<NP>::run(A, B, (int64_t)mt * 2, (int64_t)nt * 2, min(a.per, a.units - split * a.per), lds, acc);
     const int m0 = mt * TILE + (wave >> 2) * 128 + 4 * g, n0 = nt * TILE + (wave & 3) * 64 + (a.permuted ? 4 * (l & 3) + (l >> 2) : l);
     const float f = a.mode == 0 ? grad_factor<T>(a.absmax, a.gmax, a.scale) : 1.f;
 #pragma unroll
@@ -877,16 +841,16 @@ struct LossPlan {
     size_t bytes;
 };
 
-// Parts of a sum over `steps` steps, so that `tiles` of them fill the chip: each at least four steps long, and the slabs
+// Parts of a sum over `units` units, so that `tiles` of them fill the chip: each at least eight units long, and the slabs
 // together no larger than 256 MB.
-static int sum_parts(int64_t tiles, int64_t steps, int64_t out_bytes)
+static int sum_parts(int64_t tiles, int64_t units, int64_t out_bytes)
 {
     int64_t s = 256 / (tiles < 1 ? 1 : tiles);
-    if (s > steps / 4) s = steps / 4;
+    if (s > units / 8) s = units / 8;
     if (s * out_bytes > (256ll << 20)) s = (256ll << 20) / out_bytes;
     if (s <= 1) return 1;
-    const int64_t per = (steps + s - 1) / s;
-    return (int)((steps + per - 1) / per); // (no part is empty)
+    const int64_t per = (units + s - 1) / s;
+    return (int)((units + per - 1) / per); // (no part is empty)
 }
 
 // The narrow form: parts of about `per` tiles of 32, fewer where their slabs would take more than 256 MB
@@ -909,7 +873,7 @@ static LossPlan loss_plan(int dtype, int64_t n, int d, int k, bool backward, voi
     p.npad = pad_to(n, TILE);
     p.kpad = pad_to(k, TILE);
     p.d = d;
-    p.units = p.np == 2 ? (d + 31) / 32 : (d + 63) / 64 * 2;
+    p.units = (d + 31) / 32;
     p.dblocks = d <= 128 ? 1 : (int)(pad_to(d, 256) / 128);
     p.rows = n < LOSS_ROWS ? n : LOSS_ROWS;
     p.rpad = pad_to(p.rows, TILE);
@@ -957,9 +921,8 @@ static LossPlan loss_plan(int dtype, int64_t n, int d, int k, bool backward, voi
         take(p.pj, p.rpad * p.piece / 8 * p.np);
         take(p.pi, p.rpad * p.piece / 8 * p.np);
         take(p.dbpart, p.rpad / 64 * p.piece);
-        const int64_t many = p.np; // steps per unit pair: two units a step with one part, one with two
-        p.xsplit = sum_parts(p.rpad / TILE * mt, p.piece / 64 * many, n * d * 4);
-        p.csplit = sum_parts(p.piece / TILE * mt, p.rpad / 64 * many, (int64_t)k * d * 4);
+        p.xsplit = sum_parts(p.rpad / TILE * mt, p.piece / 32, n * d * 4);
+        p.csplit = sum_parts(p.piece / TILE * mt, p.rpad / 32, (int64_t)k * d * 4);
         p.xslab = p.xsplit > 1 || p.kpad > p.piece;
         p.cslab = p.csplit > 1 || n > p.rows;
         take(p.xsum, p.xslab ? (size_t)p.xsplit * n * d : 0);
@@ -1028,7 +991,7 @@ static LogitArgs logit_args(const LossPlan &p, int64_t r0, int64_t rpad, int64_t
     g.bias2 = p.bias2 + c0;
     g.row = p.row + r0;
     g.lab = p.lab + r0;
-    g.steps = p.units * NP / 2;
+    g.units = p.units;
     g.mt = (int)(cpad / TILE);
     g.nt = (int)(rpad / TILE);
     g.npad = (int)rpad;
@@ -1169,12 +1132,12 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
             if (a.dx) {
                 x.A = {p.ccols, p.kpad / 32 * NP, c0 / 32 * NP};
                 x.B = {p.pj, g.jblock, 0};
-                x.steps = g.jblock / 2;
+                x.units = g.jblock / NP;
                 x.mt = mt;
                 x.nt = g.nt;
                 x.splits = p.xsplit;
-                x.per = (x.steps + p.xsplit - 1) / p.xsplit;
-                x.splits = (x.steps + x.per - 1) / x.per; // (a shorter last piece may need fewer: its other slabs stay as they are)
+                x.per = (x.units + p.xsplit - 1) / p.xsplit;
+                x.splits = (x.units + x.per - 1) / x.per; // (a shorter last piece may need fewer: its other slabs stay as they are)
                 x.rows = (int)rows;
                 x.mode = p.xslab ? (c0 > 0 ? 2 : 1) : 0;
                 x.out = p.xslab ? (void *)(p.xsum + r0 * a.d) : (void *)((T *)a.dx + r0 * a.d);
@@ -1188,12 +1151,12 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
                 const int64_t cols = a.k - c0 < cpad ? a.k - c0 : cpad;
                 c.A = {p.xcols, p.npad / 32 * NP, r0 / 32 * NP};
                 c.B = {p.pi, g.iblock, 0};
-                c.steps = g.iblock / 2;
+                c.units = g.iblock / NP;
                 c.mt = mt;
                 c.nt = g.mt;
                 c.splits = p.csplit;
-                c.per = (c.steps + p.csplit - 1) / p.csplit;
-                c.splits = (c.steps + c.per - 1) / c.per;
+                c.per = (c.units + p.csplit - 1) / p.csplit;
+                c.splits = (c.units + c.per - 1) / c.per;
                 c.permuted = true;
                 c.rows = (int)cols;
                 c.mode = p.cslab ? (r0 > 0 ? 2 : 1) : 0;
