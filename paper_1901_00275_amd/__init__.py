@@ -36,6 +36,7 @@ class vlq_params_t(C.Structure):
 
 
 _lib = None
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def lib():
@@ -112,6 +113,8 @@ def _ptr(t, dtype=None):
 
 
 def _stream(stream):
+    if stream is None and _raw_stream is not None:  # (the stream's handle without an object for it: 0.2 instead of 2.8 us)
+        return C.c_void_p(_raw_stream(torch.cuda.current_device()))
     s = torch.cuda.current_stream() if stream is None else stream
     return C.c_void_p(s.cuda_stream)
 
@@ -329,13 +332,20 @@ def vlq_clip_grads_workspace(grads) -> int:
 def vlq_clip_grads(d_grads, max_norm, d_out, d_norm, d_ws, stream=None):
     """d_grads: a list of tensors; d_out: a list as long (its tensors may be those of d_grads), or None for the norm alone."""
     n = len(d_grads)
-    if d_out is not None and (len(d_out) != n or any(o.numel() != g.numel() for o, g in zip(d_out, d_grads))):
-        raise ValueError("d_out must have a tensor of the same size for every tensor of d_grads")
-    ptrs = _ptrs(*[(g, None, 0) for g in d_grads])
-    outs = None if d_out is None else _ptrs(*[(o, g.dtype, 0) for o, g in zip(d_out, d_grads)])
-    norm, ws = _ptrs((d_norm, torch.float32, 1), (d_ws, torch.uint8, 0))
     many = max(1, n)
-    counts = (C.c_int64 * many)(*[g.numel() for g in d_grads])
-    dtypes = (C.c_int32 * many)(*[_type(g) for g in d_grads])
-    _chk(lib().vlq_clip_grads(n, dtypes, counts, (C.c_void_p * many)(*ptrs), float(max_norm),
-                              None if outs is None else (C.c_void_p * many)(*outs), norm, ws, d_ws.numel(), _stream(stream)))
+    counts, dtypes, ptrs = (C.c_int64 * many)(), (C.c_int32 * many)(), (C.c_void_p * many)()
+    outs = None if d_out is None else (C.c_void_p * many)()
+    if d_out is not None and len(d_out) != n:
+        raise ValueError("d_out must have a tensor for every tensor of d_grads")
+    norm, ws = _ptrs((d_norm, torch.float32, 1), (d_ws, torch.uint8, 0))
+    dev = d_ws.get_device()
+    for i, g in enumerate(d_grads):
+        if not g.is_cuda or not g.is_contiguous() or g.get_device() != dev or g.dtype not in _TYPES:
+            raise ValueError("gradients must be contiguous float32, float16 or bfloat16 tensors on the current device")
+        counts[i], dtypes[i], ptrs[i] = g.numel(), _TYPES[g.dtype], g.data_ptr()
+        if outs is not None:
+            o = d_out[i]
+            if o is not g and (not o.is_cuda or not o.is_contiguous() or o.get_device() != dev or o.dtype != g.dtype or o.numel() != counts[i]):
+                raise ValueError("d_out must have a contiguous tensor of the same type, size and device for every tensor of d_grads")
+            outs[i] = o.data_ptr()
+    _chk(lib().vlq_clip_grads(n, dtypes, counts, ptrs, float(max_norm), outs, norm, ws, d_ws.numel(), _stream(stream)))

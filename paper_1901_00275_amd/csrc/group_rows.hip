@@ -289,8 +289,10 @@ int launch_group_rows(const int32_t *cell, int64_t pairs, int cells, int64_t *of
         a.bits = p.bits[0];
         a.last = true;
         const size_t bytes = (size_t)(SMALL_NT / 64 + 1) * (4u << a.bits);
-        const hipError_t e = hipFuncSetAttribute((const void *)k_group_small, hipFuncAttributeMaxDynamicSharedMemorySize, (SMALL_NT / 64 + 1) * BINS * 4);
-        if (e != hipSuccess) return (int)e;
+        if (bytes > 49152) { // (48 KB of dynamic LDS need no asking)
+            const hipError_t e = hipFuncSetAttribute((const void *)k_group_small, hipFuncAttributeMaxDynamicSharedMemorySize, (SMALL_NT / 64 + 1) * BINS * 4);
+            if (e != hipSuccess) return (int)e;
+        }
         hipLaunchKernelGGL(k_group_small, dim3(1), dim3(SMALL_NT), bytes, st, a);
         return (int)hipGetLastError();
     }

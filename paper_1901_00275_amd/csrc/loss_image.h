@@ -57,6 +57,13 @@ __device__ __forceinline__ void split8(const float (&v)[8], half8 (&h)[NP])
     }
 }
 
+// The statistics of two sets of logits together
+__device__ __forceinline__ float2 join(float2 a, float2 b)
+{
+    const float m = fmaxf(a.x, b.x), base = m == -INFINITY ? 0.f : m;
+    return make_float2(m, a.y * __builtin_amdgcn_exp2f(a.x - base) + b.y * __builtin_amdgcn_exp2f(b.x - base));
+}
+
 // Factor of a gradient: the scale of the columns' image, that of P, g's largest magnitude where P was taken relative to it
 template <typename T>
 __device__ __forceinline__ float grad_factor(const uint32_t *absmax, const uint32_t *gmax, float scale)
@@ -105,7 +112,12 @@ struct NarrowArgs {
     float *dbpart; // [splits of c][kpad] or NULL
     int kpad;
     float scale;
+    // forward (the first side alone)
+    float2 *part; // [splits][npad] {maximum, sum}
+    float *mine;  // [npad] the label's logit
+    int npad;
 };
 
 
+int launch_loss_narrow_stats(int dtype, const NarrowArgs &a, hipStream_t st); // 0 or a hipError_t
 int launch_loss_narrow(int dtype, const NarrowArgs &a, hipStream_t st); // 0 or a hipError_t

@@ -36,13 +36,10 @@
 // ---------------------------------------------------------------------------
 // images
 // ---------------------------------------------------------------------------
-// Header of a call: [0] largest magnitude of x's counted rows (bits), [1] of c, [2] of g; and the bias in units of log 2, -inf past
-// the last centroid
-__global__ __launch_bounds__(256) void k_loss_begin(const float *bias, int k, int kpad, float *bias2, uint32_t *hdr)
+// Header of a backward call: [0] largest magnitude of x's counted rows (bits), [1] of c, [2] of g
+__global__ void k_loss_begin(uint32_t *hdr)
 {
-    const int j = blockIdx.x * 256 + threadIdx.x;
-    if (j < 4) hdr[j] = 0;
-    if (j < kpad) bias2[j] = j < k ? (bias ? bias[j] * LOG2E : 0.f) : -INFINITY;
+    if (threadIdx.x < 4) hdr[threadIdx.x] = 0;
 }
 
 // The largest of the callers' values into *to: an atomic only where it is larger than what is there (all of a launch's workgroups
@@ -61,68 +58,77 @@ __device__ __forceinline__ bool row_counts(const int32_t *label, int k, const fl
 }
 
 // Image of the rows of X, 16 rows a workgroup; a scale per row (OWN) or for all 16.  inv: 1 / scale, as many.
-// Bound by memory: X is read twice (the second time from the caches), written once.  (With 128 rows a workgroup and a scale for
-// all of them 128 MB took 99 us, for want of loads under way.)
+// A wave takes every fourth unit, as the lanes lie in its pages; up to PACK_HELD units the values wait in registers for their
+// scale, beyond that they are read again.  Bound by memory.  (With 128 rows a workgroup and a scale for all of them 128 MB took
+// 99 us, for want of loads under way.)
+#define PACK_HELD 16
 template <typename T, bool OWN, int NP>
 __device__ __forceinline__ void pack_rows(int block, const T *__restrict__ X, int64_t rows, int d, int units,
-                                                   const int32_t *__restrict__ label, int k, const float *__restrict__ bias,
-                                                   u32x4 *__restrict__ pages, float *__restrict__ inv, uint32_t *absmax, bool vec)
+                                          const int32_t *__restrict__ label, int k, const float *__restrict__ bias,
+                                          u32x4 *__restrict__ pages, float *__restrict__ inv, uint32_t *absmax, bool vec)
 {
-    __shared__ float rmax[16];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ float rmax[4][16];
+    const int tid = threadIdx.x, lane = tid & 63, l = lane & 15, wave = tid >> 6;
     const int64_t r0 = (int64_t)block * 16;
-    // pass 1: 16 lanes a row
-    if constexpr (!__is_same(T, _Float16)) {
-        const int r = tid >> 4;
-        float mx = 0.f;
-        if (r0 + r < rows && row_counts(label, k, bias, r0 + r)) {
-            const T *row = X + (r0 + r) * d;
-#pragma unroll 4
-            for (int i = (tid & 15) * 8; i < d; i += 128) {
-                float v[8];
-                load8(row, i, d, vec, v);
+    const bool in = r0 + l < rows;
+    const T *row = X + (in ? r0 + l : 0) * d;
+    float v[PACK_HELD / 4][8];
+    auto load = [&](int u0) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float m = fabsf(v[e]);
-                    if (m < INFINITY) mx = fmaxf(mx, m);
-                }
-            }
+        for (int q = 0; q < PACK_HELD / 4; ++q) {
+            const int u = u0 + 4 * q + wave;
+            if (u < units) load8(row, u * 32 + (lane >> 4) * 8, d, vec, v[q]); // (rows past the end: of the first, not used)
         }
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
-        if ((tid & 15) == 0) rmax[r] = mx;
-        __syncthreads();
-    }
-    const int l = lane & 15;
-    float mine = 0.f, all = 0.f; // largest magnitudes of the lane's row, and of the 16
+    };
+    load(0);
+    const bool counts = in && row_counts(label, k, bias, r0 + l);
+    int ex = 0;
     if constexpr (!__is_same(T, _Float16)) {
-        mine = rmax[l];
-        all = mine;
+        float mx = 0.f;
+        for (int u0 = 0; u0 < units; u0 += PACK_HELD) {
+            if (u0 > 0) load(u0);
+#pragma unroll
+            for (int q = 0; q < PACK_HELD / 4; ++q)
+                if (u0 + 4 * q + wave < units)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float m = fabsf(v[q][e]);
+                        if (m < INFINITY) mx = fmaxf(mx, m);
+                    }
+        }
+        if (!counts) mx = 0.f;
+        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        if (lane < 16) rmax[wave][l] = mx;
+        __syncthreads();
+        const float mine = fmaxf(fmaxf(rmax[0][l], rmax[1][l]), fmaxf(rmax[2][l], rmax[3][l])); // of the lane's row
+        float all = mine;
 #pragma unroll
         for (int o = 8; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor(all, o, 64));
         if (tid == 0 && absmax) raise(absmax, all);
+        ex = scale_exponent(OWN ? mine : all);
     }
-    const int ex = __is_same(T, _Float16) ? 0 : scale_exponent(OWN ? mine : all);
     if (tid < 16) {
         if (OWN)
             inv[r0 + tid] = pow2i(-ex);
         else if (tid == 0)
             inv[block] = pow2i(-ex);
     }
-    const bool counts = r0 + l < rows && row_counts(label, k, bias, r0 + l);
-    const T *row = X + (counts ? r0 + l : 0) * d;
     const float s = pow2i(ex);
     u32x4 *to = pages + (int64_t)(block >> 3) * units * NP * PAGE + (block & 7) * 64 + lane;
-#pragma unroll 4
-    for (int u = wave; u < units; u += 4) {
-        float v[8] = {};
-        if (counts) load8(row, u * 32 + (lane >> 4) * 8, d, vec, v);
+    for (int u0 = 0; u0 < units; u0 += PACK_HELD) {
+        if (units > PACK_HELD && (u0 > 0 || !__is_same(T, _Float16))) load(u0);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= s;
-        half8 h[NP];
-        split8<NP>(v, h);
+        for (int q = 0; q < PACK_HELD / 4; ++q) {
+            const int u = u0 + 4 * q + wave;
+            if (u >= units) continue;
 #pragma unroll
-        for (int p = 0; p < NP; ++p) to[(int64_t)(u * NP + p) * PAGE] = __builtin_bit_cast(u32x4, h[p]);
+            for (int e = 0; e < 8; ++e) v[q][e] = counts ? v[q][e] * s : 0.f;
+            half8 h[NP];
+            split8<NP>(v[q], h);
+#pragma unroll
+            for (int p = 0; p < NP; ++p) to[(int64_t)(u * NP + p) * PAGE] = __builtin_bit_cast(u32x4, h[p]);
+        }
     }
 }
 
@@ -182,7 +188,7 @@ struct PackArgs {
     const float *bias, *g, *stats;
     float scale;
     u32x4 *ximg, *cimg, *xcols, *ccols;
-    float *rinv, *cinv, *gn;
+    float *rinv, *cinv, *gn, *bias2;
     f32x4 *row;
     int32_t *lab;
     uint32_t *hdr;
@@ -228,9 +234,11 @@ __global__ __launch_bounds__(256) void k_pack_rows(PackArgs a)
         return;
     }
     b -= a.xblocks;
-    if (b < a.cblocks)
+    if (b < a.cblocks) {
+        const int j = b * 16 + threadIdx.x; // the bias in units of log 2, -inf past the last centroid
+        if (threadIdx.x < 16) a.bias2[j] = j < a.k ? (a.bias ? a.bias[j] * LOG2E : 0.f) : -INFINITY;
         pack_rows<T, false, NP>(b, (const T *)a.c, a.k, a.d, a.units, nullptr, a.k, a.bias, a.cimg, a.cinv, a.stats ? a.hdr + 1 : nullptr, a.cvec);
-    else
+    } else
         grad_max(b - a.cblocks, a.others, a.g, a.label, a.k, a.n, a.hdr + 2);
 }
 
@@ -444,13 +452,6 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_stats(LogitArgs a)
                     if (rel == 16 * i + 4 * g + r) a.mine[n] = acc[i][j][r];
         }
     }
-}
-
-// The statistics of two sets of logits together
-__device__ __forceinline__ float2 join(float2 a, float2 b)
-{
-    const float m = fmaxf(a.x, b.x), base = m == -INFINITY ? 0.f : m;
-    return make_float2(m, a.y * __builtin_amdgcn_exp2f(a.x - base) + b.y * __builtin_amdgcn_exp2f(b.x - base));
 }
 
 // A row's statistics and loss from its parts: R rows a workgroup of 256, 256 / R threads each.  Sixteen rows are read side by
@@ -760,7 +761,7 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_grads(GradOut first, GradOut se
     }
 }
 
-// out = factor * sum of the slabs, of both gradients in one launch, four values a thread
+// out = factor * sum of the slabs, of both gradients, four values a thread
 struct SlabSum {
     const float *slabs;
     int splits, blocks;
@@ -768,9 +769,36 @@ struct SlabSum {
     const uint32_t *absmax, *gmax;
     void *out;
 };
-template <typename T>
-__global__ __launch_bounds__(256) void k_loss_slabs(SlabSum x, SlabSum c, float scale)
+// dbias of a piece: sums over the rows' parts, 64 centroids a workgroup, four waves taking the parts in turn
+struct BiasSum {
+    const float *part;
+    int slots, ld, count, blocks;
+    const uint32_t *gmax;
+    bool add;
+    float *out;
+};
+__device__ __forceinline__ void bias_sum(int block, const BiasSum &a)
 {
+    __shared__ float sum[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = block * 64 + lane;
+    float s = 0.f;
+    if (j < a.count)
+#pragma unroll 4
+        for (int p = wave; p < a.slots; p += 4) s += a.part[(int64_t)p * a.ld + j];
+    sum[wave][lane] = s;
+    __syncthreads();
+    if (wave > 0 || j >= a.count) return;
+    s = ((sum[0][lane] + sum[1][lane]) + (sum[2][lane] + sum[3][lane])) * (__uint_as_float(*a.gmax) * (1.f / P_ONE));
+    a.out[j] = a.add ? a.out[j] + s : s;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_loss_sums(SlabSum x, SlabSum c, BiasSum bias, float scale)
+{
+    if ((int)blockIdx.x >= x.blocks + c.blocks) {
+        bias_sum(blockIdx.x - x.blocks - c.blocks, bias);
+        return;
+    }
     const bool first = (int)blockIdx.x < x.blocks;
     const SlabSum &a = first ? x : c;
     const int64_t i = ((int64_t)(first ? blockIdx.x : blockIdx.x - x.blocks) * 256 + threadIdx.x) * 4;
@@ -780,7 +808,7 @@ __global__ __launch_bounds__(256) void k_loss_slabs(SlabSum x, SlabSum c, float 
     const int count = (int)min((int64_t)4, a.count - i);
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
     if (vec) {
-#pragma unroll 4
+#pragma unroll 8
         for (int p = 0; p < a.splits; ++p) s += *(const f32x4 *)(a.slabs + p * a.count + i);
     } else {
         for (int p = 0; p < a.splits; ++p)
@@ -798,22 +826,6 @@ __global__ __launch_bounds__(256) void k_loss_none(T *dc, int64_t count, float *
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (dc && i < count) dc[i] = (T)0.f;
     if (dbias && i < k) dbias[i] = 0.f;
-}
-
-// dbias of a piece: sums over the rows' parts, 64 centroids a workgroup, four waves taking the parts in turn
-__global__ __launch_bounds__(256) void k_loss_dbias(const float *part, int slots, int ld, int count, const uint32_t *gmax, bool add, float *out)
-{
-    __shared__ float sum[4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = blockIdx.x * 64 + lane;
-    float s = 0.f;
-    if (j < count)
-#pragma unroll 4
-        for (int p = wave; p < slots; p += 4) s += part[(int64_t)p * ld + j];
-    sum[wave][lane] = s;
-    __syncthreads();
-    if (wave > 0 || j >= count) return;
-    s = ((sum[0][lane] + sum[1][lane]) + (sum[2][lane] + sum[3][lane])) * (__uint_as_float(*gmax) * (1.f / P_ONE));
-    out[j] = add ? out[j] + s : s;
 }
 
 // ---------------------------------------------------------------------------
@@ -895,7 +907,13 @@ static LossPlan loss_plan(int dtype, int64_t n, int d, int k, bool backward, voi
     take(p.bias2, p.kpad);
     take(p.row, p.npad);
     take(p.lab, p.npad);
-    if (!backward) {
+    p.narrow = d <= NARROW_DIM;
+    if (!backward && p.narrow) {
+        const int64_t xq = p.npad / narrow_rows(p.np), xt = p.kpad / 32, per = xq * xt / NARROW_GROUPS;
+        p.xsplit = narrow_parts(xt, per < NARROW_LEAST ? NARROW_LEAST : per, p.npad * 8, &p.xper);
+        take(p.mine, p.npad);
+        take(p.part, p.xsplit * p.npad);
+    } else if (!backward) {
         take(p.mine, p.rpad);
         take(p.part, p.kpad / 128 * p.rpad);
     } else {
@@ -903,7 +921,6 @@ static LossPlan loss_plan(int dtype, int64_t n, int d, int k, bool backward, voi
         take(p.gn, p.npad);
         take(p.xcols, p.npad / 32 * p.dblocks * page);
         take(p.ccols, p.kpad / 32 * p.dblocks * page);
-        p.narrow = d <= NARROW_DIM;
         if (p.narrow) {
             const int64_t rows = narrow_rows(p.np), xq = p.npad / rows, cq = p.kpad / rows, xt = p.kpad / 32, ct = p.npad / 32;
             int64_t per = (xq * xt + cq * ct) / NARROW_GROUPS;
@@ -956,13 +973,13 @@ static bool rows_vec(const void *p, int d)
     return d % 8 == 0 && (uintptr_t)p % 16 == 0;
 }
 
-// The images of rows and centroids, and the rest of what the products need: two launches, three backward
+// The images of rows and centroids, and the rest of what the products need: one launch, three backward
 template <typename T, int NP>
 static void loss_images(const LossArgs &a, const LossPlan &p, bool backward, hipStream_t st)
 {
-    hipLaunchKernelGGL(k_loss_begin, dim3((unsigned)(p.kpad / 256)), dim3(256), 0, st, a.bias, a.k, (int)p.kpad, p.bias2, p.hdr);
+    if (backward) hipLaunchKernelGGL(k_loss_begin, dim3(1), dim3(64), 0, st, p.hdr);
     PackArgs g = {a.x, a.c, a.n, a.d, a.k, p.units, a.label, a.bias, a.grad, backward ? a.stats : nullptr, a.scale, p.ximg, p.cimg,
-                  p.xcols, p.ccols, p.rinv, p.cinv, p.gn, p.row, p.lab, p.hdr, rows_vec<T>(a.x, a.d), rows_vec<T>(a.c, a.d)};
+                  p.xcols, p.ccols, p.rinv, p.cinv, p.gn, p.bias2, p.row, p.lab, p.hdr, rows_vec<T>(a.x, a.d), rows_vec<T>(a.c, a.d)};
     g.xblocks = (int)(p.npad / 16);
     g.cblocks = (int)(p.kpad / 16);
     g.others = !backward ? 0 : (int)((a.n + 2047) / 2048 < 64 ? (a.n + 2047) / 2048 : 64);
@@ -1047,6 +1064,23 @@ static int loss_forward(const LossArgs &a, hipStream_t st)
     if (a.n <= FEW_ROWS) return loss_few<T>(a, st);
     const LossPlan p = loss_plan(a.dtype, a.n, a.d, a.k, false, a.ws);
     loss_images<T, NP>(a, p, false, st);
+    if (p.narrow) {
+        NarrowArgs g = {};
+        const int rows = narrow_rows(NP);
+        g.units = p.units;
+        g.d = a.d;
+        g.row = p.row;
+        g.lab = p.lab;
+        g.cinv = p.cinv;
+        g.bias2 = p.bias2;
+        g.part = p.part;
+        g.mine = p.mine;
+        g.npad = (int)p.npad;
+        g.x = {p.ximg, p.cimg, nullptr, (int)(p.npad / rows), (int)(p.kpad / 32), p.xsplit, p.xper, (int)a.n};
+        LOSS_TRY((hipError_t)launch_loss_narrow_stats(a.dtype, g, st));
+        launch_merge(p.part, p.xsplit, g.npad, p.mine, p.lab, a.k, a.n, a.stats, a.loss, st);
+        return (int)hipGetLastError();
+    }
     LOSS_TRY(allow_lds(k_loss_stats<NP>, Product<NP>::LDS));
     for (int64_t r0 = 0; r0 < a.n; r0 += p.rows) {
         const int64_t rows = a.n - r0 < p.rows ? a.n - r0 : p.rows, rpad = pad_to(rows, TILE);
@@ -1069,14 +1103,18 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
     }
     const LossPlan p = loss_plan(a.dtype, a.n, a.d, a.k, true, a.ws);
     loss_images<T, NP>(a, p, true, st);
-    auto finish = [&]() {
+    auto bias_part = [&](int slots, int64_t ld, int64_t c0, int64_t count, bool add) {
+        return BiasSum{p.dbpart, slots, (int)ld, (int)count, (int)((count + 63) / 64), p.hdr + 2, add, a.dbias + c0};
+    };
+    auto finish = [&](const BiasSum &bias) {
         auto side = [&](float *slabs, int splits, int64_t count, const uint32_t *absmax, const uint32_t *gmax, void *out) {
             return SlabSum{slabs, splits, (int)((count + 1023) / 1024), count, absmax, gmax, out};
         };
         SlabSum x = {}, c = {};
         if (a.dx && p.xslab) x = side(p.xsum, p.xsplit, a.n * a.d, p.hdr + 1, nullptr, a.dx);
         if (a.dc && p.cslab) c = side(p.csum, p.csplit, (int64_t)a.k * a.d, p.hdr, p.hdr + 2, a.dc);
-        if (x.blocks + c.blocks) hipLaunchKernelGGL(k_loss_slabs<T>, dim3((unsigned)(x.blocks + c.blocks)), dim3(256), 0, st, x, c, a.scale);
+        const int blocks = x.blocks + c.blocks + bias.blocks;
+        if (blocks) hipLaunchKernelGGL(k_loss_sums<T>, dim3((unsigned)blocks), dim3(256), 0, st, x, c, bias, a.scale);
     };
     if (p.narrow) {
         NarrowArgs g = {};
@@ -1101,10 +1139,7 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
                    !a.dc ? nullptr : p.cslab ? (void *)p.csum : a.dc, p.hdr, p.hdr + 2, nullptr,
                    a.d % 4 == 0 && (p.cslab || (uintptr_t)a.dc % 16 == 0)};
         LOSS_TRY((hipError_t)launch_loss_narrow(a.dtype, g, st));
-        finish();
-        if (a.dbias)
-            hipLaunchKernelGGL(k_loss_dbias, dim3((unsigned)((a.k + 63) / 64)), dim3(256), 0, st, p.dbpart, p.csplit, (int)p.kpad, a.k,
-                               p.hdr + 2, false, a.dbias);
+        finish(a.dbias ? bias_part(p.csplit, p.kpad, 0, a.k, false) : BiasSum{});
         return (int)hipGetLastError();
     }
     LOSS_TRY(allow_lds(k_loss_p<NP>, Product<NP>::LDS));
@@ -1124,9 +1159,8 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
             g.dbpart = a.dbias ? p.dbpart : nullptr;
             hipLaunchKernelGGL(k_loss_p<NP>, dim3((unsigned)(g.mt * g.nt)), dim3(LNT), Product<NP>::LDS, st, g);
             if (a.dbias) {
-                const int count = (int)(a.k - c0 < cpad ? a.k - c0 : cpad);
-                hipLaunchKernelGGL(k_loss_dbias, dim3((unsigned)((count + 63) / 64)), dim3(256), 0, st, p.dbpart, (int)(rpad / 64),
-                                   (int)cpad, count, p.hdr + 2, r0 > 0, a.dbias + c0);
+                const BiasSum bias = bias_part((int)(rpad / 64), cpad, c0, a.k - c0 < cpad ? a.k - c0 : cpad, r0 > 0);
+                hipLaunchKernelGGL(k_loss_sums<T>, dim3((unsigned)bias.blocks), dim3(256), 0, st, SlabSum{}, SlabSum{}, bias, a.scale);
             }
             GradOut x = {}, c = {};
             if (a.dx) {
@@ -1176,7 +1210,7 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
                 hipLaunchKernelGGL((k_loss_grads<T, NP>), dim3((unsigned)(nx + nc)), dim3(LNT), Product<NP>::LDS, st, x, c, nx);
         }
     }
-    finish();
+    finish(BiasSum{});
     return (int)hipGetLastError();
 }
 

@@ -12,12 +12,15 @@
 #include "loss_image.h"
 
 #define NARROW_NT 256
-// CENT: the gradient of the centroids
-template <typename T, int DU, bool CENT>
+// What a workgroup does: the gradient of rows, that of centroids, or forward the maxima and sums of rows
+enum { ROWS, CENTROIDS, STATS };
+
+template <typename T, int DU, int DO>
 __device__ __forceinline__ void narrow(const NarrowArgs &a, const NarrowSide &s, int b, u32x4 *lds)
 {
     constexpr int NP = sizeof(T) == 4 ? 2 : 1, Q = narrow_rows(NP), QB = Q / 64, DB = 2 * DU;
-    constexpr int CHUNKS = 4 * DU * NP;             // KB of a tile: rows, then columns
+    constexpr bool CENT = DO == CENTROIDS;
+    constexpr int CHUNKS = (DO == STATS ? 2 : 4) * DU * NP; // KB of a tile: rows, then columns
     constexpr int STAGE = (CHUNKS + 2) * 64;        // and two KB for the rows' numbers, in 16-byte pieces
     const int tid = threadIdx.x, lane = tid & 63, l = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -37,8 +40,9 @@ __device__ __forceinline__ void narrow(const NarrowArgs &a, const NarrowSide &s,
         const u32x4 *rows = s.r + (int64_t)(t >> 2) * a.units * NP * PAGE + (t & 3) * 128;
         const u32x4 *cols = s.rt + (int64_t)t * NP * PAGE;
 #pragma unroll
-        for (int e = 0; e < DU * NP; ++e) {
+        for (int e = 0; e < (CHUNKS + 3) / 4; ++e) {
             const int c = e * 4 + wave; // (rows: page c / 2, group c % 2; columns: part, then group of 16 dimensions)
+            if (CHUNKS % 4 && c >= CHUNKS) break;
             const int cc = c - 2 * DU * NP;
             const u32x4 *src = c < 2 * DU * NP ? rows + (c >> 1) * PAGE + (c & 1) * 64 : cols + (cc / DB) * PAGE + (cc % DB) * 64;
             copy16(src, 1024, dst + c * 64);
@@ -74,8 +78,8 @@ __device__ __forceinline__ void narrow(const NarrowArgs &a, const NarrowSide &s,
         } else {
             const f32x4 v = a.row[q];
             f[j] = v[0];
-            m[j] = v[1];
-            z[j] = v[2];
+            m[j] = DO == STATS ? -INFINITY : v[1];
+            z[j] = DO == STATS ? 0.f : v[2];
             lab[j] = a.lab[q];
         }
     }
@@ -118,6 +122,48 @@ __device__ __forceinline__ void narrow(const NarrowArgs &a, const NarrowSide &s,
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int j = 0; j < QB; ++j) S[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(r[0][i], qf[u][0][j], S[i][j], 0, 0, 0);
+        }
+        if constexpr (DO == STATS) {
+            // a lane keeps the maximum and the sum of the logits that it has met of each of its rows
+            const int base = 32 * t + 4 * g;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const f32x4 b2 = *(const f32x4 *)(num + 16 * i + 4 * g);
+                const float ci = a.cinv[t * 2 + i];
+#pragma unroll
+                for (int j = 0; j < QB; ++j) {
+                    const float fj = f[j] * ci;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) S[i][j][r] = fmaf(S[i][j][r], fj, b2[r]);
+                }
+            }
+            bool any = false;
+#pragma unroll
+            for (int j = 0; j < QB; ++j) {
+                float top = m[j];
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) top = fmaxf(top, S[i][j][r]);
+                const float at = top == -INFINITY ? 0.f : top; // (all masked so far: every term is zero)
+                z[j] *= __builtin_amdgcn_exp2f(m[j] - at);
+                m[j] = top;
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) z[j] += __builtin_amdgcn_exp2f(S[i][j][r] - at);
+                any |= (uint32_t)(lab[j] - 32 * t) < 32u;
+            }
+            if (__any(any)) {
+#pragma unroll
+                for (int j = 0; j < QB; ++j)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (lab[j] == base + 16 * i + r) a.mine[q0 + 16 * j + l] = S[i][j][r];
+            }
+            continue;
         }
         // P, in units of 2^15
 #pragma unroll
@@ -199,6 +245,16 @@ __device__ __forceinline__ void narrow(const NarrowArgs &a, const NarrowSide &s,
         }
     }
 
+    if constexpr (DO == STATS) {
+#pragma unroll
+        for (int j = 0; j < QB; ++j) {
+            float2 v = make_float2(m[j], z[j]);
+            v = join(v, make_float2(__shfl_xor(v.x, 16, 64), __shfl_xor(v.y, 16, 64)));
+            v = join(v, make_float2(__shfl_xor(v.x, 32, 64), __shfl_xor(v.y, 32, 64)));
+            if (g == 0) a.part[(int64_t)split * a.npad + q0 + 16 * j + l] = v;
+        }
+        return;
+    }
     const float factor = s.mode == 0 ? grad_factor<T>(s.absmax, s.gmax, a.scale) : 1.f;
     float *slab = (float *)s.out + (int64_t)split * s.rows * a.d;
 #pragma unroll
@@ -229,22 +285,31 @@ __global__ __launch_bounds__(NARROW_NT, 2) void k_loss_narrow(NarrowArgs a)
 {
     extern __shared__ u32x4 lds[];
     if ((int)blockIdx.x < a.nx)
-        narrow<T, DU, false>(a, a.x, blockIdx.x, lds);
+        narrow<T, DU, ROWS>(a, a.x, blockIdx.x, lds);
     else
-        narrow<T, DU, true>(a, a.c, blockIdx.x - a.nx, lds);
+        narrow<T, DU, CENTROIDS>(a, a.c, blockIdx.x - a.nx, lds);
 }
 
-template <typename T>
+template <typename T, int DU>
+__global__ __launch_bounds__(NARROW_NT, 2) void k_loss_narrow_stats(NarrowArgs a)
+{
+    extern __shared__ u32x4 lds[];
+    narrow<T, DU, STATS>(a, a.x, blockIdx.x, lds);
+}
+
+template <typename T, bool GRADS>
 static int narrow_units(const NarrowArgs &a, hipStream_t st)
 {
     auto go = [&](auto units) -> int {
-        constexpr int DU = decltype(units)::value;
-        constexpr size_t bytes = 2 * (4 * DU * (sizeof(T) == 4 ? 2 : 1) + 2) * 1024;
+        constexpr int DU = decltype(units)::value, KB = (GRADS ? 4 : 2) * DU * (sizeof(T) == 4 ? 2 : 1) + 2;
+        const auto kern = GRADS ? k_loss_narrow<T, DU> : k_loss_narrow_stats<T, DU>;
+        constexpr size_t bytes = 2 * KB * 1024;
         if (bytes > 49152) { // (48 KB of dynamic LDS need no asking)
-            const hipError_t e = hipFuncSetAttribute((const void *)k_loss_narrow<T, DU>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+            const hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
             if (e != hipSuccess) return (int)e;
         }
-        hipLaunchKernelGGL((k_loss_narrow<T, DU>), dim3((unsigned)(a.nx + a.c.qblocks * a.c.splits)), dim3(NARROW_NT), bytes, st, a);
+        const int blocks = GRADS ? a.nx + a.c.qblocks * a.c.splits : a.x.qblocks * a.x.splits;
+        hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(NARROW_NT), bytes, st, a);
         return 0;
     };
     switch ((a.d + 31) / 32) {
@@ -255,11 +320,20 @@ static int narrow_units(const NarrowArgs &a, hipStream_t st)
     }
 }
 
+int launch_loss_narrow_stats(int dtype, const NarrowArgs &a, hipStream_t st)
+{
+    switch (dtype) {
+    case VLQ_F32: return narrow_units<float, false>(a, st);
+    case VLQ_F16: return narrow_units<_Float16, false>(a, st);
+    default: return narrow_units<bf16_t, false>(a, st);
+    }
+}
+
 int launch_loss_narrow(int dtype, const NarrowArgs &a, hipStream_t st)
 {
     switch (dtype) {
-    case VLQ_F32: return narrow_units<float>(a, st);
-    case VLQ_F16: return narrow_units<_Float16>(a, st);
-    default: return narrow_units<bf16_t>(a, st);
+    case VLQ_F32: return narrow_units<float, true>(a, st);
+    case VLQ_F16: return narrow_units<_Float16, true>(a, st);
+    default: return narrow_units<bf16_t, true>(a, st);
     }
 }
