@@ -18,32 +18,32 @@ typedef __bf16 bf16_t;
 #define LN2 0.6931471805599453f
 
 // Exponent of the power of two that brings mx to [2^14, 2^15)
+// (a row of zeros takes the largest: it has no part in the largest inverse scale of its matrix)
 __device__ __forceinline__ int scale_exponent(float mx)
 {
-    const int ex = mx > 0.f ? 14 - ((int)(__float_as_uint(mx) >> 23) - 127) : 0;
+    const int ex = mx > 0.f ? 14 - ((int)(__float_as_uint(mx) >> 23) - 127) : 126;
     return min(max(ex, -126), 126);
 }
 __device__ __forceinline__ float pow2i(int ex) { return __uint_as_float((uint32_t)(127 + ex) << 23); }
 
 // eight values of a row from index i on, zeros past its end
 template <typename T>
-__device__ __forceinline__ void load8(const T *row, int i, int d, bool vec, float (&v)[8])
+struct Eight {
+    T v[8];
+};
+template <typename T>
+__device__ __forceinline__ Eight<T> load8(const T *row, int i, int d, bool vec)
 {
-    if (vec && i < d) { // (d is a multiple of 8)
-        if constexpr (sizeof(T) == 4) {
-            const f32x4 a = *(const f32x4 *)(row + i), b = *(const f32x4 *)(row + i + 4);
+    Eight<T> r;
+    if (vec) { // (d is a multiple of 8)
+        u32x4 *w = (u32x4 *)r.v;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = e < 4 ? a[e] : b[e - 4];
-        } else {
-            T t[8];
-            *(u32x4 *)t = *(const u32x4 *)(row + i);
+        for (int p = 0; p < (int)sizeof(T) / 2; ++p) w[p] = i < d ? ((const u32x4 *)(row + i))[p] : u32x4{0, 0, 0, 0};
+    } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = (float)t[e];
-        }
-        return;
+        for (int e = 0; e < 8; ++e) r.v[e] = i + e < d ? row[i + e] : (T)0.f;
     }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = i + e < d ? (float)row[i + e] : 0.f;
+    return r;
 }
 
 // v as one or two fp16 parts
@@ -64,13 +64,13 @@ __device__ __forceinline__ float2 join(float2 a, float2 b)
     return make_float2(m, a.y * __builtin_amdgcn_exp2f(a.x - base) + b.y * __builtin_amdgcn_exp2f(b.x - base));
 }
 
-// Factor of a gradient: the scale of the columns' image, that of P, g's largest magnitude where P was taken relative to it
-template <typename T>
-__device__ __forceinline__ float grad_factor(const uint32_t *absmax, const uint32_t *gmax, float scale)
-{
-    const float inv = __is_same(T, _Float16) ? 1.f : pow2i(-scale_exponent(__uint_as_float(*absmax)));
-    return scale * (gmax ? __uint_as_float(*gmax) : 1.f) * (1.f / P_ONE) * inv;
-}
+// What a backward call knows of its matrices as a whole
+struct LossHeader {
+    float xinv, cinv; // inverse scales of the columns' images
+    float top;        // largest |g|
+};
+// Factor of a gradient: the inverse scales of the columns' image and of P, and g's largest where P was taken relative to it
+__device__ __forceinline__ float grad_factor(float inv, float top, float scale) { return scale * top * (1.f / P_ONE) * inv; }
 
 template <typename T>
 __device__ __forceinline__ void store4(T *p, const f32x4 &v, int count, bool vec)
@@ -99,8 +99,7 @@ struct NarrowSide {
     int rows;
     int mode; // 0: typed; 1: slabs [splits][rows x d]
     void *out;
-    const uint32_t *absmax, *gmax;
-    const float *weight; // of the rows (dx), and where they do not count
+    const float *weight; // of the rows (dx)
     bool vec;
 };
 struct NarrowArgs {
@@ -109,6 +108,7 @@ struct NarrowArgs {
     const f32x4 *row; // per row of x: factor, maximum, factors of P
     const int32_t *lab;
     const float *gn, *cinv, *bias2;
+    const LossHeader *hdr;
     float *dbpart; // [splits of c][kpad] or NULL
     int kpad;
     float scale;

@@ -29,27 +29,13 @@
 #define PIECE (1 << 26)      // values of P kept at a time
 #define NARROW_DIM 128       // up to so many dimensions the gradients take the narrow form (softmax_loss_narrow.hip)
 #define NARROW_GROUPS 1024   // its workgroups, about: two rounds of two a compute unit
-#define NARROW_LEAST 8       // tiles of 32 rows that a workgroup of it takes at least
+#define NARROW_LEAST 4       // tiles of 32 rows that a workgroup of it takes at least
 #define FEW_ROWS 64          // up to so many rows the logits come from the centroids as they lie (k_loss_few)
 #define FEW_WIDE 65536       // from so many centroids on a wave takes 32 of them: then there are waves enough
 
 // ---------------------------------------------------------------------------
 // images
 // ---------------------------------------------------------------------------
-// Header of a backward call: [0] largest magnitude of x's counted rows (bits), [1] of c, [2] of g
-__global__ void k_loss_begin(uint32_t *hdr)
-{
-    if (threadIdx.x < 4) hdr[threadIdx.x] = 0;
-}
-
-// The largest of the callers' values into *to: an atomic only where it is larger than what is there (all of a launch's workgroups
-// on one address waited for each other: 3 126 of them 131 us, a third of that without)
-__device__ __forceinline__ void raise(uint32_t *to, float v)
-{
-    const uint32_t bits = __float_as_uint(v);
-    if (bits > __hip_atomic_load(to, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(to, bits);
-}
-
 // A row counts if its label is a centroid; a centroid if its bias is not -inf.  What does not count is written as zeros.
 __device__ __forceinline__ bool row_counts(const int32_t *label, int k, const float *bias, int64_t r)
 {
@@ -58,26 +44,26 @@ __device__ __forceinline__ bool row_counts(const int32_t *label, int k, const fl
 }
 
 // Image of the rows of X, 16 rows a workgroup; a scale per row (OWN) or for all 16.  inv: 1 / scale, as many.
-// A wave takes every fourth unit, as the lanes lie in its pages; up to PACK_HELD units the values wait in registers for their
-// scale, beyond that they are read again.  Bound by memory.  (With 128 rows a workgroup and a scale for all of them 128 MB took
-// 99 us, for want of loads under way.)
-#define PACK_HELD 16
-template <typename T, bool OWN, int NP>
+// A wave takes every fourth unit, as the lanes lie in its pages; up to 4 HELD units the values wait in registers for their
+// scale, beyond that they are read again.  Bound by memory.  (128 MB with 128 rows a workgroup and a scale for all of them:
+// 99 us, for want of loads under way; 238 MB of rows of 64 units read twice 138 us, what a die's workgroups hold is more
+// than its L2.)
+template <typename T, bool OWN, int NP, int HELD>
 __device__ __forceinline__ void pack_rows(int block, const T *__restrict__ X, int64_t rows, int d, int units,
                                           const int32_t *__restrict__ label, int k, const float *__restrict__ bias,
-                                          u32x4 *__restrict__ pages, float *__restrict__ inv, uint32_t *absmax, bool vec)
+                                          u32x4 *__restrict__ pages, float *__restrict__ inv, bool vec)
 {
     __shared__ float rmax[4][16];
     const int tid = threadIdx.x, lane = tid & 63, l = lane & 15, wave = tid >> 6;
     const int64_t r0 = (int64_t)block * 16;
     const bool in = r0 + l < rows;
-    const T *row = X + (in ? r0 + l : 0) * d;
-    float v[PACK_HELD / 4][8];
+    const T *row = X + (in ? r0 + l : 0) * d; // (rows past the end: the first, not used)
+    Eight<T> v[HELD];
     auto load = [&](int u0) {
 #pragma unroll
-        for (int q = 0; q < PACK_HELD / 4; ++q) {
+        for (int q = 0; q < HELD; ++q) {
             const int u = u0 + 4 * q + wave;
-            if (u < units) load8(row, u * 32 + (lane >> 4) * 8, d, vec, v[q]); // (rows past the end: of the first, not used)
+            if (u < units) v[q] = load8(row, u * 32 + (lane >> 4) * 8, d, vec);
         }
     };
     load(0);
@@ -85,14 +71,14 @@ __device__ __forceinline__ void pack_rows(int block, const T *__restrict__ X, in
     int ex = 0;
     if constexpr (!__is_same(T, _Float16)) {
         float mx = 0.f;
-        for (int u0 = 0; u0 < units; u0 += PACK_HELD) {
+        for (int u0 = 0; u0 < units; u0 += 4 * HELD) {
             if (u0 > 0) load(u0);
 #pragma unroll
-            for (int q = 0; q < PACK_HELD / 4; ++q)
+            for (int q = 0; q < HELD; ++q)
                 if (u0 + 4 * q + wave < units)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        const float m = fabsf(v[q][e]);
+                        const float m = fabsf((float)v[q].v[e]);
                         if (m < INFINITY) mx = fmaxf(mx, m);
                     }
         }
@@ -101,12 +87,11 @@ __device__ __forceinline__ void pack_rows(int block, const T *__restrict__ X, in
         mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
         if (lane < 16) rmax[wave][l] = mx;
         __syncthreads();
-        const float mine = fmaxf(fmaxf(rmax[0][l], rmax[1][l]), fmaxf(rmax[2][l], rmax[3][l])); // of the lane's row
-        float all = mine;
+        mx = fmaxf(fmaxf(rmax[0][l], rmax[1][l]), fmaxf(rmax[2][l], rmax[3][l])); // of the lane's row
+        if (!OWN)
 #pragma unroll
-        for (int o = 8; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor(all, o, 64));
-        if (tid == 0 && absmax) raise(absmax, all);
-        ex = scale_exponent(OWN ? mine : all);
+            for (int o = 8; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
+        ex = scale_exponent(mx);
     }
     if (tid < 16) {
         if (OWN)
@@ -116,68 +101,87 @@ __device__ __forceinline__ void pack_rows(int block, const T *__restrict__ X, in
     }
     const float s = pow2i(ex);
     u32x4 *to = pages + (int64_t)(block >> 3) * units * NP * PAGE + (block & 7) * 64 + lane;
-    for (int u0 = 0; u0 < units; u0 += PACK_HELD) {
-        if (units > PACK_HELD && (u0 > 0 || !__is_same(T, _Float16))) load(u0);
+    for (int u0 = 0; u0 < units; u0 += 4 * HELD) {
+        if (units > 4 * HELD && (u0 > 0 || !__is_same(T, _Float16))) load(u0);
 #pragma unroll
-        for (int q = 0; q < PACK_HELD / 4; ++q) {
+        for (int q = 0; q < HELD; ++q) {
             const int u = u0 + 4 * q + wave;
             if (u >= units) continue;
+            float f[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[q][e] = counts ? v[q][e] * s : 0.f;
+            for (int e = 0; e < 8; ++e) f[e] = counts ? (float)v[q].v[e] * s : 0.f;
             half8 h[NP];
-            split8<NP>(v[q], h);
+            split8<NP>(f, h);
 #pragma unroll
             for (int p = 0; p < NP; ++p) to[(int64_t)(u * NP + p) * PAGE] = __builtin_bit_cast(u32x4, h[p]);
         }
     }
 }
 
-// Image of X's columns: its rows are the dimensions, its indices the rows of X, 64 rows x 128 dimensions a workgroup.
+// Image of X's columns: its rows are the dimensions, its indices the rows of X, 64 rows x 128 dimensions a workgroup, turned in LDS.
 // ORDER 1: index s of 64 is row (s >> 2) + 16 (s & 3), the order in which the lanes of k_loss_p hold them; 2: index s of 32 is row
 // 16 (s / 4 % 2) + 4 (s / 8) + s % 4, as the lanes of k_loss_narrow hold them.
 template <typename T, int ORDER, int NP>
 __device__ __forceinline__ void pack_cols(int block, int dblock, const T *__restrict__ X, int64_t rows, int d, int units,
-                                                   const int32_t *__restrict__ label, int k, const float *__restrict__ bias,
-                                                   u32x4 *__restrict__ pages, const uint32_t *__restrict__ absmax, bool vec)
+                                          const int32_t *__restrict__ label, int k, const float *__restrict__ bias,
+                                          u32x4 *__restrict__ pages, float inv, bool vec)
 {
-    __shared__ float t[64][129];
+    // (an odd number of words a row: neither the rows' writes nor the columns' reads meet in a bank more than they must)
+    using Held = std::conditional_t<NP == 2, float, _Float16>;
+    constexpr int LD = NP == 2 ? 129 : 130;
+    __shared__ __align__(16) Held t[64 * LD];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t r0 = (int64_t)block * 64;
     const int d0 = dblock * 128;
-    const float s = __is_same(T, _Float16) ? 1.f : pow2i(scale_exponent(__uint_as_float(*absmax)));
+    const float s = 1.f / inv; // (a power of two)
+    Eight<T> v[4];
+    bool counts[4];
 #pragma unroll
-    for (int i = tid; i < 64 * 16; i += 256) {
-        const int r = i >> 4, c = (i & 15) * 8;
-        float v[8] = {};
-        if (r0 + r < rows && row_counts(label, k, bias, r0 + r)) load8(X + (r0 + r) * d, d0 + c, d, vec, v);
+    for (int q = 0; q < 4; ++q) {
+        const int r = q * 16 + (tid >> 4);
+        const bool in = r0 + r < rows;
+        v[q] = load8(X + (in ? r0 + r : 0) * d, d0 + (tid & 15) * 8, d, vec);
+        counts[q] = in && row_counts(label, k, bias, r0 + r);
+    }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) t[r][c + e] = v[e] * s;
+    for (int q = 0; q < 4; ++q) {
+        Held *to = t + (q * 16 + (tid >> 4)) * LD + (tid & 15) * 8;
+        float f[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = counts[q] ? (float)v[q].v[e] * s : 0.f;
+        if constexpr (NP == 2) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) to[e] = f[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                const _Float16 two[2] = {(_Float16)f[e], (_Float16)f[e + 1]};
+                *(uint32_t *)(to + e) = *(const uint32_t *)two;
+            }
+        }
     }
     __syncthreads();
-    for (int it = wave; it < 16; it += 4) {
-        const int e = it & 1, grp = it >> 1;
-        float v[8];
+#pragma unroll
+    for (int it = 0; it < 4; ++it) {
+        const int e = it & 1, grp = (it >> 1) + 2 * wave; // (a wave: two groups of 16 dimensions, both units)
+        Held f[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
             const int i = e * 32 + (lane >> 4) * 8 + q;
-            v[q] = t[ORDER == 1 ? (i >> 2) + 16 * (i & 3) : ORDER == 2 ? e * 32 + 16 * (q >> 2) + 4 * (lane >> 4) + (q & 3) : i][grp * 16 + (lane & 15)];
+            const int r = ORDER == 1 ? (i >> 2) + 16 * (i & 3) : ORDER == 2 ? e * 32 + 16 * (q >> 2) + 4 * (lane >> 4) + (q & 3) : i;
+            f[q] = t[r * LD + grp * 16 + (lane & 15)];
         }
-        half8 h[NP];
-        split8<NP>(v, h);
         const int64_t u = (int64_t)block * 2 + e;
-#pragma unroll
-        for (int p = 0; p < NP; ++p)
-            pages[(((int64_t)dblock * units + u) * NP + p) * PAGE + grp * 64 + lane] = __builtin_bit_cast(u32x4, h[p]);
+        u32x4 *to = pages + ((int64_t)dblock * units + u) * NP * PAGE + grp * 64 + lane;
+        if constexpr (NP == 2) {
+            half8 h[2];
+            split8<2>(f, h);
+            to[0] = __builtin_bit_cast(u32x4, h[0]);
+            to[PAGE] = __builtin_bit_cast(u32x4, h[1]);
+        } else {
+            to[0] = *(const u32x4 *)f;
+        }
     }
-}
-
-__device__ __forceinline__ void grad_max(int block, int blocks, const float *g, const int32_t *label, int k, int64_t n, uint32_t *out)
-{
-    float mx = 0.f;
-    for (int64_t i = (int64_t)block * 256 + threadIdx.x; i < n; i += (int64_t)blocks * 256)
-        if ((uint32_t)label[i] < (uint32_t)k && fabsf(g[i]) < INFINITY) mx = fmaxf(mx, fabsf(g[i]));
-    mx = __uint_as_float(wave_max_u32(__float_as_uint(mx)));
-    if ((threadIdx.x & 63) == 0) raise(out, mx);
 }
 
 struct PackArgs {
@@ -191,9 +195,9 @@ struct PackArgs {
     float *rinv, *cinv, *gn, *bias2;
     f32x4 *row;
     int32_t *lab;
-    uint32_t *hdr;
+    LossHeader *hdr;
     bool xvec, cvec;
-    int xblocks, cblocks, others, dblocks, xunits, cunits; // workgroups for x, for c, for the rest; units of the columns' images
+    int xblocks, cblocks, dblocks, xunits, cunits; // workgroups for x, for c; units of the columns' images
 };
 
 // A row's numbers: factor s log2(e) / scale, and backward its maximum, the factors of P in either order (2^15 / z, and with
@@ -205,7 +209,7 @@ __device__ __forceinline__ void row_numbers(const PackArgs &a, int64_t i, float 
     float f = 0.f;
     bool ok = in;
     if (a.stats && in) {
-        const float m = a.stats[2 * i], z = a.stats[2 * i + 1], top = __uint_as_float(a.hdr[2]);
+        const float m = a.stats[2 * i], z = a.stats[2 * i + 1], top = a.hdr->top;
         ok = m != -INFINITY;
         if (ok) {
             f = top > 0.f ? a.g[i] / top : 0.f;
@@ -221,25 +225,47 @@ __device__ __forceinline__ void row_numbers(const PackArgs &a, int64_t i, float 
     if (a.gn) a.gn[i] = ok ? f * P_ONE : 0.f;
 }
 
-// Both matrices' images in one launch; forward the rows' numbers, backward the largest g
-template <typename T, int NP>
+// Both matrices' images in one launch; forward the rows' numbers
+template <typename T, int NP, int HELD>
 __global__ __launch_bounds__(256) void k_pack_rows(PackArgs a)
 {
-    int b = blockIdx.x;
-    if (b < a.xblocks) {
-        pack_rows<T, true, NP>(b, (const T *)a.x, a.n, a.d, a.units, a.label, a.k, nullptr, a.ximg, a.rinv, a.stats ? a.hdr : nullptr, a.xvec);
-        if (a.stats) return;
-        __syncthreads();
-        if (threadIdx.x < 16) row_numbers(a, (int64_t)b * 16 + threadIdx.x, a.rinv[(int64_t)b * 16 + threadIdx.x]);
-        return;
-    }
-    b -= a.xblocks;
-    if (b < a.cblocks) {
+    const int b = blockIdx.x - a.xblocks;
+    if (b >= 0) {
         const int j = b * 16 + threadIdx.x; // the bias in units of log 2, -inf past the last centroid
         if (threadIdx.x < 16) a.bias2[j] = j < a.k ? (a.bias ? a.bias[j] * LOG2E : 0.f) : -INFINITY;
-        pack_rows<T, false, NP>(b, (const T *)a.c, a.k, a.d, a.units, nullptr, a.k, a.bias, a.cimg, a.cinv, a.stats ? a.hdr + 1 : nullptr, a.cvec);
-    } else
-        grad_max(b - a.cblocks, a.others, a.g, a.label, a.k, a.n, a.hdr + 2);
+        pack_rows<T, false, NP, HELD>(b, (const T *)a.c, a.k, a.d, a.units, nullptr, a.k, a.bias, a.cimg, a.cinv, a.cvec);
+        return;
+    }
+    pack_rows<T, true, NP, HELD>(blockIdx.x, (const T *)a.x, a.n, a.d, a.units, a.label, a.k, nullptr, a.ximg, a.rinv, a.xvec);
+    if (a.stats) return;
+    __syncthreads();
+    if (threadIdx.x < 16) row_numbers(a, (int64_t)blockIdx.x * 16 + threadIdx.x, a.rinv[(int64_t)blockIdx.x * 16 + threadIdx.x]);
+}
+
+// Backward: the largest inverse scales of either matrix, and the largest |g|, a workgroup each.  (An atomic of every workgroup of
+// k_pack_rows on one address took 43 us at 65 536 centroids.)
+__global__ __launch_bounds__(1024) void k_loss_header(PackArgs a)
+{
+    __shared__ float s[16];
+    float mx = 0.f;
+    if (blockIdx.x == 2) {
+#pragma unroll 4
+        for (int64_t i = threadIdx.x; i < a.n; i += 1024) {
+            const float v = fabsf(a.g[i]);
+            if ((uint32_t)a.label[i] < (uint32_t)a.k && v < INFINITY) mx = fmaxf(mx, v);
+        }
+    } else {
+        const float *v = blockIdx.x == 0 ? a.rinv : a.cinv;
+        const int64_t count = (int64_t)(blockIdx.x == 0 ? a.xblocks * 16 : a.cblocks);
+#pragma unroll 4
+        for (int64_t i = threadIdx.x; i < count; i += 1024) mx = fmaxf(mx, v[i]);
+    }
+    mx = __uint_as_float(wave_max_u32(__float_as_uint(mx)));
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = mx;
+    __syncthreads();
+    if (threadIdx.x > 0) return;
+    for (int w = 1; w < 16; ++w) mx = fmaxf(mx, s[w]);
+    (blockIdx.x == 0 ? a.hdr->xinv : blockIdx.x == 1 ? a.hdr->cinv : a.hdr->top) = mx;
 }
 
 // Backward: both matrices' columns, and the rows' numbers
@@ -248,12 +274,12 @@ __global__ __launch_bounds__(256) void k_pack_cols(PackArgs a)
 {
     int b = blockIdx.x;
     if (b < a.xblocks) {
-        pack_cols<T, XORDER, NP>(b / a.dblocks, b % a.dblocks, (const T *)a.x, a.n, a.d, a.xunits, a.label, a.k, nullptr, a.xcols, a.hdr, a.xvec);
+        pack_cols<T, XORDER, NP>(b / a.dblocks, b % a.dblocks, (const T *)a.x, a.n, a.d, a.xunits, a.label, a.k, nullptr, a.xcols, a.hdr->xinv, a.xvec);
         return;
     }
     b -= a.xblocks;
     if (b < a.cblocks) {
-        pack_cols<T, CORDER, NP>(b / a.dblocks, b % a.dblocks, (const T *)a.c, a.k, a.d, a.cunits, nullptr, a.k, a.bias, a.ccols, a.hdr + 1, a.cvec);
+        pack_cols<T, CORDER, NP>(b / a.dblocks, b % a.dblocks, (const T *)a.c, a.k, a.d, a.cunits, nullptr, a.k, a.bias, a.ccols, a.hdr->cinv, a.cvec);
         return;
     }
     const int64_t i = (int64_t)(b - a.cblocks) * 256 + threadIdx.x; // (the workgroups cover the padded rows)
@@ -704,8 +730,8 @@ struct GradOut {
     int mode;      // 0: typed, times the factor; 1: fp32 slabs, stored; 2: added to what is there
     void *out;     // typed [rows x d], or slabs [splits][rows x d]
     int64_t slab;
-    const uint32_t *absmax, *gmax; // of the columns' matrix, and of g (or NULL)
-    const float *weight;           // of the rows (or NULL), and where they do not count
+    const float *inv, *top; // inverse scale of the columns' image, largest |g| (or NULL)
+    const float *weight;    // of the rows (or NULL), and where they do not count
     const int32_t *lab;
     float scale;
     bool vec;
@@ -731,7 +757,7 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_grads(GradOut first, GradOut se
     f32x4 acc[8][4];
     Product<NP>::run(A, B, (int64_t)mt * 2, (int64_t)nt * 2, min(a.per, a.units - split * a.per), lds, acc);
     const int m0 = mt * TILE + (wave >> 2) * 128 + 4 * g, n0 = nt * TILE + (wave & 3) * 64 + (a.permuted ? 4 * (l & 3) + (l >> 2) : l);
-    const float f = a.mode == 0 ? grad_factor<T>(a.absmax, a.gmax, a.scale) : 1.f;
+    const float f = a.mode == 0 ? grad_factor(*a.inv, a.top ? *a.top : 1.f, a.scale) : 1.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int n = n0 + 16 * j;
@@ -766,14 +792,14 @@ struct SlabSum {
     const float *slabs;
     int splits, blocks;
     int64_t count;
-    const uint32_t *absmax, *gmax;
+    const float *inv, *top;
     void *out;
 };
 // dbias of a piece: sums over the rows' parts, 64 centroids a workgroup, four waves taking the parts in turn
 struct BiasSum {
     const float *part;
     int slots, ld, count, blocks;
-    const uint32_t *gmax;
+    const float *top;
     bool add;
     float *out;
 };
@@ -788,7 +814,7 @@ __device__ __forceinline__ void bias_sum(int block, const BiasSum &a)
     sum[wave][lane] = s;
     __syncthreads();
     if (wave > 0 || j >= a.count) return;
-    s = ((sum[0][lane] + sum[1][lane]) + (sum[2][lane] + sum[3][lane])) * (__uint_as_float(*a.gmax) * (1.f / P_ONE));
+    s = ((sum[0][lane] + sum[1][lane]) + (sum[2][lane] + sum[3][lane])) * (*a.top * (1.f / P_ONE));
     a.out[j] = a.add ? a.out[j] + s : s;
 }
 
@@ -803,7 +829,7 @@ __global__ __launch_bounds__(256) void k_loss_sums(SlabSum x, SlabSum c, BiasSum
     const SlabSum &a = first ? x : c;
     const int64_t i = ((int64_t)(first ? blockIdx.x : blockIdx.x - x.blocks) * 256 + threadIdx.x) * 4;
     if (i >= a.count) return;
-    const float f = grad_factor<T>(a.absmax, a.gmax, scale);
+    const float f = grad_factor(*a.inv, a.top ? *a.top : 1.f, scale);
     const bool vec = a.count % 4 == 0 && (uintptr_t)a.out % (4 * sizeof(T)) == 0;
     const int count = (int)min((int64_t)4, a.count - i);
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
@@ -844,7 +870,7 @@ struct LossPlan {
     bool xslab, cslab;
     bool narrow;             // softmax_loss_narrow.hip
     int xper, cper;          // its tiles of a part
-    uint32_t *hdr;
+    LossHeader *hdr;
     u32x4 *ximg, *cimg, *xcols, *ccols, *pj, *pi;
     float *rinv, *cinv, *bias2, *mine, *gn, *dbpart, *xsum, *csum;
     f32x4 *row;
@@ -899,7 +925,7 @@ static LossPlan loss_plan(int dtype, int64_t n, int d, int k, bool backward, voi
         off += count * sizeof(*ptr);
     };
     const size_t page = (size_t)PAGE * p.np;
-    take(p.hdr, 4);
+    take(p.hdr, 1);
     take(p.ximg, p.npad / 128 * p.units * page);
     take(p.cimg, p.kpad / 128 * p.units * page);
     take(p.rinv, p.npad);
@@ -977,13 +1003,16 @@ static bool rows_vec(const void *p, int d)
 template <typename T, int NP>
 static void loss_images(const LossArgs &a, const LossPlan &p, bool backward, hipStream_t st)
 {
-    if (backward) hipLaunchKernelGGL(k_loss_begin, dim3(1), dim3(64), 0, st, p.hdr);
     PackArgs g = {a.x, a.c, a.n, a.d, a.k, p.units, a.label, a.bias, a.grad, backward ? a.stats : nullptr, a.scale, p.ximg, p.cimg,
                   p.xcols, p.ccols, p.rinv, p.cinv, p.gn, p.bias2, p.row, p.lab, p.hdr, rows_vec<T>(a.x, a.d), rows_vec<T>(a.c, a.d)};
     g.xblocks = (int)(p.npad / 16);
     g.cblocks = (int)(p.kpad / 16);
-    g.others = !backward ? 0 : (int)((a.n + 2047) / 2048 < 64 ? (a.n + 2047) / 2048 : 64);
-    hipLaunchKernelGGL((k_pack_rows<T, NP>), dim3((unsigned)(g.xblocks + g.cblocks + g.others)), dim3(256), 0, st, g);
+    const dim3 packs((unsigned)(g.xblocks + g.cblocks));
+    if (p.units <= 16)
+        hipLaunchKernelGGL((k_pack_rows<T, NP, 4>), packs, dim3(256), 0, st, g);
+    else
+        hipLaunchKernelGGL((k_pack_rows<T, NP, 16>), packs, dim3(256), 0, st, g);
+    if (backward) hipLaunchKernelGGL(k_loss_header, dim3(3), dim3(1024), 0, st, g);
     if (!backward) return;
     g.dblocks = p.dblocks;
     g.xunits = (int)(p.npad / 32);
@@ -1104,15 +1133,15 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
     const LossPlan p = loss_plan(a.dtype, a.n, a.d, a.k, true, a.ws);
     loss_images<T, NP>(a, p, true, st);
     auto bias_part = [&](int slots, int64_t ld, int64_t c0, int64_t count, bool add) {
-        return BiasSum{p.dbpart, slots, (int)ld, (int)count, (int)((count + 63) / 64), p.hdr + 2, add, a.dbias + c0};
+        return BiasSum{p.dbpart, slots, (int)ld, (int)count, (int)((count + 63) / 64), &p.hdr->top, add, a.dbias + c0};
     };
     auto finish = [&](const BiasSum &bias) {
-        auto side = [&](float *slabs, int splits, int64_t count, const uint32_t *absmax, const uint32_t *gmax, void *out) {
-            return SlabSum{slabs, splits, (int)((count + 1023) / 1024), count, absmax, gmax, out};
+        auto side = [&](float *slabs, int splits, int64_t count, const float *inv, const float *top, void *out) {
+            return SlabSum{slabs, splits, (int)((count + 1023) / 1024), count, inv, top, out};
         };
         SlabSum x = {}, c = {};
-        if (a.dx && p.xslab) x = side(p.xsum, p.xsplit, a.n * a.d, p.hdr + 1, nullptr, a.dx);
-        if (a.dc && p.cslab) c = side(p.csum, p.csplit, (int64_t)a.k * a.d, p.hdr, p.hdr + 2, a.dc);
+        if (a.dx && p.xslab) x = side(p.xsum, p.xsplit, a.n * a.d, &p.hdr->cinv, nullptr, a.dx);
+        if (a.dc && p.cslab) c = side(p.csum, p.csplit, (int64_t)a.k * a.d, &p.hdr->xinv, &p.hdr->top, a.dc);
         const int blocks = x.blocks + c.blocks + bias.blocks;
         if (blocks) hipLaunchKernelGGL(k_loss_sums<T>, dim3((unsigned)blocks), dim3(256), 0, st, x, c, bias, a.scale);
     };
@@ -1126,17 +1155,18 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
         g.gn = p.gn;
         g.cinv = p.cinv;
         g.bias2 = p.bias2;
+        g.hdr = p.hdr;
         g.dbpart = a.dbias ? p.dbpart : nullptr;
         g.kpad = (int)p.kpad;
         g.scale = a.scale;
         if (a.dx) {
             g.x = {p.ximg, p.cimg, p.ccols, (int)(p.npad / rows), (int)(p.kpad / 32), p.xsplit, p.xper, (int)a.n, p.xslab,
-                   p.xslab ? (void *)p.xsum : a.dx, p.hdr + 1, nullptr, a.grad, a.d % 4 == 0 && (p.xslab || (uintptr_t)a.dx % 16 == 0)};
+                   p.xslab ? (void *)p.xsum : a.dx, a.grad, a.d % 4 == 0 && (p.xslab || (uintptr_t)a.dx % 16 == 0)};
             g.nx = g.x.qblocks * g.x.splits;
         }
         if (a.dc || a.dbias)
             g.c = {p.cimg, p.ximg, p.xcols, (int)(p.kpad / rows), (int)(p.npad / 32), p.csplit, p.cper, a.k, p.cslab,
-                   !a.dc ? nullptr : p.cslab ? (void *)p.csum : a.dc, p.hdr, p.hdr + 2, nullptr,
+                   !a.dc ? nullptr : p.cslab ? (void *)p.csum : a.dc, nullptr,
                    a.d % 4 == 0 && (p.cslab || (uintptr_t)a.dc % 16 == 0)};
         LOSS_TRY((hipError_t)launch_loss_narrow(a.dtype, g, st));
         finish(a.dbias ? bias_part(p.csplit, p.kpad, 0, a.k, false) : BiasSum{});
@@ -1176,7 +1206,7 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
                 x.mode = p.xslab ? (c0 > 0 ? 2 : 1) : 0;
                 x.out = p.xslab ? (void *)(p.xsum + r0 * a.d) : (void *)((T *)a.dx + r0 * a.d);
                 x.slab = a.n * a.d;
-                x.absmax = p.hdr + 1;
+                x.inv = &p.hdr->cinv;
                 x.weight = a.grad + r0;
                 x.lab = p.lab + r0;
                 x.vec = vec && (p.xslab || (uintptr_t)a.dx % 16 == 0);
@@ -1196,8 +1226,8 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
                 c.mode = p.cslab ? (r0 > 0 ? 2 : 1) : 0;
                 c.out = p.cslab ? (void *)(p.csum + c0 * a.d) : (void *)((T *)a.dc + c0 * a.d);
                 c.slab = (int64_t)a.k * a.d;
-                c.absmax = p.hdr;
-                c.gmax = p.hdr + 2;
+                c.inv = &p.hdr->xinv;
+                c.top = &p.hdr->top;
                 c.vec = vec && (p.cslab || (uintptr_t)a.dc % 16 == 0);
             }
             x.d = c.d = a.d;

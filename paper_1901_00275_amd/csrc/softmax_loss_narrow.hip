@@ -255,7 +255,7 @@ __device__ __forceinline__ void narrow(const NarrowArgs &a, const NarrowSide &s,
         }
         return;
     }
-    const float factor = s.mode == 0 ? grad_factor<T>(s.absmax, s.gmax, a.scale) : 1.f;
+    const float factor = s.mode != 0 ? 1.f : CENT ? grad_factor(a.hdr->xinv, a.hdr->top, a.scale) : grad_factor(a.hdr->cinv, 1.f, a.scale);
     float *slab = (float *)s.out + (int64_t)split * s.rows * a.d;
 #pragma unroll
     for (int j = 0; j < QB; ++j) {
