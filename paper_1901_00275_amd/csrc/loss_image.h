@@ -46,14 +46,24 @@ __device__ __forceinline__ Eight<T> load8(const T *row, int i, int d, bool vec)
     return r;
 }
 
-// v as one or two fp16 parts
+// v as one or two fp16 parts.  The value is taken as it is in fp32: where it is a product, the compiler may otherwise round it to
+// fp16 in one step for the one use of hi and in two for the other, and hi and lo no longer fit together.
+template <int NP>
+__device__ __forceinline__ void halves(float v, _Float16 &hi, _Float16 &lo)
+{
+    if (NP == 2) asm("" : "+v"(v));
+    hi = (_Float16)v;
+    if (NP == 2) lo = (_Float16)(v - (float)hi);
+}
 template <int NP>
 __device__ __forceinline__ void split8(const float (&v)[8], half8 (&h)[NP])
 {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        h[0][e] = (_Float16)v[e];
-        if (NP == 2) h[NP - 1][e] = (_Float16)(v[e] - (float)h[0][e]);
+        _Float16 hi, lo;
+        halves<NP>(v[e], hi, lo);
+        h[0][e] = hi;
+        if (NP == 2) h[NP - 1][e] = lo;
     }
 }
 
@@ -91,8 +101,8 @@ __device__ __forceinline__ void store4(T *p, const f32x4 &v, int count, bool vec
 
 
 // ---- softmax_loss_narrow.hip ----
-// rows that a workgroup keeps
-constexpr int narrow_rows(int parts) { return parts == 2 ? 128 : 256; }
+// rows that a workgroup keeps: 256 halve the traffic of LDS where their sums and fragments fit the registers
+constexpr int narrow_rows(int parts, int units) { return parts == 2 || units == 4 ? 128 : 256; }
 struct NarrowSide {
     const u32x4 *q, *r, *rt; // images of the gradient's rows, of the other matrix's rows and columns
     int qblocks, tiles, splits, per; // workgroups side by side; tiles of the other matrix, in so many parts of `per`

@@ -29,7 +29,7 @@
 #define PIECE (1 << 26)      // values of P kept at a time
 #define NARROW_DIM 128       // up to so many dimensions the gradients take the narrow form (softmax_loss_narrow.hip)
 #define NARROW_GROUPS 1024   // its workgroups, about: two rounds of two a compute unit
-#define NARROW_LEAST 4       // tiles of 32 rows that a workgroup of it takes at least
+#define NARROW_LEAST 8       // tiles of 32 rows that a workgroup of it takes at least (forward half as many)
 #define FEW_ROWS 64          // up to so many rows the logits come from the centroids as they lie (k_loss_few)
 #define FEW_WIDE 65536       // from so many centroids on a wave takes 32 of them: then there are waves enough
 
@@ -687,8 +687,10 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_p(LogitArgs a)
             half4 h, lo;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                h[r] = (_Float16)v[r];
-                lo[r] = (_Float16)(v[r] - (float)h[r]);
+                _Float16 hi, rest;
+                halves<NP>(v[r], hi, rest);
+                h[r] = hi;
+                if (NP == 2) lo[r] = rest;
             }
             to[0] = __builtin_bit_cast(u32x2, h);
             if (NP == 2) to[PAGE * 2] = __builtin_bit_cast(u32x2, lo);
@@ -707,8 +709,10 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_p(LogitArgs a)
                 float v = acc[i][j][r] * row[j][3];
                 if (labels && rel[j] == 16 * i + r) v -= gn[j];
                 sum += v;
-                h[j] = (_Float16)v;
-                lo[j] = (_Float16)(v - (float)h[j]);
+                _Float16 hi, rest;
+                halves<NP>(v, hi, rest);
+                h[j] = hi;
+                if (NP == 2) lo[j] = rest;
             }
             u32x2 *to = a.pi + (((int64_t)(m0 >> 7) * a.iblock + ((n0 >> 5) + (l >> 3)) * NP) * PAGE + i * 64 +
                                 16 * ((l >> 1) & 3) + 4 * r + g) * 2 + (l & 1);
@@ -935,8 +939,8 @@ static LossPlan loss_plan(int dtype, int64_t n, int d, int k, bool backward, voi
     take(p.lab, p.npad);
     p.narrow = d <= NARROW_DIM;
     if (!backward && p.narrow) {
-        const int64_t xq = p.npad / narrow_rows(p.np), xt = p.kpad / 32, per = xq * xt / NARROW_GROUPS;
-        p.xsplit = narrow_parts(xt, per < NARROW_LEAST ? NARROW_LEAST : per, p.npad * 8, &p.xper);
+        const int64_t xq = p.npad / narrow_rows(p.np, p.units), xt = p.kpad / 32, per = xq * xt / NARROW_GROUPS;
+        p.xsplit = narrow_parts(xt, per < NARROW_LEAST / 2 ? NARROW_LEAST / 2 : per, p.npad * 8, &p.xper);
         take(p.mine, p.npad);
         take(p.part, p.xsplit * p.npad);
     } else if (!backward) {
@@ -948,7 +952,7 @@ static LossPlan loss_plan(int dtype, int64_t n, int d, int k, bool backward, voi
         take(p.xcols, p.npad / 32 * p.dblocks * page);
         take(p.ccols, p.kpad / 32 * p.dblocks * page);
         if (p.narrow) {
-            const int64_t rows = narrow_rows(p.np), xq = p.npad / rows, cq = p.kpad / rows, xt = p.kpad / 32, ct = p.npad / 32;
+            const int64_t rows = narrow_rows(p.np, p.units), xq = p.npad / rows, cq = p.kpad / rows, xt = p.kpad / 32, ct = p.npad / 32;
             int64_t per = (xq * xt + cq * ct) / NARROW_GROUPS;
             if (per < NARROW_LEAST) per = NARROW_LEAST;
             p.xsplit = narrow_parts(xt, per, n * d * 4, &p.xper);
@@ -1095,7 +1099,7 @@ static int loss_forward(const LossArgs &a, hipStream_t st)
     loss_images<T, NP>(a, p, false, st);
     if (p.narrow) {
         NarrowArgs g = {};
-        const int rows = narrow_rows(NP);
+        const int rows = narrow_rows(NP, p.units);
         g.units = p.units;
         g.d = a.d;
         g.row = p.row;
@@ -1147,7 +1151,7 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
     };
     if (p.narrow) {
         NarrowArgs g = {};
-        const int rows = narrow_rows(NP);
+        const int rows = narrow_rows(NP, p.units);
         g.units = p.units;
         g.d = a.d;
         g.row = p.row;

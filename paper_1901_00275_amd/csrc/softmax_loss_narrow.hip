@@ -18,7 +18,7 @@ enum { ROWS, CENTROIDS, STATS };
 template <typename T, int DU, int DO>
 __device__ __forceinline__ void narrow(const NarrowArgs &a, const NarrowSide &s, int b, u32x4 *lds)
 {
-    constexpr int NP = sizeof(T) == 4 ? 2 : 1, Q = narrow_rows(NP), QB = Q / 64, DB = 2 * DU;
+    constexpr int NP = sizeof(T) == 4 ? 2 : 1, Q = narrow_rows(NP, DU), QB = Q / 64, DB = 2 * DU;
     constexpr bool CENT = DO == CENTROIDS;
     constexpr int CHUNKS = (DO == STATS ? 2 : 4) * DU * NP; // KB of a tile: rows, then columns
     constexpr int STAGE = (CHUNKS + 2) * 64;        // and two KB for the rows' numbers, in 16-byte pieces
@@ -97,6 +97,7 @@ __device__ __forceinline__ void narrow(const NarrowArgs &a, const NarrowSide &s,
         const u32x4 *st = lds + (t & 1) * STAGE;
         const float *num = (const float *)(st + CHUNKS * 64);
         f32x4 S[2][QB];
+        __builtin_amdgcn_s_setprio(1); // (the products go first, another wave's arithmetic takes the slots between them)
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -123,6 +124,7 @@ __device__ __forceinline__ void narrow(const NarrowArgs &a, const NarrowSide &s,
 #pragma unroll
                 for (int j = 0; j < QB; ++j) S[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(r[0][i], qf[u][0][j], S[i][j], 0, 0, 0);
         }
+        __builtin_amdgcn_s_setprio(0);
         if constexpr (DO == STATS) {
             // a lane keeps the maximum and the sum of the logits that it has met of each of its rows
             const int base = 32 * t + 4 * g;
@@ -225,10 +227,13 @@ __device__ __forceinline__ void narrow(const NarrowArgs &a, const NarrowSide &s,
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const float v = S[i][j][r];
-                    P[0][j][4 * i + r] = (_Float16)v;
-                    if (NP == 2) P[NP - 1][j][4 * i + r] = (_Float16)(v - (float)P[0][j][4 * i + r]);
+                    _Float16 hi, lo;
+                    halves<NP>(v, hi, lo);
+                    P[0][j][4 * i + r] = hi;
+                    if (NP == 2) P[NP - 1][j][4 * i + r] = lo;
                     if (CENT) db[j] += v;
                 }
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int i = 0; i < DB; ++i) {
             half8 c[NP];
@@ -243,6 +248,7 @@ __device__ __forceinline__ void narrow(const NarrowArgs &a, const NarrowSide &s,
 #pragma unroll
             for (int j = 0; j < QB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(c[0], P[0][j], acc[i][j], 0, 0, 0);
         }
+        __builtin_amdgcn_s_setprio(0);
     }
 
     if constexpr (DO == STATS) {
