@@ -10,23 +10,20 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16_t;
 
 #define CLIP_NT 256
-#define CLIP_TENSORS 80    // tensors of a launch (their table is part of the arguments, which end at 4 KB)
+#define CLIP_TENSORS 140   // tensors of a launch (their table is part of the arguments, which end at 4 KB)
 #define CLIP_PARTS 8192    // up to so many sums are added up by every workgroup of the second launch
 #define CLIP_CHUNKS 4096   // chunks that the gradients are cut into, about
 #define CLIP_LEAST 8192    // values of a chunk at least
 
-struct ClipTensor {
-    const void *in;
-    void *out;
-    int64_t count;
-    int first; // its first chunk within the launch
-    int dtype;
-};
 struct ClipTable {
-    ClipTensor t[CLIP_TENSORS];
+    const void *in[CLIP_TENSORS];
+    void *out[CLIP_TENSORS];
+    int64_t count[CLIP_TENSORS]; // values, times four, plus the type
+    int first[CLIP_TENSORS];     // a tensor's first chunk within the launch
     int tensors, chunks;
     int64_t chunk; // values of a chunk
 };
+static_assert(sizeof(ClipTable) + 64 <= 4096, "the arguments of a launch");
 
 // the tensor of chunk b
 __device__ __forceinline__ int find_tensor(const ClipTable &a, int b)
@@ -34,7 +31,7 @@ __device__ __forceinline__ int find_tensor(const ClipTable &a, int b)
     int lo = 0, hi = a.tensors - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (a.t[mid].first <= b)
+        if (a.first[mid] <= b)
             lo = mid;
         else
             hi = mid - 1;
@@ -91,15 +88,16 @@ __device__ __forceinline__ double squares(const T *p, int64_t count)
 __global__ __launch_bounds__(CLIP_NT) void k_grad_squares(ClipTable a, double *part)
 {
     const int b = blockIdx.x, t = find_tensor(a, b);
-    const ClipTensor &g = a.t[t];
-    const int64_t i0 = (int64_t)(b - g.first) * a.chunk, count = min(a.chunk, g.count - i0);
+    const void *in = a.in[t];
+    const int dtype = (int)(a.count[t] & 3);
+    const int64_t i0 = (int64_t)(b - a.first[t]) * a.chunk, count = min(a.chunk, (a.count[t] >> 2) - i0);
     double s;
-    if (g.dtype == VLQ_F32)
-        s = squares((const float *)g.in + i0, count);
-    else if (g.dtype == VLQ_F16)
-        s = squares((const _Float16 *)g.in + i0, count);
+    if (dtype == VLQ_F32)
+        s = squares((const float *)in + i0, count);
+    else if (dtype == VLQ_F16)
+        s = squares((const _Float16 *)in + i0, count);
     else
-        s = squares((const bf16_t *)g.in + i0, count);
+        s = squares((const bf16_t *)in + i0, count);
     s = block_sum(s);
     if (threadIdx.x == 0) part[b] = s;
 }
@@ -154,15 +152,17 @@ __global__ __launch_bounds__(CLIP_NT) void k_grad_scale(ClipTable a, const doubl
     // (a norm that is not finite leaves the gradients as they are)
     const float f = n > (double)max_norm && n < INFINITY ? (float)((double)max_norm / n) : 1.f;
     const int b = a.chunks - 1 - blockIdx.x, t = find_tensor(a, b);
-    const ClipTensor &g = a.t[t];
-    if (f == 1.f && g.in == g.out) return;
-    const int64_t i0 = (int64_t)(b - g.first) * a.chunk, count = min(a.chunk, g.count - i0);
-    if (g.dtype == VLQ_F32)
-        scale_values((const float *)g.in + i0, (float *)g.out + i0, count, f);
-    else if (g.dtype == VLQ_F16)
-        scale_values((const _Float16 *)g.in + i0, (_Float16 *)g.out + i0, count, f);
+    const void *in = a.in[t];
+    void *out = a.out[t];
+    if (f == 1.f && in == out) return;
+    const int dtype = (int)(a.count[t] & 3);
+    const int64_t i0 = (int64_t)(b - a.first[t]) * a.chunk, count = min(a.chunk, (a.count[t] >> 2) - i0);
+    if (dtype == VLQ_F32)
+        scale_values((const float *)in + i0, (float *)out + i0, count, f);
+    else if (dtype == VLQ_F16)
+        scale_values((const _Float16 *)in + i0, (_Float16 *)out + i0, count, f);
     else
-        scale_values((const bf16_t *)g.in + i0, (bf16_t *)g.out + i0, count, f);
+        scale_values((const bf16_t *)in + i0, (bf16_t *)out + i0, count, f);
 }
 
 static int64_t clip_chunk(int tensors, const int64_t *counts)
@@ -205,7 +205,10 @@ int launch_clip_grads(int tensors, const int *dtypes, const int64_t *counts, con
             int first = 0;
             for (int i = 0; i < a.tensors; ++i) {
                 const int t = picked[back ? a.tensors - 1 - i : i];
-                a.t[i] = {in[t], out ? out[t] : nullptr, counts[t], first, dtypes[t]};
+                a.in[i] = in[t];
+                a.out[i] = out ? out[t] : nullptr;
+                a.count[i] = counts[t] * 4 + dtypes[t];
+                a.first[i] = first;
                 first += (int)((counts[t] + chunk - 1) / chunk);
             }
             a.chunks = first;

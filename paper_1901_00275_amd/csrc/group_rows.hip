@@ -59,6 +59,7 @@ __global__ __launch_bounds__(GNT) void k_group_count(SortPass a)
     __syncthreads();
     const int64_t i0 = (int64_t)blockIdx.x * a.tile;
     const int count = (int)(a.pairs - i0 < a.tile ? a.pairs - i0 : a.tile);
+#pragma unroll 8
     for (int i = threadIdx.x; i < count; i += GNT) atomicAdd(&h[(key_at(a, i0 + i) >> a.shift) & (bins - 1)], 1u);
     __syncthreads();
     for (int b = threadIdx.x; b < bins; b += GNT) a.count[(int64_t)b * a.tiles + blockIdx.x] = h[b];
@@ -110,14 +111,26 @@ __device__ __forceinline__ void block_scan(uint32_t *v, int bins, uint32_t *wsum
     __syncthreads();
 }
 
-// The pairs of a wave (i0 .. i0 + count) to their places: at[digit] is the next place of a digit, kept up by the wave alone
-__device__ __forceinline__ void place_pairs(const SortPass &a, uint32_t *at, int64_t i0, int count, int lane)
+// The pairs of a wave (i0 .. i0 + count) to their places, HELD at a time: their keys, and where they have moved already the
+// pairs themselves, are asked for together.  at[digit] is the next place of a digit, kept up by the wave alone.
+#define HELD 8
+__device__ __forceinline__ void hold(const SortPass &a, int64_t i0, int count, int lane, uint32_t (&key)[HELD], uint32_t (&pair)[HELD])
+{
+#pragma unroll
+    for (int u = 0; u < HELD; ++u)
+        if (u * 64 + lane < count) {
+            key[u] = key_at(a, i0 + u * 64 + lane);
+            pair[u] = a.cell ? (uint32_t)(i0 + u * 64 + lane) : a.pair[i0 + u * 64 + lane];
+        }
+}
+__device__ __forceinline__ void place_held(const SortPass &a, uint32_t *at, int count, int lane, const uint32_t (&key)[HELD], const uint32_t (&pair)[HELD])
 {
     const uint64_t below = ((uint64_t)1 << lane) - 1;
-    for (int i = 0; i < count; i += 64) {
-        const bool there = i + lane < count;
-        const int64_t id = i0 + i + lane;
-        const uint32_t key = there ? key_at(a, id) : 0, digit = (key >> a.shift) & ((1u << a.bits) - 1);
+#pragma unroll
+    for (int u = 0; u < HELD; ++u) {
+        if (u * 64 >= count) break;
+        const bool there = u * 64 + lane < count;
+        const uint32_t digit = there ? (key[u] >> a.shift) & ((1u << a.bits) - 1) : 0;
         const uint64_t same = same_digit(digit, a.bits, there);
         uint32_t p = 0;
         if (there) p = at[digit] + __popcll(same & below);
@@ -125,16 +138,23 @@ __device__ __forceinline__ void place_pairs(const SortPass &a, uint32_t *at, int
         if (there && !(same & below)) at[digit] += __popcll(same);
         wave_lds_order();
         if (!there) continue;
-        const uint32_t pair = a.cell ? (uint32_t)id : a.pair[id];
         if (!a.last) {
-            a.key_out[p] = key;
-            a.pair_out[p] = pair;
+            a.key_out[p] = key[u];
+            a.pair_out[p] = pair[u];
         } else {
-            const bool in = key < (uint32_t)a.cells;
-            a.source[p] = in ? (int32_t)pair : -1;
-            a.place[pair] = in ? (int32_t)p : -1;
-            if (!a.only) a.key_out[p] = key;
+            const bool in = key[u] < (uint32_t)a.cells;
+            a.source[p] = in ? (int32_t)pair[u] : -1;
+            a.place[pair[u]] = in ? (int32_t)p : -1;
+            if (!a.only) a.key_out[p] = key[u];
         }
+    }
+}
+__device__ __forceinline__ void place_pairs(const SortPass &a, uint32_t *at, int64_t i0, int count, int lane)
+{
+    uint32_t key[HELD], pair[HELD];
+    for (int i = 0; i < count; i += HELD * 64) {
+        hold(a, i0 + i, count - i, lane, key, pair);
+        place_held(a, at, count - i, lane, key, pair);
     }
 }
 
@@ -142,6 +162,11 @@ __global__ __launch_bounds__(GNT) void k_group_place(SortPass a)
 {
     __shared__ uint32_t first[BINS], at[GWAVES][BINS], wsum[GWAVES];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, bins = 1 << a.bits;
+    uint32_t key[HELD], pair[HELD]; // the wave's first pairs, asked for before all else
+    {
+        const int64_t w0 = (int64_t)blockIdx.x * a.tile + wave * (a.tile / GWAVES);
+        hold(a, w0, (int)max((int64_t)0, min((int64_t)(a.tile / GWAVES), a.pairs - w0)), lane, key, pair);
+    }
     for (int b = tid; b < bins; b += GNT) {
         first[b] = a.total[b];
         for (int w = 0; w < GWAVES; ++w) at[w][b] = 0;
@@ -152,7 +177,10 @@ __global__ __launch_bounds__(GNT) void k_group_place(SortPass a)
         for (int b = tid; b <= a.cells; b += GNT) a.off[b] = first[b];
     const int64_t i0 = (int64_t)blockIdx.x * a.tile;
     const int per = a.tile / GWAVES, count = (int)max((int64_t)0, min((int64_t)per, a.pairs - i0 - wave * per));
-    for (int i = lane; i < count; i += 64) atomicAdd(&at[wave][(key_at(a, i0 + wave * per + i) >> a.shift) & (bins - 1)], 1u);
+    for (int i = HELD * 64 + lane; i < count; i += 64) atomicAdd(&at[wave][(key_at(a, i0 + wave * per + i) >> a.shift) & (bins - 1)], 1u);
+#pragma unroll
+    for (int u = 0; u < HELD; ++u)
+        if (u * 64 + lane < count) atomicAdd(&at[wave][(key[u] >> a.shift) & (bins - 1)], 1u);
     __syncthreads();
     for (int b = tid; b < bins; b += GNT) {
         uint32_t next = first[b] + a.count[(int64_t)b * a.tiles + blockIdx.x];
@@ -163,7 +191,8 @@ __global__ __launch_bounds__(GNT) void k_group_place(SortPass a)
         }
     }
     __syncthreads();
-    place_pairs(a, at[wave], i0 + wave * per, count, lane);
+    place_held(a, at[wave], count, lane, key, pair);
+    if (count > HELD * 64) place_pairs(a, at[wave], i0 + wave * per + HELD * 64, count - HELD * 64, lane);
 }
 
 // Few pairs, few cells: one workgroup, one launch
@@ -239,7 +268,7 @@ static GroupPlan group_plan(int64_t pairs, int cells)
     }
     p.small = p.passes == 1 && pairs <= SMALL_PAIRS;
     // tiles: enough of them for every compute unit, large enough that the counts are fewer than the pairs
-    p.tile = 1024;
+    p.tile = GWAVES * HELD * 64 / 2;
     while (p.tile < 8192 && pairs / p.tile > 512) p.tile *= 2;
     p.tiles = (int)((pairs + p.tile - 1) / p.tile);
     size_t off = 0;
@@ -337,7 +366,7 @@ template <typename T, bool VEC>
 __device__ __forceinline__ void store_piece(T *p, const Piece<T, VEC> &r)
 {
     if constexpr (VEC)
-        *(u32x4 *)p = *(const u32x4 *)r.v;
+        __builtin_nontemporal_store(*(const u32x4 *)r.v, (u32x4 *)p);
     else
         *p = r.v[0];
 }
