@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from array import array
 
 import torch
 
@@ -250,16 +251,16 @@ def _ptrs(*pairs):
         if t is None:
             out.append(None)
             continue
-        if not t.is_cuda or not t.is_contiguous():
-            raise ValueError("tensors passed to libvlq must be contiguous device tensors")
-        if dev is None:
+        if dev is None and t.is_cuda:
             dev = torch.cuda.current_device()
-        if t.get_device() != dev:
-            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
-        if dtype is not None and t.dtype != dtype:
+        if t.get_device() != dev or not t.is_contiguous() or t.numel() < count or not (dtype is None or t.dtype is dtype):
+            if not t.is_cuda or not t.is_contiguous():
+                raise ValueError("tensors passed to libvlq must be contiguous device tensors")
+            if t.get_device() != dev:
+                raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
+            if t.numel() < count:
+                raise ValueError(f"a tensor has {t.numel()} values, {count} are needed")
             raise ValueError(f"expected {dtype}, got {t.dtype}")
-        if t.numel() < count:
-            raise ValueError(f"a tensor has {t.numel()} values, {count} are needed")
         out.append(t.data_ptr())
     return out
 
@@ -325,27 +326,27 @@ def vlq_combine_rows_backward(d_dout, d_y, n, w, d, d_place, d_weight, d_dy, d_d
 
 
 def vlq_clip_grads_workspace(grads) -> int:
-    counts = (C.c_int64 * max(1, len(grads)))(*[g.numel() for g in grads])
-    return _bytes(lib().vlq_clip_grads_workspace(len(grads), counts))
+    counts = array("q", [g.numel() for g in grads])
+    return _bytes(lib().vlq_clip_grads_workspace(len(grads), counts.buffer_info()[0]))
 
 
 def vlq_clip_grads(d_grads, max_norm, d_out, d_norm, d_ws, stream=None):
     """d_grads: a list of tensors; d_out: a list as long (its tensors may be those of d_grads), or None for the norm alone."""
-    n = len(d_grads)
-    many = max(1, n)
-    counts, dtypes, ptrs = (C.c_int64 * many)(), (C.c_int32 * many)(), (C.c_void_p * many)()
-    outs = None if d_out is None else (C.c_void_p * many)()
-    if d_out is not None and len(d_out) != n:
-        raise ValueError("d_out must have a tensor for every tensor of d_grads")
     norm, ws = _ptrs((d_norm, torch.float32, 1), (d_ws, torch.uint8, 0))
     dev = d_ws.get_device()
-    for i, g in enumerate(d_grads):
-        if not g.is_cuda or not g.is_contiguous() or g.get_device() != dev or g.dtype not in _TYPES:
+    counts = array("q", [g.numel() for g in d_grads])
+    types = array("i", [_TYPES.get(g.dtype, -1) for g in d_grads])
+    for g in d_grads:
+        if g.get_device() != dev or not g.is_contiguous() or g.dtype not in _TYPES:
             raise ValueError("gradients must be contiguous float32, float16 or bfloat16 tensors on the current device")
-        counts[i], dtypes[i], ptrs[i] = g.numel(), _TYPES[g.dtype], g.data_ptr()
-        if outs is not None:
-            o = d_out[i]
-            if o is not g and (not o.is_cuda or not o.is_contiguous() or o.get_device() != dev or o.dtype != g.dtype or o.numel() != counts[i]):
-                raise ValueError("d_out must have a contiguous tensor of the same type, size and device for every tensor of d_grads")
-            outs[i] = o.data_ptr()
-    _chk(lib().vlq_clip_grads(n, dtypes, counts, ptrs, float(max_norm), outs, norm, ws, d_ws.numel(), _stream(stream)))
+    ptrs, outs = array("Q", [g.data_ptr() for g in d_grads]), None
+    if d_out is not None:
+        if len(d_out) != len(d_grads):
+            raise ValueError("d_out must have a tensor for every tensor of d_grads")
+        if d_out is not d_grads:
+            for g, o in zip(d_grads, d_out):
+                if o.dtype is not g.dtype or o.get_device() != dev or not o.is_contiguous() or o.numel() != g.numel():
+                    raise ValueError("d_out must have a contiguous tensor of the same type, size and device for every tensor of d_grads")
+        outs = array("Q", [o.data_ptr() for o in d_out])
+    _chk(lib().vlq_clip_grads(len(d_grads), types.buffer_info()[0], counts.buffer_info()[0], ptrs.buffer_info()[0], float(max_norm),
+                              None if outs is None else outs.buffer_info()[0], norm, ws, d_ws.numel(), _stream(stream)))
