@@ -30,8 +30,16 @@
 #define NARROW_DIM 128       // up to so many dimensions the gradients take the narrow form (softmax_loss_narrow.hip)
 #define NARROW_GROUPS 1024   // its workgroups, about: two rounds of two a compute unit
 #define NARROW_LEAST 8       // tiles of 32 rows that a workgroup of it takes at least (forward half as many)
-#define FEW_ROWS 64          // up to so many rows the logits come from the centroids as they lie (k_loss_few)
+// The logits come from the centroids as they lie (k_loss_few) where little is done with each: rewriting them first, and tiles that
+// leave most of the chip idle, cost more.  Measured in us, these against the others: 1 000 x 1 000 x 1 000 bf16 20 : 38,
+// 8 000 x 120 x 500 fp32 36 : 54, 8 000 x 120 x 1 000 bf16 25 : 45, 535 x 975 x 1 248 fp32 75 : 85, 128 x 65 536 x 64 fp16 22 : 31;
+// the narrow form holds out longer: 1 000 x 5 000 x 96 fp32 39 : 19, 2 000 x 5 000 x 96 bf16 26 : 20, 70 x 65 536 x 96 fp32 39 : 41.
+#define FEW_ROWS 64
+#define FEW_WORK 1e9          // products
+#define FEW_NARROW_ROWS 128   // up to NARROW_DIM dimensions
+#define FEW_NARROW_WORK 1.2e8
 #define FEW_WIDE 65536       // from so many centroids on a wave takes 32 of them: then there are waves enough
+#define FEW_GROUPS 512       // with fewer workgroups of eight waves they have two
 
 // ---------------------------------------------------------------------------
 // images
@@ -513,9 +521,10 @@ __global__ __launch_bounds__(256) void k_loss_merge(const float2 *part, int part
     if (loss) loss[i] = (uint32_t)lab[i] >= (uint32_t)k ? 0.f : m == -INFINITY ? INFINITY : LN2 * (m - mine[i]) + logf(z);
 }
 
-// Few rows: every wave multiplies 16 G centroids, read once from where they lie, with all rows (NT tiles of 16), eight waves
-// a workgroup; 16-bit values on their own matrix instructions, fp32 on the fp32 ones (a read of 4 bytes needs 16 NT
-// multiplications, which these do in time up to NT = 4).  Nothing is rewritten first, so the centroids pass once; bound by that.
+// Few rows, or little work: every wave multiplies 16 G centroids, read from where they lie, with up to 64 rows (NT tiles of 16),
+// two or eight waves a workgroup; 16-bit values on their own matrix instructions, fp32 on the fp32 ones (a read of 4 bytes needs 16 NT
+// multiplications, which these do in time up to NT = 4).  Nothing is rewritten first; up to 64 rows the centroids pass once and
+// bound it (65 536 x 1 024 bf16, one row: 25 us, 5.4 TB/s), beyond that the rows' fragments from the caches do.
 struct FewArgs {
     const void *x, *c;
     const float *bias;
@@ -559,13 +568,12 @@ __device__ __forceinline__ void few_multiply(const FewPiece<bf16_t> &a, const Fe
     acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8 *)a.v, *(const bf16x8 *)b.v, acc, 0, 0, 0);
 }
 
-#define FEW_WAVES 8
-template <typename T, bool VEC, int G, int NT>
-__global__ __launch_bounds__(FEW_WAVES * 64) void k_loss_few(FewArgs a)
+template <typename T, bool VEC, int W, int G, int NT>
+__global__ __launch_bounds__(W * 64) void k_loss_few(FewArgs a)
 {
     constexpr int STEP = FewPiece<T>::STEP, N = FewPiece<T>::N, U = 16 / (G + NT) < 2 ? 2 : 16 / (G + NT);
     const int tid = threadIdx.x, lane = tid & 63, l = lane & 15, g = lane >> 4, wave = tid >> 6;
-    const int m0 = (blockIdx.x * FEW_WAVES + wave) * 16 * G;
+    const int m0 = (blockIdx.x * W + wave) * 16 * G, n0 = blockIdx.y * 16 * NT;
     const T *crow[G], *xrow[NT];
     bool cin[G], xin[NT];
     f32x4 acc[G][NT];
@@ -576,8 +584,8 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_loss_few(FewArgs a)
     }
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
-        xin[j] = 16 * j + l < a.n;
-        xrow[j] = (const T *)a.x + (int64_t)(xin[j] ? 16 * j + l : 0) * a.d;
+        xin[j] = n0 + 16 * j + l < a.n;
+        xrow[j] = (const T *)a.x + (int64_t)(xin[j] ? n0 + 16 * j + l : 0) * a.d;
 #pragma unroll
         for (int i = 0; i < G; ++i) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -597,10 +605,10 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_loss_few(FewArgs a)
 #pragma unroll
                 for (int j = 0; j < NT; ++j) few_multiply(cv[u][i], xv[u][j], acc[i][j]);
     }
-    __shared__ float2 s[FEW_WAVES][16 * NT];
+    __shared__ float2 s[W][16 * NT];
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
-        const int n = 16 * j + l, lab = n < a.n ? a.label[n] : -1;
+        const int n = n0 + 16 * j + l, lab = n < a.n ? a.label[n] : -1;
         float m = -INFINITY, z = 0.f;
 #pragma unroll
         for (int i = 0; i < G; ++i)
@@ -622,14 +630,14 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_loss_few(FewArgs a)
             for (int r = 0; r < 4; ++r) z += __builtin_amdgcn_exp2f(acc[i][j][r] - m1);
         z += __shfl_xor(z, 16, 64);
         z += __shfl_xor(z, 32, 64);
-        if (g == 0) s[wave][n] = make_float2(m, z);
+        if (g == 0) s[wave][16 * j + l] = make_float2(m, z);
     }
     __syncthreads();
-    if (tid >= 16 * NT || tid >= a.n) return;
+    if (tid >= 16 * NT || n0 + tid >= a.n) return;
     float2 v = s[0][tid];
 #pragma unroll
-    for (int w = 1; w < FEW_WAVES; ++w) v = join(v, s[w][tid]);
-    a.part[(int64_t)blockIdx.x * a.n + tid] = v;
+    for (int w = 1; w < W; ++w) v = join(v, s[w][tid]);
+    a.part[(int64_t)blockIdx.x * a.n + n0 + tid] = v;
 }
 
 // Backward: P of a tile, as images in both orders, and the sums over a wave's 64 rows for the bias
@@ -906,6 +914,12 @@ static int narrow_parts(int64_t tiles, int64_t per, int64_t out_bytes, int *tile
     return (int)((tiles + each - 1) / each);
 }
 
+static bool loss_is_few(int64_t n, int d, int k)
+{
+    const double work = (double)n * d * k;
+    return n <= FEW_ROWS || (d <= NARROW_DIM ? n <= FEW_NARROW_ROWS || work <= FEW_NARROW_WORK : work <= FEW_WORK);
+}
+
 static LossPlan loss_plan(int dtype, int64_t n, int d, int k, bool backward, void *ws)
 {
     LossPlan p = {};
@@ -981,7 +995,7 @@ static LossPlan loss_plan(int dtype, int64_t n, int d, int k, bool backward, voi
 
 size_t loss_workspace(int dtype, int64_t n, int d, int k, bool backward)
 {
-    if (!backward && n <= FEW_ROWS) return ((size_t)(k / (FEW_WAVES * 16) + 1) * 8 + 4) * (n < 1 ? 1 : n);
+    if (!backward && loss_is_few(n, d, k)) return ((size_t)(k / 32 + 1) * 8 + 4) * (n < 1 ? 1 : n);
     return loss_plan(dtype, n, d, k, backward, nullptr).bytes;
 }
 
@@ -1061,27 +1075,34 @@ static void launch_merge(const float2 *part, int parts, int npad, const float *m
 template <typename T>
 static int loss_few(const LossArgs &a, hipStream_t st)
 {
-    const bool wide = a.k >= FEW_WIDE;
-    const int groups = (a.k + FEW_WAVES * (wide ? 32 : 16) - 1) / (FEW_WAVES * (wide ? 32 : 16));
+    // two waves a workgroup where eight would leave compute units without one; eight with twice the centroids each where
+    // there are plenty
+    const int64_t rows64 = (a.n + 63) / 64;
+    const bool wide = a.k >= FEW_WIDE, small = (a.k + 127) / 128 * rows64 < FEW_GROUPS;
+    const int each = small ? 32 : wide ? 256 : 128, groups = (a.k + each - 1) / each;
     float2 *part = (float2 *)a.ws;
     float *mine = (float *)(part + (int64_t)groups * a.n);
     const FewArgs f = {a.x, a.c, a.bias, a.label, a.scale * LOG2E, (int)a.n, a.d, a.k, part, mine};
-    auto go = [&](auto VEC, auto G, auto NT) {
-        hipLaunchKernelGGL((k_loss_few<T, decltype(VEC)::value, decltype(G)::value, decltype(NT)::value>), dim3(groups), dim3(FEW_WAVES * 64), 0, st, f);
+    auto go = [&](auto VEC, auto W, auto G, auto NT) {
+        constexpr int R = 16 * decltype(NT)::value;
+        hipLaunchKernelGGL((k_loss_few<T, decltype(VEC)::value, decltype(W)::value, decltype(G)::value, decltype(NT)::value>),
+                           dim3(groups, (unsigned)((a.n + R - 1) / R)), dim3(decltype(W)::value * 64), 0, st, f);
     };
-    auto rows = [&](auto VEC, auto G) {
+    auto rows = [&](auto VEC, auto W, auto G) {
         if (a.n <= 16)
-            go(VEC, G, std::integral_constant<int, 1>{});
+            go(VEC, W, G, std::integral_constant<int, 1>{});
         else if (a.n <= 32)
-            go(VEC, G, std::integral_constant<int, 2>{});
+            go(VEC, W, G, std::integral_constant<int, 2>{});
         else
-            go(VEC, G, std::integral_constant<int, 4>{});
+            go(VEC, W, G, std::integral_constant<int, 4>{});
     };
     auto cells = [&](auto VEC) {
-        if (wide)
-            rows(VEC, std::integral_constant<int, 2>{});
+        if (small)
+            rows(VEC, std::integral_constant<int, 2>{}, std::integral_constant<int, 1>{});
+        else if (wide)
+            rows(VEC, std::integral_constant<int, 8>{}, std::integral_constant<int, 2>{});
         else
-            rows(VEC, std::integral_constant<int, 1>{});
+            rows(VEC, std::integral_constant<int, 8>{}, std::integral_constant<int, 1>{});
     };
     if (a.d * sizeof(T) % 16 == 0 && ((uintptr_t)a.x | (uintptr_t)a.c) % 16 == 0)
         cells(std::true_type{});
@@ -1094,7 +1115,7 @@ static int loss_few(const LossArgs &a, hipStream_t st)
 template <typename T, int NP>
 static int loss_forward(const LossArgs &a, hipStream_t st)
 {
-    if (a.n <= FEW_ROWS) return loss_few<T>(a, st);
+    if (loss_is_few(a.n, a.d, a.k)) return loss_few<T>(a, st);
     const LossPlan p = loss_plan(a.dtype, a.n, a.d, a.k, false, a.ws);
     loss_images<T, NP>(a, p, false, st);
     if (p.narrow) {

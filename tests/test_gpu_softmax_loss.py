@@ -56,7 +56,7 @@ def compare(got, want, names=("loss", "dx", "dc", "db")):
 
 
 SHAPES = [(1, 1, 1), (1, 96, 300), (3, 7, 2), (64, 32, 256), (65, 33, 257), (255, 96, 1000), (257, 128, 513), (300, 130, 1025),
-          (40, 520, 77), (17, 1027, 515), (1000, 64, 5000), (33, 48, 65537), (9, 200, 70001)]
+          (40, 520, 77), (17, 1027, 515), (1000, 64, 5000), (33, 48, 65537), (9, 200, 70001), (129, 100, 9000), (700, 136, 1100), (2100, 500, 1001)]
 
 
 @pytest.mark.parametrize("t", [F32, F16, BF16])
