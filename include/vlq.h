@@ -304,7 +304,8 @@ enum {
  * fp32 values enter the products as two fp16 parts, off by 2^-23 of themselves, or 2^-40 of the largest in their row (of x) or
  * in their 128 consecutive centroids; bf16 values exactly down to 2^-32 of that.
  * 0 <= n < 2^31, 1 <= d <= VLQ_MAX_LOSS_DIM, 1 <= k <= VLQ_MAX_LOSS_CLASSES; n = 0 is a no-op.
- * d_ws: at least vlq_softmax_loss_workspace(dtype, n, d, k, 0) bytes, ws_bytes its size.
+ * d_stats of rows that do not count are unspecified.
+ * d_ws: at least vlq_softmax_loss_workspace(dtype, n, d, k, 0) bytes, ws_bytes its size (a smaller n may need more: ask for each).
  */
 int vlq_softmax_loss(int dtype, const void *d_x, int64_t n, int32_t d, const void *d_c, int32_t k,
                      const float *d_bias, float scale, const int32_t *d_label, float *d_loss, float *d_stats,

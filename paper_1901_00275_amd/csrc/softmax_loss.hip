@@ -56,7 +56,8 @@ __device__ __forceinline__ bool row_counts(const int32_t *label, int k, const fl
 // scale, beyond that they are read again.  Bound by memory.  (128 MB with 128 rows a workgroup and a scale for all of them:
 // 99 us, for want of loads under way; 238 MB of rows of 64 units read twice 138 us, what a die's workgroups hold is more
 // than its L2.)
-template <typename T, bool OWN, int NP, int HELD>
+// RAW: the image of the values' own bits (the scale is found all the same); pages NULL: only the scale.
+template <typename T, bool OWN, int NP, int HELD, bool RAW>
 __device__ __forceinline__ void pack_rows(int block, const T *__restrict__ X, int64_t rows, int d, int units,
                                           const int32_t *__restrict__ label, int k, const float *__restrict__ bias,
                                           u32x4 *__restrict__ pages, float *__restrict__ inv, bool vec)
@@ -107,6 +108,7 @@ __device__ __forceinline__ void pack_rows(int block, const T *__restrict__ X, in
         else if (tid == 0)
             inv[block] = pow2i(-ex);
     }
+    if (!pages) return;
     const float s = pow2i(ex);
     u32x4 *to = pages + (int64_t)(block >> 3) * units * NP * PAGE + (block & 7) * 64 + lane;
     for (int u0 = 0; u0 < units; u0 += 4 * HELD) {
@@ -115,13 +117,17 @@ __device__ __forceinline__ void pack_rows(int block, const T *__restrict__ X, in
         for (int q = 0; q < HELD; ++q) {
             const int u = u0 + 4 * q + wave;
             if (u >= units) continue;
-            float f[8];
+            if constexpr (RAW) {
+                to[(int64_t)u * PAGE] = counts ? *(const u32x4 *)v[q].v : u32x4{0, 0, 0, 0};
+            } else {
+                float f[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = counts ? (float)v[q].v[e] * s : 0.f;
-            half8 h[NP];
-            split8<NP>(f, h);
+                for (int e = 0; e < 8; ++e) f[e] = counts ? (float)v[q].v[e] * s : 0.f;
+                half8 h[NP];
+                split8<NP>(f, h);
 #pragma unroll
-            for (int p = 0; p < NP; ++p) to[(int64_t)(u * NP + p) * PAGE] = __builtin_bit_cast(u32x4, h[p]);
+                for (int p = 0; p < NP; ++p) to[(int64_t)(u * NP + p) * PAGE] = __builtin_bit_cast(u32x4, h[p]);
+            }
         }
     }
 }
@@ -204,7 +210,7 @@ struct PackArgs {
     f32x4 *row;
     int32_t *lab;
     LossHeader *hdr;
-    bool xvec, cvec;
+    bool xvec, cvec, raw, halves;
     int xblocks, cblocks, dblocks, xunits, cunits; // workgroups for x, for c; units of the columns' images
 };
 
@@ -213,7 +219,7 @@ struct PackArgs {
 __device__ __forceinline__ void row_numbers(const PackArgs &a, int64_t i, float inv)
 {
     const bool in = i < a.n && (uint32_t)a.label[i] < (uint32_t)a.k;
-    f32x4 r = {in ? a.scale * LOG2E * inv : 0.f, INFINITY, 0.f, 0.f};
+    f32x4 r = {in ? a.scale * LOG2E * (a.raw ? 1.f : inv) : 0.f, INFINITY, 0.f, 0.f};
     float f = 0.f;
     bool ok = in;
     if (a.stats && in) {
@@ -233,18 +239,19 @@ __device__ __forceinline__ void row_numbers(const PackArgs &a, int64_t i, float 
     if (a.gn) a.gn[i] = ok ? f * P_ONE : 0.f;
 }
 
-// Both matrices' images in one launch; forward the rows' numbers
-template <typename T, int NP, int HELD>
+// Both matrices' images in one launch; forward the rows' numbers.  RAW: x's image of its own bits, of c only what is asked for
+// (cimg NULL, cinv: its scales).
+template <typename T, int NP, int HELD, bool RAW>
 __global__ __launch_bounds__(256) void k_pack_rows(PackArgs a)
 {
     const int b = blockIdx.x - a.xblocks;
     if (b >= 0) {
         const int j = b * 16 + threadIdx.x; // the bias in units of log 2, -inf past the last centroid
         if (threadIdx.x < 16) a.bias2[j] = j < a.k ? (a.bias ? a.bias[j] * LOG2E : 0.f) : -INFINITY;
-        pack_rows<T, false, NP, HELD>(b, (const T *)a.c, a.k, a.d, a.units, nullptr, a.k, a.bias, a.cimg, a.cinv, a.cvec);
+        if (a.cinv) pack_rows<T, false, NP, HELD, RAW>(b, (const T *)a.c, a.k, a.d, a.units, nullptr, a.k, a.bias, a.cimg, a.cinv, a.cvec);
         return;
     }
-    pack_rows<T, true, NP, HELD>(blockIdx.x, (const T *)a.x, a.n, a.d, a.units, a.label, a.k, nullptr, a.ximg, a.rinv, a.xvec);
+    pack_rows<T, true, NP, HELD, RAW>(blockIdx.x, (const T *)a.x, a.n, a.d, a.units, a.label, a.k, nullptr, a.ximg, a.rinv, a.xvec);
     if (a.stats) return;
     __syncthreads();
     if (threadIdx.x < 16) row_numbers(a, (int64_t)blockIdx.x * 16 + threadIdx.x, a.rinv[(int64_t)blockIdx.x * 16 + threadIdx.x]);
@@ -264,7 +271,7 @@ __global__ __launch_bounds__(1024) void k_loss_header(PackArgs a)
         }
     } else {
         const float *v = blockIdx.x == 0 ? a.rinv : a.cinv;
-        const int64_t count = (int64_t)(blockIdx.x == 0 ? a.xblocks * 16 : a.cblocks);
+        const int64_t count = !v ? 0 : (int64_t)(blockIdx.x == 0 ? a.xblocks * 16 : a.cblocks);
 #pragma unroll 4
         for (int64_t i = threadIdx.x; i < count; i += 1024) mx = fmaxf(mx, v[i]);
     }
@@ -273,6 +280,7 @@ __global__ __launch_bounds__(1024) void k_loss_header(PackArgs a)
     __syncthreads();
     if (threadIdx.x > 0) return;
     for (int w = 1; w < 16; ++w) mx = fmaxf(mx, s[w]);
+    if (blockIdx.x < 2 && a.halves) mx = 1.f; // (fp16 values are not scaled)
     (blockIdx.x == 0 ? a.hdr->xinv : blockIdx.x == 1 ? a.hdr->cinv : a.hdr->top) = mx;
 }
 
@@ -406,6 +414,101 @@ struct Product {
     }
 };
 
+// The same where the rows of A are taken as they lie (16-bit values, rows on 16 bytes): the logits of an output layer, whose
+// k x d values are not rewritten first.  A step is two units, 128 bytes of a row, so that whole lines are read; of 256 rows x
+// eight chunks in LDS chunk c of row r lies at place c ^ (r % 8), so that the 16 rows of a fragment are read without bank
+// conflicts.  B is an image of the values' own bits.
+__device__ __forceinline__ f32x4 multiply16(_Float16, const u32x4 &a, const u32x4 &b, const f32x4 &c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 multiply16(bf16_t, const u32x4 &a, const u32x4 &b, const f32x4 &c)
+{
+    typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+template <typename T>
+struct ProductRows {
+    static constexpr int RING = 4, AHEAD = 3, STEP = TILE * 8; // chunks of a step
+    static constexpr int ROUND = 12;                           // memory operations of a wave and step
+    static constexpr int LDS = RING * STEP * 16;
+
+    // c: the tile's first row, `rows` of them are there
+    static __device__ __forceinline__ void run(const T *c, int rows, int d, const Operand &B, int64_t bblk, int units, u32x4 *lds,
+                                               f32x4 (&acc)[8][4])
+    {
+        const int tid = threadIdx.x, lane = tid & 63, l = lane & 15, g = lane >> 4;
+        const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        const u32x4 *b0 = B.pages + ((bblk + ((wave >> 1) & 1)) * B.block + B.first) * PAGE + (wave & 1) * 4 * 64 + lane;
+        const int steps = units / 2; // (units are even)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        // a wave copies 32 rows, eight at a time; rows past the end are the last one, not looked at
+        const int chunk = (lane & 7) ^ (lane >> 3);
+        int off[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) off[q] = min(wave * 32 + 8 * q + (lane >> 3), rows - 1) * d * 2 + chunk * 16;
+        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void *)c, 0, 1 << 30, 0x00020000);
+        auto copy = [&](int t, int q) {
+            u32x4 *dst = lds + (t & (RING - 1)) * STEP + (wave * 32 + 8 * q) * 8;
+            t = min(t, steps - 1);
+            int o = off[q];
+            if ((t + 1) * 64 > d && t * 64 + chunk * 8 >= d) o = 1 << 30; // (behind the row's end: zeros)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void *)dst, 16, o, t * 128, 0, 0);
+        };
+        u32x4 a[8], b[2][2][4];
+        const int at[2] = {((wave >> 2) * 128 + l) * 8 + (g ^ (l & 7)), ((wave >> 2) * 128 + l) * 8 + ((4 + g) ^ (l & 7))};
+        auto read_a = [&](int t, int h, int i) { a[i] = lds[(t & (RING - 1)) * STEP + at[h] + i * 128]; };
+        auto load_b = [&](int t, int slot, int h, int j) { b[slot][h][j] = b0[(int64_t)(2 * min(t, steps - 1) + h) * PAGE + j * 64]; };
+        // a wave's memory operations come in rounds, round t: B of step t + 1, A of step t + AHEAD
+#pragma unroll
+        for (int t = -AHEAD; t < 0; ++t) {
+            if (t == -1)
+#pragma unroll
+                for (int q = 0; q < 8; ++q) load_b(0, 0, q / 4, q % 4);
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int q = 0; q < 4; ++q) copy(t + AHEAD, q);
+            asm volatile("" ::: "memory");
+        }
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(4 + ROUND) : "memory");
+        read_a(0, 0, 0);
+        read_a(0, 0, 1);
+        auto half = [&](int t, auto SLOT, auto HALF) {
+            constexpr int slot = decltype(SLOT)::value, h = decltype(HALF)::value;
+            // A of step t + 1 has arrived: it came with round t - 2; everyone is done with step t - 1
+            if (h == 0) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(ROUND) : "memory");
+            read_a(t, h, 2);
+            read_a(t, h, 3);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[i][j] = multiply16(T(), a[i], b[slot][h][j], acc[i][j]);
+                __builtin_amdgcn_sched_barrier(0);
+                if (i < 4)
+                    load_b(t + 1, slot ^ 1, h, i);
+                else if (i < 6)
+                    copy(t + AHEAD, 2 * h + i - 4);
+                if (i < 4) read_a(t, h, i + 4);
+                if (i == 4 || i == 5) read_a(t + h, h ^ 1, i - 4);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        for (int t = 0; t < steps; t += 2) {
+            half(t, std::integral_constant<int, 0>{}, std::integral_constant<int, 0>{});
+            half(t, std::integral_constant<int, 0>{}, std::integral_constant<int, 1>{});
+            if (t + 1 < steps) {
+                half(t + 1, std::integral_constant<int, 1>{}, std::integral_constant<int, 0>{});
+                half(t + 1, std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{});
+            }
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); // (what was asked for behind the last step)
+    }
+};
+
 // The tile of a workgroup: workgroups go to the eight dies in turn, so each die is given a run of neighbouring tiles, within
 // which eight tiles of B by a few of A share their pages in the die's L2.
 __device__ __forceinline__ void tile_of(int b, int mt, int nt, int *m, int *n)
@@ -422,6 +525,8 @@ struct LogitArgs {
     const float *cinv, *bias2;
     const f32x4 *row;
     const int32_t *lab;
+    const void *c; // the piece's first centroid as it lies, and how many there are from there on
+    int rows, d;
     int units, mt, nt;
     int npad;
     int m_first; // first centroid of the piece
@@ -435,9 +540,32 @@ struct LogitArgs {
     float *dbpart;  // [npad / 64][mt * 256] or NULL
 };
 
+// The products of a tile from images of either matrix in NP parts, or with the centroids as they lie.  There a centroid that
+// does not count is not zero, so its logits have to be told.
+template <int PARTS>
+struct FromImages {
+    static constexpr int NP = PARTS, LDS = Product<NP>::LDS;
+    static constexpr bool TOLD = false;
+    static __device__ __forceinline__ void run(const LogitArgs &a, int mt, int nt, u32x4 *lds, f32x4 (&acc)[8][4])
+    {
+        Product<NP>::run(a.A, a.B, mt * 2, nt * 2, a.units, lds, acc);
+    }
+    static __device__ __forceinline__ float inverse(const LogitArgs &a, int group) { return a.cinv[group]; }
+};
+template <typename T>
+struct FromRows {
+    static constexpr int NP = 1, LDS = ProductRows<T>::LDS;
+    static constexpr bool TOLD = true;
+    static __device__ __forceinline__ void run(const LogitArgs &a, int mt, int nt, u32x4 *lds, f32x4 (&acc)[8][4])
+    {
+        ProductRows<T>::run((const T *)a.c + (int64_t)mt * TILE * a.d, max(1, a.rows - mt * TILE), a.d, a.B, nt * 2, a.units, lds, acc);
+    }
+    static __device__ __forceinline__ float inverse(const LogitArgs &, int) { return 1.f; }
+};
+
 // Forward: per row the maximum and the sum over the 128 centroids of a wave's part.  A lane holds 32 centroids of each of
 // four rows, so most of the reduction stays in its registers.
-template <int NP>
+template <class FORM>
 __global__ __launch_bounds__(LNT, 2) void k_loss_stats(LogitArgs a)
 {
     extern __shared__ u32x4 lds[];
@@ -446,17 +574,18 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_stats(LogitArgs a)
     int mt, nt;
     tile_of(blockIdx.x, a.mt, a.nt, &mt, &nt);
     f32x4 acc[8][4];
-    Product<NP>::run(a.A, a.B, mt * 2, nt * 2, a.units, lds, acc);
+    FORM::run(a, mt, nt, lds, acc);
     const int m0 = mt * TILE + (wave >> 2) * 128, n0 = nt * TILE + (wave & 3) * 64;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float ci = a.cinv[(m0 >> 4) + i];
+        const float ci = FORM::inverse(a, (m0 >> 4) + i);
         const f32x4 b2 = *(const f32x4 *)(a.bias2 + m0 + 16 * i + 4 * g);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const float f = a.row[n0 + 16 * j + l][0] * ci;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(acc[i][j][r], f, b2[r]);
+            for (int r = 0; r < 4; ++r)
+                acc[i][j][r] = FORM::TOLD && b2[r] == -INFINITY ? -INFINITY : fmaf(acc[i][j][r], f, b2[r]);
         }
     }
 #pragma unroll
@@ -530,8 +659,8 @@ struct FewArgs {
     const float *bias;
     const int32_t *label;
     float scale2; // in units of log 2
-    int n, d, k;
-    float2 *part; // [workgroups][n]
+    int n, d, k, groups;
+    float2 *part; // [groups][n]
     float *mine;
 };
 template <typename T>
@@ -573,7 +702,7 @@ __global__ __launch_bounds__(W * 64) void k_loss_few(FewArgs a)
 {
     constexpr int STEP = FewPiece<T>::STEP, N = FewPiece<T>::N, U = 16 / (G + NT) < 2 ? 2 : 16 / (G + NT);
     const int tid = threadIdx.x, lane = tid & 63, l = lane & 15, g = lane >> 4, wave = tid >> 6;
-    const int m0 = (blockIdx.x * W + wave) * 16 * G, n0 = blockIdx.y * 16 * NT;
+    const int group = blockIdx.x % a.groups, m0 = (group * W + wave) * 16 * G, n0 = (int)(blockIdx.x / a.groups) * 16 * NT;
     const T *crow[G], *xrow[NT];
     bool cin[G], xin[NT];
     f32x4 acc[G][NT];
@@ -637,20 +766,21 @@ __global__ __launch_bounds__(W * 64) void k_loss_few(FewArgs a)
     float2 v = s[0][tid];
 #pragma unroll
     for (int w = 1; w < W; ++w) v = join(v, s[w][tid]);
-    a.part[(int64_t)blockIdx.x * a.n + n0 + tid] = v;
+    a.part[(int64_t)group * a.n + n0 + tid] = v;
 }
 
 // Backward: P of a tile, as images in both orders, and the sums over a wave's 64 rows for the bias
-template <int NP>
+template <class FORM>
 __global__ __launch_bounds__(LNT, 2) void k_loss_p(LogitArgs a)
 {
+    constexpr int NP = FORM::NP;
     extern __shared__ u32x4 lds[];
     const int tid = threadIdx.x, lane = tid & 63, l = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int mt, nt;
     tile_of(blockIdx.x, a.mt, a.nt, &mt, &nt);
     f32x4 acc[8][4];
-    Product<NP>::run(a.A, a.B, mt * 2, nt * 2, a.units, lds, acc);
+    FORM::run(a, mt, nt, lds, acc);
     const int m0 = mt * TILE + (wave >> 2) * 128, n0 = nt * TILE + (wave & 3) * 64; // (within the piece)
     f32x4 row[4];
     int rel[4];
@@ -667,14 +797,14 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_p(LogitArgs a)
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float ci = a.cinv[(m0 >> 4) + i];
+        const float ci = FORM::inverse(a, (m0 >> 4) + i);
         const f32x4 b2 = *(const f32x4 *)(a.bias2 + m0 + 16 * i + 4 * g);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const float f = row[j][0] * ci;
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                acc[i][j][r] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], f, b2[r] - row[j][1]));
+                acc[i][j][r] = FORM::TOLD && b2[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], f, b2[r] - row[j][1]));
         }
     }
     const bool labels = __any(any);
@@ -930,6 +1060,7 @@ static LossPlan loss_plan(int dtype, int64_t n, int d, int k, bool backward, voi
     p.kpad = pad_to(k, TILE);
     p.d = d;
     p.units = (d + 31) / 32;
+    if (p.np == 1 && d > NARROW_DIM) p.units += p.units & 1; // (ProductRows takes two at a time)
     p.dblocks = d <= 128 ? 1 : (int)(pad_to(d, 256) / 128);
     p.rows = n < LOSS_ROWS ? n : LOSS_ROWS;
     p.rpad = pad_to(p.rows, TILE);
@@ -1017,19 +1148,43 @@ static bool rows_vec(const void *p, int d)
     return d % 8 == 0 && (uintptr_t)p % 16 == 0;
 }
 
+// The wide form takes the centroids as they lie (ProductRows) where that saves more than it costs: the products are a tenth
+// slower, most where a row is a multiple of 4 KB and all rows of a tile come through the same channel of the L2.  us of a step, these
+// against images: 284 x 50 632 x 1 376 fp16 506 : 580, 1 000 x 30 000 x 1 024 fp16 397 : 427, 4 096 x 32 000 x 2 048 bf16 1 976 : 2 013,
+// 8 192 x 50 001 x 2 048 bf16 5 780 : 5 750.
+#define LIE_ROWS 4096
+template <typename T>
+static bool as_they_lie(const LossArgs &a, const LossPlan &p)
+{
+    return sizeof(T) == 2 && !p.narrow && a.n <= LIE_ROWS && rows_vec<T>(a.c, a.d);
+}
+
 // The images of rows and centroids, and the rest of what the products need: one launch, three backward
 template <typename T, int NP>
 static void loss_images(const LossArgs &a, const LossPlan &p, bool backward, hipStream_t st)
 {
     PackArgs g = {a.x, a.c, a.n, a.d, a.k, p.units, a.label, a.bias, a.grad, backward ? a.stats : nullptr, a.scale, p.ximg, p.cimg,
-                  p.xcols, p.ccols, p.rinv, p.cinv, p.gn, p.bias2, p.row, p.lab, p.hdr, rows_vec<T>(a.x, a.d), rows_vec<T>(a.c, a.d)};
+                  p.xcols, p.ccols, p.rinv, p.cinv, p.gn, p.bias2, p.row, p.lab, p.hdr, rows_vec<T>(a.x, a.d), rows_vec<T>(a.c, a.d), as_they_lie<T>(a, p), __is_same(T, _Float16)};
     g.xblocks = (int)(p.npad / 16);
     g.cblocks = (int)(p.kpad / 16);
     const dim3 packs((unsigned)(g.xblocks + g.cblocks));
-    if (p.units <= 16)
-        hipLaunchKernelGGL((k_pack_rows<T, NP, 4>), packs, dim3(256), 0, st, g);
-    else
-        hipLaunchKernelGGL((k_pack_rows<T, NP, 16>), packs, dim3(256), 0, st, g);
+    auto pack = [&](auto RAW) {
+        if (p.units <= 16)
+            hipLaunchKernelGGL((k_pack_rows<T, NP, 4, decltype(RAW)::value>), packs, dim3(256), 0, st, g);
+        else
+            hipLaunchKernelGGL((k_pack_rows<T, NP, 16, decltype(RAW)::value>), packs, dim3(256), 0, st, g);
+    };
+    if constexpr (NP == 1) {
+        if (g.raw) {
+            g.cimg = nullptr;
+            if (!backward || !a.dx || g.halves) g.cinv = nullptr; // (the centroids' columns want a scale)
+            pack(std::true_type{});
+        } else {
+            pack(std::false_type{});
+        }
+    } else {
+        pack(std::false_type{});
+    }
     if (backward) hipLaunchKernelGGL(k_loss_header, dim3(3), dim3(1024), 0, st, g);
     if (!backward) return;
     g.dblocks = p.dblocks;
@@ -1045,12 +1200,15 @@ static void loss_images(const LossArgs &a, const LossPlan &p, bool backward, hip
 }
 
 template <int NP>
-static LogitArgs logit_args(const LossPlan &p, int64_t r0, int64_t rpad, int64_t c0, int64_t cpad)
+static LogitArgs logit_args(const LossArgs &a, const LossPlan &p, int64_t r0, int64_t rpad, int64_t c0, int64_t cpad)
 {
     LogitArgs g = {};
     const int64_t block = (int64_t)p.units * NP;
     g.A = {p.cimg + c0 / 128 * block * PAGE, block, 0};
     g.B = {p.ximg + r0 / 128 * block * PAGE, block, 0};
+    g.c = (const char *)a.c + c0 * a.d * (NP == 1 ? 2 : 4);
+    g.rows = (int)(a.k - c0);
+    g.d = a.d;
     g.cinv = p.cinv + c0 / 16;
     g.bias2 = p.bias2 + c0;
     g.row = p.row + r0;
@@ -1082,11 +1240,11 @@ static int loss_few(const LossArgs &a, hipStream_t st)
     const int each = small ? 32 : wide ? 256 : 128, groups = (a.k + each - 1) / each;
     float2 *part = (float2 *)a.ws;
     float *mine = (float *)(part + (int64_t)groups * a.n);
-    const FewArgs f = {a.x, a.c, a.bias, a.label, a.scale * LOG2E, (int)a.n, a.d, a.k, part, mine};
+    const FewArgs f = {a.x, a.c, a.bias, a.label, a.scale * LOG2E, (int)a.n, a.d, a.k, groups, part, mine};
     auto go = [&](auto VEC, auto W, auto G, auto NT) {
         constexpr int R = 16 * decltype(NT)::value;
         hipLaunchKernelGGL((k_loss_few<T, decltype(VEC)::value, decltype(W)::value, decltype(G)::value, decltype(NT)::value>),
-                           dim3(groups, (unsigned)((a.n + R - 1) / R)), dim3(decltype(W)::value * 64), 0, st, f);
+                           dim3((unsigned)(groups * ((a.n + R - 1) / R))), dim3(decltype(W)::value * 64), 0, st, f);
     };
     auto rows = [&](auto VEC, auto W, auto G) {
         if (a.n <= 16)
@@ -1135,13 +1293,18 @@ static int loss_forward(const LossArgs &a, hipStream_t st)
         launch_merge(p.part, p.xsplit, g.npad, p.mine, p.lab, a.k, a.n, a.stats, a.loss, st);
         return (int)hipGetLastError();
     }
-    LOSS_TRY(allow_lds(k_loss_stats<NP>, Product<NP>::LDS));
+    const bool lie = as_they_lie<T>(a, p);
+    using Rows = std::conditional_t<NP == 1, FromRows<T>, FromImages<NP>>;
+    LOSS_TRY(lie ? allow_lds(k_loss_stats<Rows>, Rows::LDS) : allow_lds(k_loss_stats<FromImages<NP>>, FromImages<NP>::LDS));
     for (int64_t r0 = 0; r0 < a.n; r0 += p.rows) {
         const int64_t rows = a.n - r0 < p.rows ? a.n - r0 : p.rows, rpad = pad_to(rows, TILE);
-        LogitArgs g = logit_args<NP>(p, r0, rpad, 0, p.kpad);
+        LogitArgs g = logit_args<NP>(a, p, r0, rpad, 0, p.kpad);
         g.part = p.part;
         g.mine = p.mine;
-        hipLaunchKernelGGL(k_loss_stats<NP>, dim3((unsigned)(g.mt * g.nt)), dim3(LNT), Product<NP>::LDS, st, g);
+        if (lie)
+            hipLaunchKernelGGL(k_loss_stats<Rows>, dim3((unsigned)(g.mt * g.nt)), dim3(LNT), Rows::LDS, st, g);
+        else
+            hipLaunchKernelGGL(k_loss_stats<FromImages<NP>>, dim3((unsigned)(g.mt * g.nt)), dim3(LNT), FromImages<NP>::LDS, st, g);
         launch_merge(p.part, g.mt * 2, g.npad, p.mine, g.lab, a.k, rows, a.stats + 2 * r0, a.loss ? a.loss + r0 : nullptr, st);
     }
     return (int)hipGetLastError();
@@ -1197,7 +1360,9 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
         finish(a.dbias ? bias_part(p.csplit, p.kpad, 0, a.k, false) : BiasSum{});
         return (int)hipGetLastError();
     }
-    LOSS_TRY(allow_lds(k_loss_p<NP>, Product<NP>::LDS));
+    const bool lie = as_they_lie<T>(a, p);
+    using Rows = std::conditional_t<NP == 1, FromRows<T>, FromImages<NP>>;
+    LOSS_TRY(lie ? allow_lds(k_loss_p<Rows>, Rows::LDS) : allow_lds(k_loss_p<FromImages<NP>>, FromImages<NP>::LDS));
     LOSS_TRY(allow_lds(k_loss_grads<T, NP>, Product<NP>::LDS));
     const int mt = p.dblocks / 2;
     const bool vec = a.d % 4 == 0;
@@ -1205,14 +1370,17 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
         const int64_t rows = a.n - r0 < p.rows ? a.n - r0 : p.rows, rpad = pad_to(rows, TILE);
         for (int64_t c0 = 0; c0 < p.kpad; c0 += p.piece) {
             const int64_t cpad = p.kpad - c0 < p.piece ? p.kpad - c0 : p.piece;
-            LogitArgs g = logit_args<NP>(p, r0, rpad, c0, cpad);
+            LogitArgs g = logit_args<NP>(a, p, r0, rpad, c0, cpad);
             g.gn = p.gn + r0;
             g.pj = (u32x2 *)p.pj;
             g.pi = (u32x2 *)p.pi;
             g.jblock = (int)(cpad / 32 * NP);
             g.iblock = (int)(rpad / 32 * NP);
             g.dbpart = a.dbias ? p.dbpart : nullptr;
-            hipLaunchKernelGGL(k_loss_p<NP>, dim3((unsigned)(g.mt * g.nt)), dim3(LNT), Product<NP>::LDS, st, g);
+            if (lie)
+                hipLaunchKernelGGL(k_loss_p<Rows>, dim3((unsigned)(g.mt * g.nt)), dim3(LNT), Rows::LDS, st, g);
+            else
+                hipLaunchKernelGGL(k_loss_p<FromImages<NP>>, dim3((unsigned)(g.mt * g.nt)), dim3(LNT), FromImages<NP>::LDS, st, g);
             if (a.dbias) {
                 const BiasSum bias = bias_part((int)(rpad / 64), cpad, c0, a.k - c0 < cpad ? a.k - c0 : cpad, r0 > 0);
                 hipLaunchKernelGGL(k_loss_sums<T>, dim3((unsigned)bias.blocks), dim3(256), 0, st, SlabSum{}, SlabSum{}, bias, a.scale);

@@ -56,7 +56,7 @@ def compare(got, want, names=("loss", "dx", "dc", "db")):
 
 
 SHAPES = [(1, 1, 1), (1, 96, 300), (3, 7, 2), (64, 32, 256), (65, 33, 257), (255, 96, 1000), (257, 128, 513), (300, 130, 1025),
-          (40, 520, 77), (17, 1027, 515), (1000, 64, 5000), (33, 48, 65537), (9, 200, 70001), (129, 100, 9000), (700, 136, 1100), (2100, 500, 1001)]
+          (40, 520, 77), (17, 1027, 515), (1000, 64, 5000), (33, 48, 65537), (9, 200, 70001), (129, 100, 9000), (700, 136, 1100), (2100, 500, 1001), (900, 264, 5003), (1500, 192, 4100)]
 
 
 @pytest.mark.parametrize("t", [F32, F16, BF16])
@@ -73,9 +73,9 @@ def test_no_bias_negative_scale(vlq, t, n, d, k):
     compare(run(vlq, x, c, None, -1.3, label, grad), softmax_loss(x, c, None, -1.3, label, grad))
 
 
+@pytest.mark.parametrize("n,d,k", [(300, 96, 900), (40, 200, 700), (1400, 328, 2600)])
 @pytest.mark.parametrize("t", [F32, F16, BF16])
-def test_rows_and_centroids_that_do_not_count(vlq, t):
-    n, d, k = 300, 96, 900
+def test_rows_and_centroids_that_do_not_count(vlq, t, n, d, k):
     x, c, bias, label, grad = problem(t, n, d, k, skip=0.3, out=0.3)
     label[5], label[6] = k, 2 ** 31 - 1  # (outside as well)
     label[7] = int(torch.nonzero(torch.isneginf(bias))[0])  # (the label was taken out)
@@ -107,6 +107,13 @@ def test_pieces_of_rows_and_centroids(vlq, t):
     n, d, k = 8192 + 300, 40, 4096 + 600
     x, c, bias, label, grad = problem(t, n, d, k, skip=0.05)
     compare(run(vlq, x, c, bias, 1.0, label, grad), softmax_loss(x, c, bias, 1.0, label, grad))
+
+
+def test_millions_of_rows(vlq):
+    # more blocks of 64 rows than a grid has in its second dimension; and more rows than a piece, in the narrow form
+    for t, n, d, k in ((F32, 4_300_000, 2, 3), (BF16, 300_001, 24, 40)):
+        x, c, bias, label, grad = problem(t, n, d, k, skip=0.1)
+        compare(run(vlq, x, c, bias, 1.0, label, grad), softmax_loss(x, c, bias, 1.0, label, grad))
 
 
 @pytest.mark.parametrize("t", [F32, BF16])
