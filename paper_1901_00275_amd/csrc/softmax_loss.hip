@@ -38,6 +38,7 @@
 #define FEW_WORK 1e9          // products
 #define FEW_NARROW_ROWS 128   // up to NARROW_DIM dimensions
 #define FEW_NARROW_WORK 1.2e8
+#define MERGE_ROWS 2048      // up to so many rows four a workgroup are merged, not sixteen
 #define FEW_WIDE 65536       // from so many centroids on a wave takes 32 of them: then there are waves enough
 #define FEW_GROUPS 512       // with fewer workgroups of eight waves they have two
 
@@ -427,6 +428,7 @@ __device__ __forceinline__ f32x4 multiply16(bf16_t, const u32x4 &a, const u32x4 
     typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
+// (B as it lies as well cost more than its image: 1 000 x 16 384 x 512 fp16 33 us instead of 22 and 5 for the image.)
 template <typename T>
 struct ProductRows {
     static constexpr int RING = 4, AHEAD = 3, STEP = TILE * 8; // chunks of a step
@@ -540,7 +542,7 @@ struct LogitArgs {
     float *dbpart;  // [npad / 64][mt * 256] or NULL
 };
 
-// The products of a tile from images of either matrix in NP parts, or with the centroids as they lie.  There a centroid that
+// The products of a tile from images of either matrix in PARTS parts, or with the centroids as they lie.  There a centroid that
 // does not count is not zero, so its logits have to be told.
 template <int PARTS>
 struct FromImages {
@@ -617,15 +619,15 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_stats(LogitArgs a)
     }
 }
 
-// A row's statistics and loss from its parts: R rows a workgroup of 256, 256 / R threads each.  Sixteen rows are read side by
-// side; where there are few rows and many parts one row has the whole workgroup.
+// A row's statistics and loss from its parts: R rows a workgroup of 256, 256 / R threads each.  Rows lie side by side; where
+// there are few of them a row has more threads.
 template <int R>
 __global__ __launch_bounds__(256) void k_loss_merge(const float2 *part, int parts, int npad, const float *mine, const int32_t *lab, int k,
                                                     int64_t n, float *stats, float *loss)
 {
     constexpr int T = 256 / R;
-    const int64_t i = (int64_t)blockIdx.x * R + threadIdx.x % R;
-    const int t = threadIdx.x / R;
+    const int r = threadIdx.x % R, t = threadIdx.x / R;
+    const int64_t i = (int64_t)blockIdx.x * R + r;
     float2 v[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) v[u] = make_float2(-INFINITY, 0.f);
@@ -634,16 +636,13 @@ __global__ __launch_bounds__(256) void k_loss_merge(const float2 *part, int part
         for (int u = 0; u < 4; ++u)
             if (p + u * T < parts && i < npad) v[u] = join(v[u], part[(int64_t)(p + u * T) * npad + i]);
     v[0] = join(join(v[0], v[1]), join(v[2], v[3]));
-    if (R == 1) {
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) v[0] = join(v[0], make_float2(__shfl_xor(v[0].x, o, 64), __shfl_xor(v[0].y, o, 64)));
-    }
-    constexpr int S = R == 1 ? 4 : T;
-    __shared__ float2 s[S][R];
-    if (R > 1 || (t & 63) == 0) s[R == 1 ? t >> 6 : t][threadIdx.x % R] = v[0];
+    for (int o = R; o < 64; o *= 2) v[0] = join(v[0], make_float2(__shfl_xor(v[0].x, o, 64), __shfl_xor(v[0].y, o, 64)));
+    __shared__ float2 s[4][R];
+    if ((threadIdx.x & 63) < R) s[threadIdx.x >> 6][r] = v[0];
     __syncthreads();
     if (t != 0 || i >= n) return;
-    for (int p = 1; p < S; ++p) v[0] = join(v[0], s[p][threadIdx.x % R]);
+    v[0] = join(join(s[0][r], s[1][r]), join(s[2][r], s[3][r]));
     const float m = v[0].x, z = v[0].y;
     stats[2 * i] = m;
     stats[2 * i + 1] = z;
@@ -1226,6 +1225,8 @@ static void launch_merge(const float2 *part, int parts, int npad, const float *m
 {
     if (n <= FEW_ROWS)
         hipLaunchKernelGGL(k_loss_merge<1>, dim3((unsigned)n), dim3(256), 0, st, part, parts, npad, mine, lab, k, n, stats, loss);
+    else if (n <= MERGE_ROWS)
+        hipLaunchKernelGGL(k_loss_merge<4>, dim3((unsigned)((n + 3) / 4)), dim3(256), 0, st, part, parts, npad, mine, lab, k, n, stats, loss);
     else
         hipLaunchKernelGGL(k_loss_merge<16>, dim3((unsigned)((n + 15) / 16)), dim3(256), 0, st, part, parts, npad, mine, lab, k, n, stats, loss);
 }
@@ -1293,18 +1294,18 @@ static int loss_forward(const LossArgs &a, hipStream_t st)
         launch_merge(p.part, p.xsplit, g.npad, p.mine, p.lab, a.k, a.n, a.stats, a.loss, st);
         return (int)hipGetLastError();
     }
+    using Images = FromImages<NP>;
+    using Rows = std::conditional_t<NP == 1, FromRows<T>, Images>;
     const bool lie = as_they_lie<T>(a, p);
-    using Rows = std::conditional_t<NP == 1, FromRows<T>, FromImages<NP>>;
-    LOSS_TRY(lie ? allow_lds(k_loss_stats<Rows>, Rows::LDS) : allow_lds(k_loss_stats<FromImages<NP>>, FromImages<NP>::LDS));
+    const auto kern = lie ? k_loss_stats<Rows> : k_loss_stats<Images>;
+    const size_t bytes = lie ? Rows::LDS : Images::LDS;
+    LOSS_TRY(allow_lds(kern, bytes));
     for (int64_t r0 = 0; r0 < a.n; r0 += p.rows) {
         const int64_t rows = a.n - r0 < p.rows ? a.n - r0 : p.rows, rpad = pad_to(rows, TILE);
         LogitArgs g = logit_args<NP>(a, p, r0, rpad, 0, p.kpad);
         g.part = p.part;
         g.mine = p.mine;
-        if (lie)
-            hipLaunchKernelGGL(k_loss_stats<Rows>, dim3((unsigned)(g.mt * g.nt)), dim3(LNT), Rows::LDS, st, g);
-        else
-            hipLaunchKernelGGL(k_loss_stats<FromImages<NP>>, dim3((unsigned)(g.mt * g.nt)), dim3(LNT), FromImages<NP>::LDS, st, g);
+        hipLaunchKernelGGL(kern, dim3((unsigned)(g.mt * g.nt)), dim3(LNT), bytes, st, g);
         launch_merge(p.part, g.mt * 2, g.npad, p.mine, g.lab, a.k, rows, a.stats + 2 * r0, a.loss ? a.loss + r0 : nullptr, st);
     }
     return (int)hipGetLastError();
