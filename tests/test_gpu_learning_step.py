@@ -91,15 +91,15 @@ def test_step_against_64_bits(vlq):
     want.mean().backward()
     # Errors of an fp32 program in norms: the logits are off by (d / 4 + 80) U of their terms' sizes, and z by some 10 U of
     # its own; every gradient is p - [j = y] (off by twice the logits' error) times operands that are off by less
-    mass = s.scale * float((z.abs() @ C.abs().t()).max())
+    mass = s.scale * float((z.detach().abs() @ C.detach().abs().t()).max())
     dl = mass * (s.d / 4 + 80) * U + 20 * U * mass
-    assert float((loss.double() - want).abs().max()) <= 2 * dl + 512 * U
+    assert float((loss.double() - want.detach()).abs().max()) <= 2 * dl + 512 * U
     grads = [C.grad, a.grad, x.grad]
     total = math.sqrt(sum(float((g ** 2).sum()) for g in grads))
     by = min(1.0, 0.5 / total)
     # a row's share: |p error| sums to at most 4 dl over the centroids, times the largest operand
     rows = 4 * dl + 1024 * U
-    big = {0: float(z.detach().abs().max()), 1: float(C.abs().max()) * float((x.abs() * s.m.max()).sum(1).max()), 2: float(C.abs().max() * s.m.max())}
+    big = {0: float(z.detach().abs().max()), 1: float(C.detach().abs().max()) * float((x.detach().abs() * s.m.max()).sum(1).max()), 2: float(C.detach().abs().max() * s.m.max())}
     slack = 0.0
     for i, (g, o) in enumerate(zip(grads, out)):
         tol = rows * s.scale * big[i] * (1.0 if i == 0 else 1.0 / s.n)
@@ -135,3 +135,27 @@ def test_steps_in_a_row(vlq):
         assert torch.isfinite(loss).all() and math.isfinite(norm.item())
         assert math.sqrt(sum(float((v.double() ** 2).sum()) for v in (dC, da, dx))) <= 0.5 * (1 + 8 * U) + 1e-6
         s.C -= 0.1 * dC
+
+
+def test_codebook_softened_by_the_recipe(vlq):
+    """One gradient step of the training recipe moves the centroids as the 64-bit loss says; the recipe runs with such steps."""
+    from datagen import codebooks
+
+    g = torch.Generator().manual_seed(3)
+    X = torch.randn(3000, 32, generator=g).to(DEV)
+    Cb = X[:64].clone()
+    vlq.vlq_kmeans(X, 3000, 32, 64, 5, Cb)
+    before = Cb.clone()
+    codebooks.soften_cells(vlq, X, Cb, 1, batch=3000, rate=0.1, max_norm=1e9)
+    C = before.double().requires_grad_()
+    d2 = ((X.double()[:, None, :] - C[None]) ** 2).sum(2)
+    near = d2.detach().min(1)
+    v = near.values.mean()
+    (torch.logsumexp(-d2 / (2 * v), 1) - (-d2 / (2 * v)).gather(1, near.indices[:, None])[:, 0]).mean().backward()
+    # step = rate v gradient: v to fp32 (3 000 sums of 32 squares: some 100 U), logits of <x, c> / v and the bias off by (D / 4 + 80) U
+    # of sizes up to |x||c| / v, the gradient's two halves up to |x| and |c| / v in size, the centroid itself by U
+    size = float(X.norm(dim=1).max() * before.norm(dim=1).max() / v)
+    tol = 0.1 * float(X.abs().max() + before.abs().max()) * (4 * size * 88 * U + 600 * U) + 2 * U * float(before.abs().max())
+    assert float((Cb.double() - (before.double() - 0.1 * v * C.grad)).abs().max()) <= tol
+    C2, P = codebooks.train_with_library(vlq, X, 64, 4, 4, iters=2, soft_steps=3)
+    assert torch.isfinite(C2).all() and torch.isfinite(P).all()
