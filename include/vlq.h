@@ -277,8 +277,8 @@ int vlq_profile_read(vlq_index_t *idx, float *ms, int32_t *launches);
  *  - Workspaces belong to the caller (aligned to 256 bytes; their contents do not matter before a call and mean nothing after
  *    it).  Calls that may overlap in time, captured graphs among them, need workspaces of their own.
  *  - The calls only launch kernels on `stream` (no allocation, no memset, no synchronisation) and can be recorded in a HIP
- *    graph.  The current device has to be the buffers' device.  Results do not depend on the launch: the same call gives
- *    the same bits.  Outputs must not overlap inputs or each other unless stated.
+ *    graph.  The current device has to be the buffers' device.  The same call gives the same bits every time.  Outputs (and the
+ *    workspace) over inputs or over each other are refused unless stated.
  */
 enum {
     VLQ_F32 = 0,
@@ -286,6 +286,7 @@ enum {
     VLQ_BF16 = 2
 };
 #define VLQ_MAX_LOSS_DIM 16384     /* d of vlq_softmax_loss */
+#define VLQ_MAX_LOSS_ROWS (1 << 27)    /* n of vlq_softmax_loss */
 #define VLQ_MAX_LOSS_CLASSES (1 << 24) /* k of vlq_softmax_loss */
 #define VLQ_MAX_GROUP_CELLS (1 << 24)  /* cells of vlq_group_rows */
 #define VLQ_MAX_ROW (1 << 20)          /* d of the calls on grouped rows */
@@ -301,9 +302,9 @@ enum {
  * A row whose label is outside [0, k) does not count: its loss is 0 and its vector is not looked at.  A bias of -infinity
  * takes its centroid out for all rows: its vector is not looked at.  A row with no centroid left, or whose label was taken
  * out, has an infinite loss.
- * fp32 values enter the products as two fp16 parts, off by 2^-23 of themselves, or 2^-40 of the largest in their row (of x) or
- * in their 128 consecutive centroids; bf16 values exactly down to 2^-32 of that.
- * 0 <= n < 2^31, 1 <= d <= VLQ_MAX_LOSS_DIM, 1 <= k <= VLQ_MAX_LOSS_CLASSES; n = 0 is a no-op.
+ * fp32 values enter the products as they are or as two fp16 parts, off by 2^-23 of themselves, or 2^-40 of the largest in their
+ * row (of x) or in their 16 consecutive centroids; bf16 values exactly down to 2^-32 of that.
+ * 0 <= n <= VLQ_MAX_LOSS_ROWS, 1 <= d <= VLQ_MAX_LOSS_DIM, 1 <= k <= VLQ_MAX_LOSS_CLASSES; n = 0 is a no-op.
  * d_stats of rows that do not count are unspecified.
  * d_ws: at least vlq_softmax_loss_workspace(dtype, n, d, k, 0) bytes, ws_bytes its size (a smaller n may need more: ask for each).
  */
@@ -317,8 +318,8 @@ int vlq_softmax_loss(int dtype, const void *d_x, int64_t n, int32_t d, const voi
  * The inputs of the forward call and its d_stats; d_grad [n] fp32, the gradient of each row's loss (1 / n for a mean).
  * d_dx [n x d], d_dc [k x d] of type dtype, d_dbias [k] fp32; each may be NULL.  Rows that do not count, and rows with no
  * centroid left, have zero gradients and add nothing to the others'.  n = 0 writes zeros to d_dc and d_dbias.
- * G is held as fp16 (two parts for fp32), relative to grad's largest magnitude, with an absolute error of at most 2^-39 (2^-40 with
- * two parts) of that beside its rounding.  The values of x and c enter relative to the largest of their matrix.
+ * G is held as fp16 (two parts for fp32) relative to grad's largest magnitude, with an absolute error of at most 2^-40 of that
+ * beside its rounding (2^-11, or 2^-22).  The values of x and c enter relative to the largest of their matrix.
  * d_ws: at least vlq_softmax_loss_workspace(dtype, n, d, k, 1) bytes.
  */
 int vlq_softmax_loss_backward(int dtype, const void *d_x, int64_t n, int32_t d, const void *d_c, int32_t k,

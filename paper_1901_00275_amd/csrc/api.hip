@@ -1257,10 +1257,29 @@ static int check_workspace(const void *d_ws, int64_t have, size_t need)
     return VLQ_OK;
 }
 
+// Outputs lie over nothing else (spans without an address or without bytes are none).
+struct Span {
+    const char *name;
+    const void *at;
+    uint64_t bytes;
+    bool out;
+};
+static int check_apart(const Span *span, int n)
+{
+    for (int i = 0; i < n; ++i)
+        for (int j = 0; j < i; ++j) {
+            const Span &a = span[i], &b = span[j];
+            if (!(a.out || b.out) || !a.at || !b.at || !a.bytes || !b.bytes) continue;
+            if ((uintptr_t)a.at < (uintptr_t)b.at + b.bytes && (uintptr_t)b.at < (uintptr_t)a.at + a.bytes)
+                return fail(VLQ_EINVAL, "%s and %s overlap", b.name, a.name);
+        }
+    return VLQ_OK;
+}
+
 static int check_loss_shape(int dtype, int64_t n, int32_t d, int32_t k)
 {
     if (int rc = check_dtype(dtype)) return rc;
-    if (n < 0 || n > 0x7FFFFFFF) return fail(VLQ_EINVAL, "n = %lld outside [0, 2^31)", (long long)n);
+    if (n < 0 || n > VLQ_MAX_LOSS_ROWS) return fail(VLQ_EINVAL, "n = %lld outside [0, %d]", (long long)n, VLQ_MAX_LOSS_ROWS);
     if (d < 1 || d > VLQ_MAX_LOSS_DIM) return fail(VLQ_EINVAL, "d = %d outside [1, %d]", d, VLQ_MAX_LOSS_DIM);
     if (k < 1 || k > VLQ_MAX_LOSS_CLASSES) return fail(VLQ_EINVAL, "k = %d outside [1, %d]", k, VLQ_MAX_LOSS_CLASSES);
     return VLQ_OK;
@@ -1282,7 +1301,13 @@ static int check_loss(const LossArgs &a, const void *d_ws, int64_t ws_bytes, boo
     if (int rc = check_ptr("d_bias", a.bias, 4, true)) return rc;
     if (int rc = check_ptr("d_label", a.label, 4, a.n == 0)) return rc;
     if (int rc = check_ptr("d_stats", a.stats, 4, a.n == 0)) return rc;
-    return check_workspace(d_ws, ws_bytes, loss_workspace(a.dtype, a.n, a.d, a.k, backward));
+    if (int rc = check_workspace(d_ws, ws_bytes, loss_workspace(a.dtype, a.n, a.d, a.k, backward))) return rc;
+    const uint64_t n = a.n, x = n * a.d * e, c = (uint64_t)a.k * a.d * e, k = 4ull * a.k;
+    const Span spans[] = {{"d_x", a.x, x, false}, {"d_c", a.c, c, false}, {"d_bias", a.bias, k, false}, {"d_label", a.label, 4 * n, false},
+                          {"d_grad", a.grad, 4 * n, false}, {"d_stats", a.stats, 8 * n, !backward}, {"d_loss", a.loss, 4 * n, true},
+                          {"d_dx", a.dx, x, true}, {"d_dc", a.dc, c, true}, {"d_dbias", a.dbias, k, true},
+                          {"d_ws", d_ws, loss_workspace(a.dtype, a.n, a.d, a.k, backward), true}};
+    return check_apart(spans, sizeof(spans) / sizeof(spans[0]));
 }
 
 extern "C" int vlq_softmax_loss(int dtype, const void *d_x, int64_t n, int32_t d, const void *d_c, int32_t k, const float *d_bias,
@@ -1344,6 +1369,10 @@ extern "C" int vlq_group_rows(const int32_t *d_cell, int64_t n, int32_t w, int32
     if (int rc = check_ptr("d_place", d_place, 4, n == 0)) return rc;
     if (int rc = check_ptr("d_source", d_source, 4, n == 0)) return rc;
     if (int rc = check_workspace(d_ws, ws_bytes, group_workspace(n * w, cells))) return rc;
+    const uint64_t pairs = 4ull * n * w;
+    const Span spans[] = {{"d_cell", d_cell, pairs, false}, {"d_off", d_off, 8ull * (cells + 1), true}, {"d_place", d_place, pairs, true},
+                          {"d_source", d_source, pairs, true}, {"d_ws", d_ws, group_workspace(n * w, cells), true}};
+    if (int rc = check_apart(spans, 5)) return rc;
     HIPCHK((hipError_t)launch_group_rows(d_cell, n * w, cells, d_off, d_place, d_source, d_ws, (hipStream_t)stream));
     return VLQ_OK;
 }
@@ -1357,6 +1386,9 @@ extern "C" int vlq_gather_rows(int dtype, const void *d_x, int64_t n, int32_t w,
     if (int rc = check_ptr("d_x", d_x, type_bytes(dtype))) return rc;
     if (int rc = check_ptr("d_source", d_source, 4)) return rc;
     if (int rc = check_ptr("d_y", d_y, type_bytes(dtype))) return rc;
+    const uint64_t row = (uint64_t)d * type_bytes(dtype);
+    const Span spans[] = {{"d_x", d_x, n * row, false}, {"d_source", d_source, 4ull * n * w, false}, {"d_y", d_y, n * w * row, true}};
+    if (int rc = check_apart(spans, 3)) return rc;
     HIPCHK((hipError_t)launch_gather_rows(dtype, d_x, n, w, d, d_source, d_y, (hipStream_t)stream));
     return VLQ_OK;
 }
@@ -1371,6 +1403,10 @@ extern "C" int vlq_combine_rows(int dtype, const void *d_y, int64_t n, int32_t w
     if (int rc = check_ptr("d_place", d_place, 4)) return rc;
     if (int rc = check_ptr("d_weight", d_weight, 4, true)) return rc;
     if (int rc = check_ptr("d_out", d_out, type_bytes(dtype))) return rc;
+    const uint64_t row = (uint64_t)d * type_bytes(dtype), pairs = 4ull * n * w;
+    const Span spans[] = {{"d_y", d_y, n * w * row, false}, {"d_place", d_place, pairs, false}, {"d_weight", d_weight, pairs, false},
+                          {"d_out", d_out, n * row, true}};
+    if (int rc = check_apart(spans, 4)) return rc;
     HIPCHK((hipError_t)launch_combine_rows(dtype, d_y, n, w, d, d_place, d_weight, d_out, (hipStream_t)stream));
     return VLQ_OK;
 }
@@ -1387,6 +1423,10 @@ extern "C" int vlq_combine_rows_backward(int dtype, const void *d_dout, const vo
     if (int rc = check_ptr("d_weight", d_weight, 4, true)) return rc;
     if (int rc = check_ptr("d_dy", d_dy, type_bytes(dtype), true)) return rc;
     if (int rc = check_ptr("d_dweight", d_dweight, 4, true)) return rc;
+    const uint64_t row = (uint64_t)d * type_bytes(dtype), pairs = 4ull * n * w;
+    const Span spans[] = {{"d_dout", d_dout, n * row, false}, {"d_y", d_y, n * w * row, false}, {"d_place", d_place, pairs, false},
+                          {"d_weight", d_weight, pairs, false}, {"d_dy", d_dy, n * w * row, true}, {"d_dweight", d_dweight, pairs, true}};
+    if (int rc = check_apart(spans, 6)) return rc;
     HIPCHK((hipError_t)launch_combine_rows_backward(dtype, d_dout, d_y, n, w, d, d_place, d_weight, d_dy, d_dweight, (hipStream_t)stream));
     return VLQ_OK;
 }
@@ -1418,12 +1458,12 @@ extern "C" int vlq_clip_grads(int32_t tensors, const int32_t *dtypes, const int6
     if (int rc = check_ptr("d_norm", d_norm, 4, true)) return rc;
     if (int rc = check_workspace(d_ws, ws_bytes, clip_workspace(tensors, counts))) return rc;
     // every buffer given and aligned, and none over another (but an output on its own input)
-    struct Span {
+    struct Range {
         uintptr_t from, to;
     };
-    Span few[128], *span = few;
+    Range few[130], *span = few;
     if (tensors > 64) {
-        span = (Span *)malloc((size_t)tensors * 2 * sizeof(Span));
+        span = (Range *)malloc(((size_t)tensors * 2 + 2) * sizeof(Range));
         if (!span) return fail(VLQ_ENOMEM, "out of host memory");
     }
     int32_t spans = 0, rc = VLQ_OK;
@@ -1437,10 +1477,18 @@ extern "C" int vlq_clip_grads(int32_t tensors, const int32_t *dtypes, const int6
         rc = check_ptr("a tensor of d_out", d_out[t], e);
         if (rc == VLQ_OK) span[spans++] = {(uintptr_t)d_out[t], (uintptr_t)d_out[t] + bytes};
     }
-    if (rc == VLQ_OK && d_out) { // (without outputs tensors may share memory)
-        std::sort(span, span + spans, [](const Span &a, const Span &b) { return a.from < b.from; });
+    const Range own[2] = {{(uintptr_t)d_ws, (uintptr_t)d_ws + clip_workspace(tensors, counts)}, {(uintptr_t)d_norm, (uintptr_t)d_norm + (d_norm ? 4 : 0)}};
+    if (rc == VLQ_OK && d_out) {
+        span[spans++] = own[0];
+        if (d_norm) span[spans++] = own[1];
+        std::sort(span, span + spans, [](const Range &a, const Range &b) { return a.from < b.from; });
         for (int32_t i = 1; i < spans && rc == VLQ_OK; ++i)
-            if (span[i].from < span[i - 1].to) rc = fail(VLQ_EINVAL, "two tensors overlap");
+            if (span[i].from < span[i - 1].to) rc = fail(VLQ_EINVAL, "two buffers overlap");
+    } else if (rc == VLQ_OK) { // (without outputs tensors may share memory)
+        bool apart = !(d_norm && own[1].from < own[0].to && own[0].from < own[1].to);
+        for (int32_t i = 0; i < spans; ++i)
+            for (const Range &o : own) apart = apart && !(o.from < span[i].to && span[i].from < o.to);
+        if (!apart) rc = fail(VLQ_EINVAL, "two buffers overlap");
     }
     if (span != few) free(span);
     if (rc != VLQ_OK) return rc;

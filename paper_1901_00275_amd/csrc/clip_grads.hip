@@ -118,8 +118,9 @@ __global__ __launch_bounds__(CLIP_NT) void k_grad_norm(const double *part, int p
     if (norm) *norm = (float)sqrt(s);
 }
 
+// (the factor is fp64: 1e-45 / 1e38 is no fp32 number, and the launch waits for memory either way)
 template <typename T>
-__device__ __forceinline__ void scale_values(const T *p, T *o, int64_t count, float f)
+__device__ __forceinline__ void scale_values(const T *p, T *o, int64_t count, double f)
 {
     constexpr int N = 16 / sizeof(T);
     int64_t i = threadIdx.x;
@@ -136,13 +137,13 @@ __device__ __forceinline__ void scale_values(const T *p, T *o, int64_t count, fl
             for (int u = 0; u < 4; ++u)
                 if (i + u * CLIP_NT < whole) {
 #pragma unroll
-                    for (int e = 0; e < N; ++e) v[u][e] = (T)((float)v[u][e] * f);
+                    for (int e = 0; e < N; ++e) v[u][e] = (T)(float)((float)v[u][e] * f);
                     __builtin_nontemporal_store(*(u32x4 *)v[u], r + i + u * CLIP_NT);
                 }
         }
         i = whole * N + threadIdx.x;
     }
-    for (; i < count; i += CLIP_NT) o[i] = (T)((float)p[i] * f);
+    for (; i < count; i += CLIP_NT) o[i] = (T)(float)((float)p[i] * f);
 }
 
 __global__ __launch_bounds__(CLIP_NT) void k_grad_scale(ClipTable a, const double *part, int parts, float max_norm, float *norm)
@@ -150,11 +151,11 @@ __global__ __launch_bounds__(CLIP_NT) void k_grad_scale(ClipTable a, const doubl
     const double n = sqrt(sum_parts(part, parts));
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)n;
     // (a norm that is not finite leaves the gradients as they are)
-    const float f = n > (double)max_norm && n < INFINITY ? (float)((double)max_norm / n) : 1.f;
+    const double f = n > (double)max_norm && n < INFINITY ? (double)max_norm / n : 1.;
     const int b = a.chunks - 1 - blockIdx.x, t = find_tensor(a, b);
     const void *in = a.in[t];
     void *out = a.out[t];
-    if (f == 1.f && in == out) return;
+    if (f == 1. && in == out) return;
     const int dtype = (int)(a.count[t] & 3);
     const int64_t i0 = (int64_t)(b - a.first[t]) * a.chunk, count = min(a.chunk, (a.count[t] >> 2) - i0);
     if (dtype == VLQ_F32)

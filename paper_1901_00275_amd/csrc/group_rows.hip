@@ -379,6 +379,7 @@ struct RowsArgs {
     int w, d;
     uint32_t per;  // pieces of a row
     uint32_t rows; // rows of a workgroup
+    int64_t block; // the launch's first workgroup
     const int32_t *index; // source or place
     const float *weight;
 };
@@ -388,7 +389,7 @@ template <typename T, bool VEC>
 __global__ __launch_bounds__(ROW_NT) void k_gather_rows(RowsArgs a, const T *__restrict__ x, T *__restrict__ y)
 {
     using P = Piece<T, VEC>;
-    const int64_t places = a.n * a.w, p0 = (int64_t)blockIdx.x * a.rows;
+    const int64_t places = a.n * a.w, p0 = (a.block + blockIdx.x) * a.rows;
     const uint32_t pieces = (uint32_t)min((int64_t)a.rows, places - p0) * a.per;
     for (uint32_t i0 = threadIdx.x; i0 < pieces; i0 += ROW_NT * ROW_ITEMS) {
         P v[ROW_ITEMS];
@@ -414,7 +415,7 @@ template <typename T, bool VEC>
 __global__ __launch_bounds__(ROW_NT) void k_combine_rows(RowsArgs a, const T *__restrict__ y, T *__restrict__ out)
 {
     using P = Piece<T, VEC>;
-    const int64_t places = a.n * a.w, r0 = (int64_t)blockIdx.x * a.rows;
+    const int64_t places = a.n * a.w, r0 = (a.block + blockIdx.x) * a.rows;
     const uint32_t pieces = (uint32_t)min((int64_t)a.rows, a.n - r0) * a.per;
     for (uint32_t i = threadIdx.x; i < pieces; i += ROW_NT) {
         const uint32_t r = i / a.per, c = i - r * a.per;
@@ -454,7 +455,7 @@ __global__ __launch_bounds__(ROW_NT) void k_combine_back(RowsArgs a, const T *__
 {
     using P = Piece<T, VEC>;
     const int lane = threadIdx.x & (L - 1);
-    const int64_t places = a.n * a.w, r = (int64_t)blockIdx.x * (ROW_NT / L) + threadIdx.x / L;
+    const int64_t places = a.n * a.w, r = (a.block + blockIdx.x) * (ROW_NT / L) + threadIdx.x / L;
     if (r >= a.n) return;
     for (int q0 = 0; q0 < a.w; q0 += 8) {
         int64_t p[8];
@@ -503,6 +504,14 @@ static bool whole_pieces(int d, const void *p, const void *q, const void *r)
 // rows of a workgroup: about `pieces` pieces
 static uint32_t rows_of(uint32_t per, uint32_t pieces) { return per >= pieces ? 1 : pieces / per; }
 
+// a.block and so many workgroups of each launch: a grid has fewer than 2^32 threads
+template <typename F>
+static void in_launches(RowsArgs &a, int64_t groups, F &&launch)
+{
+    const int64_t most = 1 << 23;
+    for (a.block = 0; a.block < groups; a.block += most) launch(dim3((unsigned)(groups - a.block < most ? groups - a.block : most)));
+}
+
 template <typename T>
 static int gather(const RowsArgs &args, const T *x, T *y, hipStream_t st)
 {
@@ -511,7 +520,9 @@ static int gather(const RowsArgs &args, const T *x, T *y, hipStream_t st)
         constexpr bool V = decltype(VEC)::value;
         a.per = a.d / Piece<T, V>::N;
         a.rows = rows_of(a.per, ROW_NT * ROW_ITEMS);
-        hipLaunchKernelGGL((k_gather_rows<T, V>), dim3((unsigned)((a.n * a.w + a.rows - 1) / a.rows)), dim3(ROW_NT), 0, st, a, x, y);
+        in_launches(a, (a.n * a.w + a.rows - 1) / a.rows, [&](dim3 groups) {
+            hipLaunchKernelGGL((k_gather_rows<T, V>), groups, dim3(ROW_NT), 0, st, a, x, y);
+        });
     };
     if (whole_pieces<T>(a.d, x, y, nullptr))
         go(std::true_type{});
@@ -528,7 +539,9 @@ static int combine(const RowsArgs &args, const T *y, T *out, hipStream_t st)
         constexpr bool V = decltype(VEC)::value;
         a.per = a.d / Piece<T, V>::N;
         a.rows = rows_of(a.per, ROW_NT);
-        hipLaunchKernelGGL((k_combine_rows<T, V>), dim3((unsigned)((a.n + a.rows - 1) / a.rows)), dim3(ROW_NT), 0, st, a, y, out);
+        in_launches(a, (a.n + a.rows - 1) / a.rows, [&](dim3 groups) {
+            hipLaunchKernelGGL((k_combine_rows<T, V>), groups, dim3(ROW_NT), 0, st, a, y, out);
+        });
     };
     if (whole_pieces<T>(a.d, y, out, nullptr))
         go(std::true_type{});
@@ -546,7 +559,9 @@ static int combine_back(const RowsArgs &args, const T *dout, const T *y, T *dy, 
         a.per = a.d / Piece<T, V>::N;
         auto lanes = [&](auto L) {
             constexpr int N = decltype(L)::value, R = ROW_NT / N;
-            hipLaunchKernelGGL((k_combine_back<T, V, N>), dim3((unsigned)((a.n + R - 1) / R)), dim3(ROW_NT), 0, st, a, dout, y, dy, dweight);
+            in_launches(a, (a.n + R - 1) / R, [&](dim3 groups) {
+                hipLaunchKernelGGL((k_combine_back<T, V, N>), groups, dim3(ROW_NT), 0, st, a, dout, y, dy, dweight);
+            });
         };
         if (a.per > 32)
             lanes(std::integral_constant<int, 64>{});
@@ -564,7 +579,7 @@ static int combine_back(const RowsArgs &args, const T *dout, const T *y, T *dy, 
 
 int launch_gather_rows(int dtype, const void *x, int64_t n, int w, int d, const int32_t *source, void *y, hipStream_t st)
 {
-    const RowsArgs a = {n, w, d, 0, 0, source, nullptr};
+    const RowsArgs a = {n, w, d, 0, 0, 0, source, nullptr};
     if (dtype == VLQ_F32) return gather(a, (const float *)x, (float *)y, st);
     return gather(a, (const uint16_t *)x, (uint16_t *)y, st); // (values are moved, not looked at)
 }
@@ -572,7 +587,7 @@ int launch_gather_rows(int dtype, const void *x, int64_t n, int w, int d, const 
 int launch_combine_rows(int dtype, const void *y, int64_t n, int w, int d, const int32_t *place, const float *weight, void *out,
                         hipStream_t st)
 {
-    const RowsArgs a = {n, w, d, 0, 0, place, weight};
+    const RowsArgs a = {n, w, d, 0, 0, 0, place, weight};
     switch (dtype) {
     case VLQ_F32: return combine(a, (const float *)y, (float *)out, st);
     case VLQ_F16: return combine(a, (const _Float16 *)y, (_Float16 *)out, st);
@@ -583,7 +598,7 @@ int launch_combine_rows(int dtype, const void *y, int64_t n, int w, int d, const
 int launch_combine_rows_backward(int dtype, const void *dout, const void *y, int64_t n, int w, int d, const int32_t *place,
                                  const float *weight, void *dy, float *dweight, hipStream_t st)
 {
-    const RowsArgs a = {n, w, d, 0, 0, place, weight};
+    const RowsArgs a = {n, w, d, 0, 0, 0, place, weight};
     switch (dtype) {
     case VLQ_F32: return combine_back(a, (const float *)dout, (const float *)y, (float *)dy, dweight, st);
     case VLQ_F16: return combine_back(a, (const _Float16 *)dout, (const _Float16 *)y, (_Float16 *)dy, dweight, st);

@@ -227,7 +227,7 @@ __device__ __forceinline__ void row_numbers(const PackArgs &a, int64_t i, float 
         const float m = a.stats[2 * i], z = a.stats[2 * i + 1], top = a.hdr->top;
         ok = m != -INFINITY;
         if (ok) {
-            f = top > 0.f ? a.g[i] / top : 0.f;
+            f = top > 0.f ? a.g[i] / top : a.g[i]; // (zero, or no finite one is there)
             r[1] = m;
             r[2] = P_ONE / z;
             r[3] = P_ONE / z * f;
@@ -990,9 +990,11 @@ __global__ __launch_bounds__(256) void k_loss_sums(SlabSum x, SlabSum c, BiasSum
 template <typename T>
 __global__ __launch_bounds__(256) void k_loss_none(T *dc, int64_t count, float *dbias, int k)
 {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (dc && i < count) dc[i] = (T)0.f;
-    if (dbias && i < k) dbias[i] = 0.f;
+    const int64_t step = (int64_t)gridDim.x * 256;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += step) {
+        if (dc) dc[i] = (T)0.f;
+        if (dbias && i < k) dbias[i] = 0.f;
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -1316,7 +1318,7 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
 {
     if (a.n == 0) {
         const int64_t count = (int64_t)a.k * a.d;
-        hipLaunchKernelGGL(k_loss_none<T>, dim3((unsigned)((count + 255) / 256)), dim3(256), 0, st, (T *)a.dc, count, a.dbias, a.k);
+        hipLaunchKernelGGL(k_loss_none<T>, dim3((unsigned)(count < 4096 * 256 ? (count + 255) / 256 : 4096)), dim3(256), 0, st, (T *)a.dc, count, a.dbias, a.k);
         return (int)hipGetLastError();
     }
     const LossPlan p = loss_plan(a.dtype, a.n, a.d, a.k, true, a.ws);

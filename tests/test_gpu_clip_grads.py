@@ -87,6 +87,14 @@ def test_squares_beyond_fp32(vlq):
         check(grads, outs, norm, float(torch.tensor(size, dtype=F32)))
 
 
+def test_factor_below_fp32(vlq):
+    # 2^-300 of the norm: the values come out among the smallest of fp32, the factor is none of them
+    grads = [torch.tensor([3.0, 4.0, 0.0], device=DEV) * 2.0 ** 125, torch.tensor([2.0], device=DEV, dtype=BF16)]
+    for limit in (2.0 ** -100, 5 * 2.0 ** -140, 1e-3):
+        outs, norm = clip(vlq, grads, limit)
+        check(grads, outs, norm, limit)
+
+
 def test_norm_that_is_not_finite(vlq):
     for bad in (math.inf, -math.inf, math.nan):
         grads = [torch.ones(100, device=DEV), torch.ones(50, device=DEV, dtype=BF16)]

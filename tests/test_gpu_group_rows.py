@@ -153,6 +153,30 @@ def test_unaligned_rows(vlq, t):
     assert kept > 0
 
 
+def test_more_pieces_than_threads_of_a_grid(vlq):
+    # 2^24 rows of an odd size, a workgroup each; 2^28 of one value, 16 lanes each
+    n, d = (1 << 24) + 3, 513
+    g = torch.Generator(device=DEV).manual_seed(11)
+    x = torch.randint(-30000, 30000, (n, d), generator=g, device=DEV, dtype=torch.int16).view(BF16)
+    back = torch.arange(n - 1, -1, -1, device=DEV, dtype=torch.int32)
+    y = torch.empty_like(x)
+    vlq.vlq_gather_rows(x, n, 1, d, back, y)
+    for p in (0, 1, n // 2, n - 1):
+        assert torch.equal(y[p].view(torch.int16), x[n - 1 - p].view(torch.int16))
+    out = torch.zeros_like(x)
+    x = x.nan_to_num_()  # (combined values are sums: NaNs need not keep their bits)
+    vlq.vlq_gather_rows(x, n, 1, d, back, y)
+    vlq.vlq_combine_rows(y, n, 1, d, back, None, out)
+    assert torch.equal(out, x)
+    del x, y, out
+    n = (1 << 28) + 5
+    dout, y = (torch.randint(-8, 9, (n, 1), generator=g, device=DEV, dtype=torch.int8).to(F16) for _ in range(2))
+    back = torch.arange(n - 1, -1, -1, device=DEV, dtype=torch.int32)
+    dy, dweight = torch.empty_like(y), torch.empty(n, 1, device=DEV)
+    vlq.vlq_combine_rows_backward(dout, y, n, 1, 1, back, None, dy, dweight)
+    assert torch.equal(dy, dout.flip(0)) and torch.equal(dweight, (dout * y.flip(0)).float())
+
+
 def test_captured_and_replayed(vlq):
     n, w, d, cells = 3000, 6, 96, 3000
     cell = torch.zeros(n, w, dtype=torch.int32, device=DEV)

@@ -116,6 +116,33 @@ def test_millions_of_rows(vlq):
         compare(run(vlq, x, c, bias, 1.0, label, grad), softmax_loss(x, c, bias, 1.0, label, grad))
 
 
+def test_most_rows_and_most_centroids(vlq):
+    g = torch.Generator(device=DEV).manual_seed(5)
+    for n, d, k in ((1 << 27, 2, 3), (33, 3, 1 << 24)):
+        x, c = (torch.randn(v, d, generator=g, device=DEV).to(BF16) for v in (n, k))
+        label = torch.randint(-1, k, (n,), generator=g, device=DEV, dtype=torch.int32)
+        label[-1] = k - 1
+        bias, grad = torch.randn(k, generator=g, device=DEV), torch.randn(n, generator=g, device=DEV)
+        compare(run(vlq, x, c, bias, 1.0, label, grad), softmax_loss(x, c, bias, 1.0, label, grad))
+
+
+@pytest.mark.parametrize("t", [F32, F16, BF16])
+@pytest.mark.parametrize("bad", [math.inf, math.nan])
+@pytest.mark.parametrize("d", [40, 140])
+def test_gradients_that_are_not_finite(vlq, t, bad, d):
+    # a row's own dx, and what is summed over the rows: whether other rows have gradients or not
+    x, c, bias, label, grad = problem(t, 70, d, 300)
+    for others in (1.0, 0.0):
+        grad = grad * others
+        grad[7] = bad
+        got, ref = run(vlq, x, c, bias, 1.0, label, grad), run(vlq, x, c, bias, 1.0, label, torch.where(grad == grad[7], 0.0, torch.nan_to_num(grad, 0.0)))
+        assert not got["dx"][7].isfinite().any()
+        for name in ("dc", "db"):
+            assert not got[name].isfinite().any(), name
+        rest = torch.arange(70, device=DEV) != 7
+        assert torch.equal(got["dx"][rest], ref["dx"][rest])
+
+
 @pytest.mark.parametrize("t", [F32, BF16])
 def test_large_and_small_logits(vlq, t):
     # logits in the hundreds, all but one probability vanish; and descriptors with a mean far above their spread
@@ -232,3 +259,11 @@ def test_no_rows(vlq):
     x, c, bias, label, grad = problem(F32, 4, 8, 50)
     got = run(vlq, x[:0], c, bias, 1.0, label[:0], grad[:0])
     assert (got["dc"] == 0).all() and (got["db"] == 0).all()
+
+
+def test_no_rows_many_centroids(vlq):
+    # 2^32 values and more, each a thread's
+    d, k = 257, 1 << 24
+    x, c = torch.empty(0, d, dtype=BF16, device=DEV), torch.empty(k, d, dtype=BF16, device=DEV)
+    got = run(vlq, x, c, None, 1.0, torch.empty(0, dtype=torch.int32, device=DEV), torch.empty(0, device=DEV), what=("dc",))
+    assert (got["dc"][:1000] == 0).all() and (got["dc"][-1000:] == 0).all() and not got["dc"].any()
