@@ -79,6 +79,15 @@ def test_large(vlq):
     check(grads, outs, norm, 3.0)
 
 
+def test_larger_than_the_cache(vlq):
+    g = torch.Generator(device=DEV).manual_seed(2)
+    grads = [torch.randn(c, generator=g, device=DEV).to(t) for c, t in ((90_000_001, BF16), (30_000_007, F32), (50_000_003, F16))]
+    outs, norm = clip(vlq, grads, 3.0)
+    check(grads, outs, norm, 3.0)
+    same, norm2 = clip(vlq, grads, 3.0, in_place=True)
+    assert torch.equal(norm, norm2) and all(torch.equal(a, b) for a, b in zip(outs, same))
+
+
 def test_squares_beyond_fp32(vlq):
     for size in (1e30, 1e-30):
         grads = [torch.tensor([3.0, 4.0], device=DEV) * size]
