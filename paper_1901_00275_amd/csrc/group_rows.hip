@@ -4,7 +4,10 @@
 // The sort goes by digits of at most DIGIT bits, the lowest first, and keeps the order of equal ones: every workgroup counts
 // the digits of a tile, the counts of a digit are summed over the tiles, and the workgroup ranks its pairs: a wave's
 // pairs in turn, 64 at a time, those of one digit told apart by ballots.  No atomics on memory, so the order is the pairs' own.
-// The rest moves memory: whole 16 bytes where rows lie on them, several rows' loads under way at a time.
+// What bounds it are launches of 5 to 11 us, each some waits for memory one behind the other: 640 000 pairs and 65 536 cells
+// (two digits) 51 us in seven launches, 13 MB of pairs and places.  Up to SMALL_PAIRS pairs of one digit take one launch.
+// The rest moves memory: whole 16 bytes where rows lie on them, several rows' loads under way at a time.  640 000 rows of 384 bytes
+// gathered 41 us (6.0 TB/s written), 16 384 rows of 8 x 4 KB combined 137 us (4.3 TB/s), the gradient of 5 003 x 6 x 2 KB 26 us (5.0).
 #include "learn.h"
 
 #include <type_traits>
@@ -33,11 +36,12 @@ __device__ __forceinline__ uint64_t same_digit(uint32_t digit, int bits, bool th
 
 struct SortPass {
     const int32_t *cell;         // the first pass reads the cells, the later ones keys and pairs
-    const uint32_t *key, *pair;
-    uint32_t *key_out, *pair_out;
-    int32_t *place, *source;     // the last pass
-    int64_t *off;                // the only pass
-    uint32_t *count;             // [bins][tiles]
+    const uint2 *moved;          // {key, pair}
+    uint2 *moved_out;
+    uint32_t *to;                // where each went, in the order they came; the last pass: -1 if it is dropped
+    int32_t *place, *source;     // the only pass
+    int64_t *off;
+    uint32_t *count;             // [tiles][bins]
     uint32_t *total;             // [bins]
     int64_t pairs;
     int cells, shift, bits, tile, tiles;
@@ -46,7 +50,7 @@ struct SortPass {
 
 __device__ __forceinline__ uint32_t key_at(const SortPass &a, int64_t i)
 {
-    if (!a.cell) return a.key[i];
+    if (!a.cell) return a.moved[i].x;
     const uint32_t c = (uint32_t)a.cell[i];
     return c < (uint32_t)a.cells ? c : (uint32_t)a.cells; // (dropped pairs stand behind all cells)
 }
@@ -62,7 +66,7 @@ __global__ __launch_bounds__(GNT) void k_group_count(SortPass a)
 #pragma unroll 8
     for (int i = threadIdx.x; i < count; i += GNT) atomicAdd(&h[(key_at(a, i0 + i) >> a.shift) & (bins - 1)], 1u);
     __syncthreads();
-    for (int b = threadIdx.x; b < bins; b += GNT) a.count[(int64_t)b * a.tiles + blockIdx.x] = h[b];
+    for (int b = threadIdx.x; b < bins; b += GNT) a.count[(int64_t)blockIdx.x * bins + b] = h[b];
 }
 
 // wave-wide inclusive sum
@@ -76,18 +80,30 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t v, int lane)
     return v;
 }
 
-// exclusive sums of a digit's counts over the tiles, a wave per digit
-__global__ __launch_bounds__(GNT) void k_group_tiles(uint32_t *count, uint32_t *total, int tiles, int bins)
+// exclusive sums of a digit's counts over the tiles: 16 digits a workgroup, the tiles in 64 slices
+#define SLICES 64
+__global__ __launch_bounds__(SLICES * 16) void k_group_tiles(uint32_t *count, uint32_t *total, int tiles, int bins)
 {
-    const int lane = threadIdx.x & 63, b = blockIdx.x * GWAVES + (threadIdx.x >> 6);
-    if (b >= bins) return;
-    uint32_t *c = count + (int64_t)b * tiles, sum = 0;
-    for (int t = 0; t < tiles; t += 64) {
-        const uint32_t v = t + lane < tiles ? c[t + lane] : 0, s = wave_scan(v, lane);
-        if (t + lane < tiles) c[t + lane] = sum + s - v;
-        sum += __shfl(s, 63, 64);
+    __shared__ uint32_t sum[16][SLICES + 1];
+    const int b = threadIdx.x & 15, slice = threadIdx.x >> 4, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int digit = blockIdx.x * 16 + b, per = (tiles + SLICES - 1) / SLICES;
+    const int t0 = slice * per, t1 = digit < bins ? min(t0 + per, tiles) : 0;
+    uint32_t s = 0;
+#pragma unroll 8
+    for (int t = t0; t < t1; ++t) s += count[(int64_t)t * bins + digit];
+    sum[b][slice] = s;
+    __syncthreads();
+    const uint32_t own = sum[wave][lane], upto = wave_scan(own, lane); // (a wave: a digit's slices)
+    sum[wave][lane] = upto - own;
+    if (lane == 63 && blockIdx.x * 16 + wave < bins) total[blockIdx.x * 16 + wave] = upto;
+    __syncthreads();
+    s = sum[b][slice];
+#pragma unroll 8
+    for (int t = t0; t < t1; ++t) {
+        const uint32_t v = count[(int64_t)t * bins + digit];
+        count[(int64_t)t * bins + digit] = s;
+        s += v;
     }
-    if (lane == 0) total[b] = sum;
 }
 
 // in place: exclusive sums of v[0 .. bins) by NT threads, v in LDS; the values behind are not touched
@@ -119,11 +135,13 @@ __device__ __forceinline__ void hold(const SortPass &a, int64_t i0, int count, i
 #pragma unroll
     for (int u = 0; u < HELD; ++u)
         if (u * 64 + lane < count) {
-            key[u] = key_at(a, i0 + u * 64 + lane);
-            pair[u] = a.cell ? (uint32_t)(i0 + u * 64 + lane) : a.pair[i0 + u * 64 + lane];
+            const int64_t i = i0 + u * 64 + lane;
+            const uint2 v = a.cell ? make_uint2(key_at(a, i), (uint32_t)i) : a.moved[i];
+            key[u] = v.x;
+            pair[u] = v.y;
         }
 }
-__device__ __forceinline__ void place_held(const SortPass &a, uint32_t *at, int count, int lane, const uint32_t (&key)[HELD], const uint32_t (&pair)[HELD])
+__device__ __forceinline__ void place_held(const SortPass &a, uint32_t *at, int64_t i0, int count, int lane, const uint32_t (&key)[HELD], const uint32_t (&pair)[HELD])
 {
     const uint64_t below = ((uint64_t)1 << lane) - 1;
 #pragma unroll
@@ -138,14 +156,13 @@ __device__ __forceinline__ void place_held(const SortPass &a, uint32_t *at, int 
         if (there && !(same & below)) at[digit] += __popcll(same);
         wave_lds_order();
         if (!there) continue;
-        if (!a.last) {
-            a.key_out[p] = key[u];
-            a.pair_out[p] = pair[u];
+        if (!a.only) {
+            a.moved_out[p] = make_uint2(key[u], pair[u]);
+            a.to[i0 + u * 64 + lane] = a.last && key[u] >= (uint32_t)a.cells ? 0xFFFFFFFFu : p;
         } else {
             const bool in = key[u] < (uint32_t)a.cells;
             a.source[p] = in ? (int32_t)pair[u] : -1;
             a.place[pair[u]] = in ? (int32_t)p : -1;
-            if (!a.only) a.key_out[p] = key[u];
         }
     }
 }
@@ -154,7 +171,7 @@ __device__ __forceinline__ void place_pairs(const SortPass &a, uint32_t *at, int
     uint32_t key[HELD], pair[HELD];
     for (int i = 0; i < count; i += HELD * 64) {
         hold(a, i0 + i, count - i, lane, key, pair);
-        place_held(a, at, count - i, lane, key, pair);
+        place_held(a, at, i0 + i, count - i, lane, key, pair);
     }
 }
 
@@ -166,6 +183,12 @@ __global__ __launch_bounds__(GNT) void k_group_place(SortPass a)
     {
         const int64_t w0 = (int64_t)blockIdx.x * a.tile + wave * (a.tile / GWAVES);
         hold(a, w0, (int)max((int64_t)0, min((int64_t)(a.tile / GWAVES), a.pairs - w0)), lane, key, pair);
+    }
+    uint32_t before[BINS / GNT]; // of each digit, in the tiles before this one
+#pragma unroll
+    for (int i = 0; i < BINS / GNT; ++i) {
+        const int b = i * GNT + tid;
+        if (b < bins) before[i] = a.count[(int64_t)blockIdx.x * bins + b];
     }
     for (int b = tid; b < bins; b += GNT) {
         first[b] = a.total[b];
@@ -182,8 +205,11 @@ __global__ __launch_bounds__(GNT) void k_group_place(SortPass a)
     for (int u = 0; u < HELD; ++u)
         if (u * 64 + lane < count) atomicAdd(&at[wave][(key[u] >> a.shift) & (bins - 1)], 1u);
     __syncthreads();
-    for (int b = tid; b < bins; b += GNT) {
-        uint32_t next = first[b] + a.count[(int64_t)b * a.tiles + blockIdx.x];
+#pragma unroll
+    for (int i = 0; i < BINS / GNT; ++i) {
+        const int b = i * GNT + tid;
+        if (b >= bins) continue;
+        uint32_t next = first[b] + before[i];
         for (int w = 0; w < GWAVES; ++w) {
             const uint32_t c = at[w][b];
             at[w][b] = next;
@@ -191,7 +217,7 @@ __global__ __launch_bounds__(GNT) void k_group_place(SortPass a)
         }
     }
     __syncthreads();
-    place_held(a, at[wave], count, lane, key, pair);
+    place_held(a, at[wave], i0 + wave * per, count, lane, key, pair);
     if (count > HELD * 64) place_pairs(a, at[wave], i0 + wave * per + HELD * 64, count - HELD * 64, lane);
 }
 
@@ -228,20 +254,48 @@ __global__ __launch_bounds__(SMALL_NT) void k_group_small(SortPass a)
     place_pairs(a, lds + wave * bins, i0, count, lane);
 }
 
-// off[c]: the first place whose cell is c or more
-__global__ __launch_bounds__(256) void k_group_offsets(const uint32_t *key, int64_t pairs, int cells, int64_t *off)
+// What several passes leave to be written, all of it in order: off[c], the first place whose cell is c or more; source; and
+// place, by following a pair through the passes.  (Written by the last pass, the places lay 4 bytes here and 4 there: 640 000
+// pairs, 65 536 cells, that pass 20 us and the offsets 6; now 11 and 9.)
+#define SAMPLES 512 // keys among which a cell's first is looked for in LDS: ten fewer reads of memory one behind the other, 11 -> 9 us
+struct GroupEnd {
+    const uint2 *moved;
+    const uint32_t *to[3];
+    int64_t pairs;
+    int passes, cells, off_blocks;
+    int64_t *off;
+    int32_t *place, *source;
+};
+__global__ __launch_bounds__(256) void k_group_end(GroupEnd a)
 {
-    const int c = blockIdx.x * 256 + threadIdx.x;
-    if (c > cells) return;
-    int64_t lo = 0, hi = pairs;
-    while (lo < hi) {
-        const int64_t mid = (lo + hi) >> 1;
-        if (key[mid] < (uint32_t)c)
-            lo = mid + 1;
-        else
-            hi = mid;
+    if ((int)blockIdx.x < a.off_blocks) {
+        __shared__ uint32_t sample[SAMPLES];
+        const int64_t step = a.pairs / (SAMPLES - 1) + 1; // (the last lies past the end)
+        for (int i = threadIdx.x; i < SAMPLES; i += 256) sample[i] = i * step < a.pairs ? a.moved[i * step].x : 0xFFFFFFFFu;
+        __syncthreads();
+        const int c = blockIdx.x * 256 + threadIdx.x;
+        if (c > a.cells) return;
+        int before = 0; // samples below c
+        for (int b = SAMPLES / 2; b > 0; b >>= 1)
+            if (sample[before + b - 1] < (uint32_t)c) before += b;
+        int64_t lo = before > 0 ? (before - 1) * step + 1 : 0, hi = min(before * step, a.pairs);
+        while (lo < hi) {
+            const int64_t mid = (lo + hi) >> 1;
+            if (a.moved[mid].x < (uint32_t)c)
+                lo = mid + 1;
+            else
+                hi = mid;
+        }
+        a.off[c] = lo;
+        return;
     }
-    off[c] = lo;
+    const int64_t i = (int64_t)(blockIdx.x - a.off_blocks) * 256 + threadIdx.x;
+    if (i >= a.pairs) return;
+    const uint2 own = a.moved[i];
+    uint32_t p = a.to[0][i];
+    for (int q = 1; q < a.passes; ++q) p = a.to[q][p];
+    a.source[i] = own.x < (uint32_t)a.cells ? (int32_t)own.y : -1;
+    a.place[i] = (int32_t)p;
 }
 
 __global__ __launch_bounds__(256) void k_group_none(int cells, int64_t *off)
@@ -252,7 +306,7 @@ __global__ __launch_bounds__(256) void k_group_none(int cells, int64_t *off)
 
 struct GroupPlan {
     int passes, bits[3], tile, tiles;
-    size_t count_off, total_off, key_off[2], pair_off[2], bytes;
+    size_t count_off, total_off, moved_off[2], to_off[3], bytes;
     bool small;
 };
 
@@ -281,10 +335,9 @@ static GroupPlan group_plan(int64_t pairs, int cells)
         p.count_off = take((size_t)BINS * p.tiles * 4);
         p.total_off = take((size_t)BINS * 4);
         if (p.passes > 1)
-            for (int i = 0; i < 2; ++i) {
-                p.key_off[i] = take((size_t)pairs * 4);
-                p.pair_off[i] = take((size_t)pairs * 4);
-            }
+            for (int i = 0; i < 2; ++i) p.moved_off[i] = take((size_t)pairs * sizeof(uint2));
+        if (p.passes > 1)
+            for (int i = 0; i < p.passes; ++i) p.to_off[i] = take((size_t)pairs * 4);
     }
     p.bytes = off + 256;
     return p;
@@ -316,7 +369,6 @@ int launch_group_rows(const int32_t *cell, int64_t pairs, int cells, int64_t *of
     a.only = p.passes == 1;
     if (p.small) {
         a.bits = p.bits[0];
-        a.last = true;
         const size_t bytes = (size_t)(SMALL_NT / 64 + 1) * (4u << a.bits);
         if (bytes > 49152) { // (48 KB of dynamic LDS need no asking)
             const hipError_t e = hipFuncSetAttribute((const void *)k_group_small, hipFuncAttributeMaxDynamicSharedMemorySize, (SMALL_NT / 64 + 1) * BINS * 4);
@@ -325,21 +377,25 @@ int launch_group_rows(const int32_t *cell, int64_t pairs, int cells, int64_t *of
         hipLaunchKernelGGL(k_group_small, dim3(1), dim3(SMALL_NT), bytes, st, a);
         return (int)hipGetLastError();
     }
+    GroupEnd end = {nullptr, {}, pairs, p.passes, cells, (int)cgrid.x, off, place, source};
     for (int i = 0; i < p.passes; ++i) {
         a.bits = p.bits[i];
         a.last = i == p.passes - 1;
-        a.key_out = (uint32_t *)(base + p.key_off[i & 1]);
-        a.pair_out = (uint32_t *)(base + p.pair_off[i & 1]);
+        a.moved_out = (uint2 *)(base + p.moved_off[i & 1]);
+        a.to = (uint32_t *)(base + p.to_off[i]);
+        end.to[i] = a.to;
         hipLaunchKernelGGL(k_group_count, dim3((unsigned)p.tiles), dim3(GNT), 0, st, a);
-        hipLaunchKernelGGL(k_group_tiles, dim3((unsigned)(((1 << a.bits) + GWAVES - 1) / GWAVES)), dim3(GNT), 0, st, a.count, a.total,
+        hipLaunchKernelGGL(k_group_tiles, dim3((unsigned)(((1 << a.bits) + 15) / 16)), dim3(SLICES * 16), 0, st, a.count, a.total,
                            p.tiles, 1 << a.bits);
         hipLaunchKernelGGL(k_group_place, dim3((unsigned)p.tiles), dim3(GNT), 0, st, a);
         a.cell = nullptr;
-        a.key = a.key_out;
-        a.pair = a.pair_out;
+        a.moved = a.moved_out;
         a.shift += a.bits;
     }
-    if (p.passes > 1) hipLaunchKernelGGL(k_group_offsets, cgrid, dim3(256), 0, st, a.key, pairs, cells, off);
+    if (p.passes > 1) {
+        end.moved = a.moved;
+        hipLaunchKernelGGL(k_group_end, dim3((unsigned)(cgrid.x + (pairs + 255) / 256)), dim3(256), 0, st, end);
+    }
     return (int)hipGetLastError();
 }
 
