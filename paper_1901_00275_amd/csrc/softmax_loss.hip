@@ -38,6 +38,9 @@
 #define FEW_WORK 1e9          // products
 #define FEW_NARROW_ROWS 128   // up to NARROW_DIM dimensions
 #define FEW_NARROW_WORK 1.2e8
+// Up to so many inverse scales every workgroup that needs their largest finds it: a step of 256 x 16 384 x 96 fp32 57.0 -> 55.5 us, of
+// 4 095 x 16 384 x 96 fp16 215 -> 212; 4 095 x 65 536 x 128 fp32 870 either way.
+#define SMALL_SCALES 8192
 #define MERGE_ROWS 2048      // up to so many rows four a workgroup are merged, not sixteen
 #define FEW_WIDE 65536       // from so many centroids on a wave takes 32 of them: then there are waves enough
 #define FEW_GROUPS 512       // with fewer workgroups of eight waves they have two
@@ -212,19 +215,21 @@ struct PackArgs {
     int32_t *lab;
     LossHeader *hdr;
     bool xvec, cvec, raw, halves;
+    bool small;          // no launch for the header
+    int64_t rinvs, cinvs; // inverse scales
     int xblocks, cblocks, dblocks, xunits, cunits; // workgroups for x, for c; units of the columns' images
 };
 
 // A row's numbers: factor s log2(e) / scale, and backward its maximum, the factors of P in either order (2^15 / z, and with
 // g / max g); a row that does not count, or has no logit above -inf, gets the maximum +inf and no label.
-__device__ __forceinline__ void row_numbers(const PackArgs &a, int64_t i, float inv)
+__device__ __forceinline__ void row_numbers(const PackArgs &a, int64_t i, float inv, float top)
 {
     const bool in = i < a.n && (uint32_t)a.label[i] < (uint32_t)a.k;
     f32x4 r = {in ? a.scale * LOG2E * (a.raw ? 1.f : inv) : 0.f, INFINITY, 0.f, 0.f};
     float f = 0.f;
     bool ok = in;
     if (a.stats && in) {
-        const float m = a.stats[2 * i], z = a.stats[2 * i + 1], top = a.hdr->top;
+        const float m = a.stats[2 * i], z = a.stats[2 * i + 1];
         ok = m != -INFINITY;
         if (ok) {
             f = top > 0.f ? a.g[i] / top : a.g[i]; // (zero, or no finite one is there)
@@ -255,52 +260,71 @@ __global__ __launch_bounds__(256) void k_pack_rows(PackArgs a)
     pack_rows<T, true, NP, HELD, RAW>(blockIdx.x, (const T *)a.x, a.n, a.d, a.units, a.label, a.k, nullptr, a.ximg, a.rinv, a.xvec);
     if (a.stats) return;
     __syncthreads();
-    if (threadIdx.x < 16) row_numbers(a, (int64_t)blockIdx.x * 16 + threadIdx.x, a.rinv[(int64_t)blockIdx.x * 16 + threadIdx.x]);
+    if (threadIdx.x < 16) row_numbers(a, (int64_t)blockIdx.x * 16 + threadIdx.x, a.rinv[(int64_t)blockIdx.x * 16 + threadIdx.x], 0.f);
 }
 
-// Backward: the largest inverse scales of either matrix, and the largest |g|, a workgroup each.  (An atomic of every workgroup of
-// k_pack_rows on one address took 43 us at 65 536 centroids.)
-__global__ __launch_bounds__(1024) void k_loss_header(PackArgs a)
+// Backward: the largest inverse scale of x's rows (0), of c's (1), the largest |g| (2), in every thread
+template <int NT>
+__device__ __forceinline__ float header_value(const PackArgs &a, int which)
 {
-    __shared__ float s[16];
+    __shared__ float s[NT / 64];
     float mx = 0.f;
-    if (blockIdx.x == 2) {
+    if (which == 2) {
 #pragma unroll 4
-        for (int64_t i = threadIdx.x; i < a.n; i += 1024) {
+        for (int64_t i = threadIdx.x; i < a.n; i += NT) {
             const float v = fabsf(a.g[i]);
             if ((uint32_t)a.label[i] < (uint32_t)a.k && v < INFINITY) mx = fmaxf(mx, v);
         }
     } else {
-        const float *v = blockIdx.x == 0 ? a.rinv : a.cinv;
-        const int64_t count = !v ? 0 : (int64_t)(blockIdx.x == 0 ? a.xblocks * 16 : a.cblocks);
+        if (a.halves) return 1.f; // (fp16 values are not scaled)
+        const float *v = which == 0 ? a.rinv : a.cinv;
+        const int64_t count = !v ? 0 : which == 0 ? a.rinvs : a.cinvs;
 #pragma unroll 4
-        for (int64_t i = threadIdx.x; i < count; i += 1024) mx = fmaxf(mx, v[i]);
+        for (int64_t i = threadIdx.x; i < count; i += NT) mx = fmaxf(mx, v[i]);
     }
     mx = __uint_as_float(wave_max_u32(__float_as_uint(mx)));
     if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = mx;
     __syncthreads();
-    if (threadIdx.x > 0) return;
-    for (int w = 1; w < 16; ++w) mx = fmaxf(mx, s[w]);
-    if (blockIdx.x < 2 && a.halves) mx = 1.f; // (fp16 values are not scaled)
-    (blockIdx.x == 0 ? a.hdr->xinv : blockIdx.x == 1 ? a.hdr->cinv : a.hdr->top) = mx;
+    mx = s[0];
+#pragma unroll
+    for (int w = 1; w < NT / 64; ++w) mx = fmaxf(mx, s[w]);
+    __syncthreads();
+    return mx;
+}
+__device__ __forceinline__ void header_write(const PackArgs &a, int which, float v)
+{
+    if (threadIdx.x == 0) (which == 0 ? a.hdr->xinv : which == 1 ? a.hdr->cinv : a.hdr->top) = v;
 }
 
-// Backward: both matrices' columns, and the rows' numbers
+// The header by a launch of its own, a workgroup each.  (An atomic of every workgroup of k_pack_rows on one address took 43 us at
+// 65 536 centroids.)
+__global__ __launch_bounds__(1024) void k_loss_header(PackArgs a) { header_write(a, blockIdx.x, header_value<1024>(a, blockIdx.x)); }
+
+// Backward: both matrices' columns, and the rows' numbers.  a.small: every workgroup finds what it needs of the header by itself,
+// the last one writes it.
 template <typename T, int XORDER, int CORDER, int NP>
 __global__ __launch_bounds__(256) void k_pack_cols(PackArgs a)
 {
     int b = blockIdx.x;
     if (b < a.xblocks) {
-        pack_cols<T, XORDER, NP>(b / a.dblocks, b % a.dblocks, (const T *)a.x, a.n, a.d, a.xunits, a.label, a.k, nullptr, a.xcols, a.hdr->xinv, a.xvec);
+        const float inv = a.small ? header_value<256>(a, 0) : a.hdr->xinv;
+        pack_cols<T, XORDER, NP>(b / a.dblocks, b % a.dblocks, (const T *)a.x, a.n, a.d, a.xunits, a.label, a.k, nullptr, a.xcols, inv, a.xvec);
         return;
     }
     b -= a.xblocks;
     if (b < a.cblocks) {
-        pack_cols<T, CORDER, NP>(b / a.dblocks, b % a.dblocks, (const T *)a.c, a.k, a.d, a.cunits, nullptr, a.k, a.bias, a.ccols, a.hdr->cinv, a.cvec);
+        const float inv = a.small ? header_value<256>(a, 1) : a.hdr->cinv;
+        pack_cols<T, CORDER, NP>(b / a.dblocks, b % a.dblocks, (const T *)a.c, a.k, a.d, a.cunits, nullptr, a.k, a.bias, a.ccols, inv, a.cvec);
         return;
     }
     const int64_t i = (int64_t)(b - a.cblocks) * 256 + threadIdx.x; // (the workgroups cover the padded rows)
-    row_numbers(a, i, a.rinv[i]);
+    const float top = a.small ? header_value<256>(a, 2) : a.hdr->top;
+    row_numbers(a, i, a.rinv[i], top);
+    if (a.small && blockIdx.x == gridDim.x - 1) {
+        header_write(a, 2, top);
+        header_write(a, 1, header_value<256>(a, 1));
+        header_write(a, 0, header_value<256>(a, 0));
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -1160,12 +1184,15 @@ static bool as_they_lie(const LossArgs &a, const LossPlan &p)
     return sizeof(T) == 2 && !p.narrow && a.n <= LIE_ROWS && rows_vec<T>(a.c, a.d);
 }
 
-// The images of rows and centroids, and the rest of what the products need: one launch, three backward
+// The images of rows and centroids, and the rest of what the products need: one launch, two or three backward
 template <typename T, int NP>
 static void loss_images(const LossArgs &a, const LossPlan &p, bool backward, hipStream_t st)
 {
     PackArgs g = {a.x, a.c, a.n, a.d, a.k, p.units, a.label, a.bias, a.grad, backward ? a.stats : nullptr, a.scale, p.ximg, p.cimg,
                   p.xcols, p.ccols, p.rinv, p.cinv, p.gn, p.bias2, p.row, p.lab, p.hdr, rows_vec<T>(a.x, a.d), rows_vec<T>(a.c, a.d), as_they_lie<T>(a, p), __is_same(T, _Float16)};
+    g.rinvs = p.npad;
+    g.cinvs = p.kpad / 16;
+    g.small = g.rinvs + g.cinvs <= SMALL_SCALES;
     g.xblocks = (int)(p.npad / 16);
     g.cblocks = (int)(p.kpad / 16);
     const dim3 packs((unsigned)(g.xblocks + g.cblocks));
@@ -1186,7 +1213,7 @@ static void loss_images(const LossArgs &a, const LossPlan &p, bool backward, hip
     } else {
         pack(std::false_type{});
     }
-    if (backward) hipLaunchKernelGGL(k_loss_header, dim3(3), dim3(1024), 0, st, g);
+    if (backward && !g.small) hipLaunchKernelGGL(k_loss_header, dim3(3), dim3(1024), 0, st, g);
     if (!backward) return;
     g.dblocks = p.dblocks;
     g.xunits = (int)(p.npad / 32);
