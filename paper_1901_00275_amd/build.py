@@ -8,7 +8,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libvlq.so")
 SOURCES = ["api.hip", "coarse.hip", "coarse_bf16.hip", "coarse_half.hip", "train.hip", "search.hip", "scan_stream.hip", "scan_wide.hip", "encode.hip", "lists.hip",
-           "softmax_loss.hip", "softmax_loss_narrow.hip", "group_rows.hip", "clip_grads.hip"]
+           "softmax_loss.hip", "softmax_loss_narrow.hip", "softmax_loss_few.hip", "group_rows.hip", "clip_grads.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
     # packed fp32 instructions are not to be generated on the test machines

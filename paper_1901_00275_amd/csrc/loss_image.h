@@ -99,6 +99,37 @@ __device__ __forceinline__ void store4(T *p, const f32x4 &v, int count, bool vec
         if (e < count) p[e] = (T)v[e];
 }
 
+// ---- softmax_loss_few.hip ----
+struct FewSide { // one gradient: rows, length of its sum, the parts that is cut into, steps of 16 of a part
+    int rows, sum, parts, per;
+    int rtiles, dtiles, blocks; // tiles of 32 rows, of 64 dimensions (256 where the waves do not share a sum), workgroups
+    bool share;                 // the four waves of a workgroup share a tile's sum
+    bool slab;                  // slabs [parts][rows x d], or typed and times the scale
+    void *out;                  // (NULL: dbias alone)
+};
+struct FewArgs {
+    const void *x, *c;
+    const float *bias;
+    const int32_t *label;
+    float scale2; // in units of log 2
+    int n, d, k;
+    int groups; // of centroids
+    // forward
+    float2 *part; // [groups][n]
+    float *mine;
+    // backward
+    const float *stats, *grad;
+    float *G; // [n][kp]
+    int kp;
+    FewSide dx, dc;
+    float *db; // [parts of dc][kp], or dbias itself
+    float scale;
+};
+int few_groups(int dtype, int64_t n, int d, int k);
+int few_parts(int64_t rows, int64_t sum, int d);
+FewSide few_side(int64_t rows, int64_t sum, int d, int parts, void *out, bool slab);
+void launch_loss_few(int dtype, const FewArgs &a, bool backward, hipStream_t st); // statistics, or G
+void launch_loss_few_grads(int dtype, const FewArgs &a, hipStream_t st);
 
 // ---- softmax_loss_narrow.hip ----
 // rows that a workgroup keeps: 256 halve the traffic of LDS where their sums and fragments fit the registers

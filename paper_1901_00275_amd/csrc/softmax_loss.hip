@@ -30,20 +30,29 @@
 #define NARROW_DIM 128       // up to so many dimensions the gradients take the narrow form (softmax_loss_narrow.hip)
 #define NARROW_GROUPS 1024   // its workgroups, about: two rounds of two a compute unit
 #define NARROW_LEAST 8       // tiles of 32 rows that a workgroup of it takes at least (forward half as many)
-// The logits come from the centroids as they lie (k_loss_few) where little is done with each: rewriting them first, and tiles that
-// leave most of the chip idle, cost more.  Measured in us, these against the others: 1 000 x 1 000 x 1 000 bf16 20 : 38,
-// 8 000 x 120 x 500 fp32 36 : 54, 8 000 x 120 x 1 000 bf16 25 : 45, 535 x 975 x 1 248 fp32 75 : 85, 128 x 65 536 x 64 fp16 22 : 31;
-// the narrow form holds out longer: 1 000 x 5 000 x 96 fp32 39 : 19, 2 000 x 5 000 x 96 bf16 26 : 20, 70 x 65 536 x 96 fp32 39 : 41.
+// Where little is done with each centroid, rows and centroids are taken as they lie (softmax_loss_few.hip): rewriting them first,
+// and tiles that leave most of the chip idle, cost more.  Measured in us, these against the others.
+// Forward: 1 000 x 1 000 x 1 000 bf16 20 : 38, 8 000 x 120 x 500 fp32 27 : 54, 8 000 x 120 x 1 000 bf16 25 : 45, 535 x 975 x 1 248
+// fp32 45 : 85, 128 x 65 536 x 64 fp16 17 : 31; the narrow form holds out longer: 1 000 x 5 000 x 96 fp32 39 : 19,
+// 2 000 x 5 000 x 96 bf16 26 : 20, 70 x 65 536 x 96 fp32 29 : 41.
 #define FEW_ROWS 64
 #define FEW_WORK 1e9          // products
 #define FEW_NARROW_ROWS 128   // up to NARROW_DIM dimensions
 #define FEW_NARROW_WORK 1.2e8
+// A step with the gradients (their products are fp32's, an eighth of the others' rate, but with few rows or centroids the others' tiles
+// are mostly empty): 5 366 x 24 x 2 016 fp16 67 : 115, 3 x 30 x 224 fp16 22 : 38, 500 x 500 x 500 fp32 46 : 103, bf16 52 : 75,
+// 8 000 x 32 x 2 000 fp32 134 : 282, 32 x 16 000 x 2 000 bf16 121 : 179; 1 000 x 1 000 x 300 bf16 76 : 79, 4 000 x 400 x 200 bf16
+// 67 : 66, 2 000 x 1 500 x 160 fp16 80 : 64.  Narrow: 300 x 300 x 128 bf16 26 : 35, 300 x 3 000 x 96 bf16 37 : 39, 1 000 x 1 000 x 96
+// fp32 45 : 43, 100 x 16 384 x 128 fp32 78 : 60.
+#define FEW_GRAD_ROWS 64      // rows or centroids, up to which FEW_WORK holds
+#define FEW_GRAD_WORK 2.5e8   // beyond that
+#define FEW_GRAD_NARROW_WORK 5e7
+#define FEW_PAIRS (1 << 24)   // values of G, in fp32
 // Up to so many inverse scales every workgroup that needs their largest finds it: a step of 256 x 16 384 x 96 fp32 57.0 -> 55.5 us, of
 // 4 095 x 16 384 x 96 fp16 215 -> 212; 4 095 x 65 536 x 128 fp32 870 either way.
 #define SMALL_SCALES 8192
+#define FEW_PAIRS (1 << 24)   // values of G, in fp32
 #define MERGE_ROWS 2048      // up to so many rows four a workgroup are merged, not sixteen
-#define FEW_WIDE 65536       // from so many centroids on a wave takes 32 of them: then there are waves enough
-#define FEW_GROUPS 512       // with fewer workgroups of eight waves they have two
 
 // ---------------------------------------------------------------------------
 // images
@@ -673,125 +682,6 @@ __global__ __launch_bounds__(256) void k_loss_merge(const float2 *part, int part
     if (loss) loss[i] = (uint32_t)lab[i] >= (uint32_t)k ? 0.f : m == -INFINITY ? INFINITY : LN2 * (m - mine[i]) + logf(z);
 }
 
-// Few rows, or little work: every wave multiplies 16 G centroids, read from where they lie, with up to 64 rows (NT tiles of 16),
-// two or eight waves a workgroup; 16-bit values on their own matrix instructions, fp32 on the fp32 ones (a read of 4 bytes needs 16 NT
-// multiplications, which these do in time up to NT = 4).  Nothing is rewritten first; up to 64 rows the centroids pass once and
-// bound it (65 536 x 1 024 bf16, one row: 25 us, 5.4 TB/s), beyond that the rows' fragments from the caches do.
-struct FewArgs {
-    const void *x, *c;
-    const float *bias;
-    const int32_t *label;
-    float scale2; // in units of log 2
-    int n, d, k, groups;
-    float2 *part; // [groups][n]
-    float *mine;
-};
-template <typename T>
-struct FewPiece { // what a lane reads of a row at a time: its share of STEP indices
-    static constexpr int N = 16 / sizeof(T), STEP = 4 * N;
-    T v[N];
-};
-template <typename T, bool VEC>
-__device__ __forceinline__ FewPiece<T> few_piece(const T *row, int i, int d, bool there)
-{
-    FewPiece<T> r;
-    if (VEC) {
-        u32x4 v = {0, 0, 0, 0};
-        if (there && i < d) v = *(const u32x4 *)(row + i);
-        *(u32x4 *)r.v = v;
-    } else {
-#pragma unroll
-        for (int e = 0; e < FewPiece<T>::N; ++e) r.v[e] = there && i + e < d ? row[i + e] : (T)0.f;
-    }
-    return r;
-}
-__device__ __forceinline__ void few_multiply(const FewPiece<float> &a, const FewPiece<float> &b, f32x4 &acc)
-{
-#pragma unroll
-    for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[e], b.v[e], acc, 0, 0, 0);
-}
-__device__ __forceinline__ void few_multiply(const FewPiece<_Float16> &a, const FewPiece<_Float16> &b, f32x4 &acc)
-{
-    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(*(const half8 *)a.v, *(const half8 *)b.v, acc, 0, 0, 0);
-}
-__device__ __forceinline__ void few_multiply(const FewPiece<bf16_t> &a, const FewPiece<bf16_t> &b, f32x4 &acc)
-{
-    typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
-    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8 *)a.v, *(const bf16x8 *)b.v, acc, 0, 0, 0);
-}
-
-template <typename T, bool VEC, int W, int G, int NT>
-__global__ __launch_bounds__(W * 64) void k_loss_few(FewArgs a)
-{
-    constexpr int STEP = FewPiece<T>::STEP, N = FewPiece<T>::N, U = 16 / (G + NT) < 2 ? 2 : 16 / (G + NT);
-    const int tid = threadIdx.x, lane = tid & 63, l = lane & 15, g = lane >> 4, wave = tid >> 6;
-    const int group = blockIdx.x % a.groups, m0 = (group * W + wave) * 16 * G, n0 = (int)(blockIdx.x / a.groups) * 16 * NT;
-    const T *crow[G], *xrow[NT];
-    bool cin[G], xin[NT];
-    f32x4 acc[G][NT];
-#pragma unroll
-    for (int i = 0; i < G; ++i) {
-        cin[i] = m0 + 16 * i + l < a.k;
-        crow[i] = (const T *)a.c + (int64_t)(cin[i] ? m0 + 16 * i + l : 0) * a.d;
-    }
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        xin[j] = n0 + 16 * j + l < a.n;
-        xrow[j] = (const T *)a.x + (int64_t)(xin[j] ? n0 + 16 * j + l : 0) * a.d;
-#pragma unroll
-        for (int i = 0; i < G; ++i) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-    for (int k0 = g * N; k0 < a.d + g * N; k0 += U * STEP) { // (the same turns for all lanes)
-        FewPiece<T> cv[U][G], xv[U][NT];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-#pragma unroll
-            for (int i = 0; i < G; ++i) cv[u][i] = few_piece<T, VEC>(crow[i], k0 + u * STEP, a.d, cin[i]);
-#pragma unroll
-            for (int j = 0; j < NT; ++j) xv[u][j] = few_piece<T, VEC>(xrow[j], k0 + u * STEP, a.d, xin[j]);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int i = 0; i < G; ++i)
-#pragma unroll
-                for (int j = 0; j < NT; ++j) few_multiply(cv[u][i], xv[u][j], acc[i][j]);
-    }
-    __shared__ float2 s[W][16 * NT];
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        const int n = n0 + 16 * j + l, lab = n < a.n ? a.label[n] : -1;
-        float m = -INFINITY, z = 0.f;
-#pragma unroll
-        for (int i = 0; i < G; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int c = m0 + 16 * i + 4 * g + r;
-                const float b = c >= a.k ? -INFINITY : a.bias ? a.bias[c] * LOG2E : 0.f;
-                const float v = b == -INFINITY ? -INFINITY : fmaf(acc[i][j][r], a.scale2, b);
-                if (c == lab && c < a.k) a.mine[n] = v;
-                m = fmaxf(m, v);
-                acc[i][j][r] = v;
-            }
-        m = fmaxf(m, __shfl_xor(m, 16, 64));
-        m = fmaxf(m, __shfl_xor(m, 32, 64));
-        const float m1 = m == -INFINITY ? 0.f : m;
-#pragma unroll
-        for (int i = 0; i < G; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) z += __builtin_amdgcn_exp2f(acc[i][j][r] - m1);
-        z += __shfl_xor(z, 16, 64);
-        z += __shfl_xor(z, 32, 64);
-        if (g == 0) s[wave][16 * j + l] = make_float2(m, z);
-    }
-    __syncthreads();
-    if (tid >= 16 * NT || n0 + tid >= a.n) return;
-    float2 v = s[0][tid];
-#pragma unroll
-    for (int w = 1; w < W; ++w) v = join(v, s[w][tid]);
-    a.part[(int64_t)group * a.n + n0 + tid] = v;
-}
-
 // Backward: P of a tile, as images in both orders, and the sums over a wave's 64 rows for the bias
 template <class FORM>
 __global__ __launch_bounds__(LNT, 2) void k_loss_p(LogitArgs a)
@@ -957,7 +847,7 @@ struct SlabSum {
     const float *slabs;
     int splits, blocks;
     int64_t count;
-    const float *inv, *top;
+    const float *inv, *top; // of P's images, or NULL
     void *out;
 };
 // dbias of a piece: sums over the rows' parts, 64 centroids a workgroup, four waves taking the parts in turn
@@ -979,7 +869,7 @@ __device__ __forceinline__ void bias_sum(int block, const BiasSum &a)
     sum[wave][lane] = s;
     __syncthreads();
     if (wave > 0 || j >= a.count) return;
-    s = ((sum[0][lane] + sum[1][lane]) + (sum[2][lane] + sum[3][lane])) * (*a.top * (1.f / P_ONE));
+    s = ((sum[0][lane] + sum[1][lane]) + (sum[2][lane] + sum[3][lane])) * (a.top ? *a.top * (1.f / P_ONE) : 1.f);
     a.out[j] = a.add ? a.out[j] + s : s;
 }
 
@@ -994,7 +884,7 @@ __global__ __launch_bounds__(256) void k_loss_sums(SlabSum x, SlabSum c, BiasSum
     const SlabSum &a = first ? x : c;
     const int64_t i = ((int64_t)(first ? blockIdx.x : blockIdx.x - x.blocks) * 256 + threadIdx.x) * 4;
     if (i >= a.count) return;
-    const float f = grad_factor(*a.inv, a.top ? *a.top : 1.f, scale);
+    const float f = a.inv ? grad_factor(*a.inv, a.top ? *a.top : 1.f, scale) : scale;
     const bool vec = a.count % 4 == 0 && (uintptr_t)a.out % (4 * sizeof(T)) == 0;
     const int count = (int)min((int64_t)4, a.count - i);
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
@@ -1035,6 +925,9 @@ struct LossPlan {
     int64_t piece;           // centroids whose P is kept at a time
     int xsplit, csplit;      // parts that the sums of dx (over a piece) and dc (over `rows`) are cut into
     bool xslab, cslab;
+    bool few;                // softmax_loss_few.hip
+    float *G;
+    int kp;
     bool narrow;             // softmax_loss_narrow.hip
     int xper, cper;          // its tiles of a part
     LossHeader *hdr;
@@ -1075,6 +968,13 @@ static bool loss_is_few(int64_t n, int d, int k)
     return n <= FEW_ROWS || (d <= NARROW_DIM ? n <= FEW_NARROW_ROWS || work <= FEW_NARROW_WORK : work <= FEW_WORK);
 }
 
+static bool grads_are_few(int64_t n, int d, int k)
+{
+    const double work = (double)n * d * k;
+    if (n * pad_to(k, 32) > FEW_PAIRS) return false;
+    return work <= (d <= NARROW_DIM ? FEW_GRAD_NARROW_WORK : n <= FEW_GRAD_ROWS || k <= FEW_GRAD_ROWS ? FEW_WORK : FEW_GRAD_WORK);
+}
+
 static LossPlan loss_plan(int dtype, int64_t n, int d, int k, bool backward, void *ws)
 {
     LossPlan p = {};
@@ -1098,6 +998,20 @@ static LossPlan loss_plan(int dtype, int64_t n, int d, int k, bool backward, voi
         ptr = ws ? (std::remove_reference_t<decltype(ptr)>)((char *)ws + off) : nullptr;
         off += count * sizeof(*ptr);
     };
+    p.few = backward && grads_are_few(n, d, k);
+    if (p.few) {
+        p.kp = (int)pad_to(k, 32);
+        take(p.G, (size_t)n * p.kp);
+        p.xsplit = few_parts(n, k, d);
+        p.csplit = few_parts(k, n, d);
+        p.xslab = p.xsplit > 1;
+        p.cslab = p.csplit > 1;
+        take(p.dbpart, (size_t)p.csplit * p.kp);
+        take(p.xsum, p.xslab ? (size_t)p.xsplit * n * d : 0);
+        take(p.csum, p.cslab ? (size_t)p.csplit * k * d : 0);
+        p.bytes = (off + 255) & ~(size_t)255;
+        return p;
+    }
     const size_t page = (size_t)PAGE * p.np;
     take(p.hdr, 1);
     take(p.ximg, p.npad / 128 * p.units * page);
@@ -1260,42 +1174,15 @@ static void launch_merge(const float2 *part, int parts, int npad, const float *m
         hipLaunchKernelGGL(k_loss_merge<16>, dim3((unsigned)((n + 15) / 16)), dim3(256), 0, st, part, parts, npad, mine, lab, k, n, stats, loss);
 }
 
-template <typename T>
 static int loss_few(const LossArgs &a, hipStream_t st)
 {
-    // two waves a workgroup where eight would leave compute units without one; eight with twice the centroids each where
-    // there are plenty
-    const int64_t rows64 = (a.n + 63) / 64;
-    const bool wide = a.k >= FEW_WIDE, small = (a.k + 127) / 128 * rows64 < FEW_GROUPS;
-    const int each = small ? 32 : wide ? 256 : 128, groups = (a.k + each - 1) / each;
+    const int groups = few_groups(a.dtype, a.n, a.d, a.k);
     float2 *part = (float2 *)a.ws;
     float *mine = (float *)(part + (int64_t)groups * a.n);
-    const FewArgs f = {a.x, a.c, a.bias, a.label, a.scale * LOG2E, (int)a.n, a.d, a.k, groups, part, mine};
-    auto go = [&](auto VEC, auto W, auto G, auto NT) {
-        constexpr int R = 16 * decltype(NT)::value;
-        hipLaunchKernelGGL((k_loss_few<T, decltype(VEC)::value, decltype(W)::value, decltype(G)::value, decltype(NT)::value>),
-                           dim3((unsigned)(groups * ((a.n + R - 1) / R))), dim3(decltype(W)::value * 64), 0, st, f);
-    };
-    auto rows = [&](auto VEC, auto W, auto G) {
-        if (a.n <= 16)
-            go(VEC, W, G, std::integral_constant<int, 1>{});
-        else if (a.n <= 32)
-            go(VEC, W, G, std::integral_constant<int, 2>{});
-        else
-            go(VEC, W, G, std::integral_constant<int, 4>{});
-    };
-    auto cells = [&](auto VEC) {
-        if (small)
-            rows(VEC, std::integral_constant<int, 2>{}, std::integral_constant<int, 1>{});
-        else if (wide)
-            rows(VEC, std::integral_constant<int, 8>{}, std::integral_constant<int, 2>{});
-        else
-            rows(VEC, std::integral_constant<int, 8>{}, std::integral_constant<int, 1>{});
-    };
-    if (a.d * sizeof(T) % 16 == 0 && ((uintptr_t)a.x | (uintptr_t)a.c) % 16 == 0)
-        cells(std::true_type{});
-    else
-        cells(std::false_type{});
+    FewArgs f = {a.x, a.c, a.bias, a.label, a.scale * LOG2E, (int)a.n, a.d, a.k};
+    f.part = part;
+    f.mine = mine;
+    launch_loss_few(a.dtype, f, false, st);
     launch_merge(part, groups, (int)a.n, mine, a.label, a.k, a.n, a.stats, a.loss, st);
     return (int)hipGetLastError();
 }
@@ -1303,7 +1190,7 @@ static int loss_few(const LossArgs &a, hipStream_t st)
 template <typename T, int NP>
 static int loss_forward(const LossArgs &a, hipStream_t st)
 {
-    if (loss_is_few(a.n, a.d, a.k)) return loss_few<T>(a, st);
+    if (loss_is_few(a.n, a.d, a.k)) return loss_few(a, st);
     const LossPlan p = loss_plan(a.dtype, a.n, a.d, a.k, false, a.ws);
     loss_images<T, NP>(a, p, false, st);
     if (p.narrow) {
@@ -1349,20 +1236,36 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
         return (int)hipGetLastError();
     }
     const LossPlan p = loss_plan(a.dtype, a.n, a.d, a.k, true, a.ws);
-    loss_images<T, NP>(a, p, true, st);
+    if (!p.few) loss_images<T, NP>(a, p, true, st);
     auto bias_part = [&](int slots, int64_t ld, int64_t c0, int64_t count, bool add) {
-        return BiasSum{p.dbpart, slots, (int)ld, (int)count, (int)((count + 63) / 64), &p.hdr->top, add, a.dbias + c0};
+        return BiasSum{p.dbpart, slots, (int)ld, (int)count, (int)((count + 63) / 64), p.few ? nullptr : &p.hdr->top, add, a.dbias + c0};
     };
     auto finish = [&](const BiasSum &bias) {
         auto side = [&](float *slabs, int splits, int64_t count, const float *inv, const float *top, void *out) {
             return SlabSum{slabs, splits, (int)((count + 1023) / 1024), count, inv, top, out};
         };
         SlabSum x = {}, c = {};
-        if (a.dx && p.xslab) x = side(p.xsum, p.xsplit, a.n * a.d, &p.hdr->cinv, nullptr, a.dx);
-        if (a.dc && p.cslab) c = side(p.csum, p.csplit, (int64_t)a.k * a.d, &p.hdr->xinv, &p.hdr->top, a.dc);
+        if (a.dx && p.xslab) x = side(p.xsum, p.xsplit, a.n * a.d, p.few ? nullptr : &p.hdr->cinv, nullptr, a.dx);
+        if (a.dc && p.cslab) c = side(p.csum, p.csplit, (int64_t)a.k * a.d, p.few ? nullptr : &p.hdr->xinv, &p.hdr->top, a.dc);
         const int blocks = x.blocks + c.blocks + bias.blocks;
         if (blocks) hipLaunchKernelGGL(k_loss_sums<T>, dim3((unsigned)blocks), dim3(256), 0, st, x, c, bias, a.scale);
     };
+    if (p.few) {
+        FewArgs f = {a.x, a.c, a.bias, a.label, a.scale * LOG2E, (int)a.n, a.d, a.k};
+        f.stats = a.stats;
+        f.grad = a.grad;
+        f.G = p.G;
+        f.kp = p.kp;
+        launch_loss_few(a.dtype, f, true, st);
+        const bool bias = a.dbias != nullptr;
+        f.scale = a.scale;
+        if (a.dx) f.dx = few_side(a.n, a.k, a.d, p.xsplit, p.xslab ? (void *)p.xsum : a.dx, p.xslab);
+        if (a.dc || bias) f.dc = few_side(a.k, a.n, a.d, p.csplit, !a.dc ? nullptr : p.cslab ? (void *)p.csum : a.dc, p.cslab);
+        f.db = !bias ? nullptr : p.cslab ? p.dbpart : a.dbias;
+        launch_loss_few_grads(a.dtype, f, st);
+        finish(bias && p.cslab ? bias_part(p.csplit, p.kp, 0, a.k, false) : BiasSum{});
+        return (int)hipGetLastError();
+    }
     if (p.narrow) {
         NarrowArgs g = {};
         const int rows = narrow_rows(NP, p.units);

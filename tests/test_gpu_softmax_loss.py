@@ -56,7 +56,8 @@ def compare(got, want, names=("loss", "dx", "dc", "db")):
 
 
 SHAPES = [(1, 1, 1), (1, 96, 300), (3, 7, 2), (64, 32, 256), (65, 33, 257), (255, 96, 1000), (257, 128, 513), (300, 130, 1025),
-          (40, 520, 77), (17, 1027, 515), (1000, 64, 5000), (33, 48, 65537), (9, 200, 70001), (129, 100, 9000), (700, 136, 1100), (2100, 500, 1001), (900, 264, 5003), (1500, 192, 4100)]
+          (40, 520, 77), (17, 1027, 515), (1000, 64, 5000), (33, 48, 65537), (9, 200, 70001), (129, 100, 9000), (700, 136, 1100), (2100, 500, 1001), (900, 264, 5003), (1500, 192, 4100),
+          (1000, 128, 3000), (2049, 31, 1500), (1200, 1027, 515), (3000, 130, 1025), (1111, 520, 777), (7, 300, 33), (5000, 129, 5), (2, 64, 40000)]
 
 
 @pytest.mark.parametrize("t", [F32, F16, BF16])
@@ -67,13 +68,13 @@ def test_against_64_bits(vlq, t, n, d, k):
 
 
 @pytest.mark.parametrize("t", [F32, F16, BF16])
-@pytest.mark.parametrize("n,d,k", [(1, 40, 100), (200, 96, 700), (513, 200, 300)])
+@pytest.mark.parametrize("n,d,k", [(1, 40, 100), (200, 96, 700), (513, 200, 300), (700, 96, 1500), (1513, 200, 1300)])
 def test_no_bias_negative_scale(vlq, t, n, d, k):
     x, c, _, label, grad = problem(t, n, d, k, bias=False, spread=3.0)
     compare(run(vlq, x, c, None, -1.3, label, grad), softmax_loss(x, c, None, -1.3, label, grad))
 
 
-@pytest.mark.parametrize("n,d,k", [(300, 96, 900), (40, 200, 700), (1400, 328, 2600)])
+@pytest.mark.parametrize("n,d,k", [(300, 96, 900), (40, 200, 700), (900, 96, 1900), (1400, 328, 2600)])
 @pytest.mark.parametrize("t", [F32, F16, BF16])
 def test_rows_and_centroids_that_do_not_count(vlq, t, n, d, k):
     x, c, bias, label, grad = problem(t, n, d, k, skip=0.3, out=0.3)
@@ -87,9 +88,9 @@ def test_rows_and_centroids_that_do_not_count(vlq, t, n, d, k):
     assert math.isinf(got["loss"][7].item()) and (got["loss"][dead] == 0).all() and (got["dx"][dead] == 0).all()
 
 
+@pytest.mark.parametrize("n,d,k", [(20, 64, 300), (300, 64, 3000), (1000, 160, 2000)])
 @pytest.mark.parametrize("t", [F32, BF16])
-def test_nothing_left(vlq, t):
-    n, d, k = 20, 64, 300
+def test_nothing_left(vlq, t, n, d, k):
     x, c, bias, label, grad = problem(t, n, d, k)
     bias.fill_(-math.inf)
     got = run(vlq, x, c, bias, 1.0, label, grad)
@@ -128,10 +129,10 @@ def test_most_rows_and_most_centroids(vlq):
 
 @pytest.mark.parametrize("t", [F32, F16, BF16])
 @pytest.mark.parametrize("bad", [math.inf, math.nan])
-@pytest.mark.parametrize("d", [40, 140])
-def test_gradients_that_are_not_finite(vlq, t, bad, d):
+@pytest.mark.parametrize("n,d,k", [(70, 40, 300), (70, 140, 300), (900, 40, 1500), (900, 140, 2100)])
+def test_gradients_that_are_not_finite(vlq, t, bad, n, d, k):
     # a row's own dx, and what is summed over the rows: whether other rows have gradients or not
-    x, c, bias, label, grad = problem(t, 70, d, 300)
+    x, c, bias, label, grad = problem(t, n, d, k)
     for others in (1.0, 0.0):
         grad = grad * others
         grad[7] = bad
@@ -139,22 +140,27 @@ def test_gradients_that_are_not_finite(vlq, t, bad, d):
         assert not got["dx"][7].isfinite().any()
         for name in ("dc", "db"):
             assert not got[name].isfinite().any(), name
-        rest = torch.arange(70, device=DEV) != 7
+        rest = torch.arange(n, device=DEV) != 7
         assert torch.equal(got["dx"][rest], ref["dx"][rest])
 
 
+SIZES = [(130, 128, 600), (1030, 128, 1600), (1030, 160, 1600)]  # of each form of the gradients
+
+
+@pytest.mark.parametrize("n,d,k", SIZES)
 @pytest.mark.parametrize("t", [F32, BF16])
-def test_large_and_small_logits(vlq, t):
+def test_large_and_small_logits(vlq, t, n, d, k):
     # logits in the hundreds, all but one probability vanish; and descriptors with a mean far above their spread
-    x, c, bias, label, grad = problem(t, 130, 128, 600, spread=60.0)
+    x, c, bias, label, grad = problem(t, n, d, k, spread=60.0)
     compare(run(vlq, x, c, bias, 1.0, label, grad), softmax_loss(x, c, bias, 1.0, label, grad))
-    x, c, bias, label, grad = problem(t, 130, 128, 600, mean=30.0)
+    x, c, bias, label, grad = problem(t, n, d, k, mean=30.0)
     compare(run(vlq, x, c, bias, 0.02, label, grad), softmax_loss(x, c, bias, 0.02, label, grad))
 
 
-def test_rows_of_uneven_size(vlq):
+@pytest.mark.parametrize("n,d,k", SIZES)
+def test_rows_of_uneven_size(vlq, n, d, k):
     # rows 24 binades apart keep their own scale forward; the gradients are relative to the largest
-    x, c, bias, label, grad = problem(F32, 200, 96, 500)
+    x, c, bias, label, grad = problem(F32, n, d, k)
     x[::3] *= 2.0 ** -24
     c[::7] *= 2.0 ** -10
     compare(run(vlq, x, c, bias, 1.0, label, grad), softmax_loss(x, c, bias, 1.0, label, grad))
@@ -174,9 +180,20 @@ def test_unaligned_operands(vlq, t, n):
         assert torch.equal(one[name], two[name]), name
 
 
+@pytest.mark.parametrize("n,d,k", SIZES + [(70, 66, 300), (70, 65, 300)])
+@pytest.mark.parametrize("t", [F32, F16, BF16])
+def test_unaligned_operands_against_64_bits(vlq, t, n, d, k):
+    x, c, bias, label, grad = problem(t, n, d, k)
+    for by in (1, 2, 4):
+        shift = lambda v: torch.cat([v.reshape(-1)[:by], v.reshape(-1)])[by:].view(v.shape)  # noqa: E731
+        ops = [shift(v) for v in (x, c, bias)]
+        compare(run(vlq, *ops, 1.0, label, grad), softmax_loss(x, c, bias, 1.0, label, grad))
+
+
+@pytest.mark.parametrize("n,d,k", [(300, 160, 700), (600, 96, 1000), (1500, 160, 1100)])
 @pytest.mark.parametrize("what", [("dx",), ("dc",), ("db",), ("dx", "db")])
-def test_some_gradients_alone(vlq, what):
-    x, c, bias, label, grad = problem(BF16, 300, 160, 700)
+def test_some_gradients_alone(vlq, what, n, d, k):
+    x, c, bias, label, grad = problem(BF16, n, d, k)
     whole, part = run(vlq, x, c, bias, 1.0, label, grad), run(vlq, x, c, bias, 1.0, label, grad, what)
     for name in what:
         assert torch.equal(whole[name], part[name]), name
@@ -210,8 +227,8 @@ def test_stats_give_the_log_sum(vlq):
     check(lse, (want["m"] + torch.log(want["z"]), want["loss"][1]), "log sum")
 
 
-def test_captured_and_replayed(vlq):
-    n, d, k = 300, 96, 2000
+@pytest.mark.parametrize("n,d,k", [(300, 96, 2000), (40, 200, 300), (5000, 150, 7), (1000, 160, 1700)])
+def test_captured_and_replayed(vlq, n, d, k):
     x, c, bias, label, grad = problem(F32, n, d, k)
     ws = torch.empty(vlq.vlq_softmax_loss_workspace(F32, n, d, k, 1), dtype=torch.uint8, device=DEV)
     loss, stats = torch.empty(n, device=DEV), torch.empty(n, 2, device=DEV)
