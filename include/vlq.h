@@ -318,8 +318,9 @@ int vlq_softmax_loss(int dtype, const void *d_x, int64_t n, int32_t d, const voi
  * The inputs of the forward call and its d_stats; d_grad [n] fp32, the gradient of each row's loss (1 / n for a mean).
  * d_dx [n x d], d_dc [k x d] of type dtype, d_dbias [k] fp32; each may be NULL.  Rows that do not count, and rows with no
  * centroid left, have zero gradients and add nothing to the others'.  n = 0 writes zeros to d_dc and d_dbias.
- * G is held as fp16 (two parts for fp32) relative to grad's largest magnitude, with an absolute error of at most 2^-40 of that
- * beside its rounding (2^-11, or 2^-22).  The values of x and c enter relative to the largest of their matrix.
+ * G is held in fp32 where little is done with each centroid, else as fp16 (two parts for fp32) relative to grad's largest magnitude,
+ * with an absolute error of at most 2^-40 of that beside its rounding (2^-11, or 2^-22); the values of x and c then enter
+ * relative to the largest of their matrix.
  * d_ws: at least vlq_softmax_loss_workspace(dtype, n, d, k, 1) bytes.
  */
 int vlq_softmax_loss_backward(int dtype, const void *d_x, int64_t n, int32_t d, const void *d_c, int32_t k,
@@ -327,7 +328,7 @@ int vlq_softmax_loss_backward(int dtype, const void *d_x, int64_t n, int32_t d, 
                               const float *d_grad, void *d_dx, void *d_dc, float *d_dbias, void *d_ws,
                               int64_t ws_bytes, void *stream);
 
-/* Bytes of workspace of either call (backward != 0: the second); a negative VLQ_E* code for sizes that are refused. */
+/* Bytes of workspace of the first call, or (backward != 0) of either; a negative VLQ_E* code for sizes that are refused. */
 int64_t vlq_softmax_loss_workspace(int dtype, int64_t n, int32_t d, int32_t k, int backward);
 
 /*

@@ -254,6 +254,66 @@ __global__ __launch_bounds__(SMALL_NT) void k_group_small(SortPass a)
     place_pairs(a, lds + wave * bins, i0, count, lane);
 }
 
+// Few pairs, many cells: one workgroup takes all passes in LDS, k_group_end the rest.  (6 pairs, 57 575 cells, with the gather: 29 us by a
+// launch for each step, 18 now; 4 096 pairs, 65 536 cells 30 and 22.)
+#define FEW_DIGIT 9
+#define FEW_PAIRS 4096
+__global__ __launch_bounds__(SMALL_NT) void k_group_few(SortPass a)
+{
+    constexpr int W = SMALL_NT / 64, MOST = 1 << FEW_DIGIT;
+    extern __shared__ uint32_t lds[]; // {key, pair} [2][FEW_PAIRS], [W][bins] a wave's next places, [bins] a digit's first
+    __shared__ uint32_t wsum[W];
+    uint2 *from = (uint2 *)lds, *to = from + FEW_PAIRS;
+    uint32_t *at = (uint32_t *)(to + FEW_PAIRS), *first = at + W * MOST;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, pairs = (int)a.pairs;
+    const int per = (pairs + W * 64 - 1) / (W * 64) * 64, i0 = wave * per, i1 = min(i0 + per, pairs);
+    for (int i = tid; i < pairs; i += SMALL_NT) from[i] = make_uint2(key_at(a, i), (uint32_t)i);
+    for (int shift = 0; shift < a.bits; shift += FEW_DIGIT) {
+        const int bits = min(FEW_DIGIT, a.bits - shift), bins = 1 << bits;
+        for (int b = tid; b < W * bins; b += SMALL_NT) at[b] = 0;
+        __syncthreads();
+        for (int i = i0 + lane; i < i1; i += 64) atomicAdd(&at[wave * bins + ((from[i].x >> shift) & (bins - 1))], 1u);
+        __syncthreads();
+        for (int b = tid; b < bins; b += SMALL_NT) {
+            uint32_t sum = 0;
+            for (int w = 0; w < W; ++w) sum += at[w * bins + b];
+            first[b] = sum;
+        }
+        __syncthreads();
+        block_scan<SMALL_NT>(first, bins, wsum);
+        for (int b = tid; b < bins; b += SMALL_NT) {
+            uint32_t next = first[b];
+            for (int w = 0; w < W; ++w) {
+                const uint32_t c = at[w * bins + b];
+                at[w * bins + b] = next;
+                next += c;
+            }
+        }
+        __syncthreads();
+        const uint64_t below = ((uint64_t)1 << lane) - 1;
+        for (int i = i0; i < i1; i += 64) {
+            const bool there = i + lane < i1;
+            const uint2 v = from[there ? i + lane : i];
+            const uint32_t digit = (v.x >> shift) & (bins - 1);
+            const uint64_t same = same_digit(digit, bits, there);
+            uint32_t *next = at + wave * bins + digit;
+            if (there) to[*next + __popcll(same & below)] = v;
+            wave_lds_order();
+            if (there && !(same & below)) *next += __popcll(same);
+            wave_lds_order();
+        }
+        __syncthreads();
+        uint2 *t = from;
+        from = to;
+        to = t;
+    }
+    for (int p = tid; p < pairs; p += SMALL_NT) {
+        const uint2 v = from[p];
+        a.moved_out[p] = v;
+        a.to[v.y] = v.x < (uint32_t)a.cells ? (uint32_t)p : 0xFFFFFFFFu;
+    }
+}
+
 // What several passes leave to be written, all of it in order: off[c], the first place whose cell is c or more; source; and
 // place, by following a pair through the passes.  (Written by the last pass, the places lay 4 bytes here and 4 there: 640 000
 // pairs, 65 536 cells, that pass 20 us and the offsets 6; now 11 and 9.)
@@ -307,7 +367,7 @@ __global__ __launch_bounds__(256) void k_group_none(int cells, int64_t *off)
 struct GroupPlan {
     int passes, bits[3], tile, tiles;
     size_t count_off, total_off, moved_off[2], to_off[3], bytes;
-    bool small;
+    bool small, few;
 };
 
 static GroupPlan group_plan(int64_t pairs, int cells)
@@ -321,6 +381,11 @@ static GroupPlan group_plan(int64_t pairs, int cells)
         left -= p.bits[i];
     }
     p.small = p.passes == 1 && pairs <= SMALL_PAIRS;
+    p.few = p.passes > 1 && pairs <= FEW_PAIRS;
+    if (p.few) {
+        p.passes = 1;
+        p.bits[0] = bits;
+    }
     // tiles: enough of them for every compute unit, large enough that the counts are fewer than the pairs
     p.tile = GWAVES * HELD * 64 / 2;
     while (p.tile < 8192 && pairs / p.tile > 512) p.tile *= 2;
@@ -334,9 +399,9 @@ static GroupPlan group_plan(int64_t pairs, int cells)
     if (!p.small) {
         p.count_off = take((size_t)BINS * p.tiles * 4);
         p.total_off = take((size_t)BINS * 4);
-        if (p.passes > 1)
+        if (p.passes > 1 || p.few)
             for (int i = 0; i < 2; ++i) p.moved_off[i] = take((size_t)pairs * sizeof(uint2));
-        if (p.passes > 1)
+        if (p.passes > 1 || p.few)
             for (int i = 0; i < p.passes; ++i) p.to_off[i] = take((size_t)pairs * 4);
     }
     p.bytes = off + 256;
@@ -378,6 +443,20 @@ int launch_group_rows(const int32_t *cell, int64_t pairs, int cells, int64_t *of
         return (int)hipGetLastError();
     }
     GroupEnd end = {nullptr, {}, pairs, p.passes, cells, (int)cgrid.x, off, place, source};
+    const dim3 ends((unsigned)(cgrid.x + (pairs + 255) / 256));
+    if (p.few) {
+        a.bits = p.bits[0];
+        a.moved_out = (uint2 *)(base + p.moved_off[0]);
+        a.to = (uint32_t *)(base + p.to_off[0]);
+        end.moved = a.moved_out;
+        end.to[0] = a.to;
+        const size_t bytes = 2 * FEW_PAIRS * sizeof(uint2) + (SMALL_NT / 64 + 1) * (4u << FEW_DIGIT);
+        const hipError_t e = hipFuncSetAttribute((const void *)k_group_few, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+        if (e != hipSuccess) return (int)e;
+        hipLaunchKernelGGL(k_group_few, dim3(1), dim3(SMALL_NT), bytes, st, a);
+        hipLaunchKernelGGL(k_group_end, ends, dim3(256), 0, st, end);
+        return (int)hipGetLastError();
+    }
     for (int i = 0; i < p.passes; ++i) {
         a.bits = p.bits[i];
         a.last = i == p.passes - 1;
@@ -394,7 +473,7 @@ int launch_group_rows(const int32_t *cell, int64_t pairs, int cells, int64_t *of
     }
     if (p.passes > 1) {
         end.moved = a.moved;
-        hipLaunchKernelGGL(k_group_end, dim3((unsigned)(cgrid.x + (pairs + 255) / 256)), dim3(256), 0, st, end);
+        hipLaunchKernelGGL(k_group_end, ends, dim3(256), 0, st, end);
     }
     return (int)hipGetLastError();
 }

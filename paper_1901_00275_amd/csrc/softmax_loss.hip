@@ -41,11 +41,13 @@
 #define FEW_NARROW_WORK 1.2e8
 // A step with the gradients (their products are fp32's, an eighth of the others' rate, but with few rows or centroids the others' tiles
 // are mostly empty): 5 366 x 24 x 2 016 fp16 67 : 115, 3 x 30 x 224 fp16 22 : 38, 500 x 500 x 500 fp32 46 : 103, bf16 52 : 75,
-// 8 000 x 32 x 2 000 fp32 134 : 282, 32 x 16 000 x 2 000 bf16 121 : 179; 1 000 x 1 000 x 300 bf16 76 : 79, 4 000 x 400 x 200 bf16
+// 8 000 x 32 x 2 000 fp32 134 : 282, 32 x 16 000 x 2 000 bf16 132 : 179, 8 000 x 64 x 4 000 bf16 269 : 327, 64 x 65 536 x 1 024 bf16
+// 410 : 322; 1 000 x 1 000 x 300 bf16 76 : 79, 4 000 x 400 x 200 bf16
 // 67 : 66, 2 000 x 1 500 x 160 fp16 80 : 64.  Narrow: 300 x 300 x 128 bf16 26 : 35, 300 x 3 000 x 96 bf16 37 : 39, 1 000 x 1 000 x 96
 // fp32 45 : 43, 100 x 16 384 x 128 fp32 78 : 60.
-#define FEW_GRAD_ROWS 64      // rows or centroids, up to which FEW_WORK holds
-#define FEW_GRAD_WORK 2.5e8   // beyond that
+#define FEW_GRAD_ROWS 64         // rows or centroids at most
+#define FEW_GRAD_THIN_WORK 2.5e9 // with so few
+#define FEW_GRAD_WORK 2.5e8      // with more
 #define FEW_GRAD_NARROW_WORK 5e7
 #define FEW_PAIRS (1 << 24)   // values of G, in fp32
 // Up to so many inverse scales every workgroup that needs their largest finds it: a step of 256 x 16 384 x 96 fp32 57.0 -> 55.5 us, of
@@ -972,7 +974,7 @@ static bool grads_are_few(int64_t n, int d, int k)
 {
     const double work = (double)n * d * k;
     if (n * pad_to(k, 32) > FEW_PAIRS) return false;
-    return work <= (d <= NARROW_DIM ? FEW_GRAD_NARROW_WORK : n <= FEW_GRAD_ROWS || k <= FEW_GRAD_ROWS ? FEW_WORK : FEW_GRAD_WORK);
+    return work <= (d <= NARROW_DIM ? FEW_GRAD_NARROW_WORK : n <= FEW_GRAD_ROWS || k <= FEW_GRAD_ROWS ? FEW_GRAD_THIN_WORK : FEW_GRAD_WORK);
 }
 
 static LossPlan loss_plan(int dtype, int64_t n, int d, int k, bool backward, void *ws)
@@ -1065,8 +1067,10 @@ static LossPlan loss_plan(int dtype, int64_t n, int d, int k, bool backward, voi
 
 size_t loss_workspace(int dtype, int64_t n, int d, int k, bool backward)
 {
-    if (!backward && loss_is_few(n, d, k)) return ((size_t)(k / 32 + 1) * 8 + 4) * (n < 1 ? 1 : n);
-    return loss_plan(dtype, n, d, k, backward, nullptr).bytes;
+    const size_t forward = loss_is_few(n, d, k) ? ((size_t)(k / 32 + 1) * 8 + 4) * (n < 1 ? 1 : n) : loss_plan(dtype, n, d, k, false, nullptr).bytes;
+    if (!backward) return forward;
+    const size_t both = loss_plan(dtype, n, d, k, true, nullptr).bytes;
+    return both < forward ? forward : both;
 }
 
 template <typename K>

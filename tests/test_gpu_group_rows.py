@@ -51,7 +51,7 @@ def check_group(vlq, cell, cells):
 
 @pytest.mark.parametrize("n,w,cells", [
     (1, 1, 1), (1, 8, 8), (17, 8, 64), (63, 1, 3), (1000, 6, 128), (2048, 8, 2047), (2048, 8, 2048), (2049, 8, 100), (5000, 7, 5),
-    (1, 1, 4096), (300, 64, 65536), (33333, 3, 2100), (10000, 64, 65536), (2555, 2, 4096), (20000, 30, 300), (700, 5, 1 << 24)])
+    (1, 1, 4096), (300, 64, 65536), (33333, 3, 2100), (10000, 64, 65536), (2555, 2, 4096), (20000, 30, 300), (700, 5, 1 << 24), (3, 2, 1 << 24), (1, 6, 57575), (4096, 1, 2048), (4097, 1, 2048), (1024, 4, 300000)])
 def test_group(vlq, n, w, cells):
     g = torch.Generator().manual_seed(n + w + cells)
     cell = torch.randint(0, cells, (n, w), generator=g, dtype=torch.int32)

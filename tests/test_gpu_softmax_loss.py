@@ -57,7 +57,7 @@ def compare(got, want, names=("loss", "dx", "dc", "db")):
 
 SHAPES = [(1, 1, 1), (1, 96, 300), (3, 7, 2), (64, 32, 256), (65, 33, 257), (255, 96, 1000), (257, 128, 513), (300, 130, 1025),
           (40, 520, 77), (17, 1027, 515), (1000, 64, 5000), (33, 48, 65537), (9, 200, 70001), (129, 100, 9000), (700, 136, 1100), (2100, 500, 1001), (900, 264, 5003), (1500, 192, 4100),
-          (1000, 128, 3000), (2049, 31, 1500), (1200, 1027, 515), (3000, 130, 1025), (1111, 520, 777), (7, 300, 33), (5000, 129, 5), (2, 64, 40000)]
+          (1000, 128, 3000), (2049, 31, 1500), (1200, 1027, 515), (3000, 130, 1025), (1111, 520, 777), (7, 300, 33), (5000, 129, 5), (2, 64, 40000), (5001, 2052, 61)]
 
 
 @pytest.mark.parametrize("t", [F32, F16, BF16])

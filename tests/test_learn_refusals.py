@@ -65,6 +65,8 @@ def test_loss_workspace(vlq):
     small, large = (L.vlq_softmax_loss_workspace(0, 10, 8, 5, b) for b in (0, 1))
     assert 0 < small < large
     assert loss_call(vlq, False, k=5, size=small - 1) == vlq.VLQ_EINVAL and "bytes" in vlq.vlq_last_error()
+    for n, d, k in ((8000, 4000, 64), (300, 200, 100), (100_000, 128, 1000), (1, 16384, 1 << 24), (1 << 27, 1, 1)):  # the second's is enough for both
+        assert L.vlq_softmax_loss_workspace(1, n, d, k, 1) >= L.vlq_softmax_loss_workspace(1, n, d, k, 0) > 0
     # the largest sizes stay within 64 bits
     assert L.vlq_softmax_loss_workspace(0, 1 << 27, 16384, 1 << 24, 1) > 0
     with pytest.raises(vlq.VlqError):
