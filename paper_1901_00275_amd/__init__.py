@@ -336,16 +336,15 @@ def vlq_clip_grads(d_grads, max_norm, d_out, d_norm, d_ws, stream=None):
     dev = d_ws.get_device()
     counts = array("q", [g.numel() for g in d_grads])
     types = array("i", [_TYPES.get(g.dtype, -1) for g in d_grads])
-    for g in d_grads:
-        if g.get_device() != dev or not g.is_contiguous() or g.dtype not in _TYPES:
-            raise ValueError("gradients must be contiguous float32, float16 or bfloat16 tensors on the current device")
+    if -1 in types or any(g.get_device() != dev or not g.is_contiguous() for g in d_grads):
+        raise ValueError("gradients must be contiguous float32, float16 or bfloat16 tensors on the current device")
     ptrs, outs = array("Q", [g.data_ptr() for g in d_grads]), None
     if d_out is not None:
         if len(d_out) != len(d_grads):
             raise ValueError("d_out must have a tensor for every tensor of d_grads")
         if d_out is not d_grads:
-            for g, o in zip(d_grads, d_out):
-                if o.dtype is not g.dtype or o.get_device() != dev or not o.is_contiguous() or o.numel() != g.numel():
+            for g, o, count in zip(d_grads, d_out, counts):
+                if o is not g and (o.dtype is not g.dtype or o.get_device() != dev or not o.is_contiguous() or o.numel() != count):
                     raise ValueError("d_out must have a contiguous tensor of the same type, size and device for every tensor of d_grads")
         outs = array("Q", [o.data_ptr() for o in d_out])
     _chk(lib().vlq_clip_grads(len(d_grads), types.buffer_info()[0], counts.buffer_info()[0], ptrs.buffer_info()[0], float(max_norm),
