@@ -4,7 +4,7 @@
 // each; squares are summed in fp64 (they neither overflow nor vanish, and the order of the chunks' sums is fixed).  The second
 // launch takes the chunks from the last to the first: what the first launch read last is still in the 256 MB cache.  What comes
 // before the last CLIP_STAY bytes is read past the caches, in both launches: 800 MB of bf16 488 -> 464 us (8.5 MB past the
-// caches cost 11.4 instead of 10.2).
+// caches cost 11.4 instead of 10.2): 5.3 TB/s, where a copy of this size has 4.7.
 // The tensors' addresses travel in the kernels' arguments, so nothing on the host has to outlive the call.
 #include "learn.h"
 

@@ -4,8 +4,16 @@
 //   l_ij = s <x_i, c_j> + b_j,  loss_i = log sum_j exp l_ij - l_iy,  G_ij = g_i (p_ij - [j = y_i]),  p_ij = exp(l_ij) / sum
 //   dx_i = s sum_j G_ij c_j,  dc_j = s sum_i G_ij x_i,  db_j = sum_i G_ij.
 //
-// Four products of n x k x d on the fp16 matrix cores: the logits forward, and backward the logits again and the two
-// gradients.  Operands are first rewritten as fp16 with a power-of-two scale (per row of x, per 16 rows of c, one per
+// Four products of n x k x d: the logits forward, and backward the logits again (instead of n k probabilities kept between the
+// calls) and the two gradients.
+// Three forms, by rules on the sizes (loss_is_few, grads_are_few, NARROW_DIM):
+//  - few (softmax_loss_few.hip): little is done with each centroid, everything is read as it lies;
+//  - narrow (softmax_loss_narrow.hip): up to 128 dimensions, the probabilities never leave the registers;
+//  - wide (here): tiles of 256 x 256 on the fp16 matrix cores, the probabilities written a piece at a time.  16-bit centroids are taken
+//    as they lie up to LIE_ROWS rows (as_they_lie), the rows' image then holds the rows' own bits.
+// This file has the images of both latter forms, the merging of statistics, the sums over parts, and all calls.
+//
+// Operands are otherwise rewritten as fp16 with a power-of-two scale (per row of x, per 16 rows of c, one per
 // matrix where the rows are the summed index):
 //  - fp16 values are taken as they are, bf16 values lose nothing within 32 binades below the largest of their scale;
 //  - an fp32 value is the sum of two fp16 values, hi + lo, with an error of 2^-23 of itself or 2^-40 of the largest of its scale;
@@ -601,7 +609,9 @@ struct FromRows {
 };
 
 // Forward: per row the maximum and the sum over the 128 centroids of a wave's part.  A lane holds 32 centroids of each of
-// four rows, so most of the reduction stays in its registers.
+// four rows, so most of the reduction stays in its registers.  Bound by the matrix cores: 8 192 x 50 001 x 2 048 bf16 1 240 us (1.35
+// PFLOP/s, the library's product of this size 1.33); 1 000 x 16 384 x 512 fp16 22 us (0.76: one round of 256 tiles, whose
+// start, sixteen units and end cannot hide behind each other).
 template <class FORM>
 __global__ __launch_bounds__(LNT, 2) void k_loss_stats(LogitArgs a)
 {
@@ -684,7 +694,8 @@ __global__ __launch_bounds__(256) void k_loss_merge(const float2 *part, int part
     if (loss) loss[i] = (uint32_t)lab[i] >= (uint32_t)k ? 0.f : m == -INFINITY ? INFINITY : LN2 * (m - mine[i]) + logf(z);
 }
 
-// Backward: P of a tile, as images in both orders, and the sums over a wave's 64 rows for the bias
+// Backward: P of a tile, as images in both orders, and the sums over a wave's 64 rows for the bias.
+// 8 192 x 50 001 x 2 048 bf16 in seven pieces 1 510 us (1.11 PFLOP/s): the product, and behind it 1.6 GB of images.
 template <class FORM>
 __global__ __launch_bounds__(LNT, 2) void k_loss_p(LogitArgs a)
 {
@@ -794,8 +805,10 @@ struct GradOut {
     bool vec;
 };
 
-// Both gradients of a piece in one launch, the one with the longer sums first: a piece's tiles are too few to fill
-// the chip twice over.
+// Both gradients of a piece in one launch, the one with the longer sums first: the tiles of one alone (256 in a piece of 8 192 x 8 192
+// at 2 048 dimensions) leave compute units waiting for the last.  8 192 x 50 001 x 2 048 bf16 2 800 us (1.20 PFLOP/s); of a
+// piece's 432 us about 27 are the sums of dx, which are read, added to and written again.  Smaller pieces repeat that more often
+// (2^25 values of P: 3 220 us), larger ones gain little for twice the memory (2^27: 2 730).
 template <typename T, int NP>
 __global__ __launch_bounds__(LNT, 2) void k_loss_grads(GradOut first, GradOut second, int nfirst)
 {

@@ -7,7 +7,9 @@
 // do; where there are few workgroups the waits for them do, and S waves share the dimensions of a tile.
 //
 // Gradients: G_ij = g_i (p_ij - [j = y_i]) is written in fp32, then dx = s G C and dc = s G^T X on the fp32 matrix instructions, 16-bit
-// values widened as they are read.
+// values widened as they are read: their rate is an eighth of fp16's, but nothing is padded to 256 rows or written as an image.
+// Bound by the waits for a few turns of loads where the work is small, else by those products: 5 366 x 24 x 2 016 fp16 G 18 us,
+// gradients 29; 500 x 500 x 500 fp32 15 and 19.
 #include "loss_image.h"
 
 #define FEW_WIDE 65536 // from so many centroids on a wave takes 32 of them: then there are waves enough
@@ -18,10 +20,17 @@ struct FewPiece { // what a lane reads of a row at a time: its share of STEP ind
     static constexpr int N = 16 / sizeof(T), STEP = 4 * N;
     T v[N];
 };
-// (Every address is clamped into the row, what lies past its end is made zero afterwards: a branch around a load would wait for it.)
-template <typename T, int ALIGN>
-__device__ __forceinline__ FewPiece<T> few_piece(const T *row, int i, int d)
+// Every address is clamped into the row, what lies past its end is made zero afterwards: a branch around a load would wait for it.
+// Where one tile of rows is all there is (THIN), memory bounds it, and what is not there is not asked for (65 536 x 1 024 bf16,
+// one row 27 us; clamped 28, with the other 15 rows 29).
+template <typename T, int ALIGN, bool THIN>
+__device__ __forceinline__ FewPiece<T> few_piece(const T *row, int i, int d, bool there)
 {
+    if (THIN && ALIGN == 16) {
+        u32x4 v = {0, 0, 0, 0};
+        if (there && i < d) v = *(const u32x4 *)(row + i);
+        return __builtin_bit_cast(FewPiece<T>, v);
+    }
     FewPiece<T> r;
     if constexpr (ALIGN == 16) {
         const u32x4 v = *(const u32x4 *)(row + min(i, d - FewPiece<T>::N));
@@ -71,22 +80,14 @@ __device__ __forceinline__ void few_logits(const FewArgs &a, int m0, int n0, int
 #pragma unroll
         for (int i = 0; i < G; ++i) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const bool xin = NT > 1 || l < a.n;
     for (int k0 = slice * U * STEP; k0 < a.d; k0 += S * U * STEP) {
         FewPiece<T> cv[U][G], xv[U][NT];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
 #pragma unroll
-            for (int i = 0; i < G; ++i) cv[u][i] = few_piece<T, ALIGN>(crow[i], k0 + g * N + u * STEP, a.d);
+            for (int i = 0; i < G; ++i) cv[u][i] = few_piece<T, ALIGN, NT == 1>(crow[i], k0 + g * N + u * STEP, a.d, true);
 #pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                if (NT > 1) {
-                    xv[u][j] = few_piece<T, ALIGN>(xrow[j], k0 + g * N + u * STEP, a.d);
-                } else { // (one row read by 16 lanes costs as much as 16: 65 536 x 1 024 bf16, one row 29 instead of 26 us)
-                    xv[u][j] = {};
-                    if (xin) xv[u][j] = few_piece<T, ALIGN>(xrow[j], k0 + g * N + u * STEP, a.d);
-                }
-            }
+            for (int j = 0; j < NT; ++j) xv[u][j] = few_piece<T, ALIGN, NT == 1>(xrow[j], k0 + g * N + u * STEP, a.d, NT > 1 || l < a.n);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
