@@ -48,7 +48,7 @@
 #define FEW_NARROW_ROWS 128   // up to NARROW_DIM dimensions
 #define FEW_NARROW_WORK 1.2e8
 // A step with the gradients (their products are fp32's, an eighth of the others' rate, but with few rows or centroids the others' tiles
-// are mostly empty): 5 366 x 24 x 2 016 fp16 67 : 115, 3 x 30 x 224 fp16 22 : 38, 500 x 500 x 500 fp32 46 : 103, bf16 52 : 75,
+// are mostly empty): 5 366 x 24 x 2 016 fp16 58 : 115, 3 x 30 x 224 fp16 22 : 38, 500 x 500 x 500 fp32 37 : 103, bf16 40 : 75,
 // 8 000 x 32 x 2 000 fp32 134 : 282, 32 x 16 000 x 2 000 bf16 132 : 179, 8 000 x 64 x 4 000 bf16 269 : 327, 64 x 65 536 x 1 024 bf16
 // 410 : 322; 1 000 x 1 000 x 300 bf16 76 : 79, 4 000 x 400 x 200 bf16
 // 67 : 66, 2 000 x 1 500 x 160 fp16 80 : 64.  Narrow: 300 x 300 x 128 bf16 26 : 35, 300 x 3 000 x 96 bf16 37 : 39, 1 000 x 1 000 x 96
@@ -858,6 +858,7 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_grads(GradOut first, GradOut se
 }
 
 // out = factor * sum of the slabs, of both gradients, four values a thread
+#define SUM_SHARED 8 // from so many parts on the four waves of a workgroup share those of 256 values
 struct SlabSum {
     const float *slabs;
     int splits, blocks;
@@ -897,20 +898,30 @@ __global__ __launch_bounds__(256) void k_loss_sums(SlabSum x, SlabSum c, BiasSum
     }
     const bool first = (int)blockIdx.x < x.blocks;
     const SlabSum &a = first ? x : c;
-    const int64_t i = ((int64_t)(first ? blockIdx.x : blockIdx.x - x.blocks) * 256 + threadIdx.x) * 4;
-    if (i >= a.count) return;
+    const bool share = a.splits >= SUM_SHARED;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, at = first ? blockIdx.x : blockIdx.x - x.blocks;
+    const int64_t i = (share ? (int64_t)at * 64 + lane : (int64_t)at * 256 + threadIdx.x) * 4;
     const float f = a.inv ? grad_factor(*a.inv, a.top ? *a.top : 1.f, scale) : scale;
     const bool vec = a.count % 4 == 0 && (uintptr_t)a.out % (4 * sizeof(T)) == 0;
-    const int count = (int)min((int64_t)4, a.count - i);
+    const int count = (int)min((int64_t)4, a.count - i), by = share ? 4 : 1;
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
-    if (vec) {
+    if (i >= a.count) {
+        if (!share) return;
+    } else if (vec) {
 #pragma unroll 8
-        for (int p = 0; p < a.splits; ++p) s += *(const f32x4 *)(a.slabs + p * a.count + i);
+        for (int p = share ? wave : 0; p < a.splits; p += by) s += *(const f32x4 *)(a.slabs + p * a.count + i);
     } else {
-        for (int p = 0; p < a.splits; ++p)
+#pragma unroll 4
+        for (int p = share ? wave : 0; p < a.splits; p += by)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (e < count) s[e] += a.slabs[p * a.count + i + e];
+            for (int e = 0; e < 4; ++e) s[e] += a.slabs[p * a.count + min(i + e, a.count - 1)];
+    }
+    if (share) {
+        __shared__ f32x4 sum[3][64];
+        if (wave > 0) sum[wave - 1][lane] = s;
+        __syncthreads();
+        if (wave > 0 || i >= a.count) return;
+        s = (s + sum[0][lane]) + (sum[1][lane] + sum[2][lane]);
     }
     store4((T *)a.out + i, s * f, count, vec);
 }
@@ -1259,7 +1270,8 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
     };
     auto finish = [&](const BiasSum &bias) {
         auto side = [&](float *slabs, int splits, int64_t count, const float *inv, const float *top, void *out) {
-            return SlabSum{slabs, splits, (int)((count + 1023) / 1024), count, inv, top, out};
+            const int each = splits >= SUM_SHARED ? 256 : 1024;
+            return SlabSum{slabs, splits, (int)((count + each - 1) / each), count, inv, top, out};
         };
         SlabSum x = {}, c = {};
         if (a.dx && p.xslab) x = side(p.xsum, p.xsplit, a.n * a.d, p.few ? nullptr : &p.hdr->cinv, nullptr, a.dx);

@@ -8,8 +8,8 @@
 //
 // Gradients: G_ij = g_i (p_ij - [j = y_i]) is written in fp32, then dx = s G C and dc = s G^T X on the fp32 matrix instructions, 16-bit
 // values widened as they are read: their rate is an eighth of fp16's, but nothing is padded to 256 rows or written as an image.
-// Bound by the waits for a few turns of loads where the work is small, else by those products: 5 366 x 24 x 2 016 fp16 G 18 us,
-// gradients 29; 500 x 500 x 500 fp32 15 and 19.
+// Bound by the waits for a few turns of loads where the work is small, else by those products: 5 366 x 24 x 2 016 fp16 G 13 us,
+// gradients 28; 500 x 500 x 500 fp32 10 and 16.
 #include "loss_image.h"
 
 #define FEW_WIDE 65536 // from so many centroids on a wave takes 32 of them: then there are waves enough
@@ -357,9 +357,13 @@ static void few(int dtype, const FewArgs &args, bool backward, hipStream_t st)
                                grid, dim3(WS * 64), 0, st, a);
     };
     auto rows = [&](auto ALIGN, auto W, auto S, auto G) {
-        if (a.n <= 16)
+        // tiles of 64 rows, of fewer where compute units would go without a workgroup (a step of 3 855 x 11 x 657 fp32 100 -> 60 us,
+        // 64 x 1 000 x 1 024 fp32 26 -> 14; asking for 700 workgroups 535 x 975 x 1 248 fp32 44 -> 53)
+        int tiles = 4;
+        while (tiles > 1 && (a.n <= 8 * tiles || (int64_t)a.groups * ((a.n + 16 * tiles - 1) / (16 * tiles)) < 256)) tiles /= 2;
+        if (tiles == 1)
             go(ALIGN, W, S, G, std::integral_constant<int, 1>{});
-        else if (a.n <= 32)
+        else if (tiles == 2)
             go(ALIGN, W, S, G, std::integral_constant<int, 2>{});
         else
             go(ALIGN, W, S, G, std::integral_constant<int, 4>{});
