@@ -858,7 +858,8 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_grads(GradOut first, GradOut se
 }
 
 // out = factor * sum of the slabs, of both gradients, four values a thread
-#define SUM_SHARED 8 // from so many parts on the four waves of a workgroup share those of 256 values
+// From so many parts on the four waves of a workgroup share those of 256 values (a step of 3 855 x 11 x 657 fp32, 46 parts of dc, 60 -> 52 us)
+#define SUM_SHARED 8
 struct SlabSum {
     const float *slabs;
     int splits, blocks;
