@@ -6,13 +6,14 @@
 // pairs in turn, 64 at a time, those of one digit told apart by ballots.  No atomics on memory, so the order is the pairs' own.
 // What bounds it are launches of 5 to 11 us, each some waits for memory one behind the other: 640 000 pairs and 65 536 cells
 // (two digits) 51 us in seven launches, 13 MB of pairs and places.  Up to SMALL_PAIRS pairs of one digit take one launch.
-// The rest moves memory: whole 16 bytes where rows lie on them, several rows' loads under way at a time.  640 000 rows of 384 bytes
+// The rest moves memory: 16 bytes at a time where rows lie on them, else 8, 4 or a value, several rows' loads under way.  640 000 rows of 384 bytes
 // gathered 41 us (6.0 TB/s written), 16 384 rows of 8 x 4 KB combined 137 us (4.3 TB/s), the gradient of 5 003 x 6 x 2 KB 26 us (5.0).
 #include "learn.h"
 
 #include <type_traits>
 
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16_t;
 
 #define DIGIT 11
@@ -481,29 +482,27 @@ int launch_group_rows(const int32_t *cell, int64_t pairs, int cells, int64_t *of
 // ---------------------------------------------------------------------------
 // rows
 // ---------------------------------------------------------------------------
-// A piece of a row: 16 bytes, or one value where rows do not lie on 16 bytes
-template <typename T, bool VEC>
+// A piece of a row: as many bytes, up to 16, as all rows lie on (5 000 x 8 rows of 2 056 bytes combined: 25 us, value by value 62)
+template <typename T, int BYTES>
 struct Piece {
-    static constexpr int N = VEC ? 16 / (int)sizeof(T) : 1;
+    static constexpr int N = BYTES / (int)sizeof(T);
+    using Word = std::conditional_t<BYTES == 16, u32x4, std::conditional_t<BYTES == 8, u32x2, std::conditional_t<BYTES == 4, uint32_t, uint16_t>>>;
     T v[N];
 };
-template <typename T, bool VEC>
-__device__ __forceinline__ Piece<T, VEC> load_piece(const T *p)
+template <typename T, int BYTES>
+__device__ __forceinline__ Piece<T, BYTES> load_piece(const T *p)
 {
-    Piece<T, VEC> r;
-    if constexpr (VEC)
-        *(u32x4 *)r.v = *(const u32x4 *)p;
-    else
-        r.v[0] = *p;
-    return r;
+    using P = Piece<T, BYTES>;
+    return __builtin_bit_cast(P, *(const typename P::Word *)p);
 }
-template <typename T, bool VEC>
-__device__ __forceinline__ void store_piece(T *p, const Piece<T, VEC> &r)
+template <typename T, int BYTES>
+__device__ __forceinline__ void store_piece(T *p, const Piece<T, BYTES> &r)
 {
-    if constexpr (VEC)
-        __builtin_nontemporal_store(*(const u32x4 *)r.v, (u32x4 *)p);
+    using W = typename Piece<T, BYTES>::Word;
+    if constexpr (BYTES == 16)
+        __builtin_nontemporal_store(__builtin_bit_cast(W, r), (W *)p);
     else
-        *p = r.v[0];
+        *(W *)p = __builtin_bit_cast(W, r);
 }
 
 #define ROW_NT 256
@@ -520,10 +519,10 @@ struct RowsArgs {
 };
 
 // y[p] = x[source[p] / w]: the pieces of a workgroup's rows, ROW_ITEMS a thread at a time
-template <typename T, bool VEC>
+template <typename T, int BYTES>
 __global__ __launch_bounds__(ROW_NT) void k_gather_rows(RowsArgs a, const T *__restrict__ x, T *__restrict__ y)
 {
-    using P = Piece<T, VEC>;
+    using P = Piece<T, BYTES>;
     const int64_t places = a.n * a.w, p0 = (a.block + blockIdx.x) * a.rows;
     const uint32_t pieces = (uint32_t)min((int64_t)a.rows, places - p0) * a.per;
     for (uint32_t i0 = threadIdx.x; i0 < pieces; i0 += ROW_NT * ROW_ITEMS) {
@@ -536,20 +535,20 @@ __global__ __launch_bounds__(ROW_NT) void k_gather_rows(RowsArgs a, const T *__r
             if (i >= pieces) continue;
             const int32_t s = a.index[p0 + r];
             if ((int64_t)s >= places || s < 0) continue; // (a place behind the last pair)
-            v[u] = load_piece<T, VEC>(x + (int64_t)((uint32_t)s / (uint32_t)a.w) * a.d + c * P::N);
+            v[u] = load_piece<T, BYTES>(x + (int64_t)((uint32_t)s / (uint32_t)a.w) * a.d + c * P::N);
             to[u] = (p0 + r) * a.d + c * P::N;
         }
 #pragma unroll
         for (int u = 0; u < ROW_ITEMS; ++u)
-            if (to[u] >= 0) store_piece<T, VEC>(y + to[u], v[u]);
+            if (to[u] >= 0) store_piece<T, BYTES>(y + to[u], v[u]);
     }
 }
 
 // out[i] = sum over the row's choices of weight y[place], in their order, in fp32
-template <typename T, bool VEC>
+template <typename T, int BYTES>
 __global__ __launch_bounds__(ROW_NT) void k_combine_rows(RowsArgs a, const T *__restrict__ y, T *__restrict__ out)
 {
-    using P = Piece<T, VEC>;
+    using P = Piece<T, BYTES>;
     const int64_t places = a.n * a.w, r0 = (a.block + blockIdx.x) * a.rows;
     const uint32_t pieces = (uint32_t)min((int64_t)a.rows, a.n - r0) * a.per;
     for (uint32_t i = threadIdx.x; i < pieces; i += ROW_NT) {
@@ -565,7 +564,7 @@ __global__ __launch_bounds__(ROW_NT) void k_combine_rows(RowsArgs a, const T *__
                 f[q] = 0.f;
                 const int32_t p = q0 + q < a.w ? pl[q0 + q] : -1;
                 const bool in = p >= 0 && p < places;
-                v[q] = load_piece<T, VEC>(y + (in ? (int64_t)p * a.d : 0) + c * P::N);
+                v[q] = load_piece<T, BYTES>(y + (in ? (int64_t)p * a.d : 0) + c * P::N);
                 if (in) f[q] = wt ? wt[q0 + q] : 1.f;
                 if (!in)
 #pragma unroll
@@ -579,61 +578,71 @@ __global__ __launch_bounds__(ROW_NT) void k_combine_rows(RowsArgs a, const T *__
         P o;
 #pragma unroll
         for (int e = 0; e < P::N; ++e) o.v[e] = (T)s[e];
-        store_piece<T, VEC>(out + (r0 + r) * a.d + c * P::N, o);
+        store_piece<T, BYTES>(out + (r0 + r) * a.d + c * P::N, o);
     }
 }
 
-// dy[place] = weight dout[i], dweight[i][c] = <dout[i], y[place]>: L lanes a row, eight choices at a time
-template <typename T, bool VEC, int L>
+// dy[place] = weight dout[i], dweight[i][c] = <dout[i], y[place]>: L lanes eight choices of a row
+// (all choices of a row one after the other: 1 337 x 64 rows of 1 516 bytes 110 us, now 64)
+template <typename T, int BYTES, int L>
 __global__ __launch_bounds__(ROW_NT) void k_combine_back(RowsArgs a, const T *__restrict__ dout, const T *__restrict__ y,
                                                          T *__restrict__ dy, float *__restrict__ dweight)
 {
-    using P = Piece<T, VEC>;
+    using P = Piece<T, BYTES>;
     const int lane = threadIdx.x & (L - 1);
-    const int64_t places = a.n * a.w, r = (a.block + blockIdx.x) * (ROW_NT / L) + threadIdx.x / L;
+    const uint32_t eights = (a.w + 7) / 8, id = (uint32_t)((a.block + blockIdx.x) * (ROW_NT / L) + threadIdx.x / L); // (n w < 2^31)
+    const int64_t places = a.n * a.w, r = id / eights;
     if (r >= a.n) return;
-    for (int q0 = 0; q0 < a.w; q0 += 8) {
-        int64_t p[8];
-        float f[8], dot[8];
+    const int q0 = (int)(id % eights) * 8;
+    int64_t p[8];
+    float f[8], dot[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        const int32_t at = q0 + q < a.w ? a.index[r * a.w + q0 + q] : -1;
+        p[q] = at >= 0 && at < places ? at : -1;
+        f[q] = p[q] < 0 ? 0.f : a.weight ? a.weight[r * a.w + q0 + q] : 1.f;
+        dot[q] = 0.f;
+    }
+    for (uint32_t c = lane; c < a.per; c += L) {
+        const P g = load_piece<T, BYTES>(dout + r * a.d + c * P::N);
+        P v[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            if (dweight && p[q] >= 0) v[q] = load_piece<T, BYTES>(y + p[q] * a.d + c * P::N);
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-            const int32_t at = q0 + q < a.w ? a.index[r * a.w + q0 + q] : -1;
-            p[q] = at >= 0 && at < places ? at : -1;
-            f[q] = p[q] < 0 ? 0.f : a.weight ? a.weight[r * a.w + q0 + q] : 1.f;
-            dot[q] = 0.f;
-        }
-        for (uint32_t c = lane; c < a.per; c += L) {
-            const P g = load_piece<T, VEC>(dout + r * a.d + c * P::N);
-            P v[8];
+            if (p[q] < 0) continue;
+            P o;
 #pragma unroll
-            for (int q = 0; q < 8; ++q)
-                if (dweight && p[q] >= 0) v[q] = load_piece<T, VEC>(y + p[q] * a.d + c * P::N);
-#pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                if (p[q] < 0) continue;
-                P o;
-#pragma unroll
-                for (int e = 0; e < P::N; ++e) {
-                    o.v[e] = (T)(f[q] * (float)g.v[e]);
-                    if (dweight) dot[q] = fmaf((float)g.v[e], (float)v[q].v[e], dot[q]);
-                }
-                if (dy) store_piece<T, VEC>(dy + p[q] * a.d + c * P::N, o);
+            for (int e = 0; e < P::N; ++e) {
+                o.v[e] = (T)(f[q] * (float)g.v[e]);
+                if (dweight) dot[q] = fmaf((float)g.v[e], (float)v[q].v[e], dot[q]);
             }
+            if (dy) store_piece<T, BYTES>(dy + p[q] * a.d + c * P::N, o);
         }
-        if (!dweight) continue;
+    }
+    if (!dweight) return;
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
+    for (int q = 0; q < 8; ++q) {
 #pragma unroll
-            for (int o = L / 2; o > 0; o >>= 1) dot[q] += __shfl_xor(dot[q], o, 64);
-            if (lane == 0 && q0 + q < a.w) dweight[r * a.w + q0 + q] = p[q] < 0 ? 0.f : dot[q];
-        }
+        for (int o = L / 2; o > 0; o >>= 1) dot[q] += __shfl_xor(dot[q], o, 64);
+        if (lane == 0 && q0 + q < a.w) dweight[r * a.w + q0 + q] = p[q] < 0 ? 0.f : dot[q];
     }
 }
 
-template <typename T>
-static bool whole_pieces(int d, const void *p, const void *q, const void *r)
+// go(bytes of a piece)
+template <typename T, typename F>
+static void by_pieces(int d, const void *p, const void *q, const void *r, F &&go)
 {
-    return (size_t)d * sizeof(T) % 16 == 0 && ((uintptr_t)p | (uintptr_t)q | (uintptr_t)r) % 16 == 0;
+    const uint64_t all = (uint64_t)d * sizeof(T) | (uintptr_t)p | (uintptr_t)q | (uintptr_t)r;
+    if (all % 16 == 0)
+        go(std::integral_constant<int, 16>{});
+    else if (all % 8 == 0)
+        go(std::integral_constant<int, 8>{});
+    else if (all % 4 == 0)
+        go(std::integral_constant<int, 4>{});
+    else
+        go(std::integral_constant<int, sizeof(T)>{});
 }
 
 // rows of a workgroup: about `pieces` pieces
@@ -651,18 +660,15 @@ template <typename T>
 static int gather(const RowsArgs &args, const T *x, T *y, hipStream_t st)
 {
     RowsArgs a = args;
-    auto go = [&](auto VEC) {
-        constexpr bool V = decltype(VEC)::value;
+    auto go = [&](auto BYTES) {
+        constexpr int V = decltype(BYTES)::value;
         a.per = a.d / Piece<T, V>::N;
         a.rows = rows_of(a.per, ROW_NT * ROW_ITEMS);
         in_launches(a, (a.n * a.w + a.rows - 1) / a.rows, [&](dim3 groups) {
             hipLaunchKernelGGL((k_gather_rows<T, V>), groups, dim3(ROW_NT), 0, st, a, x, y);
         });
     };
-    if (whole_pieces<T>(a.d, x, y, nullptr))
-        go(std::true_type{});
-    else
-        go(std::false_type{});
+    by_pieces<T>(a.d, x, y, nullptr, go);
     return (int)hipGetLastError();
 }
 
@@ -670,18 +676,15 @@ template <typename T>
 static int combine(const RowsArgs &args, const T *y, T *out, hipStream_t st)
 {
     RowsArgs a = args;
-    auto go = [&](auto VEC) {
-        constexpr bool V = decltype(VEC)::value;
+    auto go = [&](auto BYTES) {
+        constexpr int V = decltype(BYTES)::value;
         a.per = a.d / Piece<T, V>::N;
         a.rows = rows_of(a.per, ROW_NT);
         in_launches(a, (a.n + a.rows - 1) / a.rows, [&](dim3 groups) {
             hipLaunchKernelGGL((k_combine_rows<T, V>), groups, dim3(ROW_NT), 0, st, a, y, out);
         });
     };
-    if (whole_pieces<T>(a.d, y, out, nullptr))
-        go(std::true_type{});
-    else
-        go(std::false_type{});
+    by_pieces<T>(a.d, y, out, nullptr, go);
     return (int)hipGetLastError();
 }
 
@@ -689,12 +692,12 @@ template <typename T>
 static int combine_back(const RowsArgs &args, const T *dout, const T *y, T *dy, float *dweight, hipStream_t st)
 {
     RowsArgs a = args;
-    auto go = [&](auto VEC) {
-        constexpr bool V = decltype(VEC)::value;
+    auto go = [&](auto BYTES) {
+        constexpr int V = decltype(BYTES)::value;
         a.per = a.d / Piece<T, V>::N;
         auto lanes = [&](auto L) {
             constexpr int N = decltype(L)::value, R = ROW_NT / N;
-            in_launches(a, (a.n + R - 1) / R, [&](dim3 groups) {
+            in_launches(a, (a.n * ((a.w + 7) / 8) + R - 1) / R, [&](dim3 groups) {
                 hipLaunchKernelGGL((k_combine_back<T, V, N>), groups, dim3(ROW_NT), 0, st, a, dout, y, dy, dweight);
             });
         };
@@ -705,10 +708,7 @@ static int combine_back(const RowsArgs &args, const T *dout, const T *y, T *dy, 
         else
             lanes(std::integral_constant<int, 16>{});
     };
-    if (whole_pieces<T>(a.d, dout, y, dy))
-        go(std::true_type{});
-    else
-        go(std::false_type{});
+    by_pieces<T>(a.d, dout, y, dy, go);
     return (int)hipGetLastError();
 }
 

@@ -81,7 +81,7 @@ def test_group_many_pairs(vlq):
 
 @pytest.mark.parametrize("t", [F32, F16, BF16])
 @pytest.mark.parametrize("n,w,d,cells", [(1, 1, 1, 1), (5, 3, 7, 4), (100, 8, 64, 16), (257, 6, 96, 1000), (70, 17, 1023, 9), (1000, 2, 8, 64),
-                                         (33, 64, 40, 65536), (64, 5, 2056, 7)])
+                                         (33, 64, 40, 65536), (64, 5, 2056, 7), (70, 9, 1026, 9), (50, 17, 28, 40), (41, 24, 6, 3)])
 def test_rows(vlq, t, n, w, d, cells):
     g = torch.Generator().manual_seed(n + w + d)
     cell = torch.randint(0, cells, (n, w), generator=g, dtype=torch.int32)
