@@ -132,8 +132,9 @@ void launch_loss_few(int dtype, const FewArgs &a, bool backward, hipStream_t st)
 void launch_loss_few_grads(int dtype, const FewArgs &a, hipStream_t st);
 
 // ---- softmax_loss_narrow.hip ----
-// rows that a workgroup keeps: 256 halve the traffic of LDS where their sums and fragments fit the registers
-constexpr int narrow_rows(int parts, int units) { return parts == 2 || units == 4 ? 128 : 256; }
+// rows that a workgroup keeps: 256 halve the traffic of LDS where their sums and fragments fit the registers (of 256 dimensions those of
+// 128 rows just do, all 256 of a wave)
+constexpr int narrow_rows(int parts, int units) { return parts == 2 || units >= 4 ? 128 : 256; }
 struct NarrowSide {
     const u32x4 *q, *r, *rt; // images of the gradient's rows, of the other matrix's rows and columns
     int qblocks, tiles, splits, per; // workgroups side by side; tiles of the other matrix, in so many parts of `per`

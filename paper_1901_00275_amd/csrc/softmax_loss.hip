@@ -6,9 +6,9 @@
 //
 // Four products of n x k x d: the logits forward, and backward the logits again (instead of n k probabilities kept between the
 // calls) and the two gradients.
-// Three forms, by rules on the sizes (loss_is_few, grads_are_few, NARROW_DIM):
+// Three forms, by rules on the sizes (loss_is_few, grads_are_few, narrow_dim):
 //  - few (softmax_loss_few.hip): little is done with each centroid, everything is read as it lies;
-//  - narrow (softmax_loss_narrow.hip): up to 128 dimensions, the probabilities never leave the registers;
+//  - narrow (softmax_loss_narrow.hip): up to 128 dimensions (256 of 16-bit values), the probabilities never leave the registers;
 //  - wide (here): tiles of 256 x 256 on the fp16 matrix cores, the probabilities written a piece at a time.  16-bit centroids are taken
 //    as they lie up to LIE_ROWS rows (as_they_lie), the rows' image then holds the rows' own bits.
 // This file has the images of both latter forms, the merging of statistics, the sums over parts, and all calls.
@@ -35,28 +35,35 @@
 #define LNT 512              // threads of the product kernels
 #define LOSS_ROWS 8192       // rows that go through the products together
 #define PIECE (1 << 26)      // values of P kept at a time
-#define NARROW_DIM 128       // up to so many dimensions the gradients take the narrow form (softmax_loss_narrow.hip)
+// Up to so many dimensions the narrow form, of two parts and of 16-bit values: what a workgroup keeps fits the registers.  us of a
+// step against the wide form: 8 192 x 32 000 x 129 bf16 531 : 1 146, x 192 fp16 593 : 1 060, x 256 bf16 716 : 1 170; 1 000 x 20 000 x 160
+// bf16 110 : 137, 300 x 32 000 x 256 bf16 126 : 123; forward 8 192 x 32 000 x 256 bf16 166 : 205, 2 735 x 2 322 x 190 18 : 22.
+#define NARROW_DIM 128
+#define NARROW_DIM_16 256
 #define NARROW_GROUPS 1024   // its workgroups, about: two rounds of two a compute unit
 #define NARROW_LEAST 8       // tiles of 32 rows that a workgroup of it takes at least (forward half as many)
 // Where little is done with each centroid, rows and centroids are taken as they lie (softmax_loss_few.hip): rewriting them first,
 // and tiles that leave most of the chip idle, cost more.  Measured in us, these against the others.
 // Forward: 1 000 x 1 000 x 1 000 bf16 20 : 38, 8 000 x 120 x 500 fp32 27 : 54, 8 000 x 120 x 1 000 bf16 25 : 45, 535 x 975 x 1 248
 // fp32 45 : 85, 128 x 65 536 x 64 fp16 17 : 31; the narrow form holds out longer: 1 000 x 5 000 x 96 fp32 39 : 19,
-// 2 000 x 5 000 x 96 bf16 26 : 20, 70 x 65 536 x 96 fp32 29 : 41.
+// 2 000 x 5 000 x 96 bf16 26 : 20, 70 x 65 536 x 96 fp32 29 : 41, 500 x 3 000 x 160 bf16 12 : 14, 1 000 x 2 000 x 192 16 : 15, 2 000 x 1 500 x 256
+// 24 : 16, 80 x 40 000 x 160 21 : 26.
 #define FEW_ROWS 64
 #define FEW_WORK 1e9          // products
-#define FEW_NARROW_ROWS 128   // up to NARROW_DIM dimensions
+#define FEW_NARROW_ROWS 128   // against the narrow form
 #define FEW_NARROW_WORK 1.2e8
+#define FEW_NARROW_WORK_16 3e8 // beyond NARROW_DIM dimensions
 // A step with the gradients (their products are fp32's, an eighth of the others' rate, but with few rows or centroids the others' tiles
 // are mostly empty): 5 366 x 24 x 2 016 fp16 58 : 115, 3 x 30 x 224 fp16 22 : 38, 500 x 500 x 500 fp32 37 : 103, bf16 40 : 75,
 // 8 000 x 32 x 2 000 fp32 134 : 282, 32 x 16 000 x 2 000 bf16 132 : 179, 8 000 x 64 x 4 000 bf16 269 : 327, 64 x 65 536 x 1 024 bf16
-// 410 : 322; 1 000 x 1 000 x 300 bf16 76 : 79, 4 000 x 400 x 200 bf16
-// 67 : 66, 2 000 x 1 500 x 160 fp16 80 : 64.  Narrow: 300 x 300 x 128 bf16 26 : 35, 300 x 3 000 x 96 bf16 37 : 39, 1 000 x 1 000 x 96
-// fp32 45 : 43, 100 x 16 384 x 128 fp32 78 : 60.
+// 410 : 322, 1 000 x 1 000 x 300 bf16 76 : 79.  Narrow: 300 x 300 x 128 bf16 26 : 35, 300 x 3 000 x 96 bf16 37 : 39, 1 000 x 1 000 x 96
+// fp32 45 : 43, 100 x 16 384 x 128 fp32 78 : 60; 600 x 300 x 256 bf16 27 : 45, 1 000 x 500 x 160 33 : 40, 500 x 1 500 x 192 fp16 41 : 41,
+// 300 x 3 000 x 250 bf16 73 : 60, 4 000 x 400 x 200 67 : 51.
 #define FEW_GRAD_ROWS 64         // rows or centroids at most
 #define FEW_GRAD_THIN_WORK 2.5e9 // with so few
 #define FEW_GRAD_WORK 2.5e8      // with more
 #define FEW_GRAD_NARROW_WORK 5e7
+#define FEW_GRAD_NARROW_WORK_16 1.5e8
 #define FEW_PAIRS (1 << 24)   // values of G, in fp32
 // Up to so many inverse scales every workgroup that needs their largest finds it: a step of 256 x 16 384 x 96 fp32 57.0 -> 55.5 us, of
 // 4 095 x 16 384 x 96 fp16 215 -> 212; 4 095 x 65 536 x 128 fp32 870 either way.
@@ -989,17 +996,21 @@ static int narrow_parts(int64_t tiles, int64_t per, int64_t out_bytes, int *tile
     return (int)((tiles + each - 1) / each);
 }
 
-static bool loss_is_few(int64_t n, int d, int k)
+static int narrow_dim(int dtype) { return dtype == VLQ_F32 ? NARROW_DIM : NARROW_DIM_16; }
+
+static bool loss_is_few(int dtype, int64_t n, int d, int k)
 {
     const double work = (double)n * d * k;
-    return n <= FEW_ROWS || (d <= NARROW_DIM ? n <= FEW_NARROW_ROWS || work <= FEW_NARROW_WORK : work <= FEW_WORK);
+    if (n <= FEW_ROWS) return true;
+    if (d > narrow_dim(dtype)) return work <= FEW_WORK;
+    return n <= FEW_NARROW_ROWS || work <= (d <= NARROW_DIM ? FEW_NARROW_WORK : FEW_NARROW_WORK_16);
 }
-
-static bool grads_are_few(int64_t n, int d, int k)
+static bool grads_are_few(int dtype, int64_t n, int d, int k)
 {
     const double work = (double)n * d * k;
     if (n * pad_to(k, 32) > FEW_PAIRS) return false;
-    return work <= (d <= NARROW_DIM ? FEW_GRAD_NARROW_WORK : n <= FEW_GRAD_ROWS || k <= FEW_GRAD_ROWS ? FEW_GRAD_THIN_WORK : FEW_GRAD_WORK);
+    if (d > narrow_dim(dtype)) return work <= (n <= FEW_GRAD_ROWS || k <= FEW_GRAD_ROWS ? FEW_GRAD_THIN_WORK : FEW_GRAD_WORK);
+    return work <= (d <= NARROW_DIM ? FEW_GRAD_NARROW_WORK : FEW_GRAD_NARROW_WORK_16);
 }
 
 static LossPlan loss_plan(int dtype, int64_t n, int d, int k, bool backward, void *ws)
@@ -1012,7 +1023,8 @@ static LossPlan loss_plan(int dtype, int64_t n, int d, int k, bool backward, voi
     p.kpad = pad_to(k, TILE);
     p.d = d;
     p.units = (d + 31) / 32;
-    if (p.np == 1 && d > NARROW_DIM) p.units += p.units & 1; // (ProductRows takes two at a time)
+    p.narrow = d <= narrow_dim(dtype);
+    if (p.np == 1 && !p.narrow) p.units += p.units & 1; // (ProductRows takes two at a time)
     p.dblocks = d <= 128 ? 1 : (int)(pad_to(d, 256) / 128);
     p.rows = n < LOSS_ROWS ? n : LOSS_ROWS;
     p.rpad = pad_to(p.rows, TILE);
@@ -1025,7 +1037,7 @@ static LossPlan loss_plan(int dtype, int64_t n, int d, int k, bool backward, voi
         ptr = ws ? (std::remove_reference_t<decltype(ptr)>)((char *)ws + off) : nullptr;
         off += count * sizeof(*ptr);
     };
-    p.few = backward && grads_are_few(n, d, k);
+    p.few = backward && grads_are_few(dtype, n, d, k);
     if (p.few) {
         p.kp = (int)pad_to(k, 32);
         take(p.G, (size_t)n * p.kp);
@@ -1048,7 +1060,6 @@ static LossPlan loss_plan(int dtype, int64_t n, int d, int k, bool backward, voi
     take(p.bias2, p.kpad);
     take(p.row, p.npad);
     take(p.lab, p.npad);
-    p.narrow = d <= NARROW_DIM;
     if (!backward && p.narrow) {
         const int64_t xq = p.npad / narrow_rows(p.np, p.units), xt = p.kpad / 32, per = xq * xt / NARROW_GROUPS;
         p.xsplit = narrow_parts(xt, per < NARROW_LEAST / 2 ? NARROW_LEAST / 2 : per, p.npad * 8, &p.xper);
@@ -1092,7 +1103,7 @@ static LossPlan loss_plan(int dtype, int64_t n, int d, int k, bool backward, voi
 
 size_t loss_workspace(int dtype, int64_t n, int d, int k, bool backward)
 {
-    const size_t forward = loss_is_few(n, d, k) ? ((size_t)(k / 32 + 1) * 8 + 4) * (n < 1 ? 1 : n) : loss_plan(dtype, n, d, k, false, nullptr).bytes;
+    const size_t forward = loss_is_few(dtype, n, d, k) ? ((size_t)(k / 32 + 1) * 8 + 4) * (n < 1 ? 1 : n) : loss_plan(dtype, n, d, k, false, nullptr).bytes;
     if (!backward) return forward;
     const size_t both = loss_plan(dtype, n, d, k, true, nullptr).bytes;
     return both < forward ? forward : both;
@@ -1219,7 +1230,7 @@ static int loss_few(const LossArgs &a, hipStream_t st)
 template <typename T, int NP>
 static int loss_forward(const LossArgs &a, hipStream_t st)
 {
-    if (loss_is_few(a.n, a.d, a.k)) return loss_few(a, st);
+    if (loss_is_few(a.dtype, a.n, a.d, a.k)) return loss_few(a, st);
     const LossPlan p = loss_plan(a.dtype, a.n, a.d, a.k, false, a.ws);
     loss_images<T, NP>(a, p, false, st);
     if (p.narrow) {

@@ -1,6 +1,6 @@
-// The gradients of the softmax loss for up to 128 dimensions: no piece of the n x k probabilities leaves the registers.
+// The softmax loss and its gradients for up to 128 dimensions, 256 of 16-bit values: no piece of the n x k probabilities leaves the registers.
 //
-// A workgroup keeps 128 rows (256 with one fp16 part) of one matrix, of x for dx and of c for dc: their fragments and their gradient's
+// A workgroup keeps 128 rows (256 of up to 96 16-bit values) of one matrix, of x for dx and of c for dc: their fragments and their gradient's
 // sums stay in registers while tiles of 32 rows of the other matrix pass through LDS, its image and the image of its
 // columns.  Per tile a wave multiplies 32 rows of the other matrix with its own (S = R Q^T), turns S into P with the row's
 // maximum and sum, and multiplies the other matrix's columns with P (dQ^T += R^T P).  S has four consecutive r of one q in a lane; P as the
@@ -14,6 +14,8 @@
 // 1.11 PFLOP/s, the matrix cores busy 60 % of the time at the 1.87 GHz that the card then holds; forward 180 us, 1.15.  The
 // products and the arithmetic of two tiles woven into each other by hand gained nothing over two workgroups a compute unit
 // with the products' waves preferred.
+// 16-bit values: 8 192 x 32 000 x 256 bf16, forward and gradients 716 us (0.94 PFLOP/s), x 129 531; there the fragments' reads from LDS take as
+// long as the products that they feed.
 // Few rows (256 x 16 384 x 96 fp32, 20 us): 256 workgroups of eight tiles each, whose steps follow one another.
 #include "loss_image.h"
 
@@ -49,8 +51,9 @@ __device__ __forceinline__ void narrow(const NarrowArgs &a, const NarrowSide &s,
         for (int e = 0; e < (CHUNKS + 3) / 4; ++e) {
             const int c = e * 4 + wave; // (rows: page c / 2, group c % 2; columns: part, then group of 16 dimensions)
             if (CHUNKS % 4 && c >= CHUNKS) break;
-            const int cc = c - 2 * DU * NP;
-            const u32x4 *src = c < 2 * DU * NP ? rows + (c >> 1) * PAGE + (c & 1) * 64 : cols + (cc / DB) * PAGE + (cc % DB) * 64;
+            const int cc = c - 2 * DU * NP, dim = cc % DB; // (group of 16 dimensions: eight a block of the columns' image)
+            const u32x4 *src = c < 2 * DU * NP ? rows + (c >> 1) * PAGE + (c & 1) * 64
+                                               : cols + ((int64_t)(dim >> 3) * s.tiles * NP + cc / DB) * PAGE + (dim & 7) * 64;
             copy16(src, 1024, dst + c * 64);
         }
         u32x4 *num = dst + CHUNKS * 64;
@@ -324,7 +327,14 @@ static int narrow_units(const NarrowArgs &a, hipStream_t st)
         hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(NARROW_NT), bytes, st, a);
         return 0;
     };
-    switch ((a.d + 31) / 32) {
+    if constexpr (sizeof(T) == 2)
+        switch (a.units) {
+        case 5: return go(std::integral_constant<int, 5>{});
+        case 6: return go(std::integral_constant<int, 6>{});
+        case 7: return go(std::integral_constant<int, 7>{});
+        case 8: return go(std::integral_constant<int, 8>{});
+        }
+    switch (a.units) {
     case 1: return go(std::integral_constant<int, 1>{});
     case 2: return go(std::integral_constant<int, 2>{});
     case 3: return go(std::integral_constant<int, 3>{});
