@@ -36,11 +36,11 @@
 #define LOSS_ROWS 8192       // rows that go through the products together
 #define PIECE (1 << 26)      // values of P kept at a time
 // Up to so many dimensions the narrow form, of two parts and of 16-bit values: what a workgroup keeps fits the registers.  us of a
-// step against the wide form: 8 192 x 32 000 x 129 bf16 531 : 1 146, x 192 fp16 593 : 1 060, x 256 bf16 716 : 1 170; 1 000 x 20 000 x 160
-// bf16 110 : 137, 300 x 32 000 x 256 bf16 126 : 123; forward 8 192 x 32 000 x 256 bf16 166 : 205, 2 735 x 2 322 x 190 18 : 22.
+// step against the wide form: 8 192 x 32 000 x 129 bf16 453 : 1 146, x 192 fp16 534 : 1 060, x 256 bf16 648 : 1 170; 1 000 x 20 000 x 160
+// bf16 88 : 137, 300 x 32 000 x 256 bf16 100 : 123; forward 8 192 x 32 000 x 256 bf16 141 : 205, 2 735 x 2 322 x 190 19 : 22.
 #define NARROW_DIM 128
 #define NARROW_DIM_16 256
-#define NARROW_GROUPS 1024   // its workgroups, about: two rounds of two a compute unit
+#define NARROW_GROUPS 1024   // its workgroups that run at a time: four a compute unit forward, half as many backward
 #define NARROW_LEAST 8       // tiles of 32 rows that a workgroup of it takes at least (forward half as many)
 // Where little is done with each centroid, rows and centroids are taken as they lie (softmax_loss_few.hip): rewriting them first,
 // and tiles that leave most of the chip idle, cost more.  Measured in us, these against the others.
@@ -985,7 +985,7 @@ static int sum_parts(int64_t tiles, int64_t units, int64_t out_bytes)
     return (int)((units + per - 1) / per); // (no part is empty)
 }
 
-// The narrow form: parts of about `per` tiles of 32, fewer where their slabs would take more than 256 MB
+// The narrow form: parts of `per` tiles of 32, fewer where their slabs would take more than 256 MB
 static int narrow_parts(int64_t tiles, int64_t per, int64_t out_bytes, int *tiles_each)
 {
     int64_t s = (tiles + per - 1) / per;
@@ -994,6 +994,33 @@ static int narrow_parts(int64_t tiles, int64_t per, int64_t out_bytes, int *tile
     const int64_t each = (tiles + s - 1) / s;
     *tiles_each = (int)each;
     return (int)((tiles + each - 1) / each);
+}
+
+// Tiles of a workgroup, so that all of them fill the chip's `slots` a whole number of times (one to three, whatever the sums over parts
+// and the starts of more workgroups leave as the shortest): xq and cq workgroups side by side, xt and ct tiles to go through,
+// x_bytes and c_bytes of a part's sums (0: none), us of a tile.
+static int64_t narrow_per(int64_t xq, int64_t xt, int64_t cq, int64_t ct, int64_t slots, int64_t least, double x_bytes, double c_bytes, double us)
+{
+    int64_t best = least;
+    double best_us = 1e30;
+    for (int rounds = 1; rounds <= 3; ++rounds) {
+        int64_t per = (xq * xt + cq * ct) / (slots * rounds);
+        if (per < least) per = least;
+        int64_t xs, cs;
+        for (;; per += 1 + per / 16) {
+            xs = (xt + per - 1) / per;
+            cs = cq ? (ct + per - 1) / per : 0;
+            if (xq * xs + cq * cs <= slots * rounds || (xs == 1 && cs <= 1)) break;
+        }
+        const int64_t longest = xs == 1 && cs <= 1 ? (xt > ct ? xt : ct) : per, turns = (xq * xs + cq * cs + slots - 1) / slots;
+        const double sums = (xs > 1 ? xs * x_bytes : 0.) + (cs > 1 ? cs * c_bytes : 0.);
+        const double t = turns * (longest + 2) * us + sums / 2.2e6; // (written and read at 4.4 TB/s)
+        if (t < best_us) {
+            best_us = t;
+            best = per;
+        }
+    }
+    return best;
 }
 
 static int narrow_dim(int dtype) { return dtype == VLQ_F32 ? NARROW_DIM : NARROW_DIM_16; }
@@ -1024,6 +1051,7 @@ static LossPlan loss_plan(int dtype, int64_t n, int d, int k, bool backward, voi
     p.d = d;
     p.units = (d + 31) / 32;
     p.narrow = d <= narrow_dim(dtype);
+    const double tile = 0.27 * p.units * (p.np == 2 ? 2.7 : 1.) * narrow_rows(p.np, p.units) / 128; // us of one in the narrow form, two workgroups a compute unit
     if (p.np == 1 && !p.narrow) p.units += p.units & 1; // (ProductRows takes two at a time)
     p.dblocks = d <= 128 ? 1 : (int)(pad_to(d, 256) / 128);
     p.rows = n < LOSS_ROWS ? n : LOSS_ROWS;
@@ -1061,8 +1089,8 @@ static LossPlan loss_plan(int dtype, int64_t n, int d, int k, bool backward, voi
     take(p.row, p.npad);
     take(p.lab, p.npad);
     if (!backward && p.narrow) {
-        const int64_t xq = p.npad / narrow_rows(p.np, p.units), xt = p.kpad / 32, per = xq * xt / NARROW_GROUPS;
-        p.xsplit = narrow_parts(xt, per < NARROW_LEAST / 2 ? NARROW_LEAST / 2 : per, p.npad * 8, &p.xper);
+        const int64_t xq = p.npad / narrow_rows(p.np, p.units), xt = p.kpad / 32;
+        p.xsplit = narrow_parts(xt, narrow_per(xq, xt, 0, 0, NARROW_GROUPS, NARROW_LEAST / 2, p.npad * 8., 0., tile / 3), p.npad * 8, &p.xper);
         take(p.mine, p.npad);
         take(p.part, p.xsplit * p.npad);
     } else if (!backward) {
@@ -1075,8 +1103,7 @@ static LossPlan loss_plan(int dtype, int64_t n, int d, int k, bool backward, voi
         take(p.ccols, p.kpad / 32 * p.dblocks * page);
         if (p.narrow) {
             const int64_t rows = narrow_rows(p.np, p.units), xq = p.npad / rows, cq = p.kpad / rows, xt = p.kpad / 32, ct = p.npad / 32;
-            int64_t per = (xq * xt + cq * ct) / NARROW_GROUPS;
-            if (per < NARROW_LEAST) per = NARROW_LEAST;
+            const int64_t per = narrow_per(xq, xt, cq, ct, NARROW_GROUPS / 2, NARROW_LEAST, n * d * 4., (double)k * d * 4, tile);
             p.xsplit = narrow_parts(xt, per, n * d * 4, &p.xper);
             p.csplit = narrow_parts(ct, per, (int64_t)k * d * 4, &p.cper);
             p.xslab = p.xsplit > 1;

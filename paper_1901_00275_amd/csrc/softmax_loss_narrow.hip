@@ -14,7 +14,7 @@
 // 1.11 PFLOP/s, the matrix cores busy 60 % of the time at the 1.87 GHz that the card then holds; forward 180 us, 1.15.  The
 // products and the arithmetic of two tiles woven into each other by hand gained nothing over two workgroups a compute unit
 // with the products' waves preferred.
-// 16-bit values: 8 192 x 32 000 x 256 bf16, forward and gradients 716 us (0.94 PFLOP/s), x 129 531; there the fragments' reads from LDS take as
+// 16-bit values: 8 192 x 32 000 x 256 bf16, forward and gradients 650 us (1.03 PFLOP/s), x 129 453; there the fragments' reads from LDS take as
 // long as the products that they feed.
 // Few rows (256 x 16 384 x 96 fp32, 20 us): 256 workgroups of eight tiles each, whose steps follow one another.
 #include "loss_image.h"
