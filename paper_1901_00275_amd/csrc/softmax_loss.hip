@@ -998,7 +998,8 @@ static int narrow_parts(int64_t tiles, int64_t per, int64_t out_bytes, int *tile
 
 // Tiles of a workgroup, so that all of them fill the chip's `slots` a whole number of times (one to three, whatever the sums over parts
 // and the starts of more workgroups leave as the shortest): xq and cq workgroups side by side, xt and ct tiles to go through,
-// x_bytes and c_bytes of a part's sums (0: none), us of a tile.
+// x_bytes and c_bytes of a part's sums (0: none), us of a tile.  (Always two rounds, whatever was left for a
+// third: a step of 2 710 x 9 867 x 192 fp16 131 us, 107 so; 300 x 32 000 x 256 bf16 125 and 100, 8 192 x 32 000 x 256 703 and 648.)
 static int64_t narrow_per(int64_t xq, int64_t xt, int64_t cq, int64_t ct, int64_t slots, int64_t least, double x_bytes, double c_bytes, double us)
 {
     int64_t best = least;
@@ -1366,7 +1367,7 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
     LOSS_TRY(lie ? allow_lds(k_loss_p<Rows>, Rows::LDS) : allow_lds(k_loss_p<FromImages<NP>>, FromImages<NP>::LDS));
     LOSS_TRY(allow_lds(k_loss_grads<T, NP>, Product<NP>::LDS));
     const int mt = p.dblocks / 2;
-    const bool vec = a.d % 4 == 0;
+    const bool vec = a.d % 4 == 0, whole = a.n <= p.rows && p.kpad <= p.piece; // (one piece: dbias with the other sums)
     for (int64_t r0 = 0; r0 < a.n; r0 += p.rows) {
         const int64_t rows = a.n - r0 < p.rows ? a.n - r0 : p.rows, rpad = pad_to(rows, TILE);
         for (int64_t c0 = 0; c0 < p.kpad; c0 += p.piece) {
@@ -1382,7 +1383,7 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
                 hipLaunchKernelGGL(k_loss_p<Rows>, dim3((unsigned)(g.mt * g.nt)), dim3(LNT), Rows::LDS, st, g);
             else
                 hipLaunchKernelGGL(k_loss_p<FromImages<NP>>, dim3((unsigned)(g.mt * g.nt)), dim3(LNT), FromImages<NP>::LDS, st, g);
-            if (a.dbias) {
+            if (a.dbias && !whole) {
                 const BiasSum bias = bias_part((int)(rpad / 64), cpad, c0, a.k - c0 < cpad ? a.k - c0 : cpad, r0 > 0);
                 hipLaunchKernelGGL(k_loss_sums<T>, dim3((unsigned)bias.blocks), dim3(256), 0, st, SlabSum{}, SlabSum{}, bias, a.scale);
             }
@@ -1434,7 +1435,7 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
                 hipLaunchKernelGGL((k_loss_grads<T, NP>), dim3((unsigned)(nx + nc)), dim3(LNT), Product<NP>::LDS, st, x, c, nx);
         }
     }
-    finish(BiasSum{});
+    finish(a.dbias && whole ? bias_part((int)(p.rpad / 64), p.kpad, 0, a.k, false) : BiasSum{});
     return (int)hipGetLastError();
 }
 
