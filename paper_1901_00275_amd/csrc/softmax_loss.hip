@@ -56,12 +56,13 @@
 // A step with the gradients (their products are fp32's, an eighth of the others' rate, but with few rows or centroids the others' tiles
 // are mostly empty): 5 366 x 24 x 2 016 fp16 58 : 115, 3 x 30 x 224 fp16 22 : 38, 500 x 500 x 500 fp32 37 : 103, bf16 40 : 75,
 // 8 000 x 32 x 2 000 fp32 134 : 282, 32 x 16 000 x 2 000 bf16 132 : 179, 8 000 x 64 x 4 000 bf16 269 : 327, 64 x 65 536 x 1 024 bf16
-// 410 : 322, 1 000 x 1 000 x 300 bf16 76 : 79.  Narrow: 300 x 300 x 128 bf16 26 : 35, 300 x 3 000 x 96 bf16 37 : 39, 1 000 x 1 000 x 96
+// 410 : 322, 1 000 x 1 000 x 300 bf16 79 : 77,
+// 300 x 800 x 1 200 45 : 79, 300 x 3 000 x 300 fp32 72 : 97, 1 000 x 2 000 x 200 104 : 88, 2 000 x 1 000 x 300 121 : 107.  Narrow: 300 x 300 x 128 bf16 26 : 35, 300 x 3 000 x 96 bf16 37 : 39, 1 000 x 1 000 x 96
 // fp32 45 : 43, 100 x 16 384 x 128 fp32 78 : 60; 600 x 300 x 256 bf16 27 : 45, 1 000 x 500 x 160 33 : 40, 500 x 1 500 x 192 fp16 41 : 41,
 // 300 x 3 000 x 250 bf16 73 : 60, 4 000 x 400 x 200 67 : 51.
 #define FEW_GRAD_ROWS 64         // rows or centroids at most
 #define FEW_GRAD_THIN_WORK 2.5e9 // with so few
-#define FEW_GRAD_WORK 2.5e8      // with more
+#define FEW_GRAD_WORK 3e8      // with more
 #define FEW_GRAD_NARROW_WORK 5e7
 #define FEW_GRAD_NARROW_WORK_16 1.5e8
 #define FEW_PAIRS (1 << 24)   // values of G, in fp32

@@ -57,7 +57,7 @@ def compare(got, want, names=("loss", "dx", "dc", "db")):
 
 SHAPES = [(1, 1, 1), (1, 96, 300), (3, 7, 2), (64, 32, 256), (65, 33, 257), (255, 96, 1000), (257, 128, 513), (300, 130, 1025),
           (40, 520, 77), (17, 1027, 515), (1000, 64, 5000), (33, 48, 65537), (9, 200, 70001), (129, 100, 9000), (700, 136, 1100), (2100, 500, 1001), (900, 264, 5003), (1500, 192, 4100),
-          (1000, 128, 3000), (2049, 31, 1500), (1200, 1027, 515), (3000, 130, 1025), (1111, 520, 777), (7, 300, 33), (5000, 129, 5), (2, 64, 40000), (5001, 2052, 61), (1300, 217, 1111), (1200, 256, 1400), (1031, 257, 1100), (300, 193, 9000)]
+          (1000, 128, 3000), (2049, 31, 1500), (1200, 1027, 515), (3000, 130, 1025), (1111, 520, 777), (7, 300, 33), (5000, 129, 5), (2, 64, 40000), (5001, 2052, 61), (1300, 217, 1111), (1200, 256, 1400), (1131, 257, 1100), (300, 193, 9000)]
 
 
 @pytest.mark.parametrize("t", [F32, F16, BF16])
@@ -68,7 +68,7 @@ def test_against_64_bits(vlq, t, n, d, k):
 
 
 @pytest.mark.parametrize("t", [F32, F16, BF16])
-@pytest.mark.parametrize("n,d,k", [(1, 40, 100), (200, 96, 700), (513, 200, 300), (700, 96, 1500), (1513, 200, 1300), (900, 300, 1100)])
+@pytest.mark.parametrize("n,d,k", [(1, 40, 100), (200, 96, 700), (513, 200, 300), (700, 96, 1500), (1513, 200, 1300), (1000, 300, 1100)])
 def test_no_bias_negative_scale(vlq, t, n, d, k):
     x, c, _, label, grad = problem(t, n, d, k, bias=False, spread=3.0)
     compare(run(vlq, x, c, None, -1.3, label, grad), softmax_loss(x, c, None, -1.3, label, grad))
@@ -88,7 +88,7 @@ def test_rows_and_centroids_that_do_not_count(vlq, t, n, d, k):
     assert math.isinf(got["loss"][7].item()) and (got["loss"][dead] == 0).all() and (got["dx"][dead] == 0).all()
 
 
-@pytest.mark.parametrize("n,d,k", [(20, 64, 300), (300, 64, 3000), (1000, 160, 2000), (900, 300, 1100)])
+@pytest.mark.parametrize("n,d,k", [(20, 64, 300), (300, 64, 3000), (1000, 160, 2000), (1000, 300, 1100)])
 @pytest.mark.parametrize("t", [F32, BF16])
 def test_nothing_left(vlq, t, n, d, k):
     x, c, bias, label, grad = problem(t, n, d, k)
@@ -129,7 +129,7 @@ def test_most_rows_and_most_centroids(vlq):
 
 @pytest.mark.parametrize("t", [F32, F16, BF16])
 @pytest.mark.parametrize("bad", [math.inf, math.nan])
-@pytest.mark.parametrize("n,d,k", [(70, 40, 300), (70, 140, 300), (900, 40, 1500), (900, 140, 2100), (900, 300, 1100)])
+@pytest.mark.parametrize("n,d,k", [(70, 40, 300), (70, 140, 300), (900, 40, 1500), (900, 140, 2100), (1000, 300, 1100)])
 def test_gradients_that_are_not_finite(vlq, t, bad, n, d, k):
     # a row's own dx, and what is summed over the rows: whether other rows have gradients or not
     x, c, bias, label, grad = problem(t, n, d, k)
@@ -144,7 +144,7 @@ def test_gradients_that_are_not_finite(vlq, t, bad, n, d, k):
         assert torch.equal(got["dx"][rest], ref["dx"][rest])
 
 
-SIZES = [(130, 128, 600), (1030, 128, 1600), (1030, 160, 1600), (900, 300, 1100)]  # of each form of the gradients
+SIZES = [(130, 128, 600), (1030, 128, 1600), (1030, 160, 1600), (1000, 300, 1100)]  # of each form of the gradients
 
 
 @pytest.mark.parametrize("n,d,k", SIZES)
@@ -190,7 +190,7 @@ def test_unaligned_operands_against_64_bits(vlq, t, n, d, k):
         compare(run(vlq, *ops, 1.0, label, grad), softmax_loss(x, c, bias, 1.0, label, grad))
 
 
-@pytest.mark.parametrize("n,d,k", [(300, 160, 700), (600, 96, 1000), (1500, 160, 1100), (900, 300, 1100)])
+@pytest.mark.parametrize("n,d,k", [(300, 160, 700), (600, 96, 1000), (1500, 160, 1100), (1000, 300, 1100)])
 @pytest.mark.parametrize("what", [("dx",), ("dc",), ("db",), ("dx", "db")])
 def test_some_gradients_alone(vlq, what, n, d, k):
     x, c, bias, label, grad = problem(BF16, n, d, k)
