@@ -59,10 +59,17 @@ __device__ __forceinline__ double block_sum(double v)
     return v;
 }
 
-template <bool STAY>
-__device__ __forceinline__ u32x4 load16(const u32x4 *p)
+// 16 bytes at a value's address: the memory takes them at any (120 M bf16 values off 16 bytes 335 us value by value, 145 so, 122 on them)
+template <typename T>
+struct Sixteen {
+    static constexpr int N = 16 / sizeof(T);
+    typedef uint32_t At __attribute__((ext_vector_type(N * sizeof(T) / 4), aligned(sizeof(T))));
+};
+template <bool STAY, typename T>
+__device__ __forceinline__ u32x4 load16(const T *p)
 {
-    return STAY ? *p : __builtin_nontemporal_load(p);
+    using At = typename Sixteen<T>::At;
+    return STAY ? *(const At *)p : __builtin_nontemporal_load((const At *)p);
 }
 
 template <typename T, bool STAY>
@@ -71,28 +78,25 @@ __device__ __forceinline__ double squares(const T *p, int64_t count)
     constexpr int N = 16 / sizeof(T);
     double s = 0.;
     int64_t i = threadIdx.x;
-    if ((uintptr_t)p % 16 == 0) {
-        const int64_t whole = count / N;
-        const u32x4 *q = (const u32x4 *)p;
-        double s2[4] = {};
-        for (; i + 3 * CLIP_NT < whole; i += 4 * CLIP_NT) {
-            T v[4][N];
+    const int64_t whole = count / N;
+    double s2[4] = {};
+    for (; i + 3 * CLIP_NT < whole; i += 4 * CLIP_NT) {
+        T v[4][N];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) *(u32x4 *)v[u] = load16<STAY>(q + i + u * CLIP_NT);
+        for (int u = 0; u < 4; ++u) *(u32x4 *)v[u] = load16<STAY>(p + (i + u * CLIP_NT) * N);
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
+        for (int u = 0; u < 4; ++u)
 #pragma unroll
-                for (int e = 0; e < N; ++e) s2[u] = fma((double)(float)v[u][e], (double)(float)v[u][e], s2[u]);
-        }
-        for (; i < whole; i += CLIP_NT) {
-            T v[N];
-            *(u32x4 *)v = load16<STAY>(q + i);
-#pragma unroll
-            for (int e = 0; e < N; ++e) s = fma((double)(float)v[e], (double)(float)v[e], s);
-        }
-        s += (s2[0] + s2[1]) + (s2[2] + s2[3]);
-        i = whole * N + threadIdx.x;
+            for (int e = 0; e < N; ++e) s2[u] = fma((double)(float)v[u][e], (double)(float)v[u][e], s2[u]);
     }
+    for (; i < whole; i += CLIP_NT) {
+        T v[N];
+        *(u32x4 *)v = load16<STAY>(p + i * N);
+#pragma unroll
+        for (int e = 0; e < N; ++e) s = fma((double)(float)v[e], (double)(float)v[e], s);
+    }
+    s += (s2[0] + s2[1]) + (s2[2] + s2[3]);
+    i = whole * N + threadIdx.x;
     for (; i < count; i += CLIP_NT) s = fma((double)(float)p[i], (double)(float)p[i], s);
     return s;
 }
@@ -152,25 +156,27 @@ __device__ __forceinline__ void scale_values(const T *p, T *o, int64_t count, do
 {
     constexpr int N = 16 / sizeof(T);
     int64_t i = threadIdx.x;
-    if (((uintptr_t)p | (uintptr_t)o) % 16 == 0) {
-        const int64_t whole = count / N;
-        const u32x4 *q = (const u32x4 *)p;
-        u32x4 *r = (u32x4 *)o;
-        for (; i < whole; i += 4 * CLIP_NT) {
-            T v[4][N];
+    const bool past = (uintptr_t)o % 16 == 0; // (parts of a cache's line are put together in the cache)
+    using At = typename Sixteen<T>::At;
+    const int64_t whole = count / N;
+    for (; i < whole; i += 4 * CLIP_NT) {
+        T v[4][N];
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-                if (i + u * CLIP_NT < whole) *(u32x4 *)v[u] = load16<STAY>(q + i + u * CLIP_NT);
+        for (int u = 0; u < 4; ++u)
+            if (i + u * CLIP_NT < whole) *(u32x4 *)v[u] = load16<STAY>(p + (i + u * CLIP_NT) * N);
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-                if (i + u * CLIP_NT < whole) {
+        for (int u = 0; u < 4; ++u)
+            if (i + u * CLIP_NT < whole) {
 #pragma unroll
-                    for (int e = 0; e < N; ++e) v[u][e] = (T)(float)((float)v[u][e] * f);
-                    __builtin_nontemporal_store(*(u32x4 *)v[u], r + i + u * CLIP_NT);
-                }
-        }
-        i = whole * N + threadIdx.x;
+                for (int e = 0; e < N; ++e) v[u][e] = (T)(float)((float)v[u][e] * f);
+                u32x4 *to = (u32x4 *)(o + (i + u * CLIP_NT) * N);
+                if (past)
+                    __builtin_nontemporal_store(*(u32x4 *)v[u], to);
+                else
+                    *(At *)to = *(u32x4 *)v[u];
+            }
     }
+    i = whole * N + threadIdx.x;
     for (; i < count; i += CLIP_NT) o[i] = (T)(float)((float)p[i] * f);
 }
 

@@ -6,7 +6,7 @@
 // pairs in turn, 64 at a time, those of one digit told apart by ballots.  No atomics on memory, so the order is the pairs' own.
 // What bounds it are launches of 5 to 11 us, each some waits for memory one behind the other: 640 000 pairs and 65 536 cells
 // (two digits) 51 us in seven launches, 13 MB of pairs and places.  Up to SMALL_PAIRS pairs of one digit take one launch.
-// The rest moves memory: 16 bytes at a time where rows lie on them, else 8, 4 or a value, several rows' loads under way.  640 000 rows of 384 bytes
+// The rest moves memory: 16 bytes at a time, several rows' loads under way.  640 000 rows of 384 bytes
 // gathered 41 us (6.0 TB/s written), 16 384 rows of 8 x 4 KB combined 137 us (4.3 TB/s), the gradient of 5 003 x 6 x 2 KB 26 us (5.0).
 #include "learn.h"
 
@@ -482,27 +482,33 @@ int launch_group_rows(const int32_t *cell, int64_t pairs, int cells, int64_t *of
 // ---------------------------------------------------------------------------
 // rows
 // ---------------------------------------------------------------------------
-// A piece of a row: as many bytes, up to 16, as all rows lie on (5 000 x 8 rows of 2 056 bytes combined: 25 us, value by value 62)
-template <typename T, int BYTES>
+// A piece of a row: 16 bytes, less where a row has fewer.  The memory takes them at any value's address, so rows of all sizes and
+// alignments go this way; the last piece of a row ends where the row does and overlaps the one before it, whose values it
+// writes again.  WHOLE: all rows lie on 16 bytes; they are stored past the caches, which others would need to put their lines
+// together.  (5 000 x 8 rows of 2 050 bytes combined: 61 us value by value, 26 so.)
+template <typename T, int BYTES, bool WHOLE>
 struct Piece {
     static constexpr int N = BYTES / (int)sizeof(T);
     using Word = std::conditional_t<BYTES == 16, u32x4, std::conditional_t<BYTES == 8, u32x2, std::conditional_t<BYTES == 4, uint32_t, uint16_t>>>;
+    typedef Word At __attribute__((aligned(sizeof(T))));
     T v[N];
+    // the first value of piece c
+    static __device__ __forceinline__ uint32_t at(uint32_t c, int d) { return WHOLE ? c * N : min(c * N, (uint32_t)(d - N)); }
 };
-template <typename T, int BYTES>
-__device__ __forceinline__ Piece<T, BYTES> load_piece(const T *p)
+template <typename T, int BYTES, bool WHOLE>
+__device__ __forceinline__ Piece<T, BYTES, WHOLE> load_piece(const T *p)
 {
-    using P = Piece<T, BYTES>;
-    return __builtin_bit_cast(P, *(const typename P::Word *)p);
+    using P = Piece<T, BYTES, WHOLE>;
+    return __builtin_bit_cast(P, *(const typename P::At *)p);
 }
-template <typename T, int BYTES>
-__device__ __forceinline__ void store_piece(T *p, const Piece<T, BYTES> &r)
+template <typename T, int BYTES, bool WHOLE>
+__device__ __forceinline__ void store_piece(T *p, const Piece<T, BYTES, WHOLE> &r)
 {
-    using W = typename Piece<T, BYTES>::Word;
-    if constexpr (BYTES == 16)
-        __builtin_nontemporal_store(__builtin_bit_cast(W, r), (W *)p);
+    using P = Piece<T, BYTES, WHOLE>;
+    if constexpr (WHOLE)
+        __builtin_nontemporal_store(__builtin_bit_cast(typename P::Word, r), (typename P::At *)p);
     else
-        *(W *)p = __builtin_bit_cast(W, r);
+        *(typename P::At *)p = __builtin_bit_cast(typename P::Word, r);
 }
 
 #define ROW_NT 256
@@ -519,10 +525,10 @@ struct RowsArgs {
 };
 
 // y[p] = x[source[p] / w]: the pieces of a workgroup's rows, ROW_ITEMS a thread at a time
-template <typename T, int BYTES>
+template <typename T, int BYTES, bool WHOLE>
 __global__ __launch_bounds__(ROW_NT) void k_gather_rows(RowsArgs a, const T *__restrict__ x, T *__restrict__ y)
 {
-    using P = Piece<T, BYTES>;
+    using P = Piece<T, BYTES, WHOLE>;
     const int64_t places = a.n * a.w, p0 = (a.block + blockIdx.x) * a.rows;
     const uint32_t pieces = (uint32_t)min((int64_t)a.rows, places - p0) * a.per;
     for (uint32_t i0 = threadIdx.x; i0 < pieces; i0 += ROW_NT * ROW_ITEMS) {
@@ -535,24 +541,24 @@ __global__ __launch_bounds__(ROW_NT) void k_gather_rows(RowsArgs a, const T *__r
             if (i >= pieces) continue;
             const int32_t s = a.index[p0 + r];
             if ((int64_t)s >= places || s < 0) continue; // (a place behind the last pair)
-            v[u] = load_piece<T, BYTES>(x + (int64_t)((uint32_t)s / (uint32_t)a.w) * a.d + c * P::N);
-            to[u] = (p0 + r) * a.d + c * P::N;
+            v[u] = load_piece<T, BYTES, WHOLE>(x + (int64_t)((uint32_t)s / (uint32_t)a.w) * a.d + P::at(c, a.d));
+            to[u] = (p0 + r) * a.d + P::at(c, a.d);
         }
 #pragma unroll
         for (int u = 0; u < ROW_ITEMS; ++u)
-            if (to[u] >= 0) store_piece<T, BYTES>(y + to[u], v[u]);
+            if (to[u] >= 0) store_piece<T, BYTES, WHOLE>(y + to[u], v[u]);
     }
 }
 
 // out[i] = sum over the row's choices of weight y[place], in their order, in fp32
-template <typename T, int BYTES>
+template <typename T, int BYTES, bool WHOLE>
 __global__ __launch_bounds__(ROW_NT) void k_combine_rows(RowsArgs a, const T *__restrict__ y, T *__restrict__ out)
 {
-    using P = Piece<T, BYTES>;
+    using P = Piece<T, BYTES, WHOLE>;
     const int64_t places = a.n * a.w, r0 = (a.block + blockIdx.x) * a.rows;
     const uint32_t pieces = (uint32_t)min((int64_t)a.rows, a.n - r0) * a.per;
     for (uint32_t i = threadIdx.x; i < pieces; i += ROW_NT) {
-        const uint32_t r = i / a.per, c = i - r * a.per;
+        const uint32_t r = i / a.per, at = P::at(i - r * a.per, a.d);
         const int32_t *pl = a.index + (r0 + r) * a.w;
         const float *wt = a.weight ? a.weight + (r0 + r) * a.w : nullptr;
         float s[P::N] = {};
@@ -564,7 +570,7 @@ __global__ __launch_bounds__(ROW_NT) void k_combine_rows(RowsArgs a, const T *__
                 f[q] = 0.f;
                 const int32_t p = q0 + q < a.w ? pl[q0 + q] : -1;
                 const bool in = p >= 0 && p < places;
-                v[q] = load_piece<T, BYTES>(y + (in ? (int64_t)p * a.d : 0) + c * P::N);
+                v[q] = load_piece<T, BYTES, WHOLE>(y + (in ? (int64_t)p * a.d : 0) + at);
                 if (in) f[q] = wt ? wt[q0 + q] : 1.f;
                 if (!in)
 #pragma unroll
@@ -578,17 +584,17 @@ __global__ __launch_bounds__(ROW_NT) void k_combine_rows(RowsArgs a, const T *__
         P o;
 #pragma unroll
         for (int e = 0; e < P::N; ++e) o.v[e] = (T)s[e];
-        store_piece<T, BYTES>(out + (r0 + r) * a.d + c * P::N, o);
+        store_piece<T, BYTES, WHOLE>(out + (r0 + r) * a.d + at, o);
     }
 }
 
 // dy[place] = weight dout[i], dweight[i][c] = <dout[i], y[place]>: L lanes eight choices of a row
 // (all choices of a row one after the other: 1 337 x 64 rows of 1 516 bytes 110 us, now 64)
-template <typename T, int BYTES, int L>
+template <typename T, int BYTES, bool WHOLE, int L>
 __global__ __launch_bounds__(ROW_NT) void k_combine_back(RowsArgs a, const T *__restrict__ dout, const T *__restrict__ y,
                                                          T *__restrict__ dy, float *__restrict__ dweight)
 {
-    using P = Piece<T, BYTES>;
+    using P = Piece<T, BYTES, WHOLE>;
     const int lane = threadIdx.x & (L - 1);
     const uint32_t eights = (a.w + 7) / 8, id = (uint32_t)((a.block + blockIdx.x) * (ROW_NT / L) + threadIdx.x / L); // (n w < 2^31)
     const int64_t places = a.n * a.w, r = id / eights;
@@ -604,11 +610,12 @@ __global__ __launch_bounds__(ROW_NT) void k_combine_back(RowsArgs a, const T *__
         dot[q] = 0.f;
     }
     for (uint32_t c = lane; c < a.per; c += L) {
-        const P g = load_piece<T, BYTES>(dout + r * a.d + c * P::N);
+        const uint32_t at = P::at(c, a.d), again = c * P::N - at; // (values that the piece before had)
+        const P g = load_piece<T, BYTES, WHOLE>(dout + r * a.d + at);
         P v[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q)
-            if (dweight && p[q] >= 0) v[q] = load_piece<T, BYTES>(y + p[q] * a.d + c * P::N);
+            if (dweight && p[q] >= 0) v[q] = load_piece<T, BYTES, WHOLE>(y + p[q] * a.d + at);
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
             if (p[q] < 0) continue;
@@ -616,9 +623,9 @@ __global__ __launch_bounds__(ROW_NT) void k_combine_back(RowsArgs a, const T *__
 #pragma unroll
             for (int e = 0; e < P::N; ++e) {
                 o.v[e] = (T)(f[q] * (float)g.v[e]);
-                if (dweight) dot[q] = fmaf((float)g.v[e], (float)v[q].v[e], dot[q]);
+                if (dweight && e >= (int)again) dot[q] = fmaf((float)g.v[e], (float)v[q].v[e], dot[q]);
             }
-            if (dy) store_piece<T, BYTES>(dy + p[q] * a.d + c * P::N, o);
+            if (dy) store_piece<T, BYTES, WHOLE>(dy + p[q] * a.d + at, o);
         }
     }
     if (!dweight) return;
@@ -630,19 +637,21 @@ __global__ __launch_bounds__(ROW_NT) void k_combine_back(RowsArgs a, const T *__
     }
 }
 
-// go(bytes of a piece)
+// go(bytes of a piece, WHOLE)
 template <typename T, typename F>
 static void by_pieces(int d, const void *p, const void *q, const void *r, F &&go)
 {
-    const uint64_t all = (uint64_t)d * sizeof(T) | (uintptr_t)p | (uintptr_t)q | (uintptr_t)r;
-    if (all % 16 == 0)
-        go(std::integral_constant<int, 16>{});
-    else if (all % 8 == 0)
-        go(std::integral_constant<int, 8>{});
-    else if (all % 4 == 0)
-        go(std::integral_constant<int, 4>{});
+    const uint64_t bytes = (uint64_t)d * sizeof(T);
+    if ((bytes | (uintptr_t)p | (uintptr_t)q | (uintptr_t)r) % 16 == 0)
+        go(std::integral_constant<int, 16>{}, std::true_type{});
+    else if (bytes >= 16)
+        go(std::integral_constant<int, 16>{}, std::false_type{});
+    else if (bytes >= 8)
+        go(std::integral_constant<int, 8>{}, std::false_type{});
+    else if (bytes >= 4)
+        go(std::integral_constant<int, 4>{}, std::false_type{});
     else
-        go(std::integral_constant<int, sizeof(T)>{});
+        go(std::integral_constant<int, sizeof(T)>{}, std::false_type{});
 }
 
 // rows of a workgroup: about `pieces` pieces
@@ -660,12 +669,13 @@ template <typename T>
 static int gather(const RowsArgs &args, const T *x, T *y, hipStream_t st)
 {
     RowsArgs a = args;
-    auto go = [&](auto BYTES) {
+    auto go = [&](auto BYTES, auto WHOLE) {
         constexpr int V = decltype(BYTES)::value;
-        a.per = a.d / Piece<T, V>::N;
+        constexpr bool W = decltype(WHOLE)::value;
+        a.per = (a.d + Piece<T, V, W>::N - 1) / Piece<T, V, W>::N;
         a.rows = rows_of(a.per, ROW_NT * ROW_ITEMS);
         in_launches(a, (a.n * a.w + a.rows - 1) / a.rows, [&](dim3 groups) {
-            hipLaunchKernelGGL((k_gather_rows<T, V>), groups, dim3(ROW_NT), 0, st, a, x, y);
+            hipLaunchKernelGGL((k_gather_rows<T, V, W>), groups, dim3(ROW_NT), 0, st, a, x, y);
         });
     };
     by_pieces<T>(a.d, x, y, nullptr, go);
@@ -676,12 +686,13 @@ template <typename T>
 static int combine(const RowsArgs &args, const T *y, T *out, hipStream_t st)
 {
     RowsArgs a = args;
-    auto go = [&](auto BYTES) {
+    auto go = [&](auto BYTES, auto WHOLE) {
         constexpr int V = decltype(BYTES)::value;
-        a.per = a.d / Piece<T, V>::N;
+        constexpr bool W = decltype(WHOLE)::value;
+        a.per = (a.d + Piece<T, V, W>::N - 1) / Piece<T, V, W>::N;
         a.rows = rows_of(a.per, ROW_NT);
         in_launches(a, (a.n + a.rows - 1) / a.rows, [&](dim3 groups) {
-            hipLaunchKernelGGL((k_combine_rows<T, V>), groups, dim3(ROW_NT), 0, st, a, y, out);
+            hipLaunchKernelGGL((k_combine_rows<T, V, W>), groups, dim3(ROW_NT), 0, st, a, y, out);
         });
     };
     by_pieces<T>(a.d, y, out, nullptr, go);
@@ -692,13 +703,14 @@ template <typename T>
 static int combine_back(const RowsArgs &args, const T *dout, const T *y, T *dy, float *dweight, hipStream_t st)
 {
     RowsArgs a = args;
-    auto go = [&](auto BYTES) {
+    auto go = [&](auto BYTES, auto WHOLE) {
         constexpr int V = decltype(BYTES)::value;
-        a.per = a.d / Piece<T, V>::N;
+        constexpr bool W = decltype(WHOLE)::value;
+        a.per = (a.d + Piece<T, V, W>::N - 1) / Piece<T, V, W>::N;
         auto lanes = [&](auto L) {
             constexpr int N = decltype(L)::value, R = ROW_NT / N;
             in_launches(a, (a.n * ((a.w + 7) / 8) + R - 1) / R, [&](dim3 groups) {
-                hipLaunchKernelGGL((k_combine_back<T, V, N>), groups, dim3(ROW_NT), 0, st, a, dout, y, dy, dweight);
+                hipLaunchKernelGGL((k_combine_back<T, V, W, N>), groups, dim3(ROW_NT), 0, st, a, dout, y, dy, dweight);
             });
         };
         if (a.per > 32)

@@ -29,16 +29,22 @@ __device__ __forceinline__ float pow2i(int ex) { return __uint_as_float((uint32_
 // eight values of a row from index i on, zeros past its end
 template <typename T>
 struct Eight {
+    typedef uint32_t At __attribute__((ext_vector_type(4 * sizeof(T) / sizeof(T)), aligned(sizeof(T)))); // 16 bytes at a value's address
     T v[8];
 };
 template <typename T>
 __device__ __forceinline__ Eight<T> load8(const T *row, int i, int d, bool vec)
 {
     Eight<T> r;
+    using At = typename Eight<T>::At;
     if (vec) { // (d is a multiple of 8)
         u32x4 *w = (u32x4 *)r.v;
 #pragma unroll
-        for (int p = 0; p < (int)sizeof(T) / 2; ++p) w[p] = i < d ? ((const u32x4 *)(row + i))[p] : u32x4{0, 0, 0, 0};
+        for (int p = 0; p < (int)sizeof(T) / 2; ++p) w[p] = i < d ? ((const At *)(row + i))[p] : At{0, 0, 0, 0};
+    } else if (i + 8 <= d) {
+        u32x4 *w = (u32x4 *)r.v;
+#pragma unroll
+        for (int p = 0; p < (int)sizeof(T) / 2; ++p) w[p] = ((const At *)(row + i))[p];
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) r.v[e] = i + e < d ? row[i + e] : (T)0.f;

@@ -54,9 +54,9 @@
 #define FEW_NARROW_WORK 1.2e8
 #define FEW_NARROW_WORK_16 3e8 // beyond NARROW_DIM dimensions
 // A step with the gradients (their products are fp32's, an eighth of the others' rate, but with few rows or centroids the others' tiles
-// are mostly empty): 5 366 x 24 x 2 016 fp16 58 : 115, 3 x 30 x 224 fp16 22 : 38, 500 x 500 x 500 fp32 37 : 103, bf16 40 : 75,
+// are mostly empty): 5 366 x 24 x 2 016 fp16 58 : 115, 3 x 30 x 224 fp16 22 : 38, 500 x 500 x 500 fp32 31 : 103, bf16 26 : 75,
 // 8 000 x 32 x 2 000 fp32 134 : 282, 32 x 16 000 x 2 000 bf16 132 : 179, 8 000 x 64 x 4 000 bf16 269 : 327, 64 x 65 536 x 1 024 bf16
-// 410 : 322, 1 000 x 1 000 x 300 bf16 79 : 77,
+// 410 : 322, 1 000 x 1 000 x 300 bf16 55 : 77,
 // 300 x 800 x 1 200 45 : 79, 300 x 3 000 x 300 fp32 72 : 97, 1 000 x 2 000 x 200 104 : 88, 2 000 x 1 000 x 300 121 : 107.  Narrow: 300 x 300 x 128 bf16 26 : 35, 300 x 3 000 x 96 bf16 37 : 39, 1 000 x 1 000 x 96
 // fp32 45 : 43, 100 x 16 384 x 128 fp32 78 : 60; 600 x 300 x 256 bf16 27 : 45, 1 000 x 500 x 160 33 : 40, 500 x 1 500 x 192 fp16 41 : 41,
 // 300 x 3 000 x 250 bf16 73 : 60, 4 000 x 400 x 200 67 : 51.
@@ -241,7 +241,7 @@ struct PackArgs {
     f32x4 *row;
     int32_t *lab;
     LossHeader *hdr;
-    bool xvec, cvec, raw, halves;
+    bool vec, raw, halves;
     bool small;          // no launch for the header
     int64_t rinvs, cinvs; // inverse scales
     int xblocks, cblocks, dblocks, xunits, cunits; // workgroups for x, for c; units of the columns' images
@@ -281,10 +281,10 @@ __global__ __launch_bounds__(256) void k_pack_rows(PackArgs a)
     if (b >= 0) {
         const int j = b * 16 + threadIdx.x; // the bias in units of log 2, -inf past the last centroid
         if (threadIdx.x < 16) a.bias2[j] = j < a.k ? (a.bias ? a.bias[j] * LOG2E : 0.f) : -INFINITY;
-        if (a.cinv) pack_rows<T, false, NP, HELD, RAW>(b, (const T *)a.c, a.k, a.d, a.units, nullptr, a.k, a.bias, a.cimg, a.cinv, a.cvec);
+        if (a.cinv) pack_rows<T, false, NP, HELD, RAW>(b, (const T *)a.c, a.k, a.d, a.units, nullptr, a.k, a.bias, a.cimg, a.cinv, a.vec);
         return;
     }
-    pack_rows<T, true, NP, HELD, RAW>(blockIdx.x, (const T *)a.x, a.n, a.d, a.units, a.label, a.k, nullptr, a.ximg, a.rinv, a.xvec);
+    pack_rows<T, true, NP, HELD, RAW>(blockIdx.x, (const T *)a.x, a.n, a.d, a.units, a.label, a.k, nullptr, a.ximg, a.rinv, a.vec);
     if (a.stats) return;
     __syncthreads();
     if (threadIdx.x < 16) row_numbers(a, (int64_t)blockIdx.x * 16 + threadIdx.x, a.rinv[(int64_t)blockIdx.x * 16 + threadIdx.x], 0.f);
@@ -335,13 +335,13 @@ __global__ __launch_bounds__(256) void k_pack_cols(PackArgs a)
     int b = blockIdx.x;
     if (b < a.xblocks) {
         const float inv = a.small ? header_value<256>(a, 0) : a.hdr->xinv;
-        pack_cols<T, XORDER, NP>(b / a.dblocks, b % a.dblocks, (const T *)a.x, a.n, a.d, a.xunits, a.label, a.k, nullptr, a.xcols, inv, a.xvec);
+        pack_cols<T, XORDER, NP>(b / a.dblocks, b % a.dblocks, (const T *)a.x, a.n, a.d, a.xunits, a.label, a.k, nullptr, a.xcols, inv, a.vec);
         return;
     }
     b -= a.xblocks;
     if (b < a.cblocks) {
         const float inv = a.small ? header_value<256>(a, 1) : a.hdr->cinv;
-        pack_cols<T, CORDER, NP>(b / a.dblocks, b % a.dblocks, (const T *)a.c, a.k, a.d, a.cunits, nullptr, a.k, a.bias, a.ccols, inv, a.cvec);
+        pack_cols<T, CORDER, NP>(b / a.dblocks, b % a.dblocks, (const T *)a.c, a.k, a.d, a.cunits, nullptr, a.k, a.bias, a.ccols, inv, a.vec);
         return;
     }
     const int64_t i = (int64_t)(b - a.cblocks) * 256 + threadIdx.x; // (the workgroups cover the padded rows)
@@ -866,7 +866,7 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_grads(GradOut first, GradOut se
 }
 
 // out = factor * sum of the slabs, of both gradients, four values a thread
-// From so many parts on the four waves of a workgroup share those of 256 values (a step of 3 855 x 11 x 657 fp32, 46 parts of dc, 60 -> 52 us)
+// From so many parts on the four waves of a workgroup share those of 256 values (a step of 3 855 x 11 x 657 fp32, 46 parts of dc, 8 us less)
 #define SUM_SHARED 8
 struct SlabSum {
     const float *slabs;
@@ -1150,12 +1150,6 @@ static hipError_t allow_lds(K kern, size_t bytes)
         if (e_ != hipSuccess) return (int)e_;    \
     } while (0)
 
-template <typename T>
-static bool rows_vec(const void *p, int d)
-{
-    return d % 8 == 0 && (uintptr_t)p % 16 == 0;
-}
-
 // The wide form takes the centroids as they lie (ProductRows) where that saves more than it costs: the products are a tenth
 // slower, most where a row is a multiple of 4 KB and all rows of a tile come through the same channel of the L2.  us of a step, these
 // against images: 284 x 50 632 x 1 376 fp16 506 : 580, 1 000 x 30 000 x 1 024 fp16 397 : 427, 4 096 x 32 000 x 2 048 bf16 1 976 : 2 013,
@@ -1164,7 +1158,7 @@ static bool rows_vec(const void *p, int d)
 template <typename T>
 static bool as_they_lie(const LossArgs &a, const LossPlan &p)
 {
-    return sizeof(T) == 2 && !p.narrow && a.n <= LIE_ROWS && rows_vec<T>(a.c, a.d);
+    return sizeof(T) == 2 && !p.narrow && a.n <= LIE_ROWS && a.d % 8 == 0 && (uintptr_t)a.c % 16 == 0;
 }
 
 // The images of rows and centroids, and the rest of what the products need: one launch, two or three backward
@@ -1172,7 +1166,7 @@ template <typename T, int NP>
 static void loss_images(const LossArgs &a, const LossPlan &p, bool backward, hipStream_t st)
 {
     PackArgs g = {a.x, a.c, a.n, a.d, a.k, p.units, a.label, a.bias, a.grad, backward ? a.stats : nullptr, a.scale, p.ximg, p.cimg,
-                  p.xcols, p.ccols, p.rinv, p.cinv, p.gn, p.bias2, p.row, p.lab, p.hdr, rows_vec<T>(a.x, a.d), rows_vec<T>(a.c, a.d), as_they_lie<T>(a, p), __is_same(T, _Float16)};
+                  p.xcols, p.ccols, p.rinv, p.cinv, p.gn, p.bias2, p.row, p.lab, p.hdr, a.d % 8 == 0, as_they_lie<T>(a, p), __is_same(T, _Float16)};
     g.rinvs = p.npad;
     g.cinvs = p.kpad / 16;
     g.small = g.rinvs + g.cinvs <= SMALL_SCALES;

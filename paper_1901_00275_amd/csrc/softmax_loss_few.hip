@@ -18,37 +18,43 @@
 template <typename T>
 struct FewPiece { // what a lane reads of a row at a time: its share of STEP indices
     static constexpr int N = 16 / sizeof(T), STEP = 4 * N;
+    typedef uint32_t At __attribute__((ext_vector_type(N * sizeof(T) / 4), aligned(sizeof(T)))); // 16 bytes at a value's address
     T v[N];
 };
+// How rows are read: WHOLE, a row is a number of pieces; ENDED, its last piece ends where the row does, and what the one before had is
+// made zero; SHORT, a row is less than a piece.  The memory takes 16 bytes at any value's address.  (A step of 3 855 x 11 x 657
+// fp32 52 us value by value, 35 so; 500 x 500 x 500 bf16 by two values 40, 26 so.)
+enum { WHOLE, ENDED, SHORT };
 // Every address is clamped into the row, what lies past its end is made zero afterwards: a branch around a load would wait for it.
 // Where one tile of rows is all there is (THIN), memory bounds it, and what is not there is not asked for (65 536 x 1 024 bf16,
 // one row 27 us; clamped 28, with the other 15 rows 29).
-template <typename T, int ALIGN, bool THIN>
+template <typename T, int FORM, bool THIN>
 __device__ __forceinline__ FewPiece<T> few_piece(const T *row, int i, int d, bool there)
 {
-    if (THIN && ALIGN == 16) {
+    using P = FewPiece<T>;
+    using At = typename P::At;
+    if constexpr (FORM == WHOLE && THIN) {
         u32x4 v = {0, 0, 0, 0};
-        if (there && i < d) v = *(const u32x4 *)(row + i);
-        return __builtin_bit_cast(FewPiece<T>, v);
-    }
-    FewPiece<T> r;
-    if constexpr (ALIGN == 16) {
-        const u32x4 v = *(const u32x4 *)(row + min(i, d - FewPiece<T>::N));
-        *(u32x4 *)r.v = i < d ? v : u32x4{0, 0, 0, 0};
-    } else if constexpr (ALIGN > sizeof(T)) { // two 16-bit values
+        if (there && i < d) v = *(const At *)(row + i);
+        return __builtin_bit_cast(P, v);
+    } else if constexpr (FORM == WHOLE) {
+        const u32x4 v = *(const At *)(row + min(i, d - P::N));
+        return __builtin_bit_cast(P, i < d ? v : u32x4{0, 0, 0, 0});
+    } else if constexpr (FORM == ENDED) {
+        const int at = min(i, d - P::N);
+        P r = __builtin_bit_cast(P, (u32x4) * (const At *)(row + at));
 #pragma unroll
-        for (int e = 0; e < FewPiece<T>::N; e += 2) {
-            const uint32_t v = *(const uint32_t *)(row + min(i + e, d - 2));
-            *(uint32_t *)(r.v + e) = i + e < d ? v : 0u;
-        }
+        for (int e = 0; e < P::N; ++e) r.v[e] = at + e >= i ? r.v[e] : (T)0.f;
+        return r;
     } else {
+        P r;
 #pragma unroll
-        for (int e = 0; e < FewPiece<T>::N; ++e) {
+        for (int e = 0; e < P::N; ++e) {
             const T v = row[min(i + e, d - 1)];
             r.v[e] = i + e < d ? v : (T)0.f;
         }
+        return r;
     }
-    return r;
 }
 __device__ __forceinline__ void few_multiply(const FewPiece<float> &a, const FewPiece<float> &b, f32x4 &acc)
 {
@@ -66,7 +72,7 @@ __device__ __forceinline__ void few_multiply(const FewPiece<bf16_t> &a, const Fe
 }
 
 // The logits' products of centroids m0 .. and rows n0 ..; of S waves the first has them
-template <typename T, int ALIGN, int W, int S, int G, int NT>
+template <typename T, int FORM, int W, int S, int G, int NT>
 __device__ __forceinline__ void few_logits(const FewArgs &a, int m0, int n0, int tile, int slice, f32x4 (&acc)[G][NT])
 {
     constexpr int STEP = FewPiece<T>::STEP, N = FewPiece<T>::N, U = 16 / (G + NT) < 2 ? 2 : 16 / (G + NT);
@@ -85,9 +91,9 @@ __device__ __forceinline__ void few_logits(const FewArgs &a, int m0, int n0, int
 #pragma unroll
         for (int u = 0; u < U; ++u) {
 #pragma unroll
-            for (int i = 0; i < G; ++i) cv[u][i] = few_piece<T, ALIGN, NT == 1>(crow[i], k0 + g * N + u * STEP, a.d, true);
+            for (int i = 0; i < G; ++i) cv[u][i] = few_piece<T, FORM, NT == 1>(crow[i], k0 + g * N + u * STEP, a.d, true);
 #pragma unroll
-            for (int j = 0; j < NT; ++j) xv[u][j] = few_piece<T, ALIGN, NT == 1>(xrow[j], k0 + g * N + u * STEP, a.d, NT > 1 || l < a.n);
+            for (int j = 0; j < NT; ++j) xv[u][j] = few_piece<T, FORM, NT == 1>(xrow[j], k0 + g * N + u * STEP, a.d, NT > 1 || l < a.n);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
@@ -111,13 +117,13 @@ __device__ __forceinline__ void few_logits(const FewArgs &a, int m0, int n0, int
 }
 
 // Forward: maxima and sums of a workgroup's centroids, and the labels' logits
-template <typename T, int ALIGN, int W, int S, int G, int NT>
+template <typename T, int FORM, int W, int S, int G, int NT>
 __global__ __launch_bounds__(W * S * 64) void k_loss_few(FewArgs a)
 {
     const int tid = threadIdx.x, lane = tid & 63, l = lane & 15, g = lane >> 4, wave = (tid >> 6) % W, slice = (tid >> 6) / W;
     const int group = blockIdx.x % a.groups, m0 = (group * W + wave) * 16 * G, n0 = (int)(blockIdx.x / a.groups) * 16 * NT;
     f32x4 acc[G][NT];
-    few_logits<T, ALIGN, W, S, G, NT>(a, m0, n0, wave, slice, acc);
+    few_logits<T, FORM, W, S, G, NT>(a, m0, n0, wave, slice, acc);
     __shared__ float2 s[W][16 * NT];
     if (slice == 0)
 #pragma unroll
@@ -155,13 +161,13 @@ __global__ __launch_bounds__(W * S * 64) void k_loss_few(FewArgs a)
 }
 
 // Backward: G of a tile.  A row that does not count has zeros; a centroid that was taken out has p = 0.
-template <typename T, int ALIGN, int W, int S, int G, int NT>
+template <typename T, int FORM, int W, int S, int G, int NT>
 __global__ __launch_bounds__(W * S * 64) void k_loss_few_g(FewArgs a)
 {
     const int tid = threadIdx.x, lane = tid & 63, l = lane & 15, g = lane >> 4, wave = (tid >> 6) % W, slice = (tid >> 6) / W;
     const int group = blockIdx.x % a.groups, m0 = (group * W + wave) * 16 * G, n0 = (int)(blockIdx.x / a.groups) * 16 * NT;
     f32x4 acc[G][NT];
-    few_logits<T, ALIGN, W, S, G, NT>(a, m0, n0, wave, slice, acc);
+    few_logits<T, FORM, W, S, G, NT>(a, m0, n0, wave, slice, acc);
     if (slice > 0) return;
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
@@ -187,6 +193,29 @@ __global__ __launch_bounds__(W * S * 64) void k_loss_few_g(FewArgs a)
     }
 }
 
+// Four values at any value's address
+template <typename T>
+__device__ __forceinline__ void load4(T (&v)[4], const T *p)
+{
+    typedef std::conditional_t<sizeof(T) == 4, u32x4, u32x2> Word;
+    typedef Word At __attribute__((aligned(sizeof(T))));
+    *(Word *)v = *(const At *)p;
+}
+template <bool VEC, typename T>
+__device__ __forceinline__ void store_dims(T *p, const f32x4 &v, int count)
+{
+    typedef std::conditional_t<sizeof(T) == 4, u32x4, u32x2> Word;
+    typedef Word At __attribute__((aligned(sizeof(T))));
+    const T t[4] = {(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
+    if constexpr (VEC) {
+        *(At *)p = *(const Word *)t;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < count) p[e] = t[e];
+    }
+}
+
 // A gradient's tile of 32 rows x 64 dimensions a wave: sum over q of G's 32 rows and 64 values of the other matrix's row q, in steps of
 // 16 q.  The order of the 16 within a step is free as long as both operands have it, and which rows and dimensions a tile's
 // lanes stand for is, too: a lane reads four neighbouring dimensions (and, for dx, four neighbouring q of G) at once.
@@ -195,7 +224,8 @@ __device__ __forceinline__ void few_grad(const FewArgs &a, const FewSide &s, int
 {
     const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int tiles = s.rtiles * s.dtiles, part = b / tiles, tile = b - part * tiles, dt = tile / s.rtiles;
-    const int r0 = (tile - dt * s.rtiles) * 32, dim = (s.share ? dt : dt * 4 + wave) * 64 + 4 * l;
+    const int r0 = (tile - dt * s.rtiles) * 32, dim0 = (s.share ? dt : dt * 4 + wave) * 64 + 4 * l;
+    const int dim = VEC ? min(dim0, a.d - 4) : dim0; // (the last four end where the row does, some of them taken twice)
     const int steps = (s.sum + 15) / 16, p1 = min(steps, (part + 1) * s.per), by = s.share ? 4 : 1;
     const T *rows = (const T *)(CENT ? a.x : a.c);
     const float *bias = a.bias ? a.bias : a.G; // (read either way: a branch around a load would wait for it)
@@ -223,10 +253,8 @@ __device__ __forceinline__ void few_grad(const FewArgs &a, const FewSide &s, int
                 keep &= in;
                 const T *row = rows + (int64_t)q * a.d; // (dimensions past the end are not stored)
                 T v[4];
-                if constexpr (VEC && sizeof(T) == 4)
-                    *(f32x4 *)v = *(const f32x4 *)(row + min(dim, a.d - 4));
-                else if constexpr (VEC)
-                    *(u32x2 *)v = *(const u32x2 *)(row + min(dim, a.d - 4));
+                if constexpr (VEC)
+                    load4(v, row + dim);
                 else
 #pragma unroll
                     for (int u = 0; u < 4; ++u) v[u] = row[min(dim + u, a.d - 1)];
@@ -288,12 +316,11 @@ __device__ __forceinline__ void few_grad(const FewArgs &a, const FewSide &s, int
                 for (int u = 0; u < 4; ++u) acc[t][u] += sum[w][t * 4 + u][lane];
             }
     }
-    if (CENT && a.db && dim == 4 * l && g == 0)
+    if (CENT && a.db && dim0 == 4 * l && g == 0)
 #pragma unroll
         for (int t = 0; t < 2; ++t)
             if (r0 + 2 * l + t < s.rows) a.db[(int64_t)part * a.kp + r0 + 2 * l + t] = db[t];
-    if (!s.out || dim >= a.d) return;
-    // (VEC: d is a multiple of 4 and the outputs lie on four values)
+    if (!s.out || dim0 >= a.d) return;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -302,9 +329,9 @@ __device__ __forceinline__ void few_grad(const FewArgs &a, const FewSide &s, int
             if (row >= s.rows) continue;
             const f32x4 v = {acc[t][0][r], acc[t][1][r], acc[t][2][r], acc[t][3][r]};
             if (s.slab)
-                store4((float *)s.out + ((int64_t)part * s.rows + row) * a.d + dim, v, VEC ? 4 : a.d - dim, VEC);
+                store_dims<VEC>((float *)s.out + ((int64_t)part * s.rows + row) * a.d + dim, v, a.d - dim);
             else
-                store4((T *)s.out + (int64_t)row * a.d + dim, v * a.scale, VEC ? 4 : a.d - dim, VEC);
+                store_dims<VEC>((T *)s.out + (int64_t)row * a.d + dim, v * a.scale, a.d - dim);
         }
 }
 
@@ -346,49 +373,48 @@ static void few(int dtype, const FewArgs &args, bool backward, hipStream_t st)
     FewArgs a = args;
     const FewShape f = few_shape(dtype, a.n, a.d, a.k);
     a.groups = f.groups;
-    auto go = [&](auto ALIGN, auto W, auto S, auto G, auto NT) {
+    auto go = [&](auto FORM, auto W, auto S, auto G, auto NT) {
         constexpr int R = 16 * decltype(NT)::value, WS = decltype(W)::value * decltype(S)::value;
         const dim3 grid((unsigned)(a.groups * ((a.n + R - 1) / R)));
         if (backward)
-            hipLaunchKernelGGL((k_loss_few_g<T, decltype(ALIGN)::value, decltype(W)::value, decltype(S)::value, decltype(G)::value, decltype(NT)::value>),
+            hipLaunchKernelGGL((k_loss_few_g<T, decltype(FORM)::value, decltype(W)::value, decltype(S)::value, decltype(G)::value, decltype(NT)::value>),
                                grid, dim3(WS * 64), 0, st, a);
         else
-            hipLaunchKernelGGL((k_loss_few<T, decltype(ALIGN)::value, decltype(W)::value, decltype(S)::value, decltype(G)::value, decltype(NT)::value>),
+            hipLaunchKernelGGL((k_loss_few<T, decltype(FORM)::value, decltype(W)::value, decltype(S)::value, decltype(G)::value, decltype(NT)::value>),
                                grid, dim3(WS * 64), 0, st, a);
     };
-    auto rows = [&](auto ALIGN, auto W, auto S, auto G) {
+    auto rows = [&](auto FORM, auto W, auto S, auto G) {
         // tiles of 64 rows, of fewer where compute units would go without a workgroup (a step of 3 855 x 11 x 657 fp32 100 -> 60 us,
         // 64 x 1 000 x 1 024 fp32 26 -> 14; asking for 700 workgroups 535 x 975 x 1 248 fp32 44 -> 53)
         int tiles = 4;
         while (tiles > 1 && (a.n <= 8 * tiles || (int64_t)a.groups * ((a.n + 16 * tiles - 1) / (16 * tiles)) < 256)) tiles /= 2;
         if (tiles == 1)
-            go(ALIGN, W, S, G, std::integral_constant<int, 1>{});
+            go(FORM, W, S, G, std::integral_constant<int, 1>{});
         else if (tiles == 2)
-            go(ALIGN, W, S, G, std::integral_constant<int, 2>{});
+            go(FORM, W, S, G, std::integral_constant<int, 2>{});
         else
-            go(ALIGN, W, S, G, std::integral_constant<int, 4>{});
+            go(FORM, W, S, G, std::integral_constant<int, 4>{});
     };
     const std::integral_constant<int, 1> one;
     const std::integral_constant<int, 2> two;
     const std::integral_constant<int, 4> four;
     const std::integral_constant<int, 8> eight;
-    auto cells = [&](auto ALIGN) {
+    auto cells = [&](auto FORM) {
         if (f.shared)
-            rows(ALIGN, two, four, one);
+            rows(FORM, two, four, one);
         else if (f.small)
-            rows(ALIGN, two, one, one);
+            rows(FORM, two, one, one);
         else if (f.wide)
-            rows(ALIGN, eight, one, two);
+            rows(FORM, eight, one, two);
         else
-            rows(ALIGN, eight, one, one);
+            rows(FORM, eight, one, one);
     };
-    const uint64_t all = a.d * sizeof(T) | (uintptr_t)a.x | (uintptr_t)a.c; // (its lowest bit: how rows lie)
-    if (all % 16 == 0)
-        cells(std::integral_constant<int, 16>{});
-    else if (all % 4 == 0)
-        cells(std::integral_constant<int, 4>{});
+    if (a.d % FewPiece<T>::N == 0)
+        cells(std::integral_constant<int, WHOLE>{});
+    else if (a.d > FewPiece<T>::N)
+        cells(std::integral_constant<int, ENDED>{});
     else
-        cells(std::integral_constant<int, sizeof(T)>{});
+        cells(std::integral_constant<int, SHORT>{});
 }
 void launch_loss_few(int dtype, const FewArgs &a, bool backward, hipStream_t st)
 {
@@ -436,9 +462,7 @@ template <typename T>
 static void few_grads(const FewArgs &a, hipStream_t st)
 {
     const dim3 grid((unsigned)(a.dx.blocks + a.dc.blocks));
-    // (slabs lie on 16 bytes)
-    const uintptr_t all = (uintptr_t)a.x | (uintptr_t)a.c | (a.dx.slab ? 0 : (uintptr_t)a.dx.out) | (a.dc.slab ? 0 : (uintptr_t)a.dc.out);
-    if (a.d % 4 == 0 && all % (4 * sizeof(T)) == 0)
+    if (a.d >= 4)
         hipLaunchKernelGGL((k_loss_few_grads<T, true>), grid, dim3(256), 0, st, a);
     else
         hipLaunchKernelGGL((k_loss_few_grads<T, false>), grid, dim3(256), 0, st, a);

@@ -79,6 +79,17 @@ def test_large(vlq):
     check(grads, outs, norm, 3.0)
 
 
+@pytest.mark.parametrize("t", [F32, F16, BF16])
+def test_unaligned(vlq, t):
+    g = torch.Generator().manual_seed(9)
+    for off in (1, 2, 3, 5):
+        grads = [torch.randn(c + off, generator=g).to(t).to(DEV)[off:] for c in (1, 6, 20_001, 300_007)]
+        outs = [torch.full((v.numel() + off - 1,), 7.0, dtype=t, device=DEV)[off - 1:] for v in grads]
+        norm = torch.empty(1, device=DEV)
+        vlq.vlq_clip_grads(grads, 0.5, outs, norm, torch.empty(vlq.vlq_clip_grads_workspace(grads), dtype=torch.uint8, device=DEV))
+        check(grads, outs, norm, 0.5)
+
+
 def test_larger_than_the_cache(vlq):
     g = torch.Generator(device=DEV).manual_seed(2)
     grads = [torch.randn(c, generator=g, device=DEV).to(t) for c, t in ((90_000_001, BF16), (30_000_007, F32), (50_000_003, F16))]
