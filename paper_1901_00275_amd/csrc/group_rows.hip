@@ -7,7 +7,8 @@
 // What bounds it are launches of 5 to 11 us, each some waits for memory one behind the other: 640 000 pairs and 65 536 cells
 // (two digits) 51 us in seven launches, 13 MB of pairs and places.  Up to SMALL_PAIRS pairs of one digit take one launch.
 // The rest moves memory: 16 bytes at a time, several rows' loads under way.  640 000 rows of 384 bytes
-// gathered 41 us (6.0 TB/s written), 16 384 rows of 8 x 4 KB combined 137 us (4.3 TB/s), the gradient of 5 003 x 6 x 2 KB 26 us (5.0).
+// gathered 41 us (6.0 TB/s written), 16 384 rows of 8 x 4 KB combined 109 us (5.4 TB/s; with a branch around each load
+// 136), the gradient of 5 003 x 6 x 2 KB 26 us (5.0).
 #include "learn.h"
 
 #include <type_traits>
@@ -485,7 +486,7 @@ int launch_group_rows(const int32_t *cell, int64_t pairs, int cells, int64_t *of
 // A piece of a row: 16 bytes, less where a row has fewer.  The memory takes them at any value's address, so rows of all sizes and
 // alignments go this way; the last piece of a row ends where the row does and overlaps the one before it, whose values it
 // writes again.  WHOLE: all rows lie on 16 bytes; they are stored past the caches, which others would need to put their lines
-// together.  (5 000 x 8 rows of 2 050 bytes combined: 61 us value by value, 26 so.)
+// together.  (5 000 x 8 rows of 2 050 bytes combined: 61 us value by value, 17 so.)
 template <typename T, int BYTES, bool WHOLE>
 struct Piece {
     static constexpr int N = BYTES / (int)sizeof(T);
@@ -551,7 +552,7 @@ __global__ __launch_bounds__(ROW_NT) void k_gather_rows(RowsArgs a, const T *__r
 }
 
 // out[i] = sum over the row's choices of weight y[place], in their order, in fp32
-template <typename T, int BYTES, bool WHOLE>
+template <typename T, int BYTES, bool WHOLE, int U>
 __global__ __launch_bounds__(ROW_NT) void k_combine_rows(RowsArgs a, const T *__restrict__ y, T *__restrict__ out)
 {
     using P = Piece<T, BYTES, WHOLE>;
@@ -560,26 +561,28 @@ __global__ __launch_bounds__(ROW_NT) void k_combine_rows(RowsArgs a, const T *__
     for (uint32_t i = threadIdx.x; i < pieces; i += ROW_NT) {
         const uint32_t r = i / a.per, at = P::at(i - r * a.per, a.d);
         const int32_t *pl = a.index + (r0 + r) * a.w;
-        const float *wt = a.weight ? a.weight + (r0 + r) * a.w : nullptr;
+        const float *wt = a.weight ? a.weight + (r0 + r) * a.w : (const float *)pl; // (read either way: a branch around a load would wait for it)
         float s[P::N] = {};
-        for (int q0 = 0; q0 < a.w; q0 += 8) { // (eight rows' loads under way)
-            P v[8];
-            float f[8];
+        for (int q0 = 0; q0 < a.w; q0 += U) { // (so many rows' loads under way)
+            P v[U];
+            float f[U];
+            int32_t p[U];
 #pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                f[q] = 0.f;
-                const int32_t p = q0 + q < a.w ? pl[q0 + q] : -1;
-                const bool in = p >= 0 && p < places;
-                v[q] = load_piece<T, BYTES, WHOLE>(y + (in ? (int64_t)p * a.d : 0) + at);
-                if (in) f[q] = wt ? wt[q0 + q] : 1.f;
-                if (!in)
-#pragma unroll
-                    for (int e = 0; e < P::N; ++e) v[q].v[e] = (T)0.f;
+            for (int q = 0; q < U; ++q) {
+                p[q] = pl[min(q0 + q, a.w - 1)];
+                f[q] = wt[min(q0 + q, a.w - 1)];
             }
 #pragma unroll
-            for (int q = 0; q < 8; ++q)
+            for (int q = 0; q < U; ++q) {
+                const bool in = q0 + q < a.w && (uint32_t)p[q] < (uint64_t)places;
+                v[q] = load_piece<T, BYTES, WHOLE>(y + (in ? (int64_t)p[q] * a.d : 0) + at);
+                if (!a.weight) f[q] = 1.f;
+                if (!in) p[q] = -1;
+            }
 #pragma unroll
-                for (int e = 0; e < P::N; ++e) s[e] = fmaf(f[q], (float)v[q].v[e], s[e]);
+            for (int q = 0; q < U; ++q)
+#pragma unroll
+                for (int e = 0; e < P::N; ++e) s[e] = p[q] < 0 ? s[e] : fmaf(f[q], (float)v[q].v[e], s[e]);
         }
         P o;
 #pragma unroll
@@ -600,22 +603,29 @@ __global__ __launch_bounds__(ROW_NT) void k_combine_back(RowsArgs a, const T *__
     const int64_t places = a.n * a.w, r = id / eights;
     if (r >= a.n) return;
     const int q0 = (int)(id % eights) * 8;
+    const float *weight = a.weight ? a.weight : (const float *)a.index; // (read either way: a branch around a load would wait for it)
+    int32_t at[8];
     int64_t p[8];
     float f[8], dot[8];
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
-        const int32_t at = q0 + q < a.w ? a.index[r * a.w + q0 + q] : -1;
-        p[q] = at >= 0 && at < places ? at : -1;
-        f[q] = p[q] < 0 ? 0.f : a.weight ? a.weight[r * a.w + q0 + q] : 1.f;
+        const int64_t i = r * a.w + min(q0 + q, a.w - 1);
+        at[q] = a.index[i];
+        f[q] = weight[i];
         dot[q] = 0.f;
     }
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        p[q] = q0 + q < a.w && (uint32_t)at[q] < (uint64_t)places ? at[q] : -1;
+        if (!a.weight) f[q] = 1.f;
+    }
     for (uint32_t c = lane; c < a.per; c += L) {
-        const uint32_t at = P::at(c, a.d), again = c * P::N - at; // (values that the piece before had)
-        const P g = load_piece<T, BYTES, WHOLE>(dout + r * a.d + at);
+        const uint32_t c0 = P::at(c, a.d), again = c * P::N - c0; // (values that the piece before had)
+        const P g = load_piece<T, BYTES, WHOLE>(dout + r * a.d + c0);
         P v[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q)
-            if (dweight && p[q] >= 0) v[q] = load_piece<T, BYTES, WHOLE>(y + p[q] * a.d + at);
+            if (dweight) v[q] = load_piece<T, BYTES, WHOLE>(y + max(p[q], (int64_t)0) * a.d + c0);
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
             if (p[q] < 0) continue;
@@ -625,7 +635,7 @@ __global__ __launch_bounds__(ROW_NT) void k_combine_back(RowsArgs a, const T *__
                 o.v[e] = (T)(f[q] * (float)g.v[e]);
                 if (dweight && e >= (int)again) dot[q] = fmaf((float)g.v[e], (float)v[q].v[e], dot[q]);
             }
-            if (dy) store_piece<T, BYTES, WHOLE>(dy + p[q] * a.d + at, o);
+            if (dy) store_piece<T, BYTES, WHOLE>(dy + p[q] * a.d + c0, o);
         }
     }
     if (!dweight) return;
@@ -691,9 +701,8 @@ static int combine(const RowsArgs &args, const T *y, T *out, hipStream_t st)
         constexpr bool W = decltype(WHOLE)::value;
         a.per = (a.d + Piece<T, V, W>::N - 1) / Piece<T, V, W>::N;
         a.rows = rows_of(a.per, ROW_NT);
-        in_launches(a, (a.n + a.rows - 1) / a.rows, [&](dim3 groups) {
-            hipLaunchKernelGGL((k_combine_rows<T, V, W>), groups, dim3(ROW_NT), 0, st, a, y, out);
-        });
+        const auto kern = a.w > 8 ? k_combine_rows<T, V, W, 16> : k_combine_rows<T, V, W, 8>;
+        in_launches(a, (a.n + a.rows - 1) / a.rows, [&](dim3 groups) { hipLaunchKernelGGL(kern, groups, dim3(ROW_NT), 0, st, a, y, out); });
     };
     by_pieces<T>(a.d, y, out, nullptr, go);
     return (int)hipGetLastError();
