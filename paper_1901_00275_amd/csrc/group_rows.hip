@@ -132,16 +132,18 @@ __device__ __forceinline__ void block_scan(uint32_t *v, int bins, uint32_t *wsum
 // The pairs of a wave (i0 .. i0 + count) to their places, HELD at a time: their keys, and where they have moved already the
 // pairs themselves, are asked for together.  at[digit] is the next place of a digit, kept up by the wave alone.
 #define HELD 8
-__device__ __forceinline__ void hold(const SortPass &a, int64_t i0, int count, int lane, uint32_t (&key)[HELD], uint32_t (&pair)[HELD])
+__device__ __forceinline__ void hold(const SortPass &a, int64_t i0, int lane, uint32_t (&key)[HELD], uint32_t (&pair)[HELD])
 {
 #pragma unroll
-    for (int u = 0; u < HELD; ++u)
-        if (u * 64 + lane < count) {
-            const int64_t i = i0 + u * 64 + lane;
-            const uint2 v = a.cell ? make_uint2(key_at(a, i), (uint32_t)i) : a.moved[i];
-            key[u] = v.x;
-            pair[u] = v.y;
-        }
+    for (int u = 0; u < HELD; ++u) { // (no branch around a load, it would wait for it)
+        const int64_t i = min(i0 + u * 64 + lane, a.pairs - 1);
+        const uint2 v = a.cell ? make_uint2((uint32_t)a.cell[i], (uint32_t)i) : a.moved[i];
+        key[u] = v.x;
+        pair[u] = v.y;
+    }
+    if (a.cell)
+#pragma unroll
+        for (int u = 0; u < HELD; ++u) key[u] = min(key[u], (uint32_t)a.cells);
 }
 __device__ __forceinline__ void place_held(const SortPass &a, uint32_t *at, int64_t i0, int count, int lane, const uint32_t (&key)[HELD], const uint32_t (&pair)[HELD])
 {
@@ -172,7 +174,7 @@ __device__ __forceinline__ void place_pairs(const SortPass &a, uint32_t *at, int
 {
     uint32_t key[HELD], pair[HELD];
     for (int i = 0; i < count; i += HELD * 64) {
-        hold(a, i0 + i, count - i, lane, key, pair);
+        hold(a, i0 + i, lane, key, pair);
         place_held(a, at, i0 + i, count - i, lane, key, pair);
     }
 }
@@ -182,10 +184,7 @@ __global__ __launch_bounds__(GNT) void k_group_place(SortPass a)
     __shared__ uint32_t first[BINS], at[GWAVES][BINS], wsum[GWAVES];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, bins = 1 << a.bits;
     uint32_t key[HELD], pair[HELD]; // the wave's first pairs, asked for before all else
-    {
-        const int64_t w0 = (int64_t)blockIdx.x * a.tile + wave * (a.tile / GWAVES);
-        hold(a, w0, (int)max((int64_t)0, min((int64_t)(a.tile / GWAVES), a.pairs - w0)), lane, key, pair);
-    }
+    hold(a, (int64_t)blockIdx.x * a.tile + wave * (a.tile / GWAVES), lane, key, pair);
     uint32_t before[BINS / GNT]; // of each digit, in the tiles before this one
 #pragma unroll
     for (int i = 0; i < BINS / GNT; ++i) {

@@ -681,13 +681,19 @@ __global__ __launch_bounds__(256) void k_loss_merge(const float2 *part, int part
     constexpr int T = 256 / R;
     const int r = threadIdx.x % R, t = threadIdx.x / R;
     const int64_t i = (int64_t)blockIdx.x * R + r;
+    const int64_t in = min(i, n - 1);
+    const int label = lab[in];
+    const float own = mine[in];
     float2 v[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) v[u] = make_float2(-INFINITY, 0.f);
-    for (int p = t; p < parts; p += 4 * T)
+    for (int p = t; p < parts; p += 4 * T) { // (no branch around a load, it would wait for it)
+        float2 w[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-            if (p + u * T < parts && i < npad) v[u] = join(v[u], part[(int64_t)(p + u * T) * npad + i]);
+        for (int u = 0; u < 4; ++u) w[u] = part[(int64_t)min(p + u * T, parts - 1) * npad + in];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] = join(v[u], p + u * T < parts ? w[u] : make_float2(-INFINITY, 0.f));
+    }
     v[0] = join(join(v[0], v[1]), join(v[2], v[3]));
 #pragma unroll
     for (int o = R; o < 64; o *= 2) v[0] = join(v[0], make_float2(__shfl_xor(v[0].x, o, 64), __shfl_xor(v[0].y, o, 64)));
@@ -699,7 +705,7 @@ __global__ __launch_bounds__(256) void k_loss_merge(const float2 *part, int part
     const float m = v[0].x, z = v[0].y;
     stats[2 * i] = m;
     stats[2 * i + 1] = z;
-    if (loss) loss[i] = (uint32_t)lab[i] >= (uint32_t)k ? 0.f : m == -INFINITY ? INFINITY : LN2 * (m - mine[i]) + logf(z);
+    if (loss) loss[i] = (uint32_t)label >= (uint32_t)k ? 0.f : m == -INFINITY ? INFINITY : LN2 * (m - own) + logf(z);
 }
 
 // Backward: P of a tile, as images in both orders, and the sums over a wave's 64 rows for the bias.

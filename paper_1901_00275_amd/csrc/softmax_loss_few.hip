@@ -116,6 +116,21 @@ __device__ __forceinline__ void few_logits(const FewArgs &a, int m0, int n0, int
     }
 }
 
+// The bias of a lane's centroids, asked for before the products
+template <int G>
+__device__ __forceinline__ void few_bias(const FewArgs &a, int m0, int g, float (&b)[G][4])
+{
+#pragma unroll
+    for (int i = 0; i < G; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) b[i][r] = 0.f;
+    if (a.bias)
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) b[i][r] = a.bias[min(m0 + 16 * i + 4 * g + r, a.k - 1)];
+}
+
 // Forward: maxima and sums of a workgroup's centroids, and the labels' logits
 template <typename T, int FORM, int W, int S, int G, int NT>
 __global__ __launch_bounds__(W * S * 64) void k_loss_few(FewArgs a)
@@ -123,19 +138,24 @@ __global__ __launch_bounds__(W * S * 64) void k_loss_few(FewArgs a)
     const int tid = threadIdx.x, lane = tid & 63, l = lane & 15, g = lane >> 4, wave = (tid >> 6) % W, slice = (tid >> 6) / W;
     const int group = blockIdx.x % a.groups, m0 = (group * W + wave) * 16 * G, n0 = (int)(blockIdx.x / a.groups) * 16 * NT;
     f32x4 acc[G][NT];
+    float bias[G][4];
+    int label[NT];
+    few_bias<G>(a, m0, g, bias);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) label[j] = a.label[min(n0 + 16 * j + l, a.n - 1)];
     few_logits<T, FORM, W, S, G, NT>(a, m0, n0, wave, slice, acc);
     __shared__ float2 s[W][16 * NT];
     if (slice == 0)
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
-        const int n = n0 + 16 * j + l, lab = n < a.n ? a.label[n] : -1;
+        const int n = n0 + 16 * j + l, lab = n < a.n ? label[j] : -1;
         float m = -INFINITY, z = 0.f;
 #pragma unroll
         for (int i = 0; i < G; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int c = m0 + 16 * i + 4 * g + r;
-                const float b = c >= a.k ? -INFINITY : a.bias ? a.bias[c] * LOG2E : 0.f;
+                const float b = c >= a.k ? -INFINITY : bias[i][r] * LOG2E;
                 const float v = b == -INFINITY ? -INFINITY : fmaf(acc[i][j][r], a.scale2, b);
                 if (c == lab && c < a.k) a.mine[n] = v;
                 m = fmaxf(m, v);
@@ -167,14 +187,25 @@ __global__ __launch_bounds__(W * S * 64) void k_loss_few_g(FewArgs a)
     const int tid = threadIdx.x, lane = tid & 63, l = lane & 15, g = lane >> 4, wave = (tid >> 6) % W, slice = (tid >> 6) / W;
     const int group = blockIdx.x % a.groups, m0 = (group * W + wave) * 16 * G, n0 = (int)(blockIdx.x / a.groups) * 16 * NT;
     f32x4 acc[G][NT];
+    float bias[G][4], grad[NT];
+    float2 stats[NT];
+    int label[NT];
+    few_bias<G>(a, m0, g, bias);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        const int64_t n = min(n0 + 16 * j + l, a.n - 1);
+        label[j] = a.label[n];
+        stats[j].x = a.stats[2 * n];
+        stats[j].y = a.stats[2 * n + 1];
+        grad[j] = a.grad[n];
+    }
     few_logits<T, FORM, W, S, G, NT>(a, m0, n0, wave, slice, acc);
     if (slice > 0) return;
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
-        const int n = n0 + 16 * j + l;
+        const int n = n0 + 16 * j + l, lab = label[j];
         if (n >= a.n) continue;
-        const int lab = a.label[n];
-        const float m = a.stats[2 * (int64_t)n], z = a.stats[2 * (int64_t)n + 1], gn = a.grad[n];
+        const float m = stats[j].x, z = stats[j].y, gn = grad[j];
         const bool ok = (uint32_t)lab < (uint32_t)a.k && m != -INFINITY;
 #pragma unroll
         for (int i = 0; i < G; ++i) {
@@ -184,7 +215,7 @@ __global__ __launch_bounds__(W * S * 64) void k_loss_few_g(FewArgs a)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int c = c0 + r;
-                const float b = c >= a.k ? -INFINITY : a.bias ? a.bias[c] * LOG2E : 0.f;
+                const float b = c >= a.k ? -INFINITY : bias[i][r] * LOG2E;
                 const float p = b == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], a.scale2, b) - m) / z;
                 v[r] = !ok || c >= a.k ? 0.f : gn * (c == lab ? p - 1.f : p);
             }
