@@ -99,10 +99,18 @@ __device__ __forceinline__ void narrow(const NarrowArgs &a, const NarrowSide &s,
         for (int j = 0; j < QB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
     copy_tile(t0);
+    float cinv[2], next[2]; // inverse scales of this tile and the next one
+#pragma unroll
+    for (int i = 0; i < 2; ++i) next[i] = CENT ? 0.f : a.cinv[t0 * 2 + i];
     for (int t = t0; t < t1; ++t) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads(); // (this tile has arrived, and nobody reads the other buffer any more)
         if (t + 1 < t1) copy_tile(t + 1);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            cinv[i] = next[i];
+            if (!CENT) next[i] = a.cinv[min(t + 1, t1 - 1) * 2 + i];
+        }
         const u32x4 *st = lds + (t & 1) * STAGE;
         const float *num = (const float *)(st + CHUNKS * 64);
         f32x4 S[2][QB];
@@ -140,7 +148,7 @@ __device__ __forceinline__ void narrow(const NarrowArgs &a, const NarrowSide &s,
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const f32x4 b2 = *(const f32x4 *)(num + 16 * i + 4 * g);
-                const float ci = a.cinv[t * 2 + i];
+                const float ci = cinv[i];
 #pragma unroll
                 for (int j = 0; j < QB; ++j) {
                     const float fj = f[j] * ci;
@@ -190,7 +198,7 @@ __device__ __forceinline__ void narrow(const NarrowArgs &a, const NarrowSide &s,
                         S[i][j][r] = __builtin_amdgcn_exp2f(fmaf(S[i][j][r], row[r][0] * f[j], m[j] - row[r][1])) * row[r][3];
             } else {
                 const f32x4 b2 = *(const f32x4 *)(num + 16 * i + 4 * g);
-                const float ci = a.cinv[t * 2 + i];
+                const float ci = cinv[i];
 #pragma unroll
                 for (int j = 0; j < QB; ++j) {
                     const float fj = f[j] * ci;
