@@ -41,7 +41,7 @@
 #define NARROW_DIM 128
 #define NARROW_DIM_16 256
 #define NARROW_GROUPS 1024   // its workgroups that run at a time: four a compute unit forward, half as many backward
-#define NARROW_LEAST 8       // tiles of 32 rows that a workgroup of it takes at least (forward half as many)
+#define NARROW_LEAST 4       // tiles of 32 rows that a workgroup of it takes at least (forward half as many)
 // Where little is done with each centroid, rows and centroids are taken as they lie (softmax_loss_few.hip): rewriting them first,
 // and tiles that leave most of the chip idle, cost more.  Measured in us, these against the others.
 // Forward: 1 000 x 1 000 x 1 000 bf16 20 : 38, 8 000 x 120 x 500 fp32 27 : 54, 8 000 x 120 x 1 000 bf16 25 : 45, 535 x 975 x 1 248
@@ -1003,7 +1003,7 @@ static int narrow_parts(int64_t tiles, int64_t per, int64_t out_bytes, int *tile
     return (int)((tiles + each - 1) / each);
 }
 
-// Tiles of a workgroup, so that all of them fill the chip's `slots` a whole number of times (one to three, whatever the sums over parts
+// Tiles of a workgroup, so that all of them fill the chip's `slots` a whole number of times (a half to three, whatever the sums over parts
 // and the starts of more workgroups leave as the shortest): xq and cq workgroups side by side, xt and ct tiles to go through,
 // x_bytes and c_bytes of a part's sums (0: none), us of a tile.  (Always two rounds, whatever was left for a
 // third: a step of 2 710 x 9 867 x 192 fp16 131 us, 107 so; 300 x 32 000 x 256 bf16 125 and 100, 8 192 x 32 000 x 256 703 and 648.)
@@ -1011,18 +1011,20 @@ static int64_t narrow_per(int64_t xq, int64_t xt, int64_t cq, int64_t ct, int64_
 {
     int64_t best = least;
     double best_us = 1e30;
-    for (int rounds = 1; rounds <= 3; ++rounds) {
-        int64_t per = (xq * xt + cq * ct) / (slots * rounds);
+    for (int halves : {1, 2, 4, 6}) { // (half a round: a workgroup has a compute unit for itself, and takes 0.8 of the time)
+        const int64_t most = slots * halves / 2;
+        int64_t per = (xq * xt + cq * ct) / most;
         if (per < least) per = least;
         int64_t xs, cs;
         for (;; per += 1 + per / 16) {
             xs = (xt + per - 1) / per;
             cs = cq ? (ct + per - 1) / per : 0;
-            if (xq * xs + cq * cs <= slots * rounds || (xs == 1 && cs <= 1)) break;
+            if (xq * xs + cq * cs <= most || (xs == 1 && cs <= 1)) break;
         }
-        const int64_t longest = xs == 1 && cs <= 1 ? (xt > ct ? xt : ct) : per, turns = (xq * xs + cq * cs + slots - 1) / slots;
+        const int64_t longest = xs == 1 && cs <= 1 ? (xt > ct ? xt : ct) : per, groups = xq * xs + cq * cs;
         const double sums = (xs > 1 ? xs * x_bytes : 0.) + (cs > 1 ? cs * c_bytes : 0.);
-        const double t = turns * (longest + 2) * us + sums / 2.2e6; // (written and read at 4.4 TB/s)
+        const double turns = 2 * groups <= slots ? 0.8 : (double)((groups + slots - 1) / slots);
+        const double t = turns * (longest + 2) * us + sums / 3.3e6; // (written and read, mostly in the last-level cache)
         if (t < best_us) {
             best_us = t;
             best = per;
