@@ -13,7 +13,7 @@ SOURCES = ["api.hip", "coarse.hip", "coarse_bf16.hip", "coarse_half.hip", "train
            "softmax_loss.hip", "softmax_loss_narrow.hip", "softmax_loss_few.hip", "group_rows.hip", "clip_grads.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
-    # packed fp32 instructions are not to be generated on the test machines
+    # packed fp32 instructions are not to be generated: some of their forms have given wrong results on this hardware
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-command-line-argument",
 ]

@@ -73,6 +73,28 @@ def test_group_extremes(vlq, cells):
             assert off[cells].item() == (7 * n if 0 <= c < cells else 0)
 
 
+@pytest.mark.parametrize("n,w,cells", [(5, 3, 4), (700, 3, 2047), (1000, 4, 70000), (20000, 3, 300), (9000, 5, 70000), (3000, 3, 1 << 24)])
+def test_nothing_is_written_past_the_buffers(vlq, n, w, cells):
+    behind = lambda count, dtype: torch.full((count + 500,), 7, dtype=dtype, device=DEV)  # noqa: E731
+    g = torch.Generator().manual_seed(n)
+    cell = torch.randint(-1, cells, (n, w), generator=g, dtype=torch.int32).to(DEV)
+    size = vlq.vlq_group_rows_workspace(n, w, cells)
+    off, place, source, ws = behind(cells + 1, torch.int64), behind(n * w, torch.int32), behind(n * w, torch.int32), behind(size, torch.uint8)
+    vlq.vlq_group_rows(cell, n, w, cells, off, place, source, ws)
+    for buffer, count in ((off, cells + 1), (place, n * w), (source, n * w), (ws, size)):
+        assert (buffer[count:] == 7).all()
+    for got, want in zip((off[:cells + 1], place[:n * w].view(n, w), source[:n * w]), plain(cell, cells)):
+        assert np.array_equal(got.cpu().numpy(), want)
+    for t, d in ((F32, 3), (BF16, 13), (F16, 1)):
+        x, y, out = torch.randn(n, d, generator=g).to(t).to(DEV), behind(n * w * d, t), behind(n * d, t)
+        dy, dweight = behind(n * w * d, t), behind(n * w, F32)
+        vlq.vlq_gather_rows(x, n, w, d, source, y)
+        vlq.vlq_combine_rows(y, n, w, d, place, None, out)
+        vlq.vlq_combine_rows_backward(x, y, n, w, d, place, None, dy, dweight)
+        for buffer, count in ((y, n * w * d), (out, n * d), (dy, n * w * d), (dweight, n * w)):
+            assert (buffer[count:] == 7).all()
+
+
 def test_group_many_pairs(vlq):
     # tiles of the largest size
     g = torch.Generator(device=DEV).manual_seed(3)

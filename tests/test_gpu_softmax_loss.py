@@ -220,6 +220,22 @@ def test_against_differences(vlq):
         assert abs((got[name].double() * v).sum().item() - diff.item()) <= tol, name
 
 
+@pytest.mark.parametrize("t", [F32, BF16])
+@pytest.mark.parametrize("n,d,k", [(3, 5, 7), (33, 77, 3000), (1100, 201, 77), (300, 65, 3001), (1030, 160, 1601), (1030, 301, 1601), (8300, 130, 9001)])
+def test_nothing_is_written_past_the_buffers(vlq, t, n, d, k):
+    x, c, bias, label, grad = problem(t, n, d, k)
+    behind = lambda count, dtype: torch.full((count + 1000,), 7, dtype=dtype, device=DEV)  # noqa: E731
+    loss, stats, dx, dc, db = behind(n, F32), behind(2 * n, F32), behind(n * d, t), behind(k * d, t), behind(k, F32)
+    sizes = [vlq.vlq_softmax_loss_workspace(t, n, d, k, b) for b in (0, 1)]
+    ws = [behind(s, torch.uint8) for s in sizes]
+    vlq.vlq_softmax_loss(x, n, d, c, k, bias, 1.0, label, loss, stats, ws[0])
+    vlq.vlq_softmax_loss_backward(x, n, d, c, k, bias, 1.0, label, stats, grad, dx, dc, db, ws[1])
+    for buffer, count in ((loss, n), (stats, 2 * n), (dx, n * d), (dc, k * d), (db, k), (ws[0], sizes[0]), (ws[1], sizes[1])):
+        assert (buffer[count:] == 7).all()
+    want = softmax_loss(x, c, bias, 1.0, label, grad)
+    compare({"loss": loss[:n], "dx": dx[:n * d].view(n, d), "dc": dc[:k * d].view(k, d), "db": db[:k]}, want)
+
+
 def test_stats_give_the_log_sum(vlq):
     x, c, bias, label, _ = problem(F32, 100, 96, 3000)
     got, want = run(vlq, x, c, bias, 1.0, label, None), softmax_loss(x, c, bias, 1.0, label)
