@@ -159,3 +159,24 @@ def test_codebook_softened_by_the_recipe(vlq):
     assert float((Cb.double() - (before.double() - 0.1 * v * C.grad)).abs().max()) <= tol
     C2, P = codebooks.train_with_library(vlq, X, 64, 4, 4, iters=2, soft_steps=3)
     assert torch.isfinite(C2).all() and torch.isfinite(P).all()
+
+
+def test_two_steps_at_once(vlq):
+    # on two streams, each with buffers of its own
+    steps = [make(vlq) for _ in range(2)]
+    steps[1].x.mul_(1.25)
+    want = [[v.clone() for v in step()] for step in steps]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in steps]
+    for _ in range(3):
+        for step in steps:
+            for v in (step.loss, step.norm, *step.out):
+                v.fill_(9.0)
+        torch.cuda.synchronize()
+        for stream, step in zip(streams, steps):
+            with torch.cuda.stream(stream):
+                step()
+        torch.cuda.synchronize()
+        for step, ref in zip(steps, want):
+            for a, b in zip((step.loss, step.norm, *step.out), ref):
+                assert torch.equal(a, b)
