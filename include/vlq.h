@@ -318,8 +318,8 @@ int vlq_softmax_loss(int dtype, const void *d_x, int64_t n, int32_t d, const voi
  * The inputs of the forward call and its d_stats; d_grad [n] fp32, the gradient of each row's loss (1 / n for a mean).
  * d_dx [n x d], d_dc [k x d] of type dtype, d_dbias [k] fp32; each may be NULL.  Rows that do not count, and rows with no
  * centroid left, have zero gradients and add nothing to the others'.  n = 0 writes zeros to d_dc and d_dbias.
- * G is held in fp32 where little is done with each centroid, else as fp16 (two parts for fp32) relative to grad's largest magnitude,
- * with an absolute error of at most 2^-40 of that beside its rounding (2^-11, or 2^-22); the values of x and c then enter
+ * G is held in fp32 where little is done with each centroid, else as two fp16 parts relative to grad's largest magnitude,
+ * with an absolute error of at most 2^-40 of that beside its rounding (2^-22); the values of x and c then enter
  * relative to the largest of their matrix.
  * d_ws: at least vlq_softmax_loss_workspace(dtype, n, d, k, 1) bytes.
  */

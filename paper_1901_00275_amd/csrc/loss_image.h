@@ -14,6 +14,10 @@ typedef __bf16 bf16_t;
 #define PAGE 512      // 16-byte chunks of a page: 128 rows x 32 indices
 #define TILE 256      // rows of all images are padded to this
 #define P_ONE 32768.f // 2^15, what a probability of one is in P
+// P has two fp16 parts, 22 bits, whatever the operands' type: with one part the sums of a gradient were off by 1.5e-4 of their terms, which
+// showed in 2 to 8 % of bf16 outputs, and by far more than the outputs' own rounding where the terms all but cancel (centroids
+// with a mean of 30 times their spread: 4.4e-3 of dx)
+#define P_PARTS 2
 #define LOG2E 1.4426950408889634f
 #define LN2 0.6931471805599453f
 
@@ -139,7 +143,7 @@ void launch_loss_few_grads(int dtype, const FewArgs &a, hipStream_t st);
 
 // ---- softmax_loss_narrow.hip ----
 // rows that a workgroup keeps: 256 halve the traffic of LDS where their sums and fragments fit the registers (of 256 dimensions those of
-// 128 rows just do, all 256 of a wave)
+// 128 rows take all 256 of a wave, and one is spilled)
 constexpr int narrow_rows(int parts, int units) { return parts == 2 || units >= 4 ? 128 : 256; }
 struct NarrowSide {
     const u32x4 *q, *r, *rt; // images of the gradient's rows, of the other matrix's rows and columns

@@ -25,8 +25,8 @@
 // of each the 64 chunks of 8 values in the order of the lanes that read them (chunk c of row r at 16 c + r % 16), so that a page
 // is copied to LDS as it lies there and read without bank conflicts.
 //
-// Backward, a piece of the centroids at a time (at most PIECE values): P = 2^15 (p - [j = y]) is written as fp16 images in both
-// orders, for the sums over j and over i.  The lanes of the product hold four consecutive j of one i, and four i (16 apart) of one
+// Backward, a piece of the centroids at a time (at most PIECE values): P = 2^15 (p - [j = y]) is written as fp16 images of two parts
+// in both orders, for the sums over j and over i.  The lanes of the product hold four consecutive j of one i, and four i (16 apart) of one
 // j: the image summed over i has its indices in that order, so neither needs an exchange between lanes.
 #include "loss_image.h"
 
@@ -364,7 +364,7 @@ struct Operand {
     int64_t first;
 };
 
-// acc = A B^T over `units` units of 32 indices, NP pages of every block each.
+// acc = A B^T over `units` units of 32 indices, of A in NPA parts and B in NPB: as many pages of every block each.
 // A tile of two blocks of A by two of B; eight waves, 2 x 4, of 128 rows of A x 64 of B each.  A lane's acc[i][j][r] is row
 // 16 i + 4 (lane / 16) + r, column 16 j + lane % 16 of its wave's part.
 //
@@ -373,11 +373,11 @@ struct Operand {
 // operations are spread between the products of its fragments, and the first fragments of A are read a unit ahead, so that the products go on
 // behind the barrier at once.  8 192 x 8 192 x 2 048, one part, on random operands: 1.46 PFLOP/s, x 8 192: 1.51 (both operands
 // through LDS, copies asked for together: 1.10 and 1.42; products from registers alone: 1.75 and 1.92).
-template <int NP>
+template <int NPA, int NPB>
 struct Product {
-    static constexpr int RING = 4, AHEAD = 3, PAGES = 2 * NP; // pages of A of a unit
-    static constexpr int BAHEAD = NP == 1 ? 3 : 1, NB = BAHEAD + 1; // units that B's fragments are asked for ahead (a unit of two parts takes three times as long)
-    static constexpr int ROUND = 6 * NP;                      // memory operations of a wave and unit
+    static constexpr int RING = 4, AHEAD = 3, PAGES = 2 * NPA; // pages of A of a unit
+    static constexpr int BAHEAD = NPB == 1 ? 3 : 1, NB = BAHEAD + 1; // units that B's fragments are asked for ahead (a unit of two parts takes two or three times as long)
+    static constexpr int ROUND = 4 * NPB + PAGES;             // memory operations of a wave and unit
     static constexpr int LDS = RING * PAGES * PAGE * 16;
     static_assert(RING > AHEAD, "a unit takes the place of the one before the present");
 
@@ -395,24 +395,24 @@ struct Product {
         // page q of unit t (behind the last: of the last, not used); the place in LDS is that of t all the same
         auto copy_page = [&](int t, int q) {
             u32x4 *dst = lds + ((t & (RING - 1)) * PAGES + q) * PAGE + wave * 64;
-            const u32x4 *src = a0 + ((q / NP) * A.block + (int64_t)min(t, units - 1) * NP + q % NP) * PAGE;
+            const u32x4 *src = a0 + ((q / NPA) * A.block + (int64_t)min(t, units - 1) * NPA + q % NPA) * PAGE;
             const __amdgpu_buffer_rsrc_t page = __builtin_amdgcn_make_buffer_rsrc((void *)src, 0, PAGE * 16, 0x00020000);
             __builtin_amdgcn_raw_ptr_buffer_load_lds(page, (__attribute__((address_space(3))) void *)dst, 16, tid * 16, 0, 0, 0);
         };
-        half8 a[8][NP];
-        u32x4 b[NB][NP][4];
+        half8 a[8][NPA];
+        u32x4 b[NB][NPB][4];
         auto read_a = [&](int t, int i) {
 #pragma unroll
-            for (int p = 0; p < NP; ++p)
-                a[i][p] = __builtin_bit_cast(half8, lds[((t & (RING - 1)) * PAGES + (wave >> 2) * NP + p) * PAGE + i * 64 + lane]);
+            for (int p = 0; p < NPA; ++p)
+                a[i][p] = __builtin_bit_cast(half8, lds[((t & (RING - 1)) * PAGES + (wave >> 2) * NPA + p) * PAGE + i * 64 + lane]);
         };
-        auto load_b = [&](int t, int slot, int q) { b[slot][q / 4][q % 4] = b0[((int64_t)min(t, units - 1) * NP + q / 4) * PAGE + q % 4 * 64]; };
+        auto load_b = [&](int t, int slot, int q) { b[slot][q / 4][q % 4] = b0[((int64_t)min(t, units - 1) * NPB + q / 4) * PAGE + q % 4 * 64]; };
         // a wave's memory operations come in rounds, round t: B of unit t + BAHEAD, then A of unit t + AHEAD
 #pragma unroll
         for (int t = -AHEAD; t < 0; ++t) {
             if (t + BAHEAD >= 0)
 #pragma unroll
-                for (int q = 0; q < 4 * NP; ++q) load_b(t + BAHEAD, t + BAHEAD, q);
+                for (int q = 0; q < 4 * NPB; ++q) load_b(t + BAHEAD, t + BAHEAD, q);
             asm volatile("" ::: "memory");
 #pragma unroll
             for (int q = 0; q < PAGES; ++q) copy_page(t + AHEAD, q);
@@ -430,21 +430,21 @@ struct Product {
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                if (NP == 2)
+                if (NPB == 2)
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[i][0], __builtin_bit_cast(half8, b[slot][NP - 1][j]), acc[i][j], 0, 0, 0);
-                if (NP == 2)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[i][0], __builtin_bit_cast(half8, b[slot][NPB - 1][j]), acc[i][j], 0, 0, 0);
+                if (NPA == 2)
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[i][NP - 1], __builtin_bit_cast(half8, b[slot][0][j]), acc[i][j], 0, 0, 0);
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[i][NPA - 1], __builtin_bit_cast(half8, b[slot][0][j]), acc[i][j], 0, 0, 0);
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[i][0], __builtin_bit_cast(half8, b[slot][0][j]), acc[i][j], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
                 if (i < 4)
 #pragma unroll
-                    for (int q = 0; q < NP; ++q) load_b(t + BAHEAD, (slot + BAHEAD) % NB, i * NP + q);
+                    for (int q = 0; q < NPB; ++q) load_b(t + BAHEAD, (slot + BAHEAD) % NB, i * NPB + q);
                 else if (i - 4 < PAGES)
                     copy_page(t + AHEAD, i - 4);
                 if (i < 4) read_a(t, i + 4);
@@ -597,17 +597,17 @@ struct LogitArgs {
 // does not count is not zero, so its logits have to be told.
 template <int PARTS>
 struct FromImages {
-    static constexpr int NP = PARTS, LDS = Product<NP>::LDS;
+    static constexpr int LDS = Product<PARTS, PARTS>::LDS;
     static constexpr bool TOLD = false;
     static __device__ __forceinline__ void run(const LogitArgs &a, int mt, int nt, u32x4 *lds, f32x4 (&acc)[8][4])
     {
-        Product<NP>::run(a.A, a.B, mt * 2, nt * 2, a.units, lds, acc);
+        Product<PARTS, PARTS>::run(a.A, a.B, mt * 2, nt * 2, a.units, lds, acc);
     }
     static __device__ __forceinline__ float inverse(const LogitArgs &a, int group) { return a.cinv[group]; }
 };
 template <typename T>
 struct FromRows {
-    static constexpr int NP = 1, LDS = ProductRows<T>::LDS;
+    static constexpr int LDS = ProductRows<T>::LDS;
     static constexpr bool TOLD = true;
     static __device__ __forceinline__ void run(const LogitArgs &a, int mt, int nt, u32x4 *lds, f32x4 (&acc)[8][4])
     {
@@ -713,7 +713,6 @@ __global__ __launch_bounds__(256) void k_loss_merge(const float2 *part, int part
 template <class FORM>
 __global__ __launch_bounds__(LNT, 2) void k_loss_p(LogitArgs a)
 {
-    constexpr int NP = FORM::NP;
     extern __shared__ u32x4 lds[];
     const int tid = threadIdx.x, lane = tid & 63, l = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -760,18 +759,18 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_p(LogitArgs a)
                 for (int r = 0; r < 4; ++r)
                     if (rel[j] == 16 * i + r) v[r] -= P_ONE;
             const int jj = m0 + 16 * i; // index of the sum, from the piece's first
-            u32x2 *to = a.pj + (((int64_t)(n >> 7) * a.jblock + (jj >> 5) * NP) * PAGE + ((n >> 4) & 7) * 64 +
+            u32x2 *to = a.pj + (((int64_t)(n >> 7) * a.jblock + (jj >> 5) * P_PARTS) * PAGE + ((n >> 4) & 7) * 64 +
                                 16 * (2 * (i & 1) + (g >> 1)) + l) * 2 + (g & 1);
             half4 h, lo;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 _Float16 hi, rest;
-                halves<NP>(v[r], hi, rest);
+                halves<P_PARTS>(v[r], hi, rest);
                 h[r] = hi;
-                if (NP == 2) lo[r] = rest;
+                lo[r] = rest;
             }
             to[0] = __builtin_bit_cast(u32x2, h);
-            if (NP == 2) to[PAGE * 2] = __builtin_bit_cast(u32x2, lo);
+            to[PAGE * 2] = __builtin_bit_cast(u32x2, lo);
         }
     }
     // image summed over i, weighted by g: the rows of its blocks are the centroids (row 4 r + g of 16 is centroid 4 g + r),
@@ -788,14 +787,14 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_p(LogitArgs a)
                 if (labels && rel[j] == 16 * i + r) v -= gn[j];
                 sum += v;
                 _Float16 hi, rest;
-                halves<NP>(v, hi, rest);
+                halves<P_PARTS>(v, hi, rest);
                 h[j] = hi;
-                if (NP == 2) lo[j] = rest;
+                lo[j] = rest;
             }
-            u32x2 *to = a.pi + (((int64_t)(m0 >> 7) * a.iblock + ((n0 >> 5) + (l >> 3)) * NP) * PAGE + i * 64 +
+            u32x2 *to = a.pi + (((int64_t)(m0 >> 7) * a.iblock + ((n0 >> 5) + (l >> 3)) * P_PARTS) * PAGE + i * 64 +
                                 16 * ((l >> 1) & 3) + 4 * r + g) * 2 + (l & 1);
             to[0] = __builtin_bit_cast(u32x2, h);
-            if (NP == 2) to[PAGE * 2] = __builtin_bit_cast(u32x2, lo);
+            to[PAGE * 2] = __builtin_bit_cast(u32x2, lo);
             if (a.dbpart) {
                 sum = row16_sum(sum);
                 if (l == 0) a.dbpart[(int64_t)(n0 >> 6) * (a.mt * TILE) + m0 + 16 * i + 4 * g + r] = sum;
@@ -837,9 +836,9 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_grads(GradOut first, GradOut se
     tile_of(b - split * tiles, a.mt, a.nt, &mt, &nt);
     Operand A = a.A, B = a.B;
     A.first += (int64_t)split * a.per * NP;
-    B.first += (int64_t)split * a.per * NP;
+    B.first += (int64_t)split * a.per * P_PARTS;
     f32x4 acc[8][4];
-    Product<NP>::run(A, B, (int64_t)mt * 2, (int64_t)nt * 2, min(a.per, a.units - split * a.per), lds, acc);
+    Product<NP, P_PARTS>::run(A, B, (int64_t)mt * 2, (int64_t)nt * 2, min(a.per, a.units - split * a.per), lds, acc);
     const int m0 = mt * TILE + (wave >> 2) * 128 + 4 * g, n0 = nt * TILE + (wave & 3) * 64 + (a.permuted ? 4 * (l & 3) + (l >> 2) : l);
     const float f = a.mode == 0 ? grad_factor(*a.inv, a.top ? *a.top : 1.f, a.scale) : 1.f;
 #pragma unroll
@@ -1124,8 +1123,8 @@ static LossPlan loss_plan(int dtype, int64_t n, int d, int k, bool backward, voi
             p.bytes = (off + 255) & ~(size_t)255;
             return p;
         }
-        take(p.pj, p.rpad * p.piece / 8 * p.np);
-        take(p.pi, p.rpad * p.piece / 8 * p.np);
+        take(p.pj, p.rpad * p.piece / 8 * P_PARTS);
+        take(p.pi, p.rpad * p.piece / 8 * P_PARTS);
         take(p.dbpart, p.rpad / 64 * p.piece);
         p.xsplit = sum_parts(p.rpad / TILE * mt, p.piece / 32, n * d * 4);
         p.csplit = sum_parts(p.piece / TILE * mt, p.rpad / 32, (int64_t)k * d * 4);
@@ -1368,7 +1367,8 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
     const bool lie = as_they_lie<T>(a, p);
     using Rows = std::conditional_t<NP == 1, FromRows<T>, FromImages<NP>>;
     LOSS_TRY(lie ? allow_lds(k_loss_p<Rows>, Rows::LDS) : allow_lds(k_loss_p<FromImages<NP>>, FromImages<NP>::LDS));
-    LOSS_TRY(allow_lds(k_loss_grads<T, NP>, Product<NP>::LDS));
+    using Sums = Product<NP, P_PARTS>;
+    LOSS_TRY(allow_lds(k_loss_grads<T, NP>, Sums::LDS));
     const int mt = p.dblocks / 2;
     const bool vec = a.d % 4 == 0, whole = a.n <= p.rows && p.kpad <= p.piece; // (one piece: dbias with the other sums)
     for (int64_t r0 = 0; r0 < a.n; r0 += p.rows) {
@@ -1379,8 +1379,8 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
             g.gn = p.gn + r0;
             g.pj = (u32x2 *)p.pj;
             g.pi = (u32x2 *)p.pi;
-            g.jblock = (int)(cpad / 32 * NP);
-            g.iblock = (int)(rpad / 32 * NP);
+            g.jblock = (int)(cpad / 32 * P_PARTS);
+            g.iblock = (int)(rpad / 32 * P_PARTS);
             g.dbpart = a.dbias ? p.dbpart : nullptr;
             if (lie)
                 hipLaunchKernelGGL(k_loss_p<Rows>, dim3((unsigned)(g.mt * g.nt)), dim3(LNT), Rows::LDS, st, g);
@@ -1394,7 +1394,7 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
             if (a.dx) {
                 x.A = {p.ccols, p.kpad / 32 * NP, c0 / 32 * NP};
                 x.B = {p.pj, g.jblock, 0};
-                x.units = g.jblock / NP;
+                x.units = (int)(cpad / 32);
                 x.mt = mt;
                 x.nt = g.nt;
                 x.splits = p.xsplit;
@@ -1413,7 +1413,7 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
                 const int64_t cols = a.k - c0 < cpad ? a.k - c0 : cpad;
                 c.A = {p.xcols, p.npad / 32 * NP, r0 / 32 * NP};
                 c.B = {p.pi, g.iblock, 0};
-                c.units = g.iblock / NP;
+                c.units = (int)(rpad / 32);
                 c.mt = mt;
                 c.nt = g.mt;
                 c.splits = p.csplit;
@@ -1433,9 +1433,9 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
             const int nx = x.mt * x.nt * x.splits, nc = c.mt * c.nt * c.splits;
             if (nx + nc == 0) continue;
             if (c.per > x.per)
-                hipLaunchKernelGGL((k_loss_grads<T, NP>), dim3((unsigned)(nx + nc)), dim3(LNT), Product<NP>::LDS, st, c, x, nc);
+                hipLaunchKernelGGL((k_loss_grads<T, NP>), dim3((unsigned)(nx + nc)), dim3(LNT), Sums::LDS, st, c, x, nc);
             else
-                hipLaunchKernelGGL((k_loss_grads<T, NP>), dim3((unsigned)(nx + nc)), dim3(LNT), Product<NP>::LDS, st, x, c, nx);
+                hipLaunchKernelGGL((k_loss_grads<T, NP>), dim3((unsigned)(nx + nc)), dim3(LNT), Sums::LDS, st, x, c, nx);
         }
     }
     finish(a.dbias && whole ? bias_part((int)(p.rpad / 64), p.kpad, 0, a.k, false) : BiasSum{});

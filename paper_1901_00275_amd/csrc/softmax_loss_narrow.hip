@@ -8,14 +8,14 @@
 // columns' image is written in.
 //
 // Each side computes the logits, 8 n k d operations together where the wide form takes 6 n k d; but that one writes P twice
-// and reads it twice, 16 bytes a pair with two parts, which bounds it at so few dimensions.
+// and reads it twice, 16 bytes a pair, which bounds it at so few dimensions.
 //
 // Bound by the matrix cores and the arithmetic between their products: 4 095 x 65 536 x 128 fp32 (three products each) 740 us,
 // 1.11 PFLOP/s, the matrix cores busy 60 % of the time at the 1.87 GHz that the card then holds; forward 180 us, 1.15.  The
 // products and the arithmetic of two tiles woven into each other by hand gained nothing over two workgroups a compute unit
 // with the products' waves preferred.
-// 16-bit values: 8 192 x 32 000 x 256 bf16, forward and gradients 650 us (1.03 PFLOP/s), x 129 453; there the fragments' reads from LDS take as
-// long as the products that they feed.
+// 16-bit values (one product for the logits, two with the parts of P): 8 192 x 32 000 x 256 bf16, forward and gradients 820 us, x 129
+// 580; forward the fragments' reads from LDS take as long as the products that they feed.
 // Few rows (256 x 16 384 x 96 fp32, 20 us): 256 workgroups of eight tiles each, whose steps follow one another.
 #include "loss_image.h"
 
@@ -236,7 +236,7 @@ __device__ __forceinline__ void narrow(const NarrowArgs &a, const NarrowSide &s,
                             if (lab[j] - 32 * t == 16 * i + 4 * g + r) S[i][j][r] -= P_ONE;
             }
         }
-        half8 P[NP][QB];
+        half8 P[P_PARTS][QB];
 #pragma unroll
         for (int j = 0; j < QB; ++j)
 #pragma unroll
@@ -245,9 +245,9 @@ __device__ __forceinline__ void narrow(const NarrowArgs &a, const NarrowSide &s,
                 for (int r = 0; r < 4; ++r) {
                     const float v = S[i][j][r];
                     _Float16 hi, lo;
-                    halves<NP>(v, hi, lo);
+                    halves<P_PARTS>(v, hi, lo);
                     P[0][j][4 * i + r] = hi;
-                    if (NP == 2) P[NP - 1][j][4 * i + r] = lo;
+                    P[1][j][4 * i + r] = lo;
                     if (CENT) db[j] += v;
                 }
         __builtin_amdgcn_s_setprio(1);
@@ -256,12 +256,11 @@ __device__ __forceinline__ void narrow(const NarrowArgs &a, const NarrowSide &s,
             half8 c[NP];
 #pragma unroll
             for (int p = 0; p < NP; ++p) c[p] = __builtin_bit_cast(half8, st[(2 * DU * NP + p * DB + i) * 64 + lane]);
-            if (NP == 2) {
 #pragma unroll
-                for (int j = 0; j < QB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(c[0], P[NP - 1][j], acc[i][j], 0, 0, 0);
+            for (int j = 0; j < QB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(c[0], P[1][j], acc[i][j], 0, 0, 0);
+            if (NP == 2)
 #pragma unroll
                 for (int j = 0; j < QB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(c[NP - 1], P[0][j], acc[i][j], 0, 0, 0);
-            }
 #pragma unroll
             for (int j = 0; j < QB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(c[0], P[0][j], acc[i][j], 0, 0, 0);
         }
