@@ -708,7 +708,8 @@ __global__ __launch_bounds__(256) void k_loss_merge(const float2 *part, int part
     if (loss) loss[i] = (uint32_t)label >= (uint32_t)k ? 0.f : m == -INFINITY ? INFINITY : LN2 * (m - own) + logf(z);
 }
 
-// Backward: P of a tile, as images in both orders, and the sums over a wave's 64 rows for the bias.
+// Backward: P of a tile, as images in both orders, and the sums over a wave's 64 rows for the bias.  The logits are rounded as they
+// were forward, so that p adds up to one where a large bias takes up some of the products' bits, or all.
 // 8 192 x 50 001 x 2 048 bf16 in seven pieces 1 510 us (1.11 PFLOP/s): the product, and behind it 1.6 GB of images.
 template <class FORM>
 __global__ __launch_bounds__(LNT, 2) void k_loss_p(LogitArgs a)
@@ -743,7 +744,7 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_p(LogitArgs a)
             const float f = row[j][0] * ci;
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                acc[i][j][r] = FORM::TOLD && b2[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], f, b2[r] - row[j][1]));
+                acc[i][j][r] = FORM::TOLD && b2[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], f, b2[r]) - row[j][1]);
         }
     }
     const bool labels = __any(any);

@@ -184,7 +184,7 @@ __device__ __forceinline__ void narrow(const NarrowArgs &a, const NarrowSide &s,
             }
             continue;
         }
-        // P, in units of 2^15
+        // P, in units of 2^15, from the logits rounded as they were forward
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             if (CENT) {
@@ -195,7 +195,7 @@ __device__ __forceinline__ void narrow(const NarrowArgs &a, const NarrowSide &s,
                 for (int j = 0; j < QB; ++j)
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
-                        S[i][j][r] = __builtin_amdgcn_exp2f(fmaf(S[i][j][r], row[r][0] * f[j], m[j] - row[r][1])) * row[r][3];
+                        S[i][j][r] = __builtin_amdgcn_exp2f(fmaf(S[i][j][r], row[r][0] * f[j], m[j]) - row[r][1]) * row[r][3];
             } else {
                 const f32x4 b2 = *(const f32x4 *)(num + 16 * i + 4 * g);
                 const float ci = cinv[i];
@@ -203,7 +203,7 @@ __device__ __forceinline__ void narrow(const NarrowArgs &a, const NarrowSide &s,
                 for (int j = 0; j < QB; ++j) {
                     const float fj = f[j] * ci;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) S[i][j][r] = __builtin_amdgcn_exp2f(fmaf(S[i][j][r], fj, b2[r] - m[j])) * z[j];
+                    for (int r = 0; r < 4; ++r) S[i][j][r] = __builtin_amdgcn_exp2f(fmaf(S[i][j][r], fj, b2[r]) - m[j]) * z[j];
                 }
             }
         }

@@ -1,11 +1,13 @@
-"""vlq_softmax_loss and its gradient where their range or their bits could end: probabilities whose terms cancel, in every form and
-type, against the formulas in 64 bits."""
+"""vlq_softmax_loss and its gradient where their range or their bits could end: probabilities whose terms cancel, biases that take up
+the products, in every form and type, against the formulas in 64 bits."""
+
+import math
 
 import pytest
 import torch
 
-from learn_reference import half_step, softmax_loss
-from test_gpu_softmax_loss import BF16, F16, F32, DEV, run, vlq  # noqa: F401
+from learn_reference import SUB, U, half_step, softmax_loss
+from test_gpu_softmax_loss import BF16, F16, F32, DEV, problem, run, vlq  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -42,4 +44,43 @@ def test_terms_that_cancel(vlq, t, d):  # noqa: F811
     got = run(vlq, x, c, torch.zeros(k, device=DEV), scale, label, grad)
     want = bounds(x, c, torch.zeros(k, device=DEV), scale, label, grad)
     for name in ("dx", "dc"):
+        within(got, want, name)
+
+
+# the gradients' forms: few; narrow, of 16-bit values also beyond 128 dimensions; wide from images and with the centroids as they lie
+FORMS = [(70, 40, 300), (900, 96, 1500), (900, 200, 1500), (1000, 300, 1100), (1000, 304, 1100)]
+
+
+def uniform(x, c, scale, label, grad):
+    """dx, dc, db where every probability is 1 / k, and their bounds: 1 / k is a sum of ones and two roundings, a product of it two
+    more; G as two fp16 parts; the sums on the matrix cores."""
+    t, (n, d), k = x.dtype, x.shape, c.shape[0]
+    G = torch.full((n, k), 1.0 / k, dtype=torch.float64, device=DEV)
+    G[torch.arange(n, device=DEV), label.long()] -= 1.0
+    G *= grad.double()[:, None]
+    X, Cc = x.double(), c.double()
+    off = lambda N: (N / 4 + 64) * U + 24 * U + 2.0 ** -22  # noqa: E731  (8 U of them for the parts of fp32 operands)
+    top = float(grad.abs().max())
+    low = 2.0 ** -39  # of the largest of the matrix
+    out = {"dx": scale * (G @ Cc), "dc": scale * (G.t().contiguous() @ X), "db": G.sum(0)}
+    tol = {"dx": abs(scale) * (G.abs() @ Cc.abs() * off(k) + SUB * grad.double().abs()[:, None] * Cc.abs().sum(0) + G.abs().sum(1, keepdim=True) * low * Cc.abs().max()),
+           "dc": abs(scale) * (G.abs().t().contiguous() @ X.abs() * off(n) + SUB * top * X.abs().sum(0) + G.abs().sum(0)[:, None] * low * X.abs().max()),
+           "db": G.abs().sum(0) * off(n)}
+    for name in ("dx", "dc"):
+        tol[name] = tol[name] + half_step(t) * (out[name].abs() + tol[name]) + (2.0 ** -25 if t == F16 else 0.0)
+    return {name: (out[name], tol[name]) for name in out}
+
+
+@pytest.mark.parametrize("t", [F32, F16, BF16])
+@pytest.mark.parametrize("n,d,k", FORMS)
+def test_bias_that_takes_up_the_products(vlq, t, n, d, k):  # noqa: F811
+    # all centroids masked alike by a finite value next to which logits of up to some ten vanish (in 64 bits as well): the
+    # loss is log k, every probability 1 / k
+    x, c, _, label, _ = problem(t, n, d, k, spread=4.0)
+    bias = torch.full((k,), -2.0 ** 100, device=DEV)
+    grad = torch.linspace(0.5, 1.5, n, device=DEV)
+    got = run(vlq, x, c, bias, 1.0, label, grad)
+    assert float((got["loss"].double() - math.log(k)).abs().max()) <= 8 * U * math.log(k)
+    want = uniform(x, c, 1.0, label, grad)
+    for name in ("dx", "dc", "db"):
         within(got, want, name)
