@@ -301,7 +301,8 @@ enum {
  *   and the sum of the exponentials relative to it, so that log sum exp = ln 2 * stats[0] + ln stats[1].
  * A row whose label is outside [0, k) does not count: its loss is 0 and its vector is not looked at.  A bias of -infinity
  * takes its centroid out for all rows: its vector is not looked at.  A row with no centroid left, or whose label was taken
- * out, has an infinite loss.
+ * out, has an infinite loss.  Any finite bias is a number: beside others the lowest of fp32 has no weight in the softmax, centroids
+ * that all have it share it alike.  (Logits are held in units of log 2: beyond 2.35e38 in size biases are told apart no more.)
  * fp32 values enter the products as they are or as two fp16 parts, off by 2^-23 of themselves, or 2^-40 of the largest in their
  * row (of x) or in their 16 consecutive centroids; bf16 values exactly down to 2^-32 of that.
  * 0 <= n <= VLQ_MAX_LOSS_ROWS, 1 <= d <= VLQ_MAX_LOSS_DIM, 1 <= k <= VLQ_MAX_LOSS_CLASSES; n = 0 is a no-op.

@@ -20,6 +20,14 @@ typedef __bf16 bf16_t;
 #define P_PARTS 2
 #define LOG2E 1.4426950408889634f
 #define LN2 0.6931471805599453f
+#define MOST __FLT_MAX__
+
+// A bias in units of log 2.  A finite one stays finite: fp32's lowest value is a usual mask, and only -infinity takes a centroid out.
+__device__ __forceinline__ float bias_log2(float b)
+{
+    const float v = b * LOG2E;
+    return fabsf(b) < INFINITY ? fminf(fmaxf(v, -MOST), MOST) : v;
+}
 
 // Exponent of the power of two that brings mx to [2^14, 2^15)
 // (a row of zeros takes the largest: it has no part in the largest inverse scale of its matrix)

@@ -280,7 +280,7 @@ __global__ __launch_bounds__(256) void k_pack_rows(PackArgs a)
     const int b = blockIdx.x - a.xblocks;
     if (b >= 0) {
         const int j = b * 16 + threadIdx.x; // the bias in units of log 2, -inf past the last centroid
-        if (threadIdx.x < 16) a.bias2[j] = j < a.k ? (a.bias ? a.bias[j] * LOG2E : 0.f) : -INFINITY;
+        if (threadIdx.x < 16) a.bias2[j] = j < a.k ? (a.bias ? bias_log2(a.bias[j]) : 0.f) : -INFINITY;
         if (a.cinv) pack_rows<T, false, NP, HELD, RAW>(b, (const T *)a.c, a.k, a.d, a.units, nullptr, a.k, a.bias, a.cimg, a.cinv, a.vec);
         return;
     }
@@ -676,7 +676,7 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_stats(LogitArgs a)
 // there are few of them a row has more threads.
 template <int R>
 __global__ __launch_bounds__(256) void k_loss_merge(const float2 *part, int parts, int npad, const float *mine, const int32_t *lab, int k,
-                                                    int64_t n, float *stats, float *loss)
+                                                    const float *bias, int64_t n, float *stats, float *loss)
 {
     constexpr int T = 256 / R;
     const int r = threadIdx.x % R, t = threadIdx.x / R;
@@ -705,7 +705,15 @@ __global__ __launch_bounds__(256) void k_loss_merge(const float2 *part, int part
     const float m = v[0].x, z = v[0].y;
     stats[2 * i] = m;
     stats[2 * i + 1] = z;
-    if (loss) loss[i] = (uint32_t)label >= (uint32_t)k ? 0.f : m == -INFINITY ? INFINITY : LN2 * (m - own) + logf(z);
+    if (!loss) return;
+    float l = LN2 * (m - own) + logf(z);
+    if ((uint32_t)label >= (uint32_t)k)
+        l = 0.f;
+    else if (m == -INFINITY)
+        l = INFINITY;
+    else if (own == -MOST && m > -MOST && bias) // (a bias that these units have no number for: nothing shows beside it)
+        l = LN2 * m - bias[label];
+    loss[i] = l;
 }
 
 // Backward: P of a tile, as images in both orders, and the sums over a wave's 64 rows for the bias.  The logits are rounded as they
@@ -1234,15 +1242,15 @@ static LogitArgs logit_args(const LossArgs &a, const LossPlan &p, int64_t r0, in
     return g;
 }
 
-static void launch_merge(const float2 *part, int parts, int npad, const float *mine, const int32_t *lab, int k, int64_t n, float *stats,
-                         float *loss, hipStream_t st)
+static void launch_merge(const float2 *part, int parts, int npad, const float *mine, const int32_t *lab, int k, const float *bias, int64_t n,
+                         float *stats, float *loss, hipStream_t st)
 {
     if (n <= FEW_ROWS)
-        hipLaunchKernelGGL(k_loss_merge<1>, dim3((unsigned)n), dim3(256), 0, st, part, parts, npad, mine, lab, k, n, stats, loss);
+        hipLaunchKernelGGL(k_loss_merge<1>, dim3((unsigned)n), dim3(256), 0, st, part, parts, npad, mine, lab, k, bias, n, stats, loss);
     else if (n <= MERGE_ROWS)
-        hipLaunchKernelGGL(k_loss_merge<4>, dim3((unsigned)((n + 3) / 4)), dim3(256), 0, st, part, parts, npad, mine, lab, k, n, stats, loss);
+        hipLaunchKernelGGL(k_loss_merge<4>, dim3((unsigned)((n + 3) / 4)), dim3(256), 0, st, part, parts, npad, mine, lab, k, bias, n, stats, loss);
     else
-        hipLaunchKernelGGL(k_loss_merge<16>, dim3((unsigned)((n + 15) / 16)), dim3(256), 0, st, part, parts, npad, mine, lab, k, n, stats, loss);
+        hipLaunchKernelGGL(k_loss_merge<16>, dim3((unsigned)((n + 15) / 16)), dim3(256), 0, st, part, parts, npad, mine, lab, k, bias, n, stats, loss);
 }
 
 static int loss_few(const LossArgs &a, hipStream_t st)
@@ -1254,7 +1262,7 @@ static int loss_few(const LossArgs &a, hipStream_t st)
     f.part = part;
     f.mine = mine;
     launch_loss_few(a.dtype, f, false, st);
-    launch_merge(part, groups, (int)a.n, mine, a.label, a.k, a.n, a.stats, a.loss, st);
+    launch_merge(part, groups, (int)a.n, mine, a.label, a.k, a.bias, a.n, a.stats, a.loss, st);
     return (int)hipGetLastError();
 }
 
@@ -1278,7 +1286,7 @@ static int loss_forward(const LossArgs &a, hipStream_t st)
         g.npad = (int)p.npad;
         g.x = {p.ximg, p.cimg, nullptr, (int)(p.npad / rows), (int)(p.kpad / 32), p.xsplit, p.xper, (int)a.n};
         LOSS_TRY((hipError_t)launch_loss_narrow_stats(a.dtype, g, st));
-        launch_merge(p.part, p.xsplit, g.npad, p.mine, p.lab, a.k, a.n, a.stats, a.loss, st);
+        launch_merge(p.part, p.xsplit, g.npad, p.mine, p.lab, a.k, a.bias, a.n, a.stats, a.loss, st);
         return (int)hipGetLastError();
     }
     using Images = FromImages<NP>;
@@ -1293,7 +1301,7 @@ static int loss_forward(const LossArgs &a, hipStream_t st)
         g.part = p.part;
         g.mine = p.mine;
         hipLaunchKernelGGL(kern, dim3((unsigned)(g.mt * g.nt)), dim3(LNT), bytes, st, g);
-        launch_merge(p.part, g.mt * 2, g.npad, p.mine, g.lab, a.k, rows, a.stats + 2 * r0, a.loss ? a.loss + r0 : nullptr, st);
+        launch_merge(p.part, g.mt * 2, g.npad, p.mine, g.lab, a.k, a.bias, rows, a.stats + 2 * r0, a.loss ? a.loss + r0 : nullptr, st);
     }
     return (int)hipGetLastError();
 }

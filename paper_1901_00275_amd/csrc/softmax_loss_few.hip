@@ -155,7 +155,7 @@ __global__ __launch_bounds__(W * S * 64) void k_loss_few(FewArgs a)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int c = m0 + 16 * i + 4 * g + r;
-                const float b = c >= a.k ? -INFINITY : bias[i][r] * LOG2E;
+                const float b = c >= a.k ? -INFINITY : bias_log2(bias[i][r]);
                 const float v = b == -INFINITY ? -INFINITY : fmaf(acc[i][j][r], a.scale2, b);
                 if (c == lab && c < a.k) a.mine[n] = v;
                 m = fmaxf(m, v);
@@ -215,7 +215,7 @@ __global__ __launch_bounds__(W * S * 64) void k_loss_few_g(FewArgs a)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int c = c0 + r;
-                const float b = c >= a.k ? -INFINITY : bias[i][r] * LOG2E;
+                const float b = c >= a.k ? -INFINITY : bias_log2(bias[i][r]);
                 const float p = b == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], a.scale2, b) - m) / z;
                 v[r] = !ok || c >= a.k ? 0.f : gn * (c == lab ? p - 1.f : p);
             }

@@ -84,3 +84,35 @@ def test_bias_that_takes_up_the_products(vlq, t, n, d, k):  # noqa: F811
     want = uniform(x, c, 1.0, label, grad)
     for name in ("dx", "dc", "db"):
         within(got, want, name)
+
+
+LOWEST = torch.finfo(F32).min
+
+
+@pytest.mark.parametrize("t", [F32, F16, BF16])
+@pytest.mark.parametrize("n,d,k", FORMS)
+def test_lowest_bias(vlq, t, n, d, k):  # noqa: F811
+    x, c, bias, label, grad = problem(t, n, d, k)
+    # of every third centroid, the labels of many rows among them: such a centroid has the probability that a bias of -60
+    # leaves (1e-26), and a row of its label a loss next to which nothing shows
+    mask = torch.arange(k, device=DEV) % 3 == 0
+    want = softmax_loss(x, c, torch.where(mask, -60.0, bias), 0.7, label, grad)
+    got = run(vlq, x, c, torch.where(mask, LOWEST, bias), 0.7, label, grad)
+    of = mask[label.long()]
+    assert of.any() and not of.all()
+    assert torch.equal(got["loss"][of], torch.full_like(got["loss"][of], -LOWEST))
+    ref, tol = want["loss"]
+    assert ((got["loss"].double() - ref).abs() <= tol)[~of].all()
+    for name in ("dx", "dc", "db"):
+        ref, tol = want[name]
+        assert ((got[name].double() - ref).abs() <= tol).all(), name
+    # of all: the probabilities are alike
+    got = run(vlq, x, c, torch.full_like(bias, LOWEST), 0.7, label, grad)
+    assert float((got["loss"].double() - math.log(k)).abs().max()) <= 8 * U * math.log(k)
+    for name, (ref, tol) in uniform(x, c, 0.7, label, grad).items():
+        assert ((got[name].double() - ref).abs() <= tol).all(), name
+    # the largest, of one: it has everything
+    bias[5], label[3] = -LOWEST, 5
+    got = run(vlq, x, c, bias, 0.7, label, grad)
+    assert got["loss"][3].item() == 0 and (got["dx"][3] == 0).all()
+    assert all(v.isfinite().all() for v in got.values()) and (got["loss"][label != 5] > 2.3e38).all()
