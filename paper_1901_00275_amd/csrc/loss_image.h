@@ -97,8 +97,10 @@ struct LossHeader {
     float xinv, cinv; // inverse scales of the columns' images
     float top;        // largest |g|
 };
-// Factor of a gradient: the inverse scales of the columns' image and of P, and g's largest where P was taken relative to it
-__device__ __forceinline__ float grad_factor(float inv, float top, float scale) { return scale * top * (1.f / P_ONE) * inv; }
+// What a sum is multiplied with to be one of x's or c's own values times P: a power of two, the inverse scales of the columns' image and of
+// P.  The rows' gradients come in relative to the largest, that one and the call's scale last, one by one: multiplied together first they
+// left fp32's range where the results do not (largest |grad| of 2^-96 and less, 2^98 and more).
+__device__ __forceinline__ float grad_unit(float inv) { return inv * (1.f / P_ONE); }
 
 template <typename T>
 __device__ __forceinline__ void store4(T *p, const f32x4 &v, int count, bool vec)
@@ -157,9 +159,8 @@ struct NarrowSide {
     const u32x4 *q, *r, *rt; // images of the gradient's rows, of the other matrix's rows and columns
     int qblocks, tiles, splits, per; // workgroups side by side; tiles of the other matrix, in so many parts of `per`
     int rows;
-    int mode; // 0: typed; 1: slabs [splits][rows x d]
+    int mode; // 0: typed; 1: slabs [splits][rows x d], without the scale and g's largest
     void *out;
-    const float *weight; // of the rows (dx)
     bool vec;
 };
 struct NarrowArgs {

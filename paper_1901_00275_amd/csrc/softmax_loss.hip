@@ -811,18 +811,17 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_p(LogitArgs a)
         }
 }
 
-// One gradient: out[row][dim] = factor sum over the index of A[dim] B[row]
+// One gradient: out[row][dim] = scale weight sum over the index of A[dim] B[row]
 struct GradOut {
     Operand A, B; // columns' image (rows: dimensions), P's image
     int units, mt, nt, splits, per; // units of the sum, tiles, and parts that the sum is cut into, `per` units each
     int rows, d;
     bool permuted; // rows of B in the order 4 r + g
-    int mode;      // 0: typed, times the factor; 1: fp32 slabs, stored; 2: added to what is there
+    int mode;      // 0: typed; 1: fp32 slabs without the scale and `top`, stored; 2: added to what is there
     void *out;     // typed [rows x d], or slabs [splits][rows x d]
     int64_t slab;
-    const float *inv, *top; // inverse scale of the columns' image, largest |g| (or NULL)
-    const float *weight;    // of the rows (or NULL), and where they do not count
-    const int32_t *lab;
+    const float *inv, *top; // inverse scale of the columns' image, largest |g|
+    const float *gn;        // dx: a row's g relative to that, in units of P_ONE
     float scale;
     bool vec;
 };
@@ -849,22 +848,22 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_grads(GradOut first, GradOut se
     f32x4 acc[8][4];
     Product<NP, P_PARTS>::run(A, B, (int64_t)mt * 2, (int64_t)nt * 2, min(a.per, a.units - split * a.per), lds, acc);
     const int m0 = mt * TILE + (wave >> 2) * 128 + 4 * g, n0 = nt * TILE + (wave & 3) * 64 + (a.permuted ? 4 * (l & 3) + (l >> 2) : l);
-    const float f = a.mode == 0 ? grad_factor(*a.inv, a.top ? *a.top : 1.f, a.scale) : 1.f;
+    const float unit = grad_unit(*a.inv), top = *a.top;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int n = n0 + 16 * j;
         if (n >= a.rows) continue;
-        const float w = !a.weight ? f : a.lab[n] < 0 ? 0.f : a.weight[n] * f;
+        const float w = a.gn ? a.gn[n] * (1.f / P_ONE) : 1.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int m = m0 + 16 * i;
             if (m >= a.d) continue;
             const int64_t at = (int64_t)n * a.d + m;
             if (a.mode == 0) {
-                store4((T *)a.out + at, acc[i][j] * w, a.d - m, a.vec);
+                store4((T *)a.out + at, acc[i][j] * unit * w * a.scale * top, a.d - m, a.vec);
             } else {
                 float *p = (float *)a.out + split * a.slab + at;
-                f32x4 v = acc[i][j] * w;
+                f32x4 v = acc[i][j] * unit * w;
                 if (a.mode == 2) {
                     if (a.vec)
                         v += *(const f32x4 *)p;
@@ -879,14 +878,14 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_grads(GradOut first, GradOut se
     }
 }
 
-// out = factor * sum of the slabs, of both gradients, four values a thread
+// out = scale * sum of the slabs, of both gradients, four values a thread
 // From so many parts on the four waves of a workgroup share those of 256 values (a step of 3 855 x 11 x 657 fp32, 46 parts of dc, 8 us less)
 #define SUM_SHARED 8
 struct SlabSum {
     const float *slabs;
     int splits, blocks;
     int64_t count;
-    const float *inv, *top; // of P's images, or NULL
+    const float *top; // what P's images are relative to, or NULL
     void *out;
 };
 // dbias of a piece: sums over the rows' parts, 64 centroids a workgroup, four waves taking the parts in turn
@@ -908,7 +907,8 @@ __device__ __forceinline__ void bias_sum(int block, const BiasSum &a)
     sum[wave][lane] = s;
     __syncthreads();
     if (wave > 0 || j >= a.count) return;
-    s = ((sum[0][lane] + sum[1][lane]) + (sum[2][lane] + sum[3][lane])) * (a.top ? *a.top * (1.f / P_ONE) : 1.f);
+    s = (sum[0][lane] + sum[1][lane]) + (sum[2][lane] + sum[3][lane]);
+    if (a.top) s = s * (1.f / P_ONE) * *a.top;
     a.out[j] = a.add ? a.out[j] + s : s;
 }
 
@@ -924,7 +924,7 @@ __global__ __launch_bounds__(256) void k_loss_sums(SlabSum x, SlabSum c, BiasSum
     const bool share = a.splits >= SUM_SHARED;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, at = first ? blockIdx.x : blockIdx.x - x.blocks;
     const int64_t i = (share ? (int64_t)at * 64 + lane : (int64_t)at * 256 + threadIdx.x) * 4;
-    const float f = a.inv ? grad_factor(*a.inv, a.top ? *a.top : 1.f, scale) : scale;
+    const float top = a.top ? *a.top : 1.f;
     const bool vec = a.count % 4 == 0 && (uintptr_t)a.out % (4 * sizeof(T)) == 0;
     const int count = (int)min((int64_t)4, a.count - i), by = share ? 4 : 1;
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
@@ -946,7 +946,7 @@ __global__ __launch_bounds__(256) void k_loss_sums(SlabSum x, SlabSum c, BiasSum
         if (wave > 0 || i >= a.count) return;
         s = (s + sum[0][lane]) + (sum[1][lane] + sum[2][lane]);
     }
-    store4((T *)a.out + i, s * f, count, vec);
+    store4((T *)a.out + i, s * scale * top, count, vec);
 }
 
 // No rows: the gradients of centroids and bias are zero
@@ -1316,17 +1316,18 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
     }
     const LossPlan p = loss_plan(a.dtype, a.n, a.d, a.k, true, a.ws);
     if (!p.few) loss_images<T, NP>(a, p, true, st);
+    const float *top = p.few ? nullptr : &p.hdr->top;
     auto bias_part = [&](int slots, int64_t ld, int64_t c0, int64_t count, bool add) {
-        return BiasSum{p.dbpart, slots, (int)ld, (int)count, (int)((count + 63) / 64), p.few ? nullptr : &p.hdr->top, add, a.dbias + c0};
+        return BiasSum{p.dbpart, slots, (int)ld, (int)count, (int)((count + 63) / 64), top, add, a.dbias + c0};
     };
     auto finish = [&](const BiasSum &bias) {
-        auto side = [&](float *slabs, int splits, int64_t count, const float *inv, const float *top, void *out) {
+        auto side = [&](float *slabs, int splits, int64_t count, void *out) {
             const int each = splits >= SUM_SHARED ? 256 : 1024;
-            return SlabSum{slabs, splits, (int)((count + each - 1) / each), count, inv, top, out};
+            return SlabSum{slabs, splits, (int)((count + each - 1) / each), count, top, out};
         };
         SlabSum x = {}, c = {};
-        if (a.dx && p.xslab) x = side(p.xsum, p.xsplit, a.n * a.d, p.few ? nullptr : &p.hdr->cinv, nullptr, a.dx);
-        if (a.dc && p.cslab) c = side(p.csum, p.csplit, (int64_t)a.k * a.d, p.few ? nullptr : &p.hdr->xinv, &p.hdr->top, a.dc);
+        if (a.dx && p.xslab) x = side(p.xsum, p.xsplit, a.n * a.d, a.dx);
+        if (a.dc && p.cslab) c = side(p.csum, p.csplit, (int64_t)a.k * a.d, a.dc);
         const int blocks = x.blocks + c.blocks + bias.blocks;
         if (blocks) hipLaunchKernelGGL(k_loss_sums<T>, dim3((unsigned)blocks), dim3(256), 0, st, x, c, bias, a.scale);
     };
@@ -1362,12 +1363,12 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
         g.scale = a.scale;
         if (a.dx) {
             g.x = {p.ximg, p.cimg, p.ccols, (int)(p.npad / rows), (int)(p.kpad / 32), p.xsplit, p.xper, (int)a.n, p.xslab,
-                   p.xslab ? (void *)p.xsum : a.dx, a.grad, a.d % 4 == 0 && (p.xslab || (uintptr_t)a.dx % 16 == 0)};
+                   p.xslab ? (void *)p.xsum : a.dx, a.d % 4 == 0 && (p.xslab || (uintptr_t)a.dx % 16 == 0)};
             g.nx = g.x.qblocks * g.x.splits;
         }
         if (a.dc || a.dbias)
             g.c = {p.cimg, p.ximg, p.xcols, (int)(p.kpad / rows), (int)(p.npad / 32), p.csplit, p.cper, a.k, p.cslab,
-                   !a.dc ? nullptr : p.cslab ? (void *)p.csum : a.dc, nullptr,
+                   !a.dc ? nullptr : p.cslab ? (void *)p.csum : a.dc,
                    a.d % 4 == 0 && (p.cslab || (uintptr_t)a.dc % 16 == 0)};
         LOSS_TRY((hipError_t)launch_loss_narrow(a.dtype, g, st));
         finish(a.dbias ? bias_part(p.csplit, p.kpad, 0, a.k, false) : BiasSum{});
@@ -1414,8 +1415,7 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
                 x.out = p.xslab ? (void *)(p.xsum + r0 * a.d) : (void *)((T *)a.dx + r0 * a.d);
                 x.slab = a.n * a.d;
                 x.inv = &p.hdr->cinv;
-                x.weight = a.grad + r0;
-                x.lab = p.lab + r0;
+                x.gn = p.gn + r0;
                 x.vec = vec && (p.xslab || (uintptr_t)a.dx % 16 == 0);
             }
             if (a.dc) {
@@ -1434,11 +1434,11 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
                 c.out = p.cslab ? (void *)(p.csum + c0 * a.d) : (void *)((T *)a.dc + c0 * a.d);
                 c.slab = (int64_t)a.k * a.d;
                 c.inv = &p.hdr->xinv;
-                c.top = &p.hdr->top;
                 c.vec = vec && (p.cslab || (uintptr_t)a.dc % 16 == 0);
             }
             x.d = c.d = a.d;
             x.scale = c.scale = a.scale;
+            x.top = c.top = top;
             const int nx = x.mt * x.nt * x.splits, nc = c.mt * c.nt * c.splits;
             if (nx + nc == 0) continue;
             if (c.per > x.per)

@@ -277,7 +277,7 @@ __device__ __forceinline__ void narrow(const NarrowArgs &a, const NarrowSide &s,
         }
         return;
     }
-    const float factor = s.mode != 0 ? 1.f : CENT ? grad_factor(a.hdr->xinv, a.hdr->top, a.scale) : grad_factor(a.hdr->cinv, 1.f, a.scale);
+    const float unit = grad_unit(CENT ? a.hdr->xinv : a.hdr->cinv), top = a.hdr->top;
     float *slab = (float *)s.out + (int64_t)split * s.rows * a.d;
 #pragma unroll
     for (int j = 0; j < QB; ++j) {
@@ -289,15 +289,15 @@ __device__ __forceinline__ void narrow(const NarrowArgs &a, const NarrowSide &s,
             if (g == 0) a.dbpart[(int64_t)split * a.kpad + q] = v;
         }
         if (q >= s.rows || !s.out) continue;
-        const float w = CENT ? factor : lab[j] < 0 ? 0.f : s.weight[q] * factor;
+        const float w = CENT ? 1.f : a.gn[q] * (1.f / P_ONE);
 #pragma unroll
         for (int i = 0; i < DB; ++i) {
             const int dim = 16 * i + 4 * g;
             if (dim >= a.d) continue;
             if (s.mode == 0)
-                store4((T *)s.out + (int64_t)q * a.d + dim, acc[i][j] * w, a.d - dim, s.vec);
+                store4((T *)s.out + (int64_t)q * a.d + dim, acc[i][j] * unit * w * a.scale * top, a.d - dim, s.vec);
             else
-                store4(slab + (int64_t)q * a.d + dim, acc[i][j] * w, a.d - dim, s.vec);
+                store4(slab + (int64_t)q * a.d + dim, acc[i][j] * unit * w, a.d - dim, s.vec);
         }
     }
 }

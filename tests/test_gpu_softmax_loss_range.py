@@ -116,3 +116,18 @@ def test_lowest_bias(vlq, t, n, d, k):  # noqa: F811
     got = run(vlq, x, c, bias, 0.7, label, grad)
     assert got["loss"][3].item() == 0 and (got["dx"][3] == 0).all()
     assert all(v.isfinite().all() for v in got.values()) and (got["loss"][label != 5] > 2.3e38).all()
+
+
+@pytest.mark.parametrize("t", [F32, BF16])
+@pytest.mark.parametrize("e", [-118, -100, 110])
+@pytest.mark.parametrize("n,d,k", FORMS + [(900, 96, 40), (3000, 130, 5000)])
+def test_gradients_of_any_size(vlq, t, e, n, d, k):  # noqa: F811
+    # the rows' gradients near either end of fp32's range, what comes of them inside it
+    x, c, bias, label, grad = problem(t, n, d, k)
+    grad = n * grad * 2.0 ** e
+    got, want = run(vlq, x, c, bias, 0.7, label, grad), softmax_loss(x, c, bias, 0.7, label, grad)
+    for name in ("dx", "dc", "db"):
+        ref, tol = want[name]
+        if t == BF16 and name != "db":
+            tol = tol + 2.0 ** -134  # (half its smallest step)
+        assert ((got[name].double() - ref).abs() <= tol).all(), name
