@@ -883,7 +883,8 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_grads(GradOut first, GradOut se
 #define SUM_SHARED 8
 struct SlabSum {
     const float *slabs;
-    int splits, blocks;
+    int splits;
+    int64_t first, blocks; // workgroups of this launch
     int64_t count;
     const float *top; // what P's images are relative to, or NULL
     void *out;
@@ -915,15 +916,15 @@ __device__ __forceinline__ void bias_sum(int block, const BiasSum &a)
 template <typename T>
 __global__ __launch_bounds__(256) void k_loss_sums(SlabSum x, SlabSum c, BiasSum bias, float scale)
 {
-    if ((int)blockIdx.x >= x.blocks + c.blocks) {
-        bias_sum(blockIdx.x - x.blocks - c.blocks, bias);
+    if (blockIdx.x >= x.blocks + c.blocks) {
+        bias_sum((int)(blockIdx.x - x.blocks - c.blocks), bias);
         return;
     }
-    const bool first = (int)blockIdx.x < x.blocks;
+    const bool first = blockIdx.x < x.blocks;
     const SlabSum &a = first ? x : c;
     const bool share = a.splits >= SUM_SHARED;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, at = first ? blockIdx.x : blockIdx.x - x.blocks;
-    const int64_t i = (share ? (int64_t)at * 64 + lane : (int64_t)at * 256 + threadIdx.x) * 4;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int64_t at = a.first + (first ? blockIdx.x : blockIdx.x - x.blocks), i = (share ? at * 64 + lane : at * 256 + threadIdx.x) * 4;
     const float top = a.top ? *a.top : 1.f;
     const bool vec = a.count % 4 == 0 && (uintptr_t)a.out % (4 * sizeof(T)) == 0;
     const int count = (int)min((int64_t)4, a.count - i), by = share ? 4 : 1;
@@ -1320,16 +1321,25 @@ static int loss_backward(const LossArgs &a, hipStream_t st)
     auto bias_part = [&](int slots, int64_t ld, int64_t c0, int64_t count, bool add) {
         return BiasSum{p.dbpart, slots, (int)ld, (int)count, (int)((count + 63) / 64), top, add, a.dbias + c0};
     };
-    auto finish = [&](const BiasSum &bias) {
-        auto side = [&](float *slabs, int splits, int64_t count, void *out) {
-            const int each = splits >= SUM_SHARED ? 256 : 1024;
-            return SlabSum{slabs, splits, (int)((count + each - 1) / each), count, top, out};
+    auto finish = [&](BiasSum bias) {
+        auto side = [&](float *slabs, int splits, int64_t count, void *out) { return SlabSum{slabs, splits, 0, 0, count, top, out}; };
+        auto left = [](const SlabSum &s) { // workgroups of the next launch: a grid has fewer than 2^32 threads
+            const int64_t each = s.splits >= SUM_SHARED ? 256 : 1024, most = 1 << 22, l = (s.count + each - 1) / each - s.first;
+            return l < most ? l : most;
         };
         SlabSum x = {}, c = {};
         if (a.dx && p.xslab) x = side(p.xsum, p.xsplit, a.n * a.d, a.dx);
         if (a.dc && p.cslab) c = side(p.csum, p.csplit, (int64_t)a.k * a.d, a.dc);
-        const int blocks = x.blocks + c.blocks + bias.blocks;
-        if (blocks) hipLaunchKernelGGL(k_loss_sums<T>, dim3((unsigned)blocks), dim3(256), 0, st, x, c, bias, a.scale);
+        for (;;) {
+            x.blocks = left(x);
+            c.blocks = left(c);
+            const int64_t blocks = x.blocks + c.blocks + bias.blocks;
+            if (!blocks) break;
+            hipLaunchKernelGGL(k_loss_sums<T>, dim3((unsigned)blocks), dim3(256), 0, st, x, c, bias, a.scale);
+            x.first += x.blocks;
+            c.first += c.blocks;
+            bias.blocks = 0;
+        }
     };
     if (p.few) {
         FewArgs f = {a.x, a.c, a.bias, a.label, a.scale * LOG2E, (int)a.n, a.d, a.k};

@@ -131,3 +131,33 @@ def test_gradients_of_any_size(vlq, t, e, n, d, k):  # noqa: F811
         if t == BF16 and name != "db":
             tol = tol + 2.0 ** -134  # (half its smallest step)
         assert ((got[name].double() - ref).abs() <= tol).all(), name
+
+
+def test_more_sums_than_threads_of_a_grid(vlq):  # noqa: F811
+    # 2^34 values of dc, added up over two blocks of rows, four a thread
+    n, d, k = 8192 + 5, 16384, (1 << 20) + 77
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 225e9:
+        pytest.skip("needs 225 GB of device memory")
+    g = torch.Generator(device=DEV).manual_seed(3)
+    c = torch.empty(k, d, dtype=BF16, device=DEV).normal_(generator=g)
+    x = torch.empty(n, d, device=DEV).normal_(generator=g).mul_(d ** -0.5).to(BF16)
+    label = torch.randint(0, k, (n,), generator=g, device=DEV, dtype=torch.int32)
+    label[-1] = k - 1
+    grad = torch.rand(n, generator=g, device=DEV) + 0.5
+    loss, stats, dc = torch.empty(n, device=DEV), torch.empty(n, 2, device=DEV), torch.full((k, d), 7.0, dtype=BF16, device=DEV)
+    ws = torch.empty(max(vlq.vlq_softmax_loss_workspace(BF16, n, d, k, b) for b in (0, 1)), dtype=torch.uint8, device=DEV)
+    vlq.vlq_softmax_loss(x, n, d, c, k, None, 1.0, label, loss, stats, ws)
+    vlq.vlq_softmax_loss_backward(x, n, d, c, k, None, 1.0, label, stats, grad, None, dc, None, ws)
+    del ws
+    some = torch.cat([torch.arange(3, device=DEV), label[:4].long(), torch.arange(k - 200, k, device=DEV)])
+    X, lse = x.double(), math.log(2) * stats[:, 0].double() + torch.log(stats[:, 1].double())
+    p = torch.exp(X @ c[some].double().t().contiguous() - lse[:, None])
+    G = (p - (label.long()[:, None] == some[None, :]).double()) * grad.double()[:, None]
+    ref = G.t().contiguous() @ X
+    # p: logits of 16 384 products (the sum's roundings, next to their sizes of up to |x||c|) and of the statistics; G in two parts; the
+    # sums over the rows
+    size = float(X.norm(dim=1).max() * c[some].double().norm(dim=1).max())
+    off = 2 * size * (d / 4 + 64) * U + 2.0 ** -22 + (n / 4 + 64) * U
+    tol = (G.abs().t().contiguous() @ X.abs()) * off + SUB * float(grad.max()) * X.abs().sum(0)
+    assert ((dc[some].double() - ref).abs() <= tol + half_step(BF16) * (ref.abs() + tol)).all()
