@@ -374,8 +374,8 @@ int vlq_combine_rows_backward(int dtype, const void *d_dout, const void *d_y, in
  *     norm = sqrt(sum of all squares),   d_out[t] = d_grads[t] * min(1, max_norm / norm).
  * dtypes, counts, d_grads and d_out are HOST arrays, read before the call returns: tensor t has counts[t] >= 0 values of type
  * dtypes[t] at d_grads[t]; d_out[t] is d_grads[t] itself (in place) or a buffer apart from all others.  d_out NULL: the norm
- * alone.  d_norm: one fp32, or NULL.  Squares are summed in fp64.  A norm that is not finite leaves the values as they are
- * (d_norm tells).  max_norm > 0 (infinity: copies).  Buffers that overlap are refused.
+ * alone.  d_norm: one fp32, or NULL (a finite norm beyond fp32's largest value is given as that).  Squares are summed in fp64.  A norm
+ * that is not finite leaves the values as they are (d_norm tells).  max_norm > 0 (infinity: copies).  Buffers that overlap are refused.
  * d_ws: at least vlq_clip_grads_workspace(tensors, counts) bytes.
  */
 int vlq_clip_grads(int32_t tensors, const int32_t *dtypes, const int64_t *counts, const void *const *d_grads,

@@ -141,13 +141,16 @@ __device__ __forceinline__ double sum_parts(const double *part, int parts)
     return block_sum(s);
 }
 
+// The norm as it is returned: one that is finite stays so (infinity says that the values were left as they are)
+__device__ __forceinline__ float norm_out(double n) { return n < INFINITY ? fminf((float)n, __FLT_MAX__) : (float)n; }
+
 // many parts become one, and the norm of no tensors
 __global__ __launch_bounds__(CLIP_NT) void k_grad_norm(const double *part, int parts, double *sum, float *norm)
 {
     const double s = sum_parts(part, parts);
     if (threadIdx.x != 0) return;
     if (sum) *sum = s;
-    if (norm) *norm = (float)sqrt(s);
+    if (norm) *norm = norm_out(sqrt(s));
 }
 
 // (the factor is fp64: 1e-45 / 1e38 is no fp32 number, and the launch waits for memory either way)
@@ -183,7 +186,7 @@ __device__ __forceinline__ void scale_values(const T *p, T *o, int64_t count, do
 __global__ __launch_bounds__(CLIP_NT) void k_grad_scale(ClipTable a, const double *part, int parts, float max_norm, float *norm)
 {
     const double n = sqrt(sum_parts(part, parts));
-    if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)n;
+    if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = norm_out(n);
     // (a norm that is not finite leaves the gradients as they are)
     const double f = n > (double)max_norm && n < INFINITY ? (double)max_norm / n : 1.;
     const int b = a.chunks - 1 - blockIdx.x, t = find_tensor(a, b);
