@@ -303,8 +303,9 @@ enum {
  * takes its centroid out for all rows: its vector is not looked at.  A row with no centroid left, or whose label was taken
  * out, has an infinite loss.  Any finite bias is a number: beside others the lowest of fp32 has no weight in the softmax, centroids
  * that all have it share it alike.  (Logits are held in units of log 2: beyond 2.35e38 in size biases are told apart no more.)
- * fp32 values enter the products as they are or as two fp16 parts, off by 2^-23 of themselves, or 2^-40 of the largest in their
- * row (of x) or in their 16 consecutive centroids; bf16 values exactly down to 2^-32 of that.
+ * fp32 values enter the products as they are or as two fp16 parts, off by 2^-23 of themselves, or 2^-39 of the largest in their
+ * row (of x) or in their 16 consecutive centroids (or 2^-151); bf16 values exactly down to 2^-31 of that.  Values of rows and
+ * centroids that count have to be finite: what others enter is infinite or NaN.
  * 0 <= n <= VLQ_MAX_LOSS_ROWS, 1 <= d <= VLQ_MAX_LOSS_DIM, 1 <= k <= VLQ_MAX_LOSS_CLASSES; n = 0 is a no-op.
  * d_stats of rows that do not count are unspecified.
  * d_ws: at least vlq_softmax_loss_workspace(dtype, n, d, k, 0) bytes, ws_bytes its size (a smaller n may need more: ask for each).
@@ -321,7 +322,7 @@ int vlq_softmax_loss(int dtype, const void *d_x, int64_t n, int32_t d, const voi
  * centroid left, have zero gradients and add nothing to the others'.  n = 0 writes zeros to d_dc and d_dbias.
  * G is held in fp32 where little is done with each centroid, else as two fp16 parts relative to grad's largest magnitude,
  * with an absolute error of at most 2^-40 of that beside its rounding (2^-22); the values of x and c then enter
- * relative to the largest of their matrix.
+ * relative to the largest of their matrix, with the errors above.
  * d_ws: at least vlq_softmax_loss_workspace(dtype, n, d, k, 1) bytes.
  */
 int vlq_softmax_loss_backward(int dtype, const void *d_x, int64_t n, int32_t d, const void *d_c, int32_t k,

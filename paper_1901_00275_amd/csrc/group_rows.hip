@@ -258,14 +258,14 @@ __global__ __launch_bounds__(SMALL_NT) void k_group_small(SortPass a)
 // Few pairs, many cells: one workgroup takes all passes in LDS, k_group_end the rest.  (6 pairs, 57 575 cells, with the gather: 29 us by a
 // launch for each step, 18 now; 4 096 pairs, 65 536 cells 30 and 22.)
 #define FEW_DIGIT 9
-#define FEW_PAIRS 4096
+#define FEW_SORTED 4096
 __global__ __launch_bounds__(SMALL_NT) void k_group_few(SortPass a)
 {
     constexpr int W = SMALL_NT / 64, MOST = 1 << FEW_DIGIT;
-    extern __shared__ uint32_t lds[]; // {key, pair} [2][FEW_PAIRS], [W][bins] a wave's next places, [bins] a digit's first
+    extern __shared__ uint32_t lds[]; // {key, pair} [2][FEW_SORTED], [W][bins] a wave's next places, [bins] a digit's first
     __shared__ uint32_t wsum[W];
-    uint2 *from = (uint2 *)lds, *to = from + FEW_PAIRS;
-    uint32_t *at = (uint32_t *)(to + FEW_PAIRS), *first = at + W * MOST;
+    uint2 *from = (uint2 *)lds, *to = from + FEW_SORTED;
+    uint32_t *at = (uint32_t *)(to + FEW_SORTED), *first = at + W * MOST;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, pairs = (int)a.pairs;
     const int per = (pairs + W * 64 - 1) / (W * 64) * 64, i0 = wave * per, i1 = min(i0 + per, pairs);
     for (int i = tid; i < pairs; i += SMALL_NT) from[i] = make_uint2(key_at(a, i), (uint32_t)i);
@@ -382,7 +382,7 @@ static GroupPlan group_plan(int64_t pairs, int cells)
         left -= p.bits[i];
     }
     p.small = p.passes == 1 && pairs <= SMALL_PAIRS;
-    p.few = p.passes > 1 && pairs <= FEW_PAIRS;
+    p.few = p.passes > 1 && pairs <= FEW_SORTED;
     if (p.few) {
         p.passes = 1;
         p.bits[0] = bits;
@@ -451,7 +451,7 @@ int launch_group_rows(const int32_t *cell, int64_t pairs, int cells, int64_t *of
         a.to = (uint32_t *)(base + p.to_off[0]);
         end.moved = a.moved_out;
         end.to[0] = a.to;
-        const size_t bytes = 2 * FEW_PAIRS * sizeof(uint2) + (SMALL_NT / 64 + 1) * (4u << FEW_DIGIT);
+        const size_t bytes = 2 * FEW_SORTED * sizeof(uint2) + (SMALL_NT / 64 + 1) * (4u << FEW_DIGIT);
         const hipError_t e = hipFuncSetAttribute((const void *)k_group_few, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
         if (e != hipSuccess) return (int)e;
         hipLaunchKernelGGL(k_group_few, dim3(1), dim3(SMALL_NT), bytes, st, a);

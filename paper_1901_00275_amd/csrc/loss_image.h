@@ -41,7 +41,8 @@ __device__ __forceinline__ float pow2i(int ex) { return __uint_as_float((uint32_
 // eight values of a row from index i on, zeros past its end
 template <typename T>
 struct Eight {
-    typedef uint32_t At __attribute__((ext_vector_type(4 * sizeof(T) / sizeof(T)), aligned(sizeof(T)))); // 16 bytes at a value's address
+    // 16 bytes at a value's address (four words, written so that the type depends on T, as its alignment does)
+    typedef uint32_t At __attribute__((ext_vector_type(4 * sizeof(T) / sizeof(T)), aligned(sizeof(T))));
     T v[8];
 };
 template <typename T>
@@ -178,7 +179,5 @@ struct NarrowArgs {
     float *mine;  // [npad] the label's logit
     int npad;
 };
-
-
 int launch_loss_narrow_stats(int dtype, const NarrowArgs &a, hipStream_t st); // 0 or a hipError_t
 int launch_loss_narrow(int dtype, const NarrowArgs &a, hipStream_t st); // 0 or a hipError_t

@@ -15,8 +15,10 @@
 //
 // Operands are otherwise rewritten as fp16 with a power-of-two scale (per row of x, per 16 rows of c, one per
 // matrix where the rows are the summed index):
-//  - fp16 values are taken as they are, bf16 values lose nothing within 32 binades below the largest of their scale;
-//  - an fp32 value is the sum of two fp16 values, hi + lo, with an error of 2^-23 of itself or 2^-40 of the largest of its scale;
+//  - fp16 values are taken as they are, bf16 values lose nothing down to 2^-31 of the largest of their scale (that is brought to
+//    [2^14, 2^15), fp16's smallest step is 2^-24);
+//  - an fp32 value is the sum of two fp16 values, hi + lo, with an error of 2^-23 of itself or 2^-39 of the largest of its scale (scales end
+//    at 2^126: where the largest is below 2^-112 that is 2^-151, less than half of fp32's smallest step);
 //    a product of two is hi hi + hi lo + lo hi, off by 2^-21 of |a||b| at most: three products where a split in three bf16 parts
 //    takes six.
 // All sums are fp32 (the accumulators of the matrix cores), maxima and sums of the softmax are fp32.
@@ -69,7 +71,6 @@
 // Up to so many inverse scales every workgroup that needs their largest finds it: a step of 256 x 16 384 x 96 fp32 57.0 -> 55.5 us, of
 // 4 095 x 16 384 x 96 fp16 215 -> 212; 4 095 x 65 536 x 128 fp32 870 either way.
 #define SMALL_SCALES 8192
-#define FEW_PAIRS (1 << 24)   // values of G, in fp32
 #define MERGE_ROWS 2048      // up to so many rows four a workgroup are merged, not sixteen
 
 // ---------------------------------------------------------------------------
@@ -878,7 +879,6 @@ __global__ __launch_bounds__(LNT, 2) void k_loss_grads(GradOut first, GradOut se
     }
 }
 
-// out = scale * sum of the slabs, of both gradients, four values a thread
 // From so many parts on the four waves of a workgroup share those of 256 values (a step of 3 855 x 11 x 657 fp32, 46 parts of dc, 8 us less)
 #define SUM_SHARED 8
 struct SlabSum {
@@ -913,6 +913,7 @@ __device__ __forceinline__ void bias_sum(int block, const BiasSum &a)
     a.out[j] = a.add ? a.out[j] + s : s;
 }
 
+// out = scale * sum of the slabs, of both gradients, four values a thread
 template <typename T>
 __global__ __launch_bounds__(256) void k_loss_sums(SlabSum x, SlabSum c, BiasSum bias, float scale)
 {
