@@ -38,8 +38,8 @@
 #define LOSS_ROWS 8192       // rows that go through the products together
 #define PIECE (1 << 26)      // values of P kept at a time
 // Up to so many dimensions the narrow form, of two parts and of 16-bit values: what a workgroup keeps fits the registers.  us of a
-// step against the wide form: 8 192 x 32 000 x 129 bf16 453 : 1 146, x 192 fp16 534 : 1 060, x 256 bf16 648 : 1 170; 1 000 x 20 000 x 160
-// bf16 88 : 137, 300 x 32 000 x 256 bf16 100 : 123; forward 8 192 x 32 000 x 256 bf16 141 : 205, 2 735 x 2 322 x 190 19 : 22.
+// step against the wide form: 8 192 x 32 000 x 129 bf16 567 : 1 542, x 192 fp16 675 : 1 473, x 256 bf16 816 : 1 564; 1 000 x 20 000 x 160
+// bf16 92 : 177, 300 x 32 000 x 256 bf16 109 : 165; forward 8 192 x 32 000 x 256 bf16 141 : 205, 2 735 x 2 322 x 190 19 : 22.
 #define NARROW_DIM 128
 #define NARROW_DIM_16 256
 #define NARROW_GROUPS 1024   // its workgroups that run at a time: four a compute unit forward, half as many backward
@@ -56,12 +56,12 @@
 #define FEW_NARROW_WORK 1.2e8
 #define FEW_NARROW_WORK_16 3e8 // beyond NARROW_DIM dimensions
 // A step with the gradients (their products are fp32's, an eighth of the others' rate, but with few rows or centroids the others' tiles
-// are mostly empty): 5 366 x 24 x 2 016 fp16 58 : 115, 3 x 30 x 224 fp16 22 : 38, 500 x 500 x 500 fp32 31 : 103, bf16 26 : 75,
-// 8 000 x 32 x 2 000 fp32 134 : 282, 32 x 16 000 x 2 000 bf16 132 : 179, 8 000 x 64 x 4 000 bf16 269 : 327, 64 x 65 536 x 1 024 bf16
-// 410 : 322, 1 000 x 1 000 x 300 bf16 55 : 77,
-// 300 x 800 x 1 200 45 : 79, 300 x 3 000 x 300 fp32 72 : 97, 1 000 x 2 000 x 200 104 : 88, 2 000 x 1 000 x 300 121 : 107.  Narrow: 300 x 300 x 128 bf16 26 : 35, 300 x 3 000 x 96 bf16 37 : 39, 1 000 x 1 000 x 96
-// fp32 45 : 43, 100 x 16 384 x 128 fp32 78 : 60; 600 x 300 x 256 bf16 27 : 45, 1 000 x 500 x 160 33 : 40, 500 x 1 500 x 192 fp16 41 : 41,
-// 300 x 3 000 x 250 bf16 73 : 60, 4 000 x 400 x 200 67 : 51.
+// are mostly empty): 5 366 x 24 x 2 016 fp16 56 : 129, 3 x 30 x 224 fp16 22 : 29, 500 x 500 x 500 fp32 31 : 103, bf16 24 : 65,
+// 8 000 x 32 x 2 000 fp32 134 : 282, 32 x 16 000 x 2 000 bf16 138 : 211, 8 000 x 64 x 4 000 bf16 274 : 362, 64 x 65 536 x 1 024 bf16
+// 406 : 368, 1 000 x 1 000 x 300 bf16 52 : 70, 300 x 800 x 1 200 bf16 44 : 86, 1 000 x 2 000 x 300 bf16 87 : 77, 300 x 3 000 x 300 fp32 72 : 97,
+// 1 000 x 2 000 x 200 fp32 104 : 88.  Narrow: 300 x 300 x 128 bf16 22 : 26, 5 000 x 200 x 64 38 : 34, 300 x 3 000 x 96 29 : 34, 1 000 x 1 000 x 128
+// 37 : 33, 1 000 x 1 000 x 96 fp32 45 : 43, 100 x 16 384 x 128 fp32 78 : 60; 600 x 300 x 256 bf16 26 : 35, 1 000 x 500 x 160 30 : 31, 500 x 1 500 x 192
+// 36 : 35, 300 x 4 000 x 160 43 : 36, 300 x 3 000 x 250 46 : 53, 500 x 2 500 x 200 50 : 41, 4 000 x 400 x 200 58 : 44.
 #define FEW_GRAD_ROWS 64         // rows or centroids at most
 #define FEW_GRAD_THIN_WORK 2.5e9 // with so few
 #define FEW_GRAD_WORK 3e8      // with more
@@ -719,7 +719,7 @@ __global__ __launch_bounds__(256) void k_loss_merge(const float2 *part, int part
 
 // Backward: P of a tile, as images in both orders, and the sums over a wave's 64 rows for the bias.  The logits are rounded as they
 // were forward, so that p adds up to one where a large bias takes up some of the products' bits, or all.
-// 8 192 x 50 001 x 2 048 bf16 in seven pieces 1 510 us (1.11 PFLOP/s): the product, and behind it 1.6 GB of images.
+// 8 192 x 50 001 x 2 048 bf16 in seven pieces 1 750 us (0.96 PFLOP/s): the product, and behind it 3.3 GB of images.
 template <class FORM>
 __global__ __launch_bounds__(LNT, 2) void k_loss_p(LogitArgs a)
 {
@@ -828,9 +828,9 @@ struct GradOut {
 };
 
 // Both gradients of a piece in one launch, the one with the longer sums first: the tiles of one alone (256 in a piece of 8 192 x 8 192
-// at 2 048 dimensions) leave compute units waiting for the last.  8 192 x 50 001 x 2 048 bf16 2 800 us (1.20 PFLOP/s); of a
-// piece's 432 us about 27 are the sums of dx, which are read, added to and written again.  Smaller pieces repeat that more often
-// (2^25 values of P: 3 220 us), larger ones gain little for twice the memory (2^27: 2 730).
+// at 2 048 dimensions) leave compute units waiting for the last.  8 192 x 50 001 x 2 048 bf16 4 850 us (1.38 PFLOP/s, two products
+// for the parts of P); of a piece's 790 us about 27 are the sums of dx, which are read, added to and written again.  Smaller pieces
+// repeat that more often (2^25 values of P: a step of 8 780 us against 8 320), larger ones gain little for twice the memory (2^27: 8 230).
 template <typename T, int NP>
 __global__ __launch_bounds__(LNT, 2) void k_loss_grads(GradOut first, GradOut second, int nfirst)
 {
@@ -1016,7 +1016,8 @@ static int narrow_parts(int64_t tiles, int64_t per, int64_t out_bytes, int *tile
 // Tiles of a workgroup, so that all of them fill the chip's `slots` a whole number of times (a half to three, whatever the sums over parts
 // and the starts of more workgroups leave as the shortest): xq and cq workgroups side by side, xt and ct tiles to go through,
 // x_bytes and c_bytes of a part's sums (0: none), us of a tile.  (Always two rounds, whatever was left for a
-// third: a step of 2 710 x 9 867 x 192 fp16 131 us, 107 so; 300 x 32 000 x 256 bf16 125 and 100, 8 192 x 32 000 x 256 703 and 648.)
+// third: with P in one part a step of 2 710 x 9 867 x 192 fp16 131 us, 107 so; 300 x 32 000 x 256 bf16 125 and 100, 8 192 x 32 000 x 256
+// 703 and 648.  `us` of a tile 30 or 60 % larger: the same times.)
 static int64_t narrow_per(int64_t xq, int64_t xt, int64_t cq, int64_t ct, int64_t slots, int64_t least, double x_bytes, double c_bytes, double us)
 {
     int64_t best = least;
@@ -1170,8 +1171,8 @@ static hipError_t allow_lds(K kern, size_t bytes)
 
 // The wide form takes the centroids as they lie (ProductRows) where that saves more than it costs: the products are a tenth
 // slower, most where a row is a multiple of 4 KB and all rows of a tile come through the same channel of the L2.  us of a step, these
-// against images: 284 x 50 632 x 1 376 fp16 506 : 580, 1 000 x 30 000 x 1 024 fp16 397 : 427, 4 096 x 32 000 x 2 048 bf16 1 976 : 2 013,
-// 8 192 x 50 001 x 2 048 bf16 5 780 : 5 750.
+// against images: 284 x 50 632 x 1 376 fp16 590 : 659, 1 000 x 30 000 x 1 024 fp16 452 : 484, 4 096 x 32 000 x 2 048 bf16 2 720 : 2 786,
+// 8 192 x 50 001 x 2 048 bf16 8 314 : 8 316.
 #define LIE_ROWS 4096
 template <typename T>
 static bool as_they_lie(const LossArgs &a, const LossPlan &p)

@@ -8,8 +8,8 @@
 //
 // Gradients: G_ij = g_i (p_ij - [j = y_i]) is written in fp32, then dx = s G C and dc = s G^T X on the fp32 matrix instructions, 16-bit
 // values widened as they are read: their rate is an eighth of fp16's, but nothing is padded to 256 rows or written as an image.
-// Bound by the waits for a few turns of loads where the work is small, else by those products: 5 366 x 24 x 2 016 fp16 G 13 us,
-// gradients 28; 500 x 500 x 500 fp32 10 and 16.
+// Bound by the waits for turns of loads: 5 366 x 24 x 2 016 fp16 G 13 us, gradients 28, of which the products take 7; 500 x 500 x 500
+// fp32 10 and 16.  With more work the products show (64 x 65 536 x 1 024 bf16: 112 of a step's 406 us at fp32's rate of 154 TFLOP/s).
 #include "loss_image.h"
 
 #define FEW_WIDE 65536 // from so many centroids on a wave takes 32 of them: then there are waves enough

@@ -14,8 +14,8 @@
 // 1.11 PFLOP/s, the matrix cores busy 60 % of the time at the 1.87 GHz that the card then holds; forward 180 us, 1.15.  The
 // products and the arithmetic of two tiles woven into each other by hand gained nothing over two workgroups a compute unit
 // with the products' waves preferred.
-// 16-bit values (one product for the logits, two with the parts of P): 8 192 x 32 000 x 256 bf16, forward and gradients 820 us, x 129
-// 580; forward the fragments' reads from LDS take as long as the products that they feed.
+// 16-bit values (one product for the logits, two with the parts of P): 8 192 x 32 000 x 256 bf16, gradients 740 us (1.09 PFLOP/s), forward
+// 136 (0.98): there the fragments' reads from LDS take as long as the products that they feed.  A step of x 129 567.
 // Few rows (256 x 16 384 x 96 fp32, 20 us): 256 workgroups of eight tiles each, whose steps follow one another.
 #include "loss_image.h"
 
