@@ -161,3 +161,21 @@ def test_more_sums_than_threads_of_a_grid(vlq):  # noqa: F811
     off = 2 * size * (d / 4 + 64) * U + 2.0 ** -22 + (n / 4 + 64) * U
     tol = (G.abs().t().contiguous() @ X.abs()) * off + SUB * float(grad.max()) * X.abs().sum(0)
     assert ((dc[some].double() - ref).abs() <= tol + half_step(BF16) * (ref.abs() + tol)).all()
+
+
+@pytest.mark.parametrize("t", [F32, BF16])
+# powers of two of x, c and the scale: logits stay ordinary, what is on the way there, the gradients and the images' scales do not
+@pytest.mark.parametrize("ex,ec,es", [(-60, -60, 118), (55, 55, -108), (-118, 0, 112), (0, -118, 112), (100, -100, 0)])
+@pytest.mark.parametrize("n,d,k", FORMS)
+def test_operands_of_any_size(vlq, t, ex, ec, es, n, d, k):  # noqa: F811
+    x, c, bias, label, grad = problem(t, n, d, k)
+    x, c = x * 2.0 ** ex, c * 2.0 ** ec
+    scale = 2.0 ** (es if ex + ec + es >= -6 else -(ex + ec))
+    got, want = run(vlq, x, c, bias, scale, label, grad), softmax_loss(x, c, bias, scale, label, grad)
+    for name in ("loss", "dx", "dc", "db"):
+        ref, tol = want[name]
+        # The sums of G x and G c are fp32 numbers before the scale: of operands around 2^-121 and G around 2^-18 they are below the
+        # normal range, where each product and each part of a sum is off by half a step, 2^-150, and sums of steps are exact.
+        if name in ("dx", "dc"):
+            tol = tol + ((k if name == "dx" else n) + 64) * 2.0 ** -150 * scale + (2.0 ** -134 if t == BF16 else 0.0)
+        assert ((got[name].double() - ref).abs() <= tol).all(), name
